@@ -156,7 +156,7 @@ def prepare(case, seed):
             v = case["classes"]
             top = case["top"] if case["op"] == "distill" else 0
             s["desc"] = H.Head(dt, n, d, v, top=top, temperature=case.get("temperature", 1.0), stream=stream)
-            s["loss"], s["lse"] = torch.empty(n, **f32), torch.empty(n, **f32)
+            s["loss"], s["stats"] = torch.empty(n, **f32), torch.empty(n, 2, **f32)
             if top:
                 s["picked"] = torch.empty(n, top, **f32)
             if case["way"] == "step":
@@ -181,17 +181,17 @@ def _run_library(s):
         return [s["dx"], s["dgamma"], s["dbeta"]]
     step = case["way"] == "step"
     if case["op"] == "xent":
-        H.hapi_xent_forward(d, s["x"], s["w"], s["bias"], s["targets"], s["loss"], s["lse"])
+        H.hapi_xent_forward(d, s["x"], s["w"], s["bias"], s["targets"], s["loss"], s["stats"])
         if step:
-            H.hapi_xent_backward(d, s["x"], s["w"], s["bias"], s["targets"], s["loss"], s["lse"], s["dloss"], s["dx"],
+            H.hapi_xent_backward(d, s["x"], s["w"], s["bias"], s["targets"], s["loss"], s["stats"], s["dloss"], s["dx"],
                                  s["dw"], s["dbias"])
-        out = [s["loss"], s["lse"]]
+        out = [s["loss"], s["stats"]]
     else:
-        H.hapi_distill_forward(d, s["x"], s["w"], s["bias"], s["ids"], s["teacher"], s["loss"], s["lse"], s["picked"])
+        H.hapi_distill_forward(d, s["x"], s["w"], s["bias"], s["ids"], s["teacher"], s["loss"], s["stats"], s["picked"])
         if step:
-            H.hapi_distill_backward(d, s["x"], s["w"], s["bias"], s["ids"], s["teacher"], s["lse"], s["picked"],
+            H.hapi_distill_backward(d, s["x"], s["w"], s["bias"], s["ids"], s["teacher"], s["stats"], s["picked"],
                                     s["dloss"], s["dx"], s["dw"], s["dbias"])
-        out = [s["loss"], s["lse"], s["picked"]]
+        out = [s["loss"], s["stats"], s["picked"]]
     if step:
         out += [s["dx"], s["dw"]] + ([s["dbias"]] if case["bias"] else [])
     return out
@@ -223,13 +223,15 @@ def _plain_head(case, s):
     top = zt.amax(1, keepdim=True)
     e = torch.exp(zt - top)
     total = e.sum(1, keepdim=True)
-    lse = (top + torch.log(total))[:, 0]
+    logsum = torch.log(total)
+    lse = (top + logsum)[:, 0]
+    stats = torch.cat([z.amax(1, keepdim=True), logsum], 1)
     if case["op"] == "xent":
         counts = s["targets"] >= 0
         ids = s["targets"].clamp(min=0)[:, None]
         q = torch.ones_like(ids, dtype=torch.float32)
         loss = torch.where(counts, lse - z.gather(1, ids)[:, 0], 0.0)
-        out = [loss, lse]
+        out = [loss, stats]
     else:
         counts = (s["ids"] >= 0).any(1)
         ids = s["ids"].clamp(min=0)
@@ -240,7 +242,7 @@ def _plain_head(case, s):
         q = eu / su
         picked = torch.where(counts[:, None], z.gather(1, ids), 0.0)
         loss = temp * temp * (q * (u - torch.log(su) - picked / temp + lse[:, None])).sum(1)
-        out = [torch.where(counts, loss, 0.0), lse, picked]
+        out = [torch.where(counts, loss, 0.0), stats, picked]
     if case["way"] == "step":
         coef = torch.where(counts, s["dloss"] * temp, 0.0)[:, None]
         g = e * (coef / total)
@@ -267,7 +269,7 @@ def work(case):
             return {"bytes": 2 * n * d * size + 8 * n + 8 * d, "flops": 8 * n * d}
         return {"bytes": 3 * n * d * size + 8 * n + 12 * d, "flops": 14 * n * d}
     v, step = case["classes"], case["way"] == "step"
-    small = 16 * n + (4 * v * (2 if step else 1) if case["bias"] else 0)
+    small = 20 * n + (4 * v * (2 if step else 1) if case["bias"] else 0)
     if case["op"] == "distill":
         small += 16 * n * min(case["top"], v)
     return {"bytes": (n + v) * d * size * (2 if step else 1) + small, "flops": (6 if step else 2) * n * d * v}
@@ -294,14 +296,15 @@ def exact(case, seed):
     w = s["w"].double()
     bias = s["bias"].double() if case["bias"] else torch.zeros(v, dtype=torch.float64, device="cuda")
     piece = max(1, min(n, (1 << 28) // v))  # rows at once
-    loss, lse, picked, dx = [], [], [], []
+    loss, stats, picked, dx = [], [], [], []
     dw = torch.zeros(v, d, dtype=torch.float64, device="cuda") if step else None
     db = torch.zeros(v, dtype=torch.float64, device="cuda") if step else None
     for a in range(0, n, piece):
         xb = x[a:a + piece]
         z = torch.addmm(bias, xb, w.t())
         l = torch.logsumexp(z / temp, 1)
-        lse.append(l)
+        high = z.max(1)[0]
+        stats.append(torch.stack([high, l - high / temp], 1))
         rows = torch.arange(xb.shape[0], device="cuda")
         if case["op"] == "xent":
             t = s["targets"][a:a + piece]
@@ -331,7 +334,7 @@ def exact(case, seed):
             dx.append(g @ w)
             dw.addmm_(g.t(), xb)
             db += g.sum(0)
-    out = [torch.cat(loss), torch.cat(lse)] + ([torch.cat(picked)] if picked else [])
+    out = [torch.cat(loss), torch.cat(stats)] + ([torch.cat(picked)] if picked else [])
     if step:
         out += [torch.cat(dx), dw] + ([db] if case["bias"] else [])
     return out
