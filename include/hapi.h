@@ -424,6 +424,128 @@ typedef struct {
 int hapi_choose_split(const hapi_split_job *job, hapi_split_estimate *est,
                       hapi_split_choice *choice);
 
+/* ---------------------------------------------------------------------------
+ * The trained tail.  Behind the frozen layers the compute tier trains (Design,
+ * "Request flow": the client continues from the split's output and trains;
+ * Algorithm 1's cli_rest_s is the time of that work).  These are its
+ * operators: layer norm with its gradients, and the losses of a linear
+ * classifier over many classes with theirs.
+ *
+ * As the other entry points they take device pointers, allocate nothing, check
+ * every argument before they launch anything, run asynchronously on
+ * desc->stream, which must belong to the current device (HAPI_E_INVAL
+ * otherwise), as must every tensor, and give the same bits for the same inputs
+ * every time.  They launch kernels only, so a caller may capture them into a
+ * HIP graph.  Calls that share a workspace must be ordered by the caller; a
+ * workspace holds nothing between calls.  Outputs must not overlap inputs,
+ * each other or the workspace.  Gradients are overwritten, not added to. */
+
+/* y = (x - mean) * rstd * gamma + beta over the last dimension. */
+typedef struct {
+  int32_t dtype;            /* hapi_dtype of x, y, dy, dx */
+  int32_t dim;              /* values of a row, 1 .. 16384 */
+  int64_t rows;             /* >= 0 */
+  int64_t x_stride;         /* elements between rows of x and dx; 0 = dim */
+  int64_t y_stride;         /* elements between rows of y and dy; 0 = dim */
+  float eps;                /* >= 0 (the layers of this library use 1e-6) */
+  int32_t reserved;         /* must be 0 */
+  void *stream;             /* hipStream_t; NULL = the null stream */
+  void *workspace;          /* backward only: device scratch, 256-byte aligned */
+  size_t workspace_bytes;
+} hapi_norm_desc;
+
+/* Bytes of workspace hapi_layernorm_backward needs, or < 0 on error.  Host only. */
+int64_t hapi_layernorm_workspace_bytes(const hapi_norm_desc *desc);
+
+/* x, y [rows, dim] in desc->dtype, at least element-aligned; gamma, beta [dim]
+ * float32; mean, rstd [rows] float32 outputs: the row's mean and
+ * 1 / sqrt(variance + eps), which the backward pass reads.  Only the dim values
+ * of each row of y are written.  rows = 0 does nothing.
+ * Errors: HAPI_E_INVAL, HAPI_E_UNSUPPORTED (dim too large), HAPI_E_DEVICE. */
+int hapi_layernorm_forward(const hapi_norm_desc *desc, const void *x, const float *gamma, const float *beta, void *y,
+                           float *mean, float *rstd);
+
+/* With h = (x - mean) rstd and a = dy gamma:
+ *   dx = rstd (a - mean(a) - h mean(a h)), dgamma = sum over rows of dy h,
+ *   dbeta = sum over rows of dy (float32 [dim]; zeros when rows = 0).
+ * Errors: as forward; HAPI_E_NOMEM (workspace too small). */
+int hapi_layernorm_backward(const hapi_norm_desc *desc, const void *dy, const void *x, const float *gamma,
+                            const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta);
+
+/* A linear classifier z = x weight^T + bias and a loss of its logits, which are
+ * never stored: the forward pass keeps a maximum and a sum of exponentials per
+ * row and tile of classes, the backward pass forms the logits again, one piece
+ * of the classes at a time. */
+typedef struct {
+  int32_t dtype;            /* hapi_dtype of x, weight, dx, dweight */
+  int32_t dim;              /* features, 1 .. 2^20 */
+  int64_t rows;             /* 0 .. 2^20 */
+  int64_t classes;          /* 1 .. 2^24 */
+  int64_t x_stride;         /* elements between rows of x and dx; 0 = dim; <= 2^20 */
+  int64_t w_stride;         /* elements between rows of weight and dweight; 0 = dim; <= 2^20 */
+  int32_t top;              /* distillation: the teacher's entries per row, 1 .. 1024; cross entropy: 0 */
+  float temperature;        /* distillation: T > 0; cross entropy: 1 */
+  void *stream;             /* hipStream_t; NULL = the null stream */
+  void *workspace;          /* device scratch, 256-byte aligned */
+  size_t workspace_bytes;
+} hapi_head_desc;
+
+/* Bytes of workspace of a forward call (backward = 0), or of either direction
+ * (backward != 0); < 0 on error.  Widths or strides that are no whole 16-byte
+ * multiples cost a padded copy of x or weight in it.  Host only. */
+int64_t hapi_head_workspace_bytes(const hapi_head_desc *desc, int32_t backward);
+
+/* Softmax cross entropy: per row loss = log sum exp(z) - z[target].
+ *   x        [rows, dim] features; weight [classes, dim]; both in desc->dtype,
+ *            16-byte aligned when dim and the row stride are whole 16-byte
+ *            multiples, else element-aligned
+ *   bias     [classes] float32, or NULL
+ *   targets  [rows] int64.  Negative: the row does not count: its loss is 0, and
+ *            the backward pass reads none of its features (they may be NaN).
+ *            >= classes: an error in the data, the loss and every gradient the
+ *            row reaches are NaN.
+ *   loss     [rows] float32 output
+ *   stats    [rows, 2] float32 output, 8-byte aligned: m, the row's largest logit,
+ *            and l = log sum exp(z - m); the backward pass reads them (apart, so that
+ *            a row of large logits keeps its l; log sum exp(z) is m + l)
+ * A bias of -inf takes its class out; a row all of whose classes are out has
+ * loss NaN.  rows = 0 does nothing.
+ * Errors: HAPI_E_INVAL, HAPI_E_UNSUPPORTED, HAPI_E_NOMEM, HAPI_E_DEVICE. */
+int hapi_xent_forward(const hapi_head_desc *desc, const void *x, const void *weight, const float *bias,
+                      const int64_t *targets, float *loss, float *stats);
+
+/* Gradients of sum(dloss * loss): with dz = dloss (softmax(z) - onehot(target)),
+ *   dx = dz weight [rows, dim], dweight = dz^T x [classes, dim], in desc->dtype,
+ *   dbias = sum over rows of dz, float32 [classes], or NULL.
+ * loss and stats are the forward pass's.  Rows that do not count, and rows whose
+ * dloss is 0, get dx = 0 and add nothing.  Between its two products dz is held
+ * in desc->dtype.  rows = 0: dweight and dbias are zeros.  Errors as forward. */
+int hapi_xent_backward(const hapi_head_desc *desc, const void *x, const void *weight, const float *bias,
+                       const int64_t *targets, const float *loss, const float *stats, const float *dloss, void *dx,
+                       void *dweight, float *dbias);
+
+/* Distillation from a teacher's top logits: with q = softmax(teacher / T) over a
+ * row's top entries and p = softmax(z / T) over all classes,
+ *   loss = T^2 sum_k q_k (log q_k - log p[ids_k])   (the divergence KL(q | p))
+ *   ids     [rows, top] int64: the classes of the teacher's logits, in any order.
+ *           An id < 0 or a logit of -inf is no entry; a row without entries does
+ *           not count (as a negative target).  A class named twice has both
+ *           entries' weight.  An id >= classes, or a logit of NaN or +inf of an
+ *           entry: the loss and the gradients it reaches are NaN.
+ *   teacher [rows, top] float32
+ *   loss [rows], stats [rows, 2] (m, the largest logit, and
+ *           l = log sum exp((z - m) / T)), picked [rows, top] (the classifier's
+ *           logits z at the ids, 0 where there is none) float32 outputs
+ * Everything else as in the cross entropy. */
+int hapi_distill_forward(const hapi_head_desc *desc, const void *x, const void *weight, const float *bias,
+                         const int64_t *ids, const float *teacher, float *loss, float *stats, float *picked);
+
+/* Gradients of sum(dloss * loss): dz = dloss T (p - q); stats and picked are the
+ * forward pass's.  The teacher's logits get no gradient. */
+int hapi_distill_backward(const hapi_head_desc *desc, const void *x, const void *weight, const float *bias,
+                          const int64_t *ids, const float *teacher, const float *stats, const float *picked,
+                          const float *dloss, void *dx, void *dweight, float *dbias);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *hapi_last_error(void);
 

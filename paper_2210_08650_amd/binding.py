@@ -31,7 +31,9 @@ __all__ = ["HapiError", "Desc", "hapi_layer", "hapi_model_desc", "hapi_kernel_st
            "hapi_layer_shape", "hapi_workspace_bytes", "hapi_chunk_count", "hapi_extract",
            "hapi_workspace_guards", "HAPI_GUARD_BYTES", "hapi_extract_range",
            "hapi_extract_noalloc", "HAPI_NOALLOC_SCRATCH_BYTES", "hapi_profile_layers", "hapi_profile_memory",
-           "hapi_stats_enable", "hapi_stats_collect", "hapi_last_error", "hapi_split_job", "hapi_split_estimate", "hapi_split_choice", "hapi_choose_split"]
+           "hapi_stats_enable", "hapi_stats_collect", "hapi_last_error", "hapi_split_job", "hapi_split_estimate", "hapi_split_choice", "hapi_choose_split",
+           "Norm", "Head", "hapi_norm_desc", "hapi_head_desc", "hapi_layernorm_workspace_bytes", "hapi_layernorm_forward", "hapi_layernorm_backward",
+           "hapi_head_workspace_bytes", "hapi_xent_forward", "hapi_xent_backward", "hapi_distill_forward", "hapi_distill_backward"]
 
 _STATUS = {HAPI_E_INVAL: "HAPI_E_INVAL", HAPI_E_UNSUPPORTED: "HAPI_E_UNSUPPORTED",
            HAPI_E_NOMEM: "HAPI_E_NOMEM", HAPI_E_DEVICE: "HAPI_E_DEVICE"}
@@ -99,6 +101,21 @@ class hapi_split_choice(ctypes.Structure):
                 ("nosplit", ctypes.c_int32), ("nsg", ctypes.c_int32)]
 
 
+class hapi_norm_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("dim", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("stream", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class hapi_head_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("dim", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("classes", ctypes.c_int64), ("x_stride", ctypes.c_int64),
+                ("w_stride", ctypes.c_int64), ("top", ctypes.c_int32),
+                ("temperature", ctypes.c_float), ("stream", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 def _hip_runtimes():
     try:
         with open("/proc/self/maps") as f:
@@ -141,6 +158,17 @@ def _load():
                                              ctypes.POINTER(hapi_split_estimate),
                                              ctypes.POINTER(hapi_split_choice)]),
     }
+    N, T = ctypes.POINTER(hapi_norm_desc), ctypes.POINTER(hapi_head_desc)
+    sig.update({
+        "hapi_layernorm_workspace_bytes": (i64, [N]),
+        "hapi_layernorm_forward": (ctypes.c_int, [N] + [vp] * 6),
+        "hapi_layernorm_backward": (ctypes.c_int, [N] + [vp] * 8),
+        "hapi_head_workspace_bytes": (i64, [T, i32]),
+        "hapi_xent_forward": (ctypes.c_int, [T] + [vp] * 6),
+        "hapi_xent_backward": (ctypes.c_int, [T] + [vp] * 10),
+        "hapi_distill_forward": (ctypes.c_int, [T] + [vp] * 8),
+        "hapi_distill_backward": (ctypes.c_int, [T] + [vp] * 11),
+    })
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
         f.restype, f.argtypes = res, args
@@ -151,7 +179,9 @@ _lib = _load()
 EXPORTED = ("hapi_raw_weight_count", "hapi_packed_weight_bytes", "hapi_pack_weights",
             "hapi_layer_shape", "hapi_workspace_bytes", "hapi_chunk_count", "hapi_extract",
             "hapi_workspace_guards", "hapi_extract_range", "hapi_extract_noalloc", "hapi_profile_layers", "hapi_profile_memory",
-            "hapi_stats_enable", "hapi_stats_collect", "hapi_last_error", "hapi_choose_split")
+            "hapi_stats_enable", "hapi_stats_collect", "hapi_last_error", "hapi_choose_split",
+            "hapi_layernorm_workspace_bytes", "hapi_layernorm_forward", "hapi_layernorm_backward", "hapi_head_workspace_bytes",
+            "hapi_xent_forward", "hapi_xent_backward", "hapi_distill_forward", "hapi_distill_backward")
 
 
 def _ptr(p):
@@ -346,3 +376,138 @@ def hapi_choose_split(**job):
              for name, v in ((f, getattr(est[s], f)) for f, _ in hapi_split_estimate._fields_)
              if name != "reserved"} for s in range(nf)]
     return choice, rows
+
+
+# ------------------------------------------------------------ the trained tail
+
+class _TailDesc:
+    """Owns a descriptor of the trained tail's operators."""
+    _struct = None
+
+    def __init__(self, stream=None, workspace=None, workspace_bytes=0):
+        self.c = self._struct()
+        self.set(stream=stream, workspace=workspace, workspace_bytes=workspace_bytes)
+
+    def set(self, stream=None, workspace=None, workspace_bytes=None):
+        if stream is not None:
+            self.c.stream = _stream(stream)
+        if workspace is not None:
+            self._workspace = workspace  # kept alive while the descriptor points at it
+            self.c.workspace = _ptr(workspace)
+        if workspace_bytes is not None:
+            self.c.workspace_bytes = int(workspace_bytes)
+        return self
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+class Norm(_TailDesc):
+    """Owns a ``hapi_norm_desc``."""
+    _struct = hapi_norm_desc
+
+    def __init__(self, dtype, rows, dim, eps=1e-6, x_stride=0, y_stride=0, **kw):
+        super().__init__(**kw)
+        self.c.dtype, self.c.rows, self.c.dim, self.c.eps = dtype, int(rows), int(dim), float(eps)
+        self.c.x_stride, self.c.y_stride = int(x_stride), int(y_stride)
+
+
+class Head(_TailDesc):
+    """Owns a ``hapi_head_desc``; ``top = 0`` is the cross entropy."""
+    _struct = hapi_head_desc
+
+    def __init__(self, dtype, rows, dim, classes, top=0, temperature=1.0, x_stride=0, w_stride=0, **kw):
+        super().__init__(**kw)
+        self.c.dtype, self.c.rows, self.c.dim = dtype, int(rows), int(dim)
+        self.c.classes, self.c.top, self.c.temperature = int(classes), int(top), float(temperature)
+        self.c.x_stride, self.c.w_stride = int(x_stride), int(w_stride)
+
+
+def _tensor(p, name, dtype, rows, dim=None, stride=0):
+    """The address of an argument.  Of a tensor the type, the sizes and the row
+    stride have to be the descriptor's (an address is taken as it is)."""
+    if p is None or not hasattr(p, "data_ptr"):
+        return _ptr(p)
+    shape = (rows,) if dim is None else (rows, dim)
+    want = {HAPI_F32: "torch.float32", HAPI_BF16: "torch.bfloat16"}.get(dtype, dtype)
+    if str(p.dtype) != want or tuple(p.shape) != shape:
+        raise HapiError(HAPI_E_INVAL, f"{name} must be {want} of shape {shape}, got {p.dtype} {tuple(p.shape)}")
+    if (p.stride(-1) != 1 and p.shape[-1] > 1) or (dim is not None and rows > 1 and p.stride(0) != (stride or dim)):
+        raise HapiError(HAPI_E_INVAL, f"{name} must have rows of consecutive values, {stride or dim} apart, "
+                                      f"got strides {tuple(p.stride())}")
+    import torch
+    if not p.is_cuda or p.device.index != torch.cuda.current_device():
+        raise HapiError(HAPI_E_INVAL, f"{name} is on {p.device}, not on the current GPU")
+    return p.data_ptr()
+
+
+def _f32(p, name, *shape):
+    return _tensor(p, name, HAPI_F32, *shape)
+
+
+def hapi_layernorm_workspace_bytes(desc: Norm) -> int:
+    return _check(_lib.hapi_layernorm_workspace_bytes(desc.ref))
+
+
+def hapi_layernorm_forward(desc: Norm, x, gamma, beta, y, mean, rstd) -> None:
+    c = desc.c
+    _check(_lib.hapi_layernorm_forward(
+        desc.ref, _tensor(x, "x", c.dtype, c.rows, c.dim, c.x_stride), _f32(gamma, "gamma", c.dim),
+        _f32(beta, "beta", c.dim), _tensor(y, "y", c.dtype, c.rows, c.dim, c.y_stride),
+        _f32(mean, "mean", c.rows), _f32(rstd, "rstd", c.rows)))
+
+
+def hapi_layernorm_backward(desc: Norm, dy, x, gamma, mean, rstd, dx, dgamma, dbeta) -> None:
+    c = desc.c
+    _check(_lib.hapi_layernorm_backward(
+        desc.ref, _tensor(dy, "dy", c.dtype, c.rows, c.dim, c.y_stride),
+        _tensor(x, "x", c.dtype, c.rows, c.dim, c.x_stride), _f32(gamma, "gamma", c.dim),
+        _f32(mean, "mean", c.rows), _f32(rstd, "rstd", c.rows),
+        _tensor(dx, "dx", c.dtype, c.rows, c.dim, c.x_stride), _f32(dgamma, "dgamma", c.dim),
+        _f32(dbeta, "dbeta", c.dim)))
+
+
+def hapi_head_workspace_bytes(desc: Head, backward: bool = False) -> int:
+    return _check(_lib.hapi_head_workspace_bytes(desc.ref, int(bool(backward))))
+
+
+def _head_inputs(c, x, weight, bias):
+    return [_tensor(x, "x", c.dtype, c.rows, c.dim, c.x_stride),
+            _tensor(weight, "weight", c.dtype, c.classes, c.dim, c.w_stride), _f32(bias, "bias", c.classes)]
+
+
+def _head_gradients(c, dx, dweight, dbias):
+    return [_tensor(dx, "dx", c.dtype, c.rows, c.dim, c.x_stride),
+            _tensor(dweight, "dweight", c.dtype, c.classes, c.dim, c.w_stride), _f32(dbias, "dbias", c.classes)]
+
+
+def hapi_xent_forward(desc: Head, x, weight, bias, targets, loss, stats) -> None:
+    c = desc.c
+    _check(_lib.hapi_xent_forward(
+        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(targets, "targets", "torch.int64", c.rows),
+        _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2)))
+
+
+def hapi_xent_backward(desc: Head, x, weight, bias, targets, loss, stats, dloss, dx, dweight, dbias) -> None:
+    c = desc.c
+    _check(_lib.hapi_xent_backward(
+        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(targets, "targets", "torch.int64", c.rows),
+        _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2), _f32(dloss, "dloss", c.rows),
+        *_head_gradients(c, dx, dweight, dbias)))
+
+
+def hapi_distill_forward(desc: Head, x, weight, bias, ids, teacher, loss, stats, picked) -> None:
+    c = desc.c
+    _check(_lib.hapi_distill_forward(
+        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(ids, "ids", "torch.int64", c.rows, c.top),
+        _f32(teacher, "teacher", c.rows, c.top), _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2),
+        _f32(picked, "picked", c.rows, c.top)))
+
+
+def hapi_distill_backward(desc: Head, x, weight, bias, ids, teacher, stats, picked, dloss, dx, dweight, dbias) -> None:
+    c = desc.c
+    _check(_lib.hapi_distill_backward(
+        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(ids, "ids", "torch.int64", c.rows, c.top),
+        _f32(teacher, "teacher", c.rows, c.top), _f32(stats, "stats", c.rows, 2), _f32(picked, "picked", c.rows, c.top),
+        _f32(dloss, "dloss", c.rows), *_head_gradients(c, dx, dweight, dbias)))

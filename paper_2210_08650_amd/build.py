@@ -18,8 +18,8 @@ LIB = os.path.join(HERE, "libhapi.so")
 ARCH = os.environ.get("HAPI_OFFLOAD_ARCH", "gfx950")
 
 SOURCES = ["conv.hip", "conv3x3.hip", "conv_first.hip", "stem.hip", "attention.hip", "elementwise.hip", "bottleneck.hip", "conv_pp.hip", "conv_f32.hip",
-           "api.cpp", "split.cpp"]
-HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "gemm_util.h"), os.path.join(ROOT, "include", "hapi.h")]
+           "norm.hip", "head.hip", "api.cpp", "split.cpp", "tail.cpp"]
+HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "gemm_util.h"), os.path.join(CSRC, "tail.h"), os.path.join(ROOT, "include", "hapi.h")]
 
 
 def _hipcc() -> str:

@@ -1,0 +1,83 @@
+// Internal declarations of the trained tail's operators: layer norm, and the
+// cross entropy and distillation losses of a linear classifier.
+#pragma once
+
+#include "internal.h"
+
+namespace hapi {
+
+// ---------------------------------------------------------------- layer norm
+
+constexpr int kNormMaxDim = 16384;
+constexpr int kNormParts = 512;  // partial sums of gamma's and beta's gradients, at most
+
+struct NormArgs {
+  const void *x, *dy;
+  const float *gamma, *beta;
+  void *y, *dx;
+  float *mean, *rstd;   // forward: written; backward: read
+  float *part;          // [parts][2][dim]
+  float *dgamma, *dbeta;
+  int64_t rows, x_ld, y_ld;  // y_ld: of y and dy; x_ld: of x and dx
+  int dim;
+  float eps;
+};
+hipError_t launch_norm_forward(bool bf16, const NormArgs &a, hipStream_t s);
+hipError_t launch_norm_backward(bool bf16, const NormArgs &a, hipStream_t s);
+
+// ------------------------------------------------------ classifier and losses
+
+// Sparse target distribution of a row: `top` classes ids[n][k] with weights.
+// Cross entropy: top = 1, ids = the targets, the weight is 1.  Distillation:
+// softmax of teacher[n][k] / T over the entries with id >= 0.
+struct HeadArgs {
+  const void *x, *w;        // [rows][x_ld], [classes][w_ld]: k contiguous, as the products read them
+  const void *x_in, *w_in;  // the caller's, any alignment
+  int64_t x_ld, w_ld, x_in_ld, w_in_ld;
+  const float *bias;        // [classes] or null
+  const int64_t *ids;       // [rows][top]
+  const float *teacher;     // [rows][top]; null: cross entropy
+  int64_t rows, classes;
+  int dim, top;
+  float inv_t, t;           // 1 / T and T
+  // forward
+  float2 *part;             // [parts][rows] (max, sum of exp) of a row over a part's classes
+  int parts;
+  float *loss, *picked;
+  float2 *stats;            // [rows] (largest logit m, log sum exp((z - m) / T))
+  // backward
+  const float *dloss;
+  float2 *info;             // [rows_pad] (m, coefficient / sum of exp); rows that do not count: (inf, 0)
+  float *q;                 // [rows][top] weights (distillation)
+  void *gt;                 // [piece][rows_pad] dz^T of one piece of the classes
+  int64_t rows_pad, v0, piece;  // the piece is classes [v0, v0 + piece)
+  float *db_part;           // [db_parts][classes], null: no bias gradient
+  int db_parts;
+  float *dx_part;           // [splits][rows][dx_pad]
+  int splits, dx_pad;
+  bool first, last;         // first / last piece
+  void *dx, *dw;
+  int64_t dx_ld, dw_ld;
+  float *dbias;
+};
+
+// The parts launch_head_forward writes for this many classes and rows, and the
+// row parts and splits of the backward pass: functions of the sizes only.
+int head_parts(bool bf16, int64_t rows, int64_t classes);
+int head_db_parts(bool bf16, int64_t rows);
+int head_splits(bool bf16, int64_t rows, int dim, int64_t piece);
+constexpr int kHeadRowPad = 64;
+constexpr int kHeadPiece = 256;  // pieces are multiples of this many classes
+
+// rows of T values from ld_in to a padded, aligned [rows][ld_out], zero from dim on.
+hipError_t launch_head_stage(bool bf16, const void *in, int64_t ld_in, void *out, int64_t ld_out, int64_t rows, int dim,
+                             hipStream_t s);
+hipError_t launch_head_forward(bool bf16, const HeadArgs &a, hipStream_t s);  // parts
+hipError_t launch_head_finish(bool bf16, const HeadArgs &a, hipStream_t s);   // loss, stats, picked
+// info, q and a copy of x (xs, [rows][xs_ld]) whose rows that do not count are zero.
+hipError_t launch_head_prepare(bool bf16, const HeadArgs &a, void *xs, int64_t xs_ld, hipStream_t s);
+hipError_t launch_head_dlogits(bool bf16, const HeadArgs &a, hipStream_t s);  // gt, db_part; targets' entries put in
+hipError_t launch_head_grads(bool bf16, const HeadArgs &a, hipStream_t s);    // dw of the piece, dx_part
+hipError_t launch_head_reduce(bool bf16, const HeadArgs &a, hipStream_t s);   // dx, dbias
+
+}  // namespace hapi
