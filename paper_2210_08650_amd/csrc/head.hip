@@ -141,6 +141,182 @@ struct Side {
   }
 };
 
+// What the epilogue needs of the tile's reg side: the bias of its classes (-inf
+// past the last one), or its rows' info.
+template <int EPI, int BA, int THREADS>
+__device__ __forceinline__ void load_side(const Gemm &g, const HeadArgs &h, float2 *side_s, int a0, int t) {
+  if constexpr (EPI == E_STATS)
+    for (int i = t; i < BA; i += THREADS)
+      side_s[i].x = a0 + i < g.a_ext ? (h.bias ? h.bias[a0 + i] : 0.0f) : -INFINITY;
+  if constexpr (EPI == E_DLOGITS)
+    for (int i = t; i < BA; i += THREADS) side_s[i] = a0 + i < h.rows_pad ? h.info[a0 + i] : make_float2(INFINITY, 0.0f);
+}
+
+// Where a wave's blocks lie: block (i, j) is out[lane(j) + lane % 32][reg(i) + 8 q +
+// 4 lh + e] = acc[i][j][4 q + e]; part: which of the reg side's parts the wave holds.
+template <int REG_STEP, int LANE_A, int LANE_B>
+struct Place {
+  int a0, r0, l0, part;
+  __device__ __forceinline__ int reg(int i) const { return r0 + REG_STEP * i; }
+  __device__ __forceinline__ int lane(int j) const { return l0 + (j >> 1) * LANE_B + (j & 1) * LANE_A; }
+};
+
+template <typename T, int EPI, int TA, int TB, typename P>
+__device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x16_t (&acc)[TA][TB], const P &at,
+                                         const float2 *side_s, int split, int lane) {
+  const int lh = lane >> 5;
+  if constexpr (EPI == E_STATS) {
+    const float c = kLog2e * h.inv_t;
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          acc[i][j][r] += side_s[at.reg(i) - at.a0 + 8 * (r >> 2) + 4 * lh + (r & 3)].x;
+          m = fmaxf(m, acc[i][j][r]);
+        }
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      const float mm = m == -INFINITY ? 0.0f : m;  // no class with weight: the sum is 0, not NaN
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - mm) * c);
+      s += __shfl_xor(s, 32, 64);
+      const int row = at.lane(j) + (lane & 31);
+      if (lh == 0 && row < g.b_ext) h.part[(int64_t)at.part * h.rows + row] = make_float2(m, s);
+    }
+  }
+  if constexpr (EPI == E_DLOGITS) {
+    T *gt = static_cast<T *>(h.gt);
+    const float c = kLog2e * h.inv_t;
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      const int cls = at.lane(j) + (lane & 31);  // in the piece
+      const bool live = cls < g.b_ext;
+      const float bias = live && h.bias ? h.bias[h.v0 + cls] : 0.0f;
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < TA; ++i) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float2 in = side_s[at.reg(i) - at.a0 + 8 * (r >> 2) + 4 * lh + (r & 3)];
+          const float z = acc[i][j][r] + bias;
+          const float v = __builtin_amdgcn_exp2f((z - in.x) * c) * in.y;
+          acc[i][j][r] = v;
+          sum += v;
+        }
+        const int a = at.reg(i);
+        T *o = gt + (int64_t)cls * h.rows_pad + a;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][8 * p + e]),
+                                                               __float_as_uint(acc[i][j][8 * p + 4 + e]), false, false);
+              v[e] = __uint_as_float(s2[0]);
+              v[4 + e] = __uint_as_float(s2[1]);
+            }
+            const int n = 16 * p + 8 * lh;
+            if (live && a + n < h.rows_pad)
+              *reinterpret_cast<uint4 *>(o + n) =
+                  make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int n = 8 * q + 4 * lh;
+            if (live && a + n < h.rows_pad)
+              *reinterpret_cast<float4 *>(o + n) =
+                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+          }
+        }
+      }
+      if (h.db_part) {
+        sum += __shfl_xor(sum, 32, 64);
+        if (lh == 0 && live) h.db_part[(int64_t)at.part * h.classes + h.v0 + cls] = sum;
+      }
+    }
+  }
+  if constexpr (EPI == E_DX) {
+    float *out = h.dx_part + (int64_t)split * h.rows * h.dx_pad;
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      const int row = at.lane(j) + (lane & 31);
+      if (row >= g.b_ext) continue;
+#pragma unroll
+      for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int a = at.reg(i) + 8 * q + 4 * lh;
+          if (a >= h.dx_pad) continue;
+          float4 *p = reinterpret_cast<float4 *>(out + (int64_t)row * h.dx_pad + a);
+          float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+          if (!h.first) {
+            const float4 u = *p;
+            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+          }
+          *p = v;
+        }
+    }
+  }
+  if constexpr (EPI == E_DW) {
+    T *out = static_cast<T *>(h.dw);
+    const bool vec = h.dw_ld % (16 / (int)sizeof(T)) == 0 && (uintptr_t)out % 16 == 0;
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      const int cls = at.lane(j) + (lane & 31);
+      const bool live = cls < g.b_ext;
+      T *o = out + (h.v0 + cls) * h.dw_ld;
+#pragma unroll
+      for (int i = 0; i < TA; ++i) {
+        const int a = at.reg(i);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][8 * p + e]),
+                                                               __float_as_uint(acc[i][j][8 * p + 4 + e]), false, false);
+              v[e] = __uint_as_float(s2[0]);
+              v[4 + e] = __uint_as_float(s2[1]);
+            }
+            const int n = a + 16 * p + 8 * lh;
+            if (!live) continue;
+            if (vec && n + 8 <= h.dim) {
+              *reinterpret_cast<uint4 *>(o + n) =
+                  make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (n + e < h.dim) o[n + e] = f2bf(v[e]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int n = a + 8 * q + 4 * lh;
+            if (!live) continue;
+            if (vec && n + 4 <= h.dim) {
+              *reinterpret_cast<float4 *>(o + n) =
+                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (n + e < h.dim) o[n + e] = acc[i][j][4 * q + e];
+            }
+          }
+        }
+      }
+    }
+  }
+}
+
 template <typename T, int BA, int BB, int WA, int WB, int ST, bool KRA, bool KRB, int EPI>
 __global__ __launch_bounds__(64 * WA * WB) void head_gemm_kernel(Gemm g, HeadArgs h) {
   constexpr int WAVES = WA * WB, TA = BA / WA / 32, TB = BB / WB / 32;
@@ -165,14 +341,7 @@ __global__ __launch_bounds__(64 * WA * WB) void head_gemm_kernel(Gemm g, HeadArg
   const int kt0 = (int)((int64_t)nkt * split / g.splits), kt1 = (int)((int64_t)nkt * (split + 1) / g.splits);
   const int nk = kt1 - kt0;
 
-  if constexpr (EPI == E_STATS) {
-    // the bias of this tile's classes; -inf past the last one
-    for (int i = t; i < BA; i += 64 * WAVES)
-      side_s[i].x = a0 + i < g.a_ext ? (h.bias ? h.bias[a0 + i] : 0.0f) : -INFINITY;
-  }
-  if constexpr (EPI == E_DLOGITS) {
-    for (int i = t; i < BA; i += 64 * WAVES) side_s[i] = a0 + i < h.rows_pad ? h.info[a0 + i] : make_float2(INFINITY, 0.0f);
-  }
+  load_side<EPI, BA, 64 * WAVES>(g, h, side_s, a0, t);
 
   SA sa;
   SB sb;
@@ -236,159 +405,8 @@ __global__ __launch_bounds__(64 * WA * WB) void head_gemm_kernel(Gemm g, HeadArg
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __syncthreads();
 
-  // acc[i][j][4 q + e] = out[b0 + 32 (wb TB + j) + lane % 32][a0 + 32 (wa TA + i) + 8 q + 4 lh + e]
-  const int lh = lane >> 5;
-  const int aw = wa * TA * 32, bw = wb * TB * 32;
-  if constexpr (EPI == E_STATS) {
-    const float c = kLog2e * h.inv_t;
-#pragma unroll
-    for (int j = 0; j < TB; ++j) {
-      float m = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < TA; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          acc[i][j][r] += side_s[aw + 32 * i + 8 * (r >> 2) + 4 * lh + (r & 3)].x;
-          m = fmaxf(m, acc[i][j][r]);
-        }
-      m = fmaxf(m, __shfl_xor(m, 32, 64));
-      const float mm = m == -INFINITY ? 0.0f : m;  // no class with weight: the sum is 0, not NaN
-      float s = 0.0f;
-#pragma unroll
-      for (int i = 0; i < TA; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - mm) * c);
-      s += __shfl_xor(s, 32, 64);
-      const int row = b0 + bw + 32 * j + (lane & 31);
-      if (lh == 0 && row < g.b_ext) h.part[(int64_t)(ta * WA + wa) * h.rows + row] = make_float2(m, s);
-    }
-  }
-  if constexpr (EPI == E_DLOGITS) {
-    T *gt = static_cast<T *>(h.gt);
-    const float c = kLog2e * h.inv_t;
-#pragma unroll
-    for (int j = 0; j < TB; ++j) {
-      const int cls = b0 + bw + 32 * j + (lane & 31);  // in the piece
-      const bool live = cls < g.b_ext;
-      const float bias = live && h.bias ? h.bias[h.v0 + cls] : 0.0f;
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < TA; ++i) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float2 in = side_s[aw + 32 * i + 8 * (r >> 2) + 4 * lh + (r & 3)];
-          const float z = acc[i][j][r] + bias;
-          const float v = __builtin_amdgcn_exp2f((z - in.x) * c) * in.y;
-          acc[i][j][r] = v;
-          sum += v;
-        }
-        const int a = a0 + aw + 32 * i;
-        T *o = gt + (int64_t)cls * h.rows_pad + a;
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][8 * p + e]),
-                                                               __float_as_uint(acc[i][j][8 * p + 4 + e]), false, false);
-              v[e] = __uint_as_float(s2[0]);
-              v[4 + e] = __uint_as_float(s2[1]);
-            }
-            const int n = 16 * p + 8 * lh;
-            if (live && a + n < h.rows_pad)
-              *reinterpret_cast<uint4 *>(o + n) =
-                  make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int n = 8 * q + 4 * lh;
-            if (live && a + n < h.rows_pad)
-              *reinterpret_cast<float4 *>(o + n) =
-                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-          }
-        }
-      }
-      if (h.db_part) {
-        sum += __shfl_xor(sum, 32, 64);
-        if (lh == 0 && live) h.db_part[(int64_t)(ta * WA + wa) * h.classes + h.v0 + cls] = sum;
-      }
-    }
-  }
-  if constexpr (EPI == E_DX) {
-    float *out = h.dx_part + (int64_t)split * h.rows * h.dx_pad;
-#pragma unroll
-    for (int j = 0; j < TB; ++j) {
-      const int row = b0 + bw + 32 * j + (lane & 31);
-      if (row >= g.b_ext) continue;
-#pragma unroll
-      for (int i = 0; i < TA; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int a = a0 + aw + 32 * i + 8 * q + 4 * lh;
-          if (a >= h.dx_pad) continue;
-          float4 *p = reinterpret_cast<float4 *>(out + (int64_t)row * h.dx_pad + a);
-          float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-          if (!h.first) {
-            const float4 u = *p;
-            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
-          }
-          *p = v;
-        }
-    }
-  }
-  if constexpr (EPI == E_DW) {
-    T *out = static_cast<T *>(h.dw);
-    const bool vec = h.dw_ld % SA::V == 0 && (uintptr_t)out % 16 == 0;
-#pragma unroll
-    for (int j = 0; j < TB; ++j) {
-      const int cls = b0 + bw + 32 * j + (lane & 31);
-      const bool live = cls < g.b_ext;
-      T *o = out + (h.v0 + cls) * h.dw_ld;
-#pragma unroll
-      for (int i = 0; i < TA; ++i) {
-        const int a = a0 + aw + 32 * i;
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][8 * p + e]),
-                                                               __float_as_uint(acc[i][j][8 * p + 4 + e]), false, false);
-              v[e] = __uint_as_float(s2[0]);
-              v[4 + e] = __uint_as_float(s2[1]);
-            }
-            const int n = a + 16 * p + 8 * lh;
-            if (!live) continue;
-            if (vec && n + 8 <= h.dim) {
-              *reinterpret_cast<uint4 *>(o + n) =
-                  make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (n + e < h.dim) o[n + e] = f2bf(v[e]);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int n = a + 8 * q + 4 * lh;
-            if (!live) continue;
-            if (vec && n + 4 <= h.dim) {
-              *reinterpret_cast<float4 *>(o + n) =
-                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (n + e < h.dim) o[n + e] = acc[i][j][4 * q + e];
-            }
-          }
-        }
-      }
-    }
-  }
+  const Place<32, 32, 64> at = {a0, a0 + wa * TA * 32, b0 + wb * TB * 32, ta * WA + wa};
+  epilogue<T, EPI>(g, h, acc, at, side_s, split, lane);
 }
 
 template <typename T, int BA, int BB, int WA, int WB, int ST, bool KRA, bool KRB, int EPI>
@@ -400,6 +418,157 @@ hipError_t launch_gemm(Gemm g, const HeadArgs &h, hipStream_t s) {
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
   hapi_launch((head_gemm_kernel<T, BA, BB, WA, WB, ST, KRA, KRB, EPI>), dim3((uint32_t)blocks), dim3(64 * WA * WB), 0, s,
               g, h);
+  return hipGetLastError();
+}
+
+// The same product on 256 x 256 tiles.  Eight waves, two per SIMD: wave (g, c)
+// owns rows 64 g .. + 63 of both 128-row halves of B and rows 32 c .. + 31 of both
+// halves of A, 128 accumulator registers.  A k-tile is two steps, each a memory
+// slot (fragments of the next 16 MFMAs out of LDS, DMAs of a later k-tile into
+// it) and a matrix slot, with a barrier after every slot; the two groups g run one
+// slot apart, so one group's MFMAs cover the other's LDS reads.  Two stages of
+// 64 KB; half a stage is loaded again as soon as both groups have read it.
+template <typename T, bool KRA, bool KRB, int EPI>
+__device__ __forceinline__ void big_tile(const Gemm &g, const HeadArgs &h, uint8_t *smem, float2 *side_s, int bid) {
+  typedef Side<T, 128, KRA, 8> SA;
+  typedef Side<T, 128, KRB, 8> SB;
+  constexpr int HALF = SA::BYTES, STAGE = 4 * HALF;  // B halves 0, 1, A halves 0, 1
+  typedef typename Elem<T>::Frag Frag;
+  const int t = threadIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const int tiles = g.tiles_a * g.tiles_b;
+  const int split = bid / tiles, tile = bid % tiles;
+  const int ta = g.tiles_a <= g.tiles_b ? tile % g.tiles_a : tile / g.tiles_b;
+  const int tb = g.tiles_a <= g.tiles_b ? tile / g.tiles_a : tile % g.tiles_b;
+  const int a0 = ta * 256, b0 = tb * 256;
+  const int nkt = (g.k_ext + SA::KT - 1) / SA::KT;
+  const int kt0 = (int)((int64_t)nkt * split / g.splits), kt1 = (int)((int64_t)nkt * (split + 1) / g.splits);
+  const int nk = kt1 - kt0;
+  load_side<EPI, 256, 512>(g, h, side_s, a0, t);
+
+  SA sa[2];
+  SB sb[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    sa[i].init(a0 + 128 * i, g.a_ext, g.a_ld, wave, lane);
+    sb[i].init(b0 + 128 * i, g.b_ext, g.b_ld, wave, lane);
+  }
+  const int64_t da = SA::k_step(g.a_ld), db = SB::k_step(g.b_ld);
+  const int64_t ha = SA::row_base(128, g.a_ld), hb = SB::row_base(128, g.b_ld);
+  const uint8_t *pa = static_cast<const uint8_t *>(g.a) + SA::row_base(a0, g.a_ld) + kt0 * da;
+  const uint8_t *pb = static_cast<const uint8_t *>(g.b) + SB::row_base(b0, g.b_ld) + kt0 * db;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+  int k_left = nk > 0 ? g.k_ext - kt0 * SA::KT : 0, s_kt = 0;
+  // The load stream's next k-tile; past the last one loads read nothing.
+  auto stream_next = [&] {
+    if (++s_kt < nk) {
+      pa += da;
+      pb += db;
+      k_left -= SA::KT;
+    } else {
+      k_left = 0;
+    }
+  };
+  auto issue_a = [&](uint32_t stage, int i) { sa[i].issue(pa + i * ha, lds0 + stage + (2 + i) * HALF, k_left, wave); };
+  auto issue_b = [&](uint32_t stage, int i) { sb[i].issue(pb + i * hb, lds0 + stage + i * HALF, k_left, wave); };
+
+  Frag fb[2][4], fa0[4], fa1[4];
+  auto read_b = [&](uint32_t stage, int half) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+        fb[i][ks] = SB::frag(smem + stage + half * HALF, wm * 64 + 32 * i, ks, lane);
+  };
+  auto read_a = [&](uint32_t stage, int half, Frag(&f)[4]) {
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) f[ks] = SA::frag(smem + stage + (2 + half) * HALF, wn * 32, ks, lane);
+  };
+  auto bar = [&] {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // End of a memory slot: this wave's fragments are in registers, and its part of
+  // what the next memory slot reads has landed (8 younger DMAs may be in flight).
+  auto mem_end = [&] {
+    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+    bar();
+  };
+  f32x16_t acc[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+  auto mmas = [&](int half) {
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        acc[0][2 * half + i] = mma(fa0[ks], fb[i][ks], acc[0][2 * half + i]);
+        acc[1][2 * half + i] = mma(fa1[ks], fb[i][ks], acc[1][2 * half + i]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  issue_b(0, 0);
+  issue_a(0, 0);
+  issue_a(0, 1);
+  issue_b(0, 1);
+  stream_next();
+  issue_b(STAGE, 0);
+  issue_a(STAGE, 0);
+  issue_a(STAGE, 1);
+  uint32_t st = 0;
+  mem_end();
+  if (wm == 1) bar();  // the second group runs one slot behind
+  for (int kt = 0; kt < nk; ++kt) {
+    read_b(st, 0);
+    read_a(st, 0, fa0);
+    read_a(st, 1, fa1);
+    issue_b(st ^ STAGE, 1);
+    stream_next();
+    mem_end();
+    mmas(0);
+    bar();
+    issue_b(st, 0);
+    issue_a(st, 0);
+    issue_a(st, 1);
+    read_b(st, 1);
+    mem_end();
+    mmas(1);
+    if (kt + 1 < nk) bar();
+    st ^= STAGE;
+  }
+  if (wm == 0) bar();
+  // No DMA may outlive the workgroup's LDS (the last ones read nothing).
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  const Place<128, 32, 128> at = {a0, a0 + wn * 32, b0 + wm * 64, ta * 4 + wn};
+  epilogue<T, EPI>(g, h, acc, at, side_s, split, lane);
+}
+
+constexpr int kBigSmem = 8 * 128 * 128;
+
+template <typename T, bool KRA, bool KRB, int EPI>
+__global__ __launch_bounds__(512) void head_big_kernel(Gemm g, HeadArgs h) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kBigSmem];
+  __shared__ __attribute__((aligned(16))) float2 side_s[EPI == E_STATS || EPI == E_DLOGITS ? 256 : 1];
+  big_tile<T, KRA, KRB, EPI>(g, h, smem, side_s, xcd_remap(blockIdx.x, gridDim.x));
+}
+
+template <typename T, bool KRA, bool KRB, int EPI>
+hipError_t launch_big(Gemm g, const HeadArgs &h, hipStream_t s) {
+  g.tiles_a = (g.a_ext + 255) / 256;
+  g.tiles_b = (g.b_ext + 255) / 256;
+  const int64_t blocks = (int64_t)g.tiles_a * g.tiles_b * g.splits;
+  if (blocks == 0) return hipSuccess;
+  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  hapi_launch((head_big_kernel<T, KRA, KRB, EPI>), dim3((uint32_t)blocks), dim3(512), 0, s, g, h);
   return hipGetLastError();
 }
 
@@ -705,6 +874,7 @@ int grid_for(int64_t n, int per) {
 
 // Rows at which the row side of a tile is 128 wide; below, 32.
 constexpr int kWideRows = 64;
+bool big_rows(int64_t rows) { return rows > 512; }
 
 template <typename T>
 hipError_t forward(const HeadArgs &a, hipStream_t s) {
@@ -712,6 +882,7 @@ hipError_t forward(const HeadArgs &a, hipStream_t s) {
   g.a = a.w; g.a_ld = a.w_ld; g.a_ext = (int)a.classes;
   g.b = a.x; g.b_ld = a.x_ld; g.b_ext = (int)a.rows;
   g.k_ext = a.dim; g.splits = 1;
+  if (big_rows(a.rows)) return launch_big<T, false, false, E_STATS>(g, a, s);
   if (a.rows > kWideRows) return launch_gemm<T, 128, 128, 2, 2, 3, false, false, E_STATS>(g, a, s);
   return launch_gemm<T, 128, 32, 4, 1, 4, false, false, E_STATS>(g, a, s);
 }
@@ -721,7 +892,8 @@ hipError_t dlogits(const HeadArgs &a, hipStream_t s) {
   g.a = a.x; g.a_ld = a.x_ld; g.a_ext = (int)a.rows;
   g.b = static_cast<const T *>(a.w) + a.v0 * a.w_ld; g.b_ld = a.w_ld; g.b_ext = (int)a.piece;
   g.k_ext = a.dim; g.splits = 1;
-  const hipError_t e = a.rows > kWideRows ? launch_gemm<T, 128, 128, 2, 2, 3, false, false, E_DLOGITS>(g, a, s)
+  const hipError_t e = big_rows(a.rows) ? launch_big<T, false, false, E_DLOGITS>(g, a, s) :
+                       a.rows > kWideRows ? launch_gemm<T, 128, 128, 2, 2, 3, false, false, E_DLOGITS>(g, a, s)
                                           : launch_gemm<T, 32, 128, 1, 4, 4, false, false, E_DLOGITS>(g, a, s);
   if (e != hipSuccess || a.rows == 0) return e;
   hapi_launch(head_targets_kernel<T>, dim3((uint32_t)((a.rows * a.top + 255) / 256)), dim3(256), 0, s, a);
@@ -733,24 +905,30 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
   g.a = static_cast<const T *>(a.w) + a.v0 * a.w_ld; g.a_ld = a.w_ld; g.a_ext = a.dx_pad;
   g.b = a.gt; g.b_ld = a.rows_pad; g.b_ext = (int)a.rows;
   g.k_ext = (int)a.piece; g.splits = a.splits;
-  hipError_t e = a.rows > kWideRows ? launch_gemm<T, 128, 128, 2, 2, 3, true, true, E_DX>(g, a, s)
+  hipError_t e = big_rows(a.rows)  ? launch_big<T, true, true, E_DX>(g, a, s)
+                 : a.rows > kWideRows ? launch_gemm<T, 128, 128, 2, 2, 3, true, true, E_DX>(g, a, s)
                                     : launch_gemm<T, 128, 32, 4, 1, 4, true, true, E_DX>(g, a, s);
   if (e != hipSuccess) return e;
   g.a = a.x; g.a_ld = a.x_ld; g.a_ext = a.dx_pad;
   g.b = a.gt; g.b_ld = a.rows_pad; g.b_ext = (int)a.piece;
   g.k_ext = (int)a.rows; g.splits = 1;
+  if (big_rows(a.rows)) return launch_big<T, true, false, E_DW>(g, a, s);
   return launch_gemm<T, 128, 128, 2, 2, 3, true, false, E_DW>(g, a, s);
 }
 
 }  // namespace
 
 int head_parts(bool, int64_t rows, int64_t classes) {
+  if (big_rows(rows)) return (int)((classes + 255) / 256) * 4;
   return (int)((classes + 127) / 128) * (rows > kWideRows ? 2 : 4);
 }
-int head_db_parts(bool, int64_t rows) { return rows > kWideRows ? (int)((rows + 127) / 128) * 2 : (int)((rows + 31) / 32); }
+int head_db_parts(bool, int64_t rows) {
+  if (big_rows(rows)) return (int)((rows + 255) / 256) * 4;
+  return rows > kWideRows ? (int)((rows + 127) / 128) * 2 : (int)((rows + 31) / 32);
+}
 int head_splits(bool, int64_t rows, int dim, int64_t piece) {
-  const int64_t br = rows > kWideRows ? 128 : 32;
-  const int64_t tiles = ((rows + br - 1) / br) * ((dim + 127) / 128);
+  const int64_t br = big_rows(rows) ? 256 : rows > kWideRows ? 128 : 32, ba = big_rows(rows) ? 256 : 128;
+  const int64_t tiles = ((rows + br - 1) / br) * ((dim + ba - 1) / ba);
   if (tiles == 0) return 1;
   int64_t s = (512 + tiles - 1) / tiles;           // two workgroups a CU
   const int64_t most = (piece + 511) / 512;        // at least 512 classes each
