@@ -22,6 +22,8 @@
 // cores' bf16 operands; 2^-8 of each entry at most, against 2^-8 of the
 // outputs' own rounding); sums, softmax statistics and the bias's gradient are
 // float32 throughout.
+#include <algorithm>
+
 #include "gemm_util.h"
 #include "tail.h"
 
@@ -71,9 +73,10 @@ __device__ __forceinline__ f32x16_t mma(f32x4_t a, f32x4_t b, f32x16_t c) {
 template <typename T, int R, bool KR, int WAVES>
 struct Side {
   static constexpr int V = 16 / (int)sizeof(T), KT = 128 / (int)sizeof(T);
-  static constexpr int LOADS = R / 8 / WAVES;  // DMAs of 1 KB a wave issues per k-tile
   static constexpr int BYTES = R * 128;
-  static_assert(LOADS * 8 * WAVES == R, "whole DMAs per wave");
+  static constexpr int LOADS = BYTES / 1024 / WAVES;  // DMAs of 1 KB a wave issues per k-tile
+  static_assert(LOADS * 1024 * WAVES == BYTES, "whole DMAs per wave");
+  static constexpr int KSTEPS = 4;             // MFMA k-steps of a k-tile
   static constexpr int CPR = KR ? R / V : 8;      // 16-byte slots of an LDS row (a power of two)
   static constexpr int RPD = 64 / CPR;            // LDS rows of one DMA
   static_assert(CPR <= 64, "a DMA covers whole LDS rows");
@@ -83,7 +86,9 @@ struct Side {
 
   static __device__ __forceinline__ int swz(int row) {
     if constexpr (!KR) return (row >> 1) & 7;
-    if constexpr (KR && sizeof(T) == 2) return (4 * (row & 3)) & (CPR - 1);
+    // 16-bit reads take 32 bytes of each of 4 rows
+    if constexpr (KR && sizeof(T) == 2 && CPR >= 16) return 4 * (row & 3);
+    if constexpr (KR && sizeof(T) == 2 && CPR == 8) return 4 * ((row >> 1) & 1);
     return 0;
   }
   __device__ __forceinline__ void init(int r0, int ext, int64_t ld, int wave, int lane) {
@@ -141,16 +146,34 @@ struct Side {
   }
 };
 
-// What the epilogue needs of the tile's reg side: the bias of its classes (-inf
-// past the last one), or its rows' info.
-template <int EPI, int BA, int THREADS>
-__device__ __forceinline__ void load_side(const Gemm &g, const HeadArgs &h, float2 *side_s, int a0, int t) {
-  if constexpr (EPI == E_STATS)
-    for (int i = t; i < BA; i += THREADS)
-      side_s[i].x = a0 + i < g.a_ext ? (h.bias ? h.bias[a0 + i] : 0.0f) : -INFINITY;
-  if constexpr (EPI == E_DLOGITS)
-    for (int i = t; i < BA; i += THREADS) side_s[i] = a0 + i < h.rows_pad ? h.info[a0 + i] : make_float2(INFINITY, 0.0f);
-}
+// What the epilogue needs of the tile's reg side, in LDS.  Forward: the bias of
+// its classes, -inf past the last one.  dz: its rows' largest logit and scale, and
+// for cross entropy the target class (in the piece; far off if none) and the
+// coefficient to take off there.
+template <int EPI, int BA>
+struct SideTable {
+  static constexpr int N = EPI == E_STATS || EPI == E_DLOGITS ? BA : 4;
+  float m[N];
+  float scale[EPI == E_DLOGITS ? BA : 4], coef[EPI == E_DLOGITS ? BA : 4];
+  int target[EPI == E_DLOGITS ? BA : 4];
+  template <int THREADS>
+  __device__ __forceinline__ void load(const Gemm &g, const HeadArgs &h, int a0, int t) {
+    if constexpr (EPI == E_STATS)
+      for (int i = t; i < BA; i += THREADS) m[i] = a0 + i < g.a_ext ? (h.bias ? h.bias[a0 + i] : 0.0f) : -INFINITY;
+    if constexpr (EPI == E_DLOGITS)
+      for (int i = t; i < BA; i += THREADS) {
+        const int n = a0 + i;
+        const float2 in = n < h.rows_pad ? h.info[n] : make_float2(INFINITY, 0.0f);
+        m[i] = in.x;
+        scale[i] = in.y;
+        if (!h.teacher) {
+          const int id = n < h.rows ? h.id32[n] : -1;
+          target[i] = id >= 0 ? id - (int)h.v0 : INT32_MIN / 2;
+          coef[i] = n < h.rows ? h.cq[n] : 0.0f;
+        }
+      }
+  }
+};
 
 // Where a wave's blocks lie: block (i, j) is out[lane(j) + lane % 32][reg(i) + 8 q +
 // 4 lh + e] = acc[i][j][4 q + e]; part: which of the reg side's parts the wave holds.
@@ -161,84 +184,114 @@ struct Place {
   __device__ __forceinline__ int lane(int j) const { return l0 + (j >> 1) * LANE_B + (j & 1) * LANE_A; }
 };
 
-template <typename T, int EPI, int TA, int TB, typename P>
+template <typename T, int EPI, int TA, int TB, typename P, typename S>
 __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x16_t (&acc)[TA][TB], const P &at,
-                                         const float2 *side_s, int split, int lane) {
+                                         const S &side, int split, int lane) {
   const int lh = lane >> 5;
   if constexpr (EPI == E_STATS) {
     const float c = kLog2e * h.inv_t;
+    float m[TB], s[TB];
+#pragma unroll
+    for (int j = 0; j < TB; ++j) m[j] = -INFINITY, s[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TA; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4_t bias = *reinterpret_cast<const f32x4_t *>(side.m + (at.reg(i) - at.a0 + 8 * q + 4 * lh));
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            acc[i][j][4 * q + e] += bias[e];
+            m[j] = fmaxf(m[j], acc[i][j][4 * q + e]);
+          }
+      }
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
-      float m = -INFINITY;
+      m[j] = fmaxf(m[j], __shfl_xor(m[j], 32, 64));
+      const float mm = m[j] == -INFINITY ? 0.0f : m[j];  // no class with weight: the sum is 0, not NaN
 #pragma unroll
       for (int i = 0; i < TA; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          acc[i][j][r] += side_s[at.reg(i) - at.a0 + 8 * (r >> 2) + 4 * lh + (r & 3)].x;
-          m = fmaxf(m, acc[i][j][r]);
-        }
-      m = fmaxf(m, __shfl_xor(m, 32, 64));
-      const float mm = m == -INFINITY ? 0.0f : m;  // no class with weight: the sum is 0, not NaN
-      float s = 0.0f;
-#pragma unroll
-      for (int i = 0; i < TA; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - mm) * c);
-      s += __shfl_xor(s, 32, 64);
+        for (int r = 0; r < 16; ++r) s[j] += __builtin_amdgcn_exp2f((acc[i][j][r] - mm) * c);
+      s[j] += __shfl_xor(s[j], 32, 64);
       const int row = at.lane(j) + (lane & 31);
-      if (lh == 0 && row < g.b_ext) h.part[(int64_t)at.part * h.rows + row] = make_float2(m, s);
+      if (lh == 0 && row < g.b_ext) h.part[(int64_t)at.part * h.rows + row] = make_float2(m[j], s[j]);
     }
   }
   if constexpr (EPI == E_DLOGITS) {
     T *gt = static_cast<T *>(h.gt);
     const float c = kLog2e * h.inv_t;
+    float sum[TB], bias[TB];
+    int cls[TB];  // in the piece
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
-      const int cls = at.lane(j) + (lane & 31);  // in the piece
-      const bool live = cls < g.b_ext;
-      const float bias = live && h.bias ? h.bias[h.v0 + cls] : 0.0f;
-      float sum = 0.0f;
+      cls[j] = at.lane(j) + (lane & 31);
+      bias[j] = h.bias && cls[j] < g.b_ext ? h.bias[h.v0 + cls[j]] : 0.0f;
+      sum[j] = 0.0f;
+    }
 #pragma unroll
-      for (int i = 0; i < TA; ++i) {
+    for (int i = 0; i < TA; ++i) {
+      const int a = at.reg(i), loc = a - at.a0;
+      // a row's target lies in few of the blocks: the others compare nothing
+      bool hit[TB];
+      const int tg = h.teacher ? INT32_MIN / 2 : side.target[loc + (lane & 31)];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float2 in = side_s[at.reg(i) - at.a0 + 8 * (r >> 2) + 4 * lh + (r & 3)];
-          const float z = acc[i][j][r] + bias;
-          const float v = __builtin_amdgcn_exp2f((z - in.x) * c) * in.y;
-          acc[i][j][r] = v;
-          sum += v;
+      for (int j = 0; j < TB; ++j) hit[j] = __ballot((unsigned)(tg - at.lane(j)) < 32u) != 0;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        f32x4_t m[2], sc[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          m[u] = *reinterpret_cast<const f32x4_t *>(side.m + (loc + 16 * p + 8 * u + 4 * lh));
+          sc[u] = *reinterpret_cast<const f32x4_t *>(side.scale + (loc + 16 * p + 8 * u + 4 * lh));
         }
-        const int a = at.reg(i);
-        T *o = gt + (int64_t)cls * h.rows_pad + a;
-        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            float v[8];
+        for (int j = 0; j < TB; ++j) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            v[e] = __builtin_amdgcn_exp2f((acc[i][j][8 * p + e] + bias[j] - m[e >> 2][e & 3]) * c) * sc[e >> 2][e & 3];
+          if (hit[j]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int n = loc + 16 * p + 8 * (e >> 2) + 4 * lh + (e & 3);
+              v[e] -= side.target[n] == cls[j] ? side.coef[n] : 0.0f;
+            }
+          }
+          if (h.db_part) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[j] += v[e];
+          }
+          T *o = gt + (int64_t)cls[j] * h.rows_pad + a + 16 * p;
+          if constexpr (sizeof(T) == 2) {
+            float w[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][8 * p + e]),
-                                                               __float_as_uint(acc[i][j][8 * p + 4 + e]), false, false);
-              v[e] = __uint_as_float(s2[0]);
-              v[4 + e] = __uint_as_float(s2[1]);
+              const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[e]), __float_as_uint(v[4 + e]), false, false);
+              w[e] = __uint_as_float(s2[0]);
+              w[4 + e] = __uint_as_float(s2[1]);
             }
-            const int n = 16 * p + 8 * lh;
-            if (live && a + n < h.rows_pad)
+            const int n = 8 * lh;
+            if (cls[j] < g.b_ext && a + 16 * p + n < h.rows_pad)
               *reinterpret_cast<uint4 *>(o + n) =
-                  make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
-          }
-        } else {
+                  make_uint4(f2bf2(w[0], w[1]), f2bf2(w[2], w[3]), f2bf2(w[4], w[5]), f2bf2(w[6], w[7]));
+          } else {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int n = 8 * q + 4 * lh;
-            if (live && a + n < h.rows_pad)
-              *reinterpret_cast<float4 *>(o + n) =
-                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            for (int u = 0; u < 2; ++u) {
+              const int n = 8 * u + 4 * lh;
+              if (cls[j] < g.b_ext && a + 16 * p + n < h.rows_pad)
+                *reinterpret_cast<float4 *>(o + n) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+            }
           }
         }
       }
-      if (h.db_part) {
-        sum += __shfl_xor(sum, 32, 64);
-        if (lh == 0 && live) h.db_part[(int64_t)at.part * h.classes + h.v0 + cls] = sum;
+    }
+    if (h.db_part) {
+#pragma unroll
+      for (int j = 0; j < TB; ++j) {
+        sum[j] += __shfl_xor(sum[j], 32, 64);
+        if (lh == 0 && cls[j] < g.b_ext) h.db_part[(int64_t)at.part * h.classes + h.v0 + cls[j]] = sum[j];
       }
     }
   }
@@ -318,18 +371,20 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
 }
 
 template <typename T, int BA, int BB, int WA, int WB, int ST, bool KRA, bool KRB, int EPI>
-__global__ __launch_bounds__(64 * WA * WB) void head_gemm_kernel(Gemm g, HeadArgs h) {
+struct RingTile {
+  static constexpr int THREADS = 64 * WA * WB, TILE_A = BA, TILE_B = BB;
+  static constexpr int SMEM = ST * (BA + BB) * 128;
+  typedef SideTable<EPI, BA> Sides;
+  // One barrier a k-tile, ST stages of LDS.
+  static __device__ __forceinline__ void run(const Gemm &g, const HeadArgs &h, uint8_t *smem, Sides &side, int bid) {
   constexpr int WAVES = WA * WB, TA = BA / WA / 32, TB = BB / WB / 32;
   typedef Side<T, BA, KRA, WAVES> SA;
   typedef Side<T, BB, KRB, WAVES> SB;
   constexpr int STAGE = SA::BYTES + SB::BYTES;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[ST * STAGE];
-  __shared__ __attribute__((aligned(16))) float2 side_s[EPI == E_STATS || EPI == E_DLOGITS ? BA : 1];
 
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wa = wave / WB, wb = wave % WB;
-  const int bid = xcd_remap(blockIdx.x, gridDim.x);
   const int tiles = g.tiles_a * g.tiles_b;
   const int split = bid / tiles, tile = bid % tiles;
   // the smaller side of the grid runs fastest, so the larger one's operand is
@@ -340,8 +395,7 @@ __global__ __launch_bounds__(64 * WA * WB) void head_gemm_kernel(Gemm g, HeadArg
   const int nkt = (g.k_ext + SA::KT - 1) / SA::KT;
   const int kt0 = (int)((int64_t)nkt * split / g.splits), kt1 = (int)((int64_t)nkt * (split + 1) / g.splits);
   const int nk = kt1 - kt0;
-
-  load_side<EPI, BA, 64 * WAVES>(g, h, side_s, a0, t);
+  side.template load<THREADS>(g, h, a0, t);
 
   SA sa;
   SB sb;
@@ -386,40 +440,41 @@ __global__ __launch_bounds__(64 * WA * WB) void head_gemm_kernel(Gemm g, HeadArg
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    issue();
     const uint8_t *at = smem + (kt % ST) * STAGE, *bt = at + SA::BYTES;
+    // Fragments ahead of the MFMAs: a whole k-tile's where a wave has one block
+    // (nothing else covers the LDS's latency), else one k-step's.
+    constexpr int AHEAD = TA * TB == 1 ? SA::KSTEPS : 1, BUFS = AHEAD == 1 ? 2 : AHEAD;
+    typename Elem<T>::Frag fa[BUFS][TA], fb[BUFS][TB];
+    auto read = [&](int ks) {
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      typename Elem<T>::Frag fa[TA], fb[TB];
+      for (int i = 0; i < TA; ++i) fa[ks % BUFS][i] = SA::frag(at, (wa * TA + i) * 32, ks, lane);
 #pragma unroll
-      for (int i = 0; i < TA; ++i) fa[i] = SA::frag(at, (wa * TA + i) * 32, ks, lane);
+      for (int j = 0; j < TB; ++j) fb[ks % BUFS][j] = SB::frag(bt, (wb * TB + j) * 32, ks, lane);
+    };
 #pragma unroll
-      for (int j = 0; j < TB; ++j) fb[j] = SB::frag(bt, (wb * TB + j) * 32, ks, lane);
+    for (int ks = 0; ks < AHEAD; ++ks) read(ks);
+    __builtin_amdgcn_sched_barrier(0);
+    issue();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < SA::KSTEPS; ++ks) {
+      if (AHEAD == 1 && ks + 1 < SA::KSTEPS) read(ks + 1);
+      if (AHEAD == 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < TA; ++i)
 #pragma unroll
-        for (int j = 0; j < TB; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
+        for (int j = 0; j < TB; ++j) acc[i][j] = mma(fa[ks % BUFS][i], fb[ks % BUFS][j], acc[i][j]);
+      if (AHEAD == 1) __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // No DMA may outlive the workgroup's LDS, and side_s is read by all waves.
+  // No DMA may outlive the workgroup's LDS, and the side table is read by all waves.
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __syncthreads();
 
   const Place<32, 32, 64> at = {a0, a0 + wa * TA * 32, b0 + wb * TB * 32, ta * WA + wa};
-  epilogue<T, EPI>(g, h, acc, at, side_s, split, lane);
-}
-
-template <typename T, int BA, int BB, int WA, int WB, int ST, bool KRA, bool KRB, int EPI>
-hipError_t launch_gemm(Gemm g, const HeadArgs &h, hipStream_t s) {
-  g.tiles_a = (g.a_ext + BA - 1) / BA;
-  g.tiles_b = (g.b_ext + BB - 1) / BB;
-  const int64_t blocks = (int64_t)g.tiles_a * g.tiles_b * g.splits;
-  if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hapi_launch((head_gemm_kernel<T, BA, BB, WA, WB, ST, KRA, KRB, EPI>), dim3((uint32_t)blocks), dim3(64 * WA * WB), 0, s,
-              g, h);
-  return hipGetLastError();
-}
+  epilogue<T, EPI>(g, h, acc, at, side, split, lane);
+  }
+};
 
 // The same product on 256 x 256 tiles.  Eight waves, two per SIMD: wave (g, c)
 // owns rows 64 g .. + 63 of both 128-row halves of B and rows 32 c .. + 31 of both
@@ -429,7 +484,11 @@ hipError_t launch_gemm(Gemm g, const HeadArgs &h, hipStream_t s) {
 // slot apart, so one group's MFMAs cover the other's LDS reads.  Two stages of
 // 64 KB; half a stage is loaded again as soon as both groups have read it.
 template <typename T, bool KRA, bool KRB, int EPI>
-__device__ __forceinline__ void big_tile(const Gemm &g, const HeadArgs &h, uint8_t *smem, float2 *side_s, int bid) {
+struct BigTile {
+  static constexpr int THREADS = 512, TILE_A = 256, TILE_B = 256;
+  static constexpr int SMEM = 2 * 512 * 128;
+  typedef SideTable<EPI, 256> Sides;
+  static __device__ __forceinline__ void run(const Gemm &g, const HeadArgs &h, uint8_t *smem, Sides &side, int bid) {
   typedef Side<T, 128, KRA, 8> SA;
   typedef Side<T, 128, KRB, 8> SB;
   constexpr int HALF = SA::BYTES, STAGE = 4 * HALF;  // B halves 0, 1, A halves 0, 1
@@ -445,7 +504,7 @@ __device__ __forceinline__ void big_tile(const Gemm &g, const HeadArgs &h, uint8
   const int nkt = (g.k_ext + SA::KT - 1) / SA::KT;
   const int kt0 = (int)((int64_t)nkt * split / g.splits), kt1 = (int)((int64_t)nkt * (split + 1) / g.splits);
   const int nk = kt1 - kt0;
-  load_side<EPI, 256, 512>(g, h, side_s, a0, t);
+  side.template load<THREADS>(g, h, a0, t);
 
   SA sa[2];
   SB sb[2];
@@ -549,26 +608,52 @@ __device__ __forceinline__ void big_tile(const Gemm &g, const HeadArgs &h, uint8
   // No DMA may outlive the workgroup's LDS (the last ones read nothing).
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   const Place<128, 32, 128> at = {a0, a0 + wn * 32, b0 + wm * 64, ta * 4 + wn};
-  epilogue<T, EPI>(g, h, acc, at, side_s, split, lane);
+  epilogue<T, EPI>(g, h, acc, at, side, split, lane);
+  }
+};
+
+// One product a launch.
+template <typename Tile>
+__global__ __launch_bounds__(Tile::THREADS) void head_product_kernel(Gemm g, HeadArgs h) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[Tile::SMEM];
+  __shared__ __attribute__((aligned(16))) typename Tile::Sides side;
+  Tile::run(g, h, smem, side, xcd_remap(blockIdx.x, gridDim.x));
 }
 
-constexpr int kBigSmem = 8 * 128 * 128;
-
-template <typename T, bool KRA, bool KRB, int EPI>
-__global__ __launch_bounds__(512) void head_big_kernel(Gemm g, HeadArgs h) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[kBigSmem];
-  __shared__ __attribute__((aligned(16))) float2 side_s[EPI == E_STATS || EPI == E_DLOGITS ? 256 : 1];
-  big_tile<T, KRA, KRB, EPI>(g, h, smem, side_s, xcd_remap(blockIdx.x, gridDim.x));
+// Both products of dz^T in one launch, dx's workgroups first: each fills the
+// CUs that the other's last round leaves idle.
+template <typename DX, typename DW>
+__global__ __launch_bounds__(DX::THREADS) void head_grads_kernel(Gemm gx, Gemm gw, int nx, HeadArgs h) {
+  static_assert(DX::THREADS == DW::THREADS, "one block size");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[DX::SMEM > DW::SMEM ? DX::SMEM : DW::SMEM];
+  const int b = blockIdx.x;
+  typename DX::Sides sx;  // of no use to these epilogues
+  typename DW::Sides sw;
+  if (b < nx) DX::run(gx, h, smem, sx, xcd_remap(b, nx));
+  else DW::run(gw, h, smem, sw, xcd_remap(b - nx, gridDim.x - nx));
 }
 
-template <typename T, bool KRA, bool KRB, int EPI>
-hipError_t launch_big(Gemm g, const HeadArgs &h, hipStream_t s) {
-  g.tiles_a = (g.a_ext + 255) / 256;
-  g.tiles_b = (g.b_ext + 255) / 256;
-  const int64_t blocks = (int64_t)g.tiles_a * g.tiles_b * g.splits;
+template <typename Tile>
+int64_t count_tiles(Gemm &g) {
+  g.tiles_a = (g.a_ext + Tile::TILE_A - 1) / Tile::TILE_A;
+  g.tiles_b = (g.b_ext + Tile::TILE_B - 1) / Tile::TILE_B;
+  return (int64_t)g.tiles_a * g.tiles_b * g.splits;
+}
+
+template <typename Tile>
+hipError_t launch_product(Gemm g, const HeadArgs &h, hipStream_t s) {
+  const int64_t blocks = count_tiles<Tile>(g);
   if (blocks == 0) return hipSuccess;
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hapi_launch((head_big_kernel<T, KRA, KRB, EPI>), dim3((uint32_t)blocks), dim3(512), 0, s, g, h);
+  hapi_launch(head_product_kernel<Tile>, dim3((uint32_t)blocks), dim3(Tile::THREADS), 0, s, g, h);
+  return hipGetLastError();
+}
+
+template <typename DX, typename DW>
+hipError_t launch_grads(Gemm gx, Gemm gw, const HeadArgs &h, hipStream_t s) {
+  const int64_t nx = count_tiles<DX>(gx), nw = count_tiles<DW>(gw);
+  if (nx + nw > 0x7fffffff) return hipErrorInvalidValue;
+  hapi_launch((head_grads_kernel<DX, DW>), dim3((uint32_t)(nx + nw)), dim3(DX::THREADS), 0, s, gx, gw, (int)nx, h);
   return hipGetLastError();
 }
 
@@ -580,10 +665,9 @@ __device__ __forceinline__ void put(uint16_t *p, float v) { *p = f2bf(v); }
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 
 // out[r][0 .. ld_out) = in[r][0 .. dim), zeros behind; a thread per 16 bytes.
-// info (optional): rows whose coefficient is 0 become zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void stage_kernel(const T *__restrict__ in, int64_t ld_in, T *__restrict__ out,
-                                                    int64_t ld_out, int64_t rows, int dim, const float2 *info) {
+                                                    int64_t ld_out, int64_t rows, int dim) {
   constexpr int V = 16 / (int)sizeof(T);
   const int64_t per = ld_out / V;
   const int64_t n = rows * per;
@@ -592,14 +676,12 @@ __global__ __launch_bounds__(256) void stage_kernel(const T *__restrict__ in, in
     const int d = (int)(i - r * per) * V;
     const T *p = in + r * ld_in + d;
     T v[V] = {};
-    if (!info || info[r].y != 0.0f) {
-      if (d + V <= dim) {
-        __builtin_memcpy(v, p, 16);
-      } else {
+    if (d + V <= dim) {
+      __builtin_memcpy(v, p, 16);
+    } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (d + j < dim) v[j] = p[j];
-      }
+      for (int j = 0; j < V; ++j)
+        if (d + j < dim) v[j] = p[j];
     }
     uint4 q;
     __builtin_memcpy(&q, v, 16);
@@ -618,25 +700,36 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// x[row] . w[id] by one wave.
-template <typename T>
-__device__ __forceinline__ float wave_dot(const T *x, const T *w, int dim, int lane) {
+// x . w[id] of up to K classes at once by one wave (ids < 0: 0), w's rows ld apart:
+// the K rows' loads are in flight together.
+template <typename T, int K>
+__device__ __forceinline__ void wave_dots(const T *x, const T *w, int64_t ld, const int64_t (&id)[K], int dim, int lane,
+                                          float (&s)[K]) {
   constexpr int V = 16 / (int)sizeof(T);
-  float s = 0.0f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) s[k] = 0.0f;
   for (int d = lane * V; d < dim; d += 64 * V) {
-    T a[V], b[V];
+    T a[V], b[K][V];
     if (d + V <= dim) {
       __builtin_memcpy(a, x + d, 16);
-      __builtin_memcpy(b, w + d, 16);
 #pragma unroll
-      for (int j = 0; j < V; ++j) s = fmaf(to_f(a[j]), to_f(b[j]), s);
+      for (int k = 0; k < K; ++k) __builtin_memcpy(b[k], w + (id[k] < 0 ? 0 : id[k]) * ld + d, 16);
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[k] = fmaf(to_f(a[j]), to_f(b[k][j]), s[k]);
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (d + j < dim) s = fmaf(to_f(x[d + j]), to_f(w[d + j]), s);
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (d + j < dim) s[k] = fmaf(to_f(x[d + j]), to_f(w[(id[k] < 0 ? 0 : id[k]) * ld + d + j]), s[k]);
     }
   }
-  return wave_sum(s);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < K; ++k) s[k] += __shfl_xor(s[k], o, 64);
 }
 
 // Joins a row's partial statistics and forms its loss: 16 rows a block, 64
@@ -690,9 +783,11 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
     if (id >= h.classes) {
       loss = NAN;
     } else if (id >= 0) {
-      float z = wave_dot(x, w + id * h.w_in_ld, h.dim, lane);
-      if (h.bias) z += h.bias[id];
-      loss = (m - z) + l;
+      const int64_t one[1] = {id};
+      float z[1];
+      wave_dots<T, 1>(x, w, h.w_in_ld, one, h.dim, lane, z);
+      if (h.bias) z[0] += h.bias[id];
+      loss = (m - z[0]) + l;
     }
     if (lane == 0) h.loss[n] = loss;
     return;
@@ -715,41 +810,55 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
   ts = wave_sum(ts);
   const float lts = logf(ts);
   float loss = 0.0f;
-  for (int k = 0; k < h.top; ++k) {
-    const int64_t id = ids[k];
-    float z = 0.0f;
-    if (id >= 0 && id < h.classes) {
-      z = wave_dot(x, w + id * h.w_in_ld, h.dim, lane);
-      if (h.bias) z += h.bias[id];
-      const float u = (te[k] - tm) * h.inv_t;
-      const float q = __builtin_amdgcn_exp2f(u * kLog2e) / ts;
-      // an entry without weight adds nothing, whatever its logit
-      if (q > 0.0f) loss += q * ((u - lts) + ((m - z) * h.inv_t + l));
+  constexpr int KB = 8;
+  for (int k0 = 0; k0 < h.top; k0 += KB) {
+    int64_t id[KB];
+    float z[KB];
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+      const int64_t v = k0 + k < h.top ? ids[k0 + k] : -1;
+      id[k] = v < h.classes ? v : -1;
     }
-    if (lane == 0) h.picked[n * h.top + k] = z;
+    wave_dots<T, KB>(x, w, h.w_in_ld, id, h.dim, lane, z);
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+      if (k0 + k >= h.top) continue;
+      if (id[k] >= 0) {
+        if (h.bias) z[k] += h.bias[id[k]];
+        const float u = (te[k0 + k] - tm) * h.inv_t;
+        const float q = __builtin_amdgcn_exp2f(u * kLog2e) / ts;
+        // an entry without weight adds nothing, whatever its logit
+        if (q > 0.0f) loss += q * ((u - lts) + ((m - z[k]) * h.inv_t + l));
+      }
+      if (lane == 0) h.picked[n * h.top + k0 + k] = id[k] >= 0 ? z[k] : 0.0f;
+    }
   }
   if (lane == 0) h.loss[n] = bad != 0.0f ? NAN : none ? 0.0f : h.t * h.t * loss;
 }
 
-// Row info of the backward pass, a wave per row: the largest logit m and the
-// coefficient over the sum of exp((z - m) / T), so that dz = exp((z - m) / T) times
-// it, or (inf, 0) for a row that does not count; distillation's weights q.
-__global__ __launch_bounds__(256) void head_info_kernel(HeadArgs h) {
+// What the backward pass needs of a row, a wave per row: its largest logit m and
+// the coefficient over the sum of exp((z - m) / T), so that dz = exp((z - m) / T)
+// times it, or (inf, 0) for a row that does not count; the targets as 32-bit
+// classes (-1: none) with the weight to take off there; and a copy of x whose rows
+// that do not count are zero, so that nothing they hold reaches a sum.
+template <typename T>
+__global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__restrict__ xs, int64_t xs_ld) {
+  constexpr int V = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 63;
   const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (n >= h.rows_pad) return;
   float2 info = make_float2(INFINITY, 0.0f);
   if (n < h.rows) {
+    const int64_t *ids = h.ids + n * h.top;
     float coef = h.dloss[n] * h.t;
-    bool none;
     float bad = 0.0f;
+    bool none;
+    float tm = -INFINITY, ts = 1.0f;
     if (!h.teacher) {
-      none = h.ids[n] < 0;
-      if (h.ids[n] >= h.classes) bad = 1.0f;
+      none = ids[0] < 0;
+      if (ids[0] >= h.classes) bad = 1.0f;
     } else {
-      const int64_t *ids = h.ids + n * h.top;
       const float *te = h.teacher + n * h.top;
-      float tm = -INFINITY;
       for (int k = lane; k < h.top; k += 64)
         if (ids[k] >= 0) {
           tm = fmaxf(tm, te[k]);
@@ -758,113 +867,161 @@ __global__ __launch_bounds__(256) void head_info_kernel(HeadArgs h) {
       tm = wave_max(tm);
       bad = wave_max(bad);
       none = tm == -INFINITY && bad == 0.0f;
-      float ts = 0.0f;
+      ts = 0.0f;
       for (int k = lane; k < h.top; k += 64)
         if (ids[k] >= 0 && !none) ts += __builtin_amdgcn_exp2f((te[k] - tm) * kLog2e * h.inv_t);
       ts = wave_sum(ts);
-      for (int k = lane; k < h.top; k += 64)
-        h.q[n * h.top + k] = ids[k] >= 0 && !none ? __builtin_amdgcn_exp2f((te[k] - tm) * kLog2e * h.inv_t) / ts : 0.0f;
     }
     if (bad != 0.0f) coef = NAN;
-    if (!none && coef != 0.0f) {
+    const bool counts = !none && coef != 0.0f;
+    if (counts) {
       const float2 st = h.stats[n];
       info = make_float2(st.x, coef * __builtin_amdgcn_exp2f(-st.y * kLog2e));
+    }
+    for (int k = lane; k < h.top; k += 64) {
+      const bool entry = counts && ids[k] >= 0 && ids[k] < h.classes;
+      h.id32[n * h.top + k] = entry ? (int)ids[k] : -1;
+      const float q = h.teacher ? __builtin_amdgcn_exp2f((h.teacher[n * h.top + k] - tm) * kLog2e * h.inv_t) / ts : 1.0f;
+      h.cq[n * h.top + k] = entry ? coef * q : 0.0f;
+    }
+    const T *p = static_cast<const T *>(h.x_in) + n * h.x_in_ld;
+    for (int d = lane * V; d < xs_ld; d += 64 * V) {
+      T v[V] = {};
+      if (counts) {
+        if (d + V <= h.dim) {
+          __builtin_memcpy(v, p + d, 16);
+        } else {
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (d + j < h.dim) v[j] = p[d + j];
+        }
+      }
+      uint4 q;
+      __builtin_memcpy(&q, v, 16);
+      *reinterpret_cast<uint4 *>(xs + n * xs_ld + d) = q;
     }
   }
   if (lane == 0) h.info[n] = info;
 }
 
-// The targets' entries of dz^T: coefficient (p - q), q summed over the row's
-// entries of the same class (equal entries write equal values).
+// Distillation's entries of dz^T: coefficient p less the weights of the row's
+// entries of this class (entries of one class write equal values).
 template <typename T>
 __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= h.rows * h.top) return;
-  const int64_t n = i / h.top;
-  const int64_t id = h.ids[i];
+  const int id = h.id32[i];
   if (id < h.v0 || id >= h.v0 + h.piece) return;
+  const int64_t n = i / h.top;
   const float2 info = h.info[n];
-  if (info.y == 0.0f) return;
-  float p, q;
-  const float coef = h.dloss[n] * h.t;
-  if (!h.teacher) {
-    p = __builtin_amdgcn_exp2f(-h.loss[n] * kLog2e);
-    q = 1.0f;
-  } else {
-    p = __builtin_amdgcn_exp2f(((h.picked[i] - info.x) * h.inv_t - h.stats[n].y) * kLog2e);
-    q = 0.0f;
-    for (int k = 0; k < h.top; ++k)
-      if (h.ids[n * h.top + k] == id) q += h.q[n * h.top + k];
-  }
-  put(static_cast<T *>(h.gt) + (id - h.v0) * h.rows_pad + n, coef * (p - q));
+  float v = __builtin_amdgcn_exp2f((h.picked[i] - info.x) * h.inv_t * kLog2e) * info.y;
+  for (int k = 0; k < h.top; ++k)
+    if (h.id32[n * h.top + k] == id) v -= h.cq[n * h.top + k];
+  put(static_cast<T *>(h.gt) + (id - h.v0) * h.rows_pad + n, v);
 }
 
-// dx[n][d] = the splits' partial sums in order, 0 in rows that do not count.
+// dx[n][d] = the splits' partial sums in order, 0 in rows that do not count; in
+// blocks [0, nx) of the launch.  dbias, in the others, 128 classes a block: the row
+// parts' sums of dz's softmax part in order (dz whole for cross entropy), and for
+// distillation less the targets' weights: the block goes through all entries,
+// 8192 a round, keeps those of its classes in a list in a fixed order, and eight
+// threads a class each take every eighth entry of the list.  Fixed orders, so
+// results do not vary.
+constexpr int kReduceThreads = 1024, kBiasClasses = 128, kBiasRound = 8 * kReduceThreads;
 template <typename T>
-__global__ __launch_bounds__(256) void head_dx_kernel(HeadArgs h) {
-  const int per = (h.dim + 3) / 4;
-  const int64_t total = h.rows * per;
-  T *dx = static_cast<T *>(h.dx);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t n = i / per;
-    const int d = (int)(i - n * per) * 4;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (h.info[n].y != 0.0f)
-      for (int s = 0; s < h.splits; ++s) {
-        const float4 u = *reinterpret_cast<const float4 *>(h.dx_part + ((int64_t)s * h.rows + n) * h.dx_pad + d);
-        v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
-      }
-    T *o = dx + n * h.dx_ld + d;
+__global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h, int nx) {
+  __shared__ float sums[8][kBiasClasses];
+  __shared__ int cnt[16];
+  __shared__ uint8_t list_c[kBiasRound];
+  __shared__ float list_v[kBiasRound];
+  const int t = threadIdx.x;
+  if ((int)blockIdx.x < nx) {
+    const int per = (h.dim + 3) / 4;
+    const int64_t total = h.rows * per;
+    T *dx = static_cast<T *>(h.dx);
+    for (int64_t i = (int64_t)blockIdx.x * kReduceThreads + t; i < total; i += (int64_t)nx * kReduceThreads) {
+      const int64_t n = i / per;
+      const int d = (int)(i - n * per) * 4;
+      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (h.info[n].y != 0.0f)
+        for (int s = 0; s < h.splits; ++s) {
+          const float4 u = *reinterpret_cast<const float4 *>(h.dx_part + ((int64_t)s * h.rows + n) * h.dx_pad + d);
+          v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+        }
+      T *o = dx + n * h.dx_ld + d;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (d + j < h.dim) put(o + j, v[j]);
+      for (int j = 0; j < 4; ++j)
+        if (d + j < h.dim) put(o + j, v[j]);
+    }
+    return;
   }
-}
-
-// dbias of 256 classes a block: the row parts' sums of coefficient p in order,
-// less the targets' coefficient q.  The block goes through all targets, 256 a
-// round, and keeps those of its classes in a list in their order; each thread
-// then takes its own class's entries from it.
-__global__ __launch_bounds__(256) void head_dbias_kernel(HeadArgs h) {
-  __shared__ int cnt[4];
-  __shared__ int list_c[256];
-  __shared__ float list_v[256];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int64_t c0 = (int64_t)blockIdx.x * 256;
-  const int64_t cls = c0 + t;
+  const int lane = t & 63, wave = t >> 6;
+  const int64_t c0 = (int64_t)(blockIdx.x - nx) * kBiasClasses;
+  const int slice = t / kBiasClasses, mine = t % kBiasClasses;
   float sum = 0.0f;
-  if (cls < h.classes)
-    for (int p = 0; p < h.db_parts; ++p) sum += h.db_part[(int64_t)p * h.classes + cls];
-  const int64_t total = h.rows * h.top;
-  float less = 0.0f;
-  for (int64_t i0 = 0; i0 < total; i0 += 256) {
-    const int64_t i = i0 + t;
-    const int64_t id = i < total ? h.ids[i] : -1;
-    const bool hit = id >= c0 && id < c0 + 256;
-    const uint64_t mask = __ballot(hit);
-    if (lane == 0) cnt[wave] = __popcll(mask);
-    __syncthreads();
-    int base = 0, n = 0;
+  if (c0 + mine < h.classes)
+    for (int p = slice; p < h.db_parts; p += 8) sum += h.db_part[(int64_t)p * h.classes + c0 + mine];
+  const int64_t total = h.teacher ? h.rows * h.top : 0;
+  // entries 4 t .. + 3 of each half of a round; a round's are loaded during the last one's
+  int4 nx4[2];
+  auto fetch = [&](int64_t i0) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) base += cnt[w];
-      n += cnt[w];
-    }
-    if (n > 0) {
-      if (hit) {
-        const int at = base + __popcll(mask & ((1ull << lane) - 1));
-        const int64_t n1 = i / h.top;
-        const float coef = h.info[n1].y != 0.0f ? h.dloss[n1] * h.t : 0.0f;
-        list_c[at] = (int)(id - c0);
-        list_v[at] = h.teacher ? coef * h.q[i] : coef;
+    for (int u = 0; u < 2; ++u) {
+      const int64_t i = i0 + u * (kBiasRound / 2) + 4 * t;
+      if (i + 4 <= total) {
+        nx4[u] = *reinterpret_cast<const int4 *>(h.id32 + i);
+      } else {
+        int v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = i + k < total ? h.id32[i + k] : -1;
+        nx4[u] = make_int4(v[0], v[1], v[2], v[3]);
       }
-      __syncthreads();
-      for (int k = 0; k < n; ++k)
-        if (list_c[k] == t) less += list_v[k];
     }
+  };
+  fetch(0);
+  for (int64_t i0 = 0; i0 < total; i0 += kBiasRound) {
+    const int c = (int)c0;
+    const int id[8] = {nx4[0].x - c, nx4[0].y - c, nx4[0].z - c, nx4[0].w - c,
+                       nx4[1].x - c, nx4[1].y - c, nx4[1].z - c, nx4[1].w - c};
+    fetch(i0 + kBiasRound);
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) n += (unsigned)id[k] < (unsigned)kBiasClasses;
+    int before = n;  // entries up to this lane's
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(before, o, 64);
+      if (lane >= o) before += u;
+    }
+    if (lane == 63) cnt[wave] = before;
     __syncthreads();
+    int at = before - n, all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) at += cnt[w];
+      all += cnt[w];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if ((unsigned)id[k] < (unsigned)kBiasClasses) {
+        list_c[at] = (uint8_t)id[k];
+        list_v[at] = h.cq[i0 + (k >> 2) * (kBiasRound / 2) + 4 * t + (k & 3)];
+        ++at;
+      }
+    __syncthreads();
+    for (int k = slice; k < all; k += 8)
+      if (list_c[k] == mine) sum -= list_v[k];
+    // the next round's counts are written before its first barrier, read after
+    // it; its list is written after it
   }
-  if (cls < h.classes) h.dbias[cls] = sum - less;
+  sums[slice][mine] = sum;
+  __syncthreads();
+  if (slice == 0 && c0 + mine < h.classes) {
+    float v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v += sums[k][mine];
+    h.dbias[c0 + mine] = v;
+  }
 }
 
 int grid_for(int64_t n, int per) {
@@ -872,9 +1029,87 @@ int grid_for(int64_t n, int per) {
   return (int)(b < 1 ? 1 : b > 16384 ? 16384 : b);
 }
 
-// Rows at which the row side of a tile is 128 wide; below, 32.
-constexpr int kWideRows = 64;
-bool big_rows(int64_t rows) { return rows > 512; }
+// ---------------------------------------------------------------- variants
+
+// Tiles of the products.  FEW: up to 32 rows, the weights stream past.
+enum Variant { BIG, MID, SMALL, FEW, TINY };
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t kCus = 256;
+
+Variant variant(bool bf16, int64_t rows, int64_t classes) {
+  // The smallest calls: a k-tile costs a workgroup some 0.3 us of loads, LDS reads
+  // and MFMAs one after the other, whatever the tile, so one-wave tiles over more CUs
+  // lose nothing (128 x 2048 x 1000: 14.0 us, 32 workgroups of 64 x 64 tiles
+  // 13.6 us; 8 x 768 x 1000: 7.4 us, 8 workgroups of 32 x 128 tiles 8.4 us).
+  if (ceil_div(rows, 32) * ceil_div(classes, 32) <= kCus) return TINY;
+  if (rows <= 32) return FEW;
+  const int64_t big = ceil_div(rows, 256) * ceil_div(classes, 256), mid = ceil_div(rows, 128) * ceil_div(classes, 128),
+                small = ceil_div(rows, 64) * ceil_div(classes, 64);
+  double tb, tm, ts;
+  if (bf16) {
+    // 27.5, 19 and 10.3 us a round of 256, 512 and 768 workgroups at 768 features
+    // (4096 x 768 x 32000); the last round less when it holds one to a CU.
+    tb = 27.5 * (double)ceil_div(big, kCus);
+    tm = 19.0 * (double)(mid / (2 * kCus)) + (mid % (2 * kCus) == 0 ? 0.0 : mid % (2 * kCus) <= kCus ? 12.0 : 19.0);
+    const int64_t r = small % (3 * kCus);
+    ts = 10.3 * (double)(small / (3 * kCus)) + (r == 0 ? 0.0 : r <= kCus ? 5.0 : r <= 2 * kCus ? 7.5 : 10.3);
+  } else {
+    // the matrix pipes are the bound: a CU's workgroups take turns on them
+    tb = 16.0 * (double)ceil_div(big, kCus);
+    tm = 4.25 * (double)ceil_div(mid, kCus);
+    ts = 1.06 * (double)ceil_div(small, kCus);
+  }
+  return tb <= tm && tb <= ts ? BIG : tm <= ts ? MID : SMALL;
+}
+
+template <typename T, int EPI>
+struct Tiles;
+template <typename T>
+struct Tiles<T, E_STATS> {
+  typedef BigTile<T, false, false, E_STATS> Big;
+  typedef RingTile<T, 128, 128, 2, 2, 2, false, false, E_STATS> Mid;
+  typedef RingTile<T, 64, 64, 2, 2, 3, false, false, E_STATS> Small;
+  typedef RingTile<T, 128, 32, 4, 1, 7, false, false, E_STATS> Few;
+  typedef RingTile<T, 64, 64, 2, 2, 8, false, false, E_STATS> Deep;
+  typedef RingTile<T, 32, 32, 1, 1, 8, false, false, E_STATS> Tiny;
+};
+template <typename T>
+struct Tiles<T, E_DLOGITS> {
+  typedef BigTile<T, false, false, E_DLOGITS> Big;
+  typedef RingTile<T, 128, 128, 2, 2, 2, false, false, E_DLOGITS> Mid;
+  typedef RingTile<T, 64, 64, 2, 2, 3, false, false, E_DLOGITS> Small;
+  typedef RingTile<T, 32, 128, 1, 4, 7, false, false, E_DLOGITS> Few;
+  typedef RingTile<T, 64, 64, 2, 2, 8, false, false, E_DLOGITS> Deep;
+  typedef RingTile<T, 32, 32, 1, 1, 8, false, false, E_DLOGITS> Tiny;
+};
+template <typename T>
+struct Tiles<T, E_DX> {
+  typedef BigTile<T, true, true, E_DX> Big;
+  typedef RingTile<T, 128, 128, 2, 2, 2, true, true, E_DX> Mid;
+  typedef RingTile<T, 64, 64, 2, 2, 3, true, true, E_DX> Small;
+  typedef RingTile<T, 128, 32, 4, 1, 4, true, true, E_DX> Few;
+};
+template <typename T>
+struct Tiles<T, E_DW> {
+  typedef BigTile<T, true, false, E_DW> Big;
+  typedef RingTile<T, 128, 128, 2, 2, 2, true, false, E_DW> Mid;
+  typedef RingTile<T, 64, 64, 2, 2, 3, true, false, E_DW> Small;
+};
+
+template <typename T, int EPI>
+hipError_t product(Variant v, const Gemm &g, const HeadArgs &a, hipStream_t s) {
+  typedef Tiles<T, EPI> X;
+  switch (v) {
+    case BIG: return launch_product<typename X::Big>(g, a, s);
+    case MID: return launch_product<typename X::Mid>(g, a, s);
+    case SMALL:
+      // no more than one workgroup to a CU: seven k-tiles in flight, not two
+      if (ceil_div(g.a_ext, 64) * ceil_div(g.b_ext, 64) <= kCus) return launch_product<typename X::Deep>(g, a, s);
+      return launch_product<typename X::Small>(g, a, s);
+    case TINY: return launch_product<typename X::Tiny>(g, a, s);
+    default: return launch_product<typename X::Few>(g, a, s);
+  }
+}
 
 template <typename T>
 hipError_t forward(const HeadArgs &a, hipStream_t s) {
@@ -882,58 +1117,97 @@ hipError_t forward(const HeadArgs &a, hipStream_t s) {
   g.a = a.w; g.a_ld = a.w_ld; g.a_ext = (int)a.classes;
   g.b = a.x; g.b_ld = a.x_ld; g.b_ext = (int)a.rows;
   g.k_ext = a.dim; g.splits = 1;
-  if (big_rows(a.rows)) return launch_big<T, false, false, E_STATS>(g, a, s);
-  if (a.rows > kWideRows) return launch_gemm<T, 128, 128, 2, 2, 3, false, false, E_STATS>(g, a, s);
-  return launch_gemm<T, 128, 32, 4, 1, 4, false, false, E_STATS>(g, a, s);
+  return product<T, E_STATS>(variant(sizeof(T) == 2, a.rows, a.classes), g, a, s);
 }
 template <typename T>
 hipError_t dlogits(const HeadArgs &a, hipStream_t s) {
+  if (a.rows == 0) return hipSuccess;
   Gemm g{};
   g.a = a.x; g.a_ld = a.x_ld; g.a_ext = (int)a.rows;
   g.b = static_cast<const T *>(a.w) + a.v0 * a.w_ld; g.b_ld = a.w_ld; g.b_ext = (int)a.piece;
   g.k_ext = a.dim; g.splits = 1;
-  const hipError_t e = big_rows(a.rows) ? launch_big<T, false, false, E_DLOGITS>(g, a, s) :
-                       a.rows > kWideRows ? launch_gemm<T, 128, 128, 2, 2, 3, false, false, E_DLOGITS>(g, a, s)
-                                          : launch_gemm<T, 32, 128, 1, 4, 4, false, false, E_DLOGITS>(g, a, s);
-  if (e != hipSuccess || a.rows == 0) return e;
+  const hipError_t e = product<T, E_DLOGITS>(variant(sizeof(T) == 2, a.rows, a.classes), g, a, s);
+  if (e != hipSuccess || !a.teacher) return e;
   hapi_launch(head_targets_kernel<T>, dim3((uint32_t)((a.rows * a.top + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t grads(const HeadArgs &a, hipStream_t s) {
-  Gemm g{};
-  g.a = static_cast<const T *>(a.w) + a.v0 * a.w_ld; g.a_ld = a.w_ld; g.a_ext = a.dx_pad;
-  g.b = a.gt; g.b_ld = a.rows_pad; g.b_ext = (int)a.rows;
-  g.k_ext = (int)a.piece; g.splits = a.splits;
-  hipError_t e = big_rows(a.rows)  ? launch_big<T, true, true, E_DX>(g, a, s)
-                 : a.rows > kWideRows ? launch_gemm<T, 128, 128, 2, 2, 3, true, true, E_DX>(g, a, s)
-                                    : launch_gemm<T, 128, 32, 4, 1, 4, true, true, E_DX>(g, a, s);
-  if (e != hipSuccess) return e;
-  g.a = a.x; g.a_ld = a.x_ld; g.a_ext = a.dx_pad;
-  g.b = a.gt; g.b_ld = a.rows_pad; g.b_ext = (int)a.piece;
-  g.k_ext = (int)a.rows; g.splits = 1;
-  if (big_rows(a.rows)) return launch_big<T, true, false, E_DW>(g, a, s);
-  return launch_gemm<T, 128, 128, 2, 2, 3, true, false, E_DW>(g, a, s);
+  Gemm x{}, w{};
+  x.a = static_cast<const T *>(a.w) + a.v0 * a.w_ld; x.a_ld = a.w_ld; x.a_ext = a.dx_pad;
+  x.b = a.gt; x.b_ld = a.rows_pad; x.b_ext = (int)a.rows;
+  x.k_ext = (int)a.piece; x.splits = a.splits;
+  w.a = a.x; w.a_ld = a.x_ld; w.a_ext = a.dx_pad;
+  w.b = a.gt; w.b_ld = a.rows_pad; w.b_ext = (int)a.piece;
+  w.k_ext = (int)a.rows; w.splits = 1;
+  typedef Tiles<T, E_DX> X;
+  typedef Tiles<T, E_DW> W;
+  Variant v = variant(sizeof(T) == 2, a.rows, a.classes);
+  if (v == TINY) v = a.rows <= 32 ? FEW : SMALL;
+  switch (v) {
+    case BIG: return launch_grads<typename X::Big, typename W::Big>(x, w, a, s);
+    case MID: return launch_grads<typename X::Mid, typename W::Mid>(x, w, a, s);
+    case SMALL: return launch_grads<typename X::Small, typename W::Small>(x, w, a, s);
+    default: return launch_grads<typename X::Few, typename W::Small>(x, w, a, s);
+  }
 }
-
 }  // namespace
 
-int head_parts(bool, int64_t rows, int64_t classes) {
-  if (big_rows(rows)) return (int)((classes + 255) / 256) * 4;
-  return (int)((classes + 127) / 128) * (rows > kWideRows ? 2 : 4);
+int head_parts(bool bf16, int64_t rows, int64_t classes) {
+  switch (variant(bf16, rows, classes)) {
+    case BIG: return (int)ceil_div(classes, 256) * 4;
+    case MID: return (int)ceil_div(classes, 128) * 2;
+    case SMALL: return (int)ceil_div(classes, 64) * 2;
+    case TINY: return (int)ceil_div(classes, 32);
+    default: return (int)ceil_div(classes, 128) * 4;
+  }
 }
-int head_db_parts(bool, int64_t rows) {
-  if (big_rows(rows)) return (int)((rows + 255) / 256) * 4;
-  return rows > kWideRows ? (int)((rows + 127) / 128) * 2 : (int)((rows + 31) / 32);
+int head_db_parts(bool bf16, int64_t rows, int64_t classes) {
+  switch (variant(bf16, rows, classes)) {
+    case BIG: return (int)ceil_div(rows, 256) * 4;
+    case MID: return (int)ceil_div(rows, 128) * 2;
+    case SMALL: return (int)ceil_div(rows, 64) * 2;
+    default: return (int)ceil_div(rows, 32);
+  }
 }
-int head_splits(bool, int64_t rows, int dim, int64_t piece) {
-  const int64_t br = big_rows(rows) ? 256 : rows > kWideRows ? 128 : 32, ba = big_rows(rows) ? 256 : 128;
-  const int64_t tiles = ((rows + br - 1) / br) * ((dim + ba - 1) / ba);
-  if (tiles == 0) return 1;
-  int64_t s = (512 + tiles - 1) / tiles;           // two workgroups a CU
-  const int64_t most = (piece + 511) / 512;        // at least 512 classes each
-  s = s < most ? s : most;
-  return (int)(s < 1 ? 1 : s);
+int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece) {
+  Variant v = variant(bf16, rows, classes);
+  if (v == TINY) v = rows <= 32 ? FEW : SMALL;
+  const int64_t br = v == BIG ? 256 : v == MID ? 128 : v == SMALL ? 64 : 32, ba = v == BIG ? 256 : v == SMALL ? 64 : 128;
+  const int64_t bc = v == BIG ? 256 : v == MID ? 128 : 64;
+  const int64_t nx = ceil_div(rows, br) * ceil_div(dim, ba), nw = ceil_div(piece, bc) * ceil_div(dim, v == FEW ? 64 : ba);
+  if (nx == 0) return 1;
+  const int64_t kt = bf16 ? 64 : 32;
+  const double kx = (double)ceil_div(piece, kt), kw = (double)ceil_div(rows, kt) + 4.0;
+  // The launch's time in k-tiles of one workgroup per CU: dx's rounds, then dW's on
+  // the CUs as they come free; and the partial sums' way through memory.
+  const int64_t cus = kCus;
+  double best = 0.0;
+  int64_t pick = 1;
+  for (int64_t s = 1; s <= 64 && s * 4 <= (int64_t)kx + 3; ++s) {
+    const double lx = kx / (double)s + 4.0;
+    const int64_t n = nx * s, full = n / cus, rest = n % cus;
+    const double t0 = (double)full * lx, t1 = t0 + lx;
+    // earliest time by which the CUs have run all of dW's workgroups: the early
+    // CUs' k-th round of them, with what the late ones have done by then
+    double end = rest ? t1 : t0;
+    if (nw > 0)
+      for (int64_t k = std::max<int64_t>(1, (int64_t)((double)nw / cus) - 1);; ++k) {
+        const double t = t0 + (double)k * kw;
+        const int64_t late = t > t1 ? (int64_t)((t - t1) / kw) : 0;
+        if ((cus - rest) * k + rest * late < nw) continue;
+        end = std::max(end, t);
+        break;
+      }
+    const double bytes = (double)s * (double)rows * (double)dim * 8.0;
+    const double ktile_bytes = v == BIG ? 8.0e6 : v == MID ? 3.0e6 : 1.0e6;  // memory traffic in a k-tile's time
+    const double cost = end + bytes / ktile_bytes;
+    if (s == 1 || cost < best) {
+      best = cost;
+      pick = s;
+    }
+  }
+  return (int)pick;
 }
 
 hipError_t launch_head_stage(bool bf16, const void *in, int64_t ld_in, void *out, int64_t ld_out, int64_t rows, int dim,
@@ -942,10 +1216,10 @@ hipError_t launch_head_stage(bool bf16, const void *in, int64_t ld_in, void *out
   const int64_t n = rows * ld_out * (bf16 ? 2 : 4) / 16;
   if (bf16)
     hapi_launch(stage_kernel<uint16_t>, dim3(grid_for(n, 256)), dim3(256), 0, s, (const uint16_t *)in, ld_in,
-                (uint16_t *)out, ld_out, rows, dim, (const float2 *)nullptr);
+                (uint16_t *)out, ld_out, rows, dim);
   else
     hapi_launch(stage_kernel<float>, dim3(grid_for(n, 256)), dim3(256), 0, s, (const float *)in, ld_in, (float *)out,
-                ld_out, rows, dim, (const float2 *)nullptr);
+                ld_out, rows, dim);
   return hipGetLastError();
 }
 
@@ -963,14 +1237,9 @@ hipError_t launch_head_finish(bool bf16, const HeadArgs &a, hipStream_t s) {
 
 hipError_t launch_head_prepare(bool bf16, const HeadArgs &a, void *xs, int64_t xs_ld, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  hapi_launch(head_info_kernel, dim3((uint32_t)((a.rows_pad + 3) / 4)), dim3(256), 0, s, a);
-  const int64_t n = a.rows * xs_ld * (bf16 ? 2 : 4) / 16;
-  if (bf16)
-    hapi_launch(stage_kernel<uint16_t>, dim3(grid_for(n, 256)), dim3(256), 0, s, (const uint16_t *)a.x_in, a.x_in_ld,
-                (uint16_t *)xs, xs_ld, a.rows, a.dim, (const float2 *)a.info);
-  else
-    hapi_launch(stage_kernel<float>, dim3(grid_for(n, 256)), dim3(256), 0, s, (const float *)a.x_in, a.x_in_ld,
-                (float *)xs, xs_ld, a.rows, a.dim, (const float2 *)a.info);
+  const dim3 grid((uint32_t)((a.rows_pad + 3) / 4));
+  if (bf16) hapi_launch(head_prepare_kernel<uint16_t>, grid, dim3(256), 0, s, a, (uint16_t *)xs, xs_ld);
+  else hapi_launch(head_prepare_kernel<float>, grid, dim3(256), 0, s, a, (float *)xs, xs_ld);
   return hipGetLastError();
 }
 
@@ -983,12 +1252,12 @@ hipError_t launch_head_grads(bool bf16, const HeadArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_head_reduce(bool bf16, const HeadArgs &a, hipStream_t s) {
-  if (a.rows > 0) {
-    const int64_t n = a.rows * ((a.dim + 3) / 4);
-    if (bf16) hapi_launch(head_dx_kernel<uint16_t>, dim3(grid_for(n, 256)), dim3(256), 0, s, a);
-    else hapi_launch(head_dx_kernel<float>, dim3(grid_for(n, 256)), dim3(256), 0, s, a);
-  }
-  if (a.dbias) hapi_launch(head_dbias_kernel, dim3((uint32_t)((a.classes + 255) / 256)), dim3(256), 0, s, a);
+  const int64_t n = a.rows * ((a.dim + 3) / 4);
+  const int nx = a.rows > 0 ? (int)std::min<int64_t>(ceil_div(n, kReduceThreads), 2048) : 0;
+  const int nb = a.dbias ? (int)ceil_div(a.classes, kBiasClasses) : 0;
+  if (nx + nb == 0) return hipSuccess;
+  if (bf16) hapi_launch(head_reduce_kernel<uint16_t>, dim3(nx + nb), dim3(kReduceThreads), 0, s, a, nx);
+  else hapi_launch(head_reduce_kernel<float>, dim3(nx + nb), dim3(kReduceThreads), 0, s, a, nx);
   return hipGetLastError();
 }
 

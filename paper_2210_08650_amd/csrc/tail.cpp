@@ -95,7 +95,7 @@ struct Head {
   int64_t piece;     // classes of a piece
   int64_t bytes_fwd, bytes_bwd;
   // byte offsets into the workspace
-  int64_t o_part, o_xs, o_ws, o_info, o_q, o_gt, o_db, o_dx;
+  int64_t o_part, o_xs, o_ws, o_info, o_id, o_cq, o_gt, o_db, o_dx;
 };
 
 int read_head(const hapi_head_desc *d, Head &h) {
@@ -140,8 +140,8 @@ int read_head(const hapi_head_desc *d, Head &h) {
   const int64_t most = std::max<int64_t>(kPieceBytes / (a.rows_pad * h.esz) / kHeadPiece * kHeadPiece, kHeadPiece);
   const int64_t pieces = (d->classes + most - 1) / most;
   h.piece = std::min(up((d->classes + pieces - 1) / pieces, kHeadPiece), up(d->classes, kHeadPiece));
-  a.db_parts = head_db_parts(h.bf16, d->rows);
-  a.splits = head_splits(h.bf16, d->rows, d->dim, h.piece);
+  a.db_parts = head_db_parts(h.bf16, d->rows, d->classes);
+  a.splits = head_splits(h.bf16, d->rows, d->dim, d->classes, h.piece);
 
   const int64_t xs = up(d->rows * a.dx_pad * h.esz, kAlign), ws = up(d->classes * a.dx_pad * h.esz, kAlign);
   int64_t o = 0;
@@ -157,7 +157,8 @@ int read_head(const hapi_head_desc *d, Head &h) {
   o = h.o_xs;
   take(xs);
   h.o_info = take(a.rows_pad * 8);
-  h.o_q = take(d->top > 0 ? d->rows * a.top * 4 : 0);
+  h.o_id = take(d->rows * a.top * 4);
+  h.o_cq = take(d->rows * a.top * 4);
   h.o_gt = take(h.piece * a.rows_pad * h.esz);
   h.o_db = take((int64_t)a.db_parts * d->classes * 4);
   h.o_dx = take((int64_t)a.splits * d->rows * a.dx_pad * 4);
@@ -236,7 +237,8 @@ int head_backward(const hapi_head_desc *d, Head &h, const void *x, const void *w
   a.picked = const_cast<float *>(picked);
   a.dloss = dloss;
   a.info = reinterpret_cast<float2 *>(base + h.o_info);
-  a.q = reinterpret_cast<float *>(base + h.o_q);
+  a.id32 = reinterpret_cast<int32_t *>(base + h.o_id);
+  a.cq = reinterpret_cast<float *>(base + h.o_cq);
   a.gt = base + h.o_gt;
   a.db_part = dbias ? reinterpret_cast<float *>(base + h.o_db) : nullptr;
   a.dx_part = reinterpret_cast<float *>(base + h.o_dx);

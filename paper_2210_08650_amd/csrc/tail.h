@@ -48,7 +48,8 @@ struct HeadArgs {
   // backward
   const float *dloss;
   float2 *info;             // [rows_pad] (m, coefficient / sum of exp); rows that do not count: (inf, 0)
-  float *q;                 // [rows][top] weights (distillation)
+  int32_t *id32;            // [rows][top] the targets' classes, -1: none
+  float *cq;                // [rows][top] what they take off dz: coefficient times weight
   void *gt;                 // [piece][rows_pad] dz^T of one piece of the classes
   int64_t rows_pad, v0, piece;  // the piece is classes [v0, v0 + piece)
   float *db_part;           // [db_parts][classes], null: no bias gradient
@@ -64,8 +65,8 @@ struct HeadArgs {
 // The parts launch_head_forward writes for this many classes and rows, and the
 // row parts and splits of the backward pass: functions of the sizes only.
 int head_parts(bool bf16, int64_t rows, int64_t classes);
-int head_db_parts(bool bf16, int64_t rows);
-int head_splits(bool bf16, int64_t rows, int dim, int64_t piece);
+int head_db_parts(bool bf16, int64_t rows, int64_t classes);
+int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece);
 constexpr int kHeadRowPad = 64;
 constexpr int kHeadPiece = 256;  // pieces are multiples of this many classes
 
@@ -74,7 +75,7 @@ hipError_t launch_head_stage(bool bf16, const void *in, int64_t ld_in, void *out
                              hipStream_t s);
 hipError_t launch_head_forward(bool bf16, const HeadArgs &a, hipStream_t s);  // parts
 hipError_t launch_head_finish(bool bf16, const HeadArgs &a, hipStream_t s);   // loss, stats, picked
-// info, q and a copy of x (xs, [rows][xs_ld]) whose rows that do not count are zero.
+// info, id32, cq and a copy of x (xs, [rows][xs_ld]) whose rows that do not count are zero.
 hipError_t launch_head_prepare(bool bf16, const HeadArgs &a, void *xs, int64_t xs_ld, hipStream_t s);
 hipError_t launch_head_dlogits(bool bf16, const HeadArgs &a, hipStream_t s);  // gt, db_part; targets' entries put in
 hipError_t launch_head_grads(bool bf16, const HeadArgs &a, hipStream_t s);    // dw of the piece, dx_part
