@@ -380,6 +380,10 @@ def hapi_choose_split(**job):
 
 # ------------------------------------------------------------ the trained tail
 
+import torch  # noqa: E402  (mapped already: see _load)
+
+_TORCH_TYPES = {HAPI_F32: torch.float32, HAPI_BF16: torch.bfloat16}
+
 class _TailDesc:
     """Owns a descriptor of the trained tail's operators."""
     _struct = None
@@ -426,18 +430,22 @@ class Head(_TailDesc):
 
 def _tensor(p, name, dtype, rows, dim=None, stride=0):
     """The address of an argument.  Of a tensor the type, the sizes and the row
-    stride have to be the descriptor's (an address is taken as it is)."""
-    if p is None or not hasattr(p, "data_ptr"):
+    stride have to be the descriptor's, and its device the current one (an address
+    is taken as it is)."""
+    if p is None or type(p) is int:
+        return p
+    if not hasattr(p, "data_ptr"):
         return _ptr(p)
     shape = (rows,) if dim is None else (rows, dim)
-    want = {HAPI_F32: "torch.float32", HAPI_BF16: "torch.bfloat16"}.get(dtype, dtype)
-    if str(p.dtype) != want or tuple(p.shape) != shape:
+    want = _TORCH_TYPES.get(dtype, dtype)
+    if p.dtype is not want or p.shape != shape:
         raise HapiError(HAPI_E_INVAL, f"{name} must be {want} of shape {shape}, got {p.dtype} {tuple(p.shape)}")
-    if (p.stride(-1) != 1 and p.shape[-1] > 1) or (dim is not None and rows > 1 and p.stride(0) != (stride or dim)):
-        raise HapiError(HAPI_E_INVAL, f"{name} must have rows of consecutive values, {stride or dim} apart, "
-                                      f"got strides {tuple(p.stride())}")
-    import torch
-    if not p.is_cuda or p.device.index != torch.cuda.current_device():
+    if not p.is_contiguous() or (stride and stride != dim and rows > 1):
+        step = stride or dim
+        if (p.stride(-1) != 1 and p.shape[-1] > 1) or (dim is not None and rows > 1 and p.stride(0) != step):
+            raise HapiError(HAPI_E_INVAL, f"{name} must have rows of consecutive values, {step} apart, "
+                                          f"got strides {tuple(p.stride())}")
+    if p.get_device() != (torch.cuda.current_device() if p.is_cuda else None):
         raise HapiError(HAPI_E_INVAL, f"{name} is on {p.device}, not on the current GPU")
     return p.data_ptr()
 
@@ -485,14 +493,14 @@ def _head_gradients(c, dx, dweight, dbias):
 def hapi_xent_forward(desc: Head, x, weight, bias, targets, loss, stats) -> None:
     c = desc.c
     _check(_lib.hapi_xent_forward(
-        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(targets, "targets", "torch.int64", c.rows),
+        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(targets, "targets", torch.int64, c.rows),
         _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2)))
 
 
 def hapi_xent_backward(desc: Head, x, weight, bias, targets, loss, stats, dloss, dx, dweight, dbias) -> None:
     c = desc.c
     _check(_lib.hapi_xent_backward(
-        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(targets, "targets", "torch.int64", c.rows),
+        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(targets, "targets", torch.int64, c.rows),
         _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2), _f32(dloss, "dloss", c.rows),
         *_head_gradients(c, dx, dweight, dbias)))
 
@@ -500,7 +508,7 @@ def hapi_xent_backward(desc: Head, x, weight, bias, targets, loss, stats, dloss,
 def hapi_distill_forward(desc: Head, x, weight, bias, ids, teacher, loss, stats, picked) -> None:
     c = desc.c
     _check(_lib.hapi_distill_forward(
-        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(ids, "ids", "torch.int64", c.rows, c.top),
+        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(ids, "ids", torch.int64, c.rows, c.top),
         _f32(teacher, "teacher", c.rows, c.top), _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2),
         _f32(picked, "picked", c.rows, c.top)))
 
@@ -508,6 +516,6 @@ def hapi_distill_forward(desc: Head, x, weight, bias, ids, teacher, loss, stats,
 def hapi_distill_backward(desc: Head, x, weight, bias, ids, teacher, stats, picked, dloss, dx, dweight, dbias) -> None:
     c = desc.c
     _check(_lib.hapi_distill_backward(
-        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(ids, "ids", "torch.int64", c.rows, c.top),
+        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(ids, "ids", torch.int64, c.rows, c.top),
         _f32(teacher, "teacher", c.rows, c.top), _f32(stats, "stats", c.rows, 2), _f32(picked, "picked", c.rows, c.top),
         _f32(dloss, "dloss", c.rows), *_head_gradients(c, dx, dweight, dbias)))

@@ -76,7 +76,7 @@ __device__ __forceinline__ void store_chunk(T *p, int n, const uint4 &q) {
 // Sums of K values over the TPR threads of a row, known to all of them.  red:
 // two alternating buffers, so one barrier a call is enough.
 template <int TPR, int K>
-__device__ __forceinline__ void row_sum(float (&v)[K], float (*red)[16][2], int &flip) {
+__device__ __forceinline__ void row_sum(float (&v)[K], float (*red)[8][2], int &flip) {
 #pragma unroll
   for (int o = (TPR < 64 ? TPR : 64) / 2; o >= 1; o >>= 1)
 #pragma unroll
@@ -100,22 +100,24 @@ __device__ __forceinline__ void row_sum(float (&v)[K], float (*red)[16][2], int 
 
 constexpr int block_of(int tpr) { return tpr < 256 ? 256 : tpr; }
 
+// N float32 weights from d on, zero past dim.
+template <int N>
+__device__ __forceinline__ void load_weights(const float *p, int d, int dim, float (&v)[N]) {
+  if (d + N <= dim) {
+    __builtin_memcpy(v, p + d, 4 * N);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = d + j < dim ? p[d + j] : 0.0f;
+  }
+}
+
 template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(block_of(TPR)) void norm_forward_kernel(NormArgs a) {
   constexpr int N = Pack<T>::N, RPB = block_of(TPR) / TPR;
-  __shared__ float red[2][16][2];
+  __shared__ float red[2][8][2];
   int flip = 0;
   const int tl = threadIdx.x % TPR, D = a.dim;
   const float inv_d = 1.0f / (float)D;
-  float g[CH][N], b[CH][N];
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int d = (tl + TPR * c) * N + j;
-      g[c][j] = d < D ? a.gamma[d] : 0.0f;
-      b[c][j] = d < D ? a.beta[d] : 0.0f;
-    }
   const int64_t step = (int64_t)gridDim.x * RPB;
   int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
   const T *x = static_cast<const T *>(a.x);
@@ -129,6 +131,12 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_forward_kernel(NormArgs a)
     }
   };
   load(row);
+  float g[CH][N], b[CH][N];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    load_weights<N>(a.gamma, (tl + TPR * c) * N, D, g[c]);
+    load_weights<N>(a.beta, (tl + TPR * c) * N, D, b[c]);
+  }
   // every thread of a block walks as many rows: the barriers in row_sum
   for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step, row += step) {
     float v[CH][N];
@@ -139,19 +147,19 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_forward_kernel(NormArgs a)
 #pragma unroll
       for (int j = 0; j < N; ++j) s[0] += v[c][j];
     }
-    load(row + step);
+    if (r0 + step < a.rows) load(row + step);
     row_sum<TPR>(s, red, flip);
     const float mean = s[0] * inv_d;
-    float q[1] = {0.0f};
+    float var[1] = {0.0f};
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         v[c][j] -= mean;
-        if ((tl + TPR * c) * N + j < D) q[0] = fmaf(v[c][j], v[c][j], q[0]);
+        if ((tl + TPR * c) * N + j < D) var[0] = fmaf(v[c][j], v[c][j], var[0]);
       }
-    row_sum<TPR>(q, red, flip);
-    const float rstd = 1.0f / sqrtf(fmaf(q[0], inv_d, a.eps));
+    row_sum<TPR>(var, red, flip);
+    const float rstd = 1.0f / sqrtf(fmaf(var[0], inv_d, a.eps));
     if (row < a.rows) {
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
@@ -172,20 +180,18 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_forward_kernel(NormArgs a)
 template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(block_of(TPR)) void norm_backward_kernel(NormArgs a) {
   constexpr int N = Pack<T>::N, RPB = block_of(TPR) / TPR;
-  __shared__ float red[2][16][2];
+  __shared__ float red[2][8][2];
   __shared__ float acc_s[RPB > 1 ? 2 * TPR * CH * N : 1];
   int flip = 0;
   const int tl = threadIdx.x % TPR, D = a.dim;
   const float inv_d = 1.0f / (float)D;
   float g[CH][N], dg[CH][N], db[CH][N];
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+  for (int c = 0; c < CH; ++c) {
+    load_weights<N>(a.gamma, (tl + TPR * c) * N, D, g[c]);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int d = (tl + TPR * c) * N + j;
-      g[c][j] = d < D ? a.gamma[d] : 0.0f;
-      dg[c][j] = db[c][j] = 0.0f;
-    }
+    for (int j = 0; j < N; ++j) dg[c][j] = db[c][j] = 0.0f;
+  }
   const int64_t step = (int64_t)gridDim.x * RPB;
   int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
   const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
@@ -203,8 +209,11 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_backward_kernel(NormArgs a
     mean = live ? a.mean[r] : 0.0f;
     rstd = live ? a.rstd[r] : 0.0f;
   };
-  load(row);
+  // the next row's loads in flight during this one's sums, where the registers hold both
+  constexpr bool kAhead = TPR < 512;
+  if (kAhead) load(row);
   for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step, row += step) {
+    if (!kAhead) load(row);
     // past the row's end x and dy are 0 and gamma is 0: h is -mean rstd there,
     // and every product with it is 0
     float h[CH][N], u[CH][N];
@@ -224,7 +233,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_backward_kernel(NormArgs a
         s[1] = fmaf(u[c][j], h[c][j], s[1]);
       }
     }
-    load(row + step);
+    if (kAhead) load(row + step);
     row_sum<TPR>(s, red, flip);
     const float m0 = s[0] * inv_d, m1 = s[1] * inv_d;
     if (row < a.rows) {
@@ -272,22 +281,27 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_backward_kernel(NormArgs a
   }
 }
 
-// dgamma and dbeta: the sum of the blocks' partial sums, 16 slices of the
-// blocks side by side, then the slices in order.
+// dgamma and dbeta: the sum of the blocks' partial sums, 16 columns a block and 64
+// slices of the parts side by side, then the slices in order.
 __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *__restrict__ part, int parts, int D,
                                                            float *__restrict__ dgamma, float *__restrict__ dbeta) {
-  __shared__ float red[16][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + lane;
+  __shared__ float red[64][17];
+  const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
+  const int c = blockIdx.x * 16 + col;
   float t = 0.0f;
-  if (c < 2 * D)
-    for (int p = w; p < parts; p += 16) t += part[(int64_t)p * 2 * D + c];
-  red[w][lane] = t;
+  if (c < 2 * D) {
+#pragma unroll
+    for (int i = 0; i < kNormParts / 64; ++i) {
+      const int p = slice + 64 * i;
+      t += p < parts ? part[(int64_t)p * 2 * D + c] : 0.0f;
+    }
+  }
+  red[slice][col] = t;
   __syncthreads();
-  if (w == 0 && c < 2 * D) {
+  if (slice == 0 && c < 2 * D) {
     t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += red[i][lane];
+    for (int i = 0; i < 64; ++i) t += red[i][col];
     (c < D ? dgamma[c] : dbeta[c - D]) = t;
   }
 }
@@ -297,31 +311,54 @@ hipError_t launch_one(const NormArgs &a, hipStream_t s) {
   constexpr int RPB = block_of(TPR) / TPR;
   const int64_t want = (a.rows + RPB - 1) / RPB;
   if constexpr (BACK) {
-    const int blocks = (int)(want < kNormParts ? want : kNormParts);
+    // two blocks a CU, as many rows to each
+    const int64_t iters = (want + kNormParts - 1) / kNormParts;
+    const int blocks = want > 0 ? (int)((want + iters - 1) / iters) : 0;
     if (blocks > 0) hapi_launch((norm_backward_kernel<T, TPR, CH>), dim3(blocks), dim3(block_of(TPR)), 0, s, a);
-    hapi_launch(norm_reduce_kernel, dim3((2 * a.dim + 63) / 64), dim3(1024), 0, s, (const float *)a.part, blocks, a.dim,
+    hapi_launch(norm_reduce_kernel, dim3((2 * a.dim + 15) / 16), dim3(1024), 0, s, (const float *)a.part, blocks, a.dim,
                 a.dgamma, a.dbeta);
   } else {
-    const int64_t cap = 2048 / (block_of(TPR) / 256);
-    const int blocks = (int)(want < cap ? want : cap);
-    if (blocks > 0) hapi_launch((norm_forward_kernel<T, TPR, CH>), dim3(blocks), dim3(block_of(TPR)), 0, s, a);
+    // As many rows to every block, up to four: gamma and beta are read once, and
+    // there are blocks enough for the CUs (25,216 x 768: 15.2 us with one, 14.8 with
+    // two, 15.3 with four, 17.0 with eight).
+    int64_t iters = want / 1536;
+    iters = iters < 1 ? 1 : iters > 4 ? 4 : iters;
+    const int64_t blocks = (want + iters - 1) / iters;
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    if (blocks > 0) hapi_launch((norm_forward_kernel<T, TPR, CH>), dim3((uint32_t)blocks), dim3(block_of(TPR)), 0, s, a);
   }
   return hipGetLastError();
 }
 
+// The threads a row gets: as few as hold it in 32 values each (one pass over the
+// registers), and of the shapes that hold it the one with the fewest idle lanes.
 template <typename T, bool BACK>
 hipError_t launch_dim(const NormArgs &a, hipStream_t s) {
   constexpr int N = Pack<T>::N;
   const int ch = (a.dim + N - 1) / N;  // 16-byte chunks of a row
   if (ch <= 16) return launch_one<T, 16, 1, BACK>(a, s);
-  if (ch <= 64) return launch_one<T, 64, 1, BACK>(a, s);
-  if (ch <= 128) return launch_one<T, 64, 2, BACK>(a, s);
+  if (ch <= 32) return launch_one<T, 32, 1, BACK>(a, s);
+  if (ch <= 64) return launch_one<T, 32, 2, BACK>(a, s);
+  if (ch <= 96) return launch_one<T, 32, 3, BACK>(a, s);
+  if (ch <= 128) return launch_one<T, 32, 4, BACK>(a, s);
+  if (ch <= 192) return launch_one<T, 64, 3, BACK>(a, s);
   if (ch <= 256) return launch_one<T, 64, 4, BACK>(a, s);
-  if (ch <= 512) return launch_one<T, 256, 2, BACK>(a, s);
-  if (ch <= 1024) return launch_one<T, 256, 4, BACK>(a, s);
-  if (ch <= 2048) return launch_one<T, 1024, 2, BACK>(a, s);
   if constexpr (sizeof(T) == 4) {
-    if (ch <= 4096) return launch_one<T, 1024, 4, BACK>(a, s);
+    if (ch <= 320) return launch_one<T, 64, 5, BACK>(a, s);
+    if (ch <= 384) return launch_one<T, 64, 6, BACK>(a, s);
+    if (ch <= 512) return launch_one<T, 64, 8, BACK>(a, s);
+  } else {
+    if (ch <= 512) return launch_one<T, 256, 2, BACK>(a, s);
+  }
+  if (ch <= 768) return launch_one<T, 256, 3, BACK>(a, s);
+  if (ch <= 1024) return launch_one<T, 256, 4, BACK>(a, s);
+  if constexpr (sizeof(T) == 4) {
+    if (ch <= 1536) return launch_one<T, 256, 6, BACK>(a, s);
+  }
+  if (ch <= 2048) return launch_one<T, 512, 4, BACK>(a, s);
+  if constexpr (sizeof(T) == 4) {
+    if (ch <= 3072) return launch_one<T, 512, 6, BACK>(a, s);
+    if (ch <= 4096) return launch_one<T, 512, 8, BACK>(a, s);
   }
   return hipErrorInvalidValue;
 }
