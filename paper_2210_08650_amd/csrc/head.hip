@@ -91,16 +91,18 @@ struct Side {
     if constexpr (KR && sizeof(T) == 2 && CPR == 8) return 4 * ((row >> 1) & 1);
     return 0;
   }
-  __device__ __forceinline__ void init(int r0, int ext, int64_t ld, int wave, int lane) {
+  // r0: the tile's first row (its offset is in the base).  half 0 or 1: the operand's
+  // rows are every other 32 of the tile's, starting with that one; -1: all of them.
+  __device__ __forceinline__ void init(int r0, int ext, int64_t ld, int wave, int lane, int half = -1) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int lr = (wave * LOADS + i) * RPD + lane / CPR;  // LDS row
       const int c = (lane % CPR) ^ swz(lr);                  // 16-byte slot of the memory row
-      const int r = KR ? r0 + c * V : r0 + lr;
+      int r = KR ? c * V : lr;
+      if (half >= 0) r = (r >> 5) * 64 + 32 * half + (r & 31);
       lk[i] = KR ? lr : c * V;
-      // r0's own offset is in the base
-      const int64_t o = KR ? (int64_t)lr * ld + c * V : (int64_t)lr * ld + c * V;
-      off[i] = r < ext ? (uint32_t)(o * (int64_t)sizeof(T)) : kOob;
+      const uint32_t o = KR ? (uint32_t)lr * (uint32_t)ld + r : (uint32_t)r * (uint32_t)ld + c * V;  // < 2^31 bytes
+      off[i] = r0 + r < ext ? o * (uint32_t)sizeof(T) : kOob;
     }
   }
   __device__ __forceinline__ void issue(const uint8_t *base, uint32_t lds, int k_left, int wave) const {
@@ -177,35 +179,67 @@ struct SideTable {
 
 // Where a wave's blocks lie: block (i, j) is out[lane(j) + lane % 32][reg(i) + 8 q +
 // 4 lh + e] = acc[i][j][4 q + e]; part: which of the reg side's parts the wave holds.
-template <int REG_STEP, int LANE_A, int LANE_B>
+template <int LANE_A, int LANE_B>
 struct Place {
   int a0, r0, l0, part;
-  __device__ __forceinline__ int reg(int i) const { return r0 + REG_STEP * i; }
+  __device__ __forceinline__ int reg(int i) const { return r0 + 32 * i; }
   __device__ __forceinline__ int lane(int j) const { return l0 + (j >> 1) * LANE_B + (j & 1) * LANE_A; }
+};
+
+// A wave's 32 output rows of L values of type O (a lane's 16 of each block of 32), turned
+// in its part of LDS so that a store writes whole rows: put(b, q, v) takes values
+// 8 q + 4 lh .. + 3 of block b of the lane's row; rows(f) calls f(row, column, 16
+// bytes) with consecutive lanes on consecutive columns.  Stores of the lanes' own
+// values would write 32 bytes of 32 rows each, and the L2 takes a request for every
+// such piece (dz of 8192 x 2048 x 16384: 525 us, turned TURNEDUS).
+template <typename O, int L>
+struct RowsOut {
+  static constexpr int PITCH = L * (int)sizeof(O) + 16, V = 16 / (int)sizeof(O), PER = L / V, RPS = 64 / PER;
+  static constexpr int BYTES = 32 * PITCH;
+  uint8_t *p;
+  int lane;
+  __device__ __forceinline__ void put(int b, int q, float v0, float v1, float v2, float v3) const {
+    uint8_t *d = p + (lane & 31) * PITCH + (32 * b + 8 * q + 4 * (lane >> 5)) * (int)sizeof(O);
+    if constexpr (sizeof(O) == 2) *reinterpret_cast<uint2 *>(d) = make_uint2(f2bf2(v0, v1), f2bf2(v2, v3));
+    else *reinterpret_cast<float4 *>(d) = make_float4(v0, v1, v2, v3);
+  }
+  template <typename F>
+  __device__ __forceinline__ void rows(F &&f) const {
+#pragma unroll
+    for (int s = 0; s < 32 / RPS; ++s) {
+      const int row = s * RPS + lane / PER, c = lane % PER;
+      f(row, c * V, *reinterpret_cast<const uint4 *>(p + row * PITCH + c * 16));
+    }
+  }
 };
 
 template <typename T, int EPI, int TA, int TB, typename P, typename S>
 __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x16_t (&acc)[TA][TB], const P &at,
-                                         const S &side, int split, int lane) {
+                                         const S &side, uint8_t *turn, int split, int lane) {
   const int lh = lane >> 5;
   if constexpr (EPI == E_STATS) {
     const float c = kLog2e * h.inv_t;
     float m[TB], s[TB];
 #pragma unroll
     for (int j = 0; j < TB; ++j) m[j] = -INFINITY, s[j] = 0.0f;
+    if (h.bias || at.reg(TA) > g.a_ext) {  // else the table holds zeros
+#pragma unroll
+      for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4_t bias = *reinterpret_cast<const f32x4_t *>(side.m + (at.reg(i) - at.a0 + 8 * q + 4 * lh));
+#pragma unroll
+          for (int j = 0; j < TB; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += bias[e];
+        }
+    }
 #pragma unroll
     for (int i = 0; i < TA; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4_t bias = *reinterpret_cast<const f32x4_t *>(side.m + (at.reg(i) - at.a0 + 8 * q + 4 * lh));
+      for (int j = 0; j < TB; ++j)
 #pragma unroll
-        for (int j = 0; j < TB; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            acc[i][j][4 * q + e] += bias[e];
-            m[j] = fmaxf(m[j], acc[i][j][4 * q + e]);
-          }
-      }
+        for (int r = 0; r < 16; ++r) m[j] = fmaxf(m[j], acc[i][j][r]);
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
       m[j] = fmaxf(m[j], __shfl_xor(m[j], 32, 64));
@@ -222,150 +256,99 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
   if constexpr (EPI == E_DLOGITS) {
     T *gt = static_cast<T *>(h.gt);
     const float c = kLog2e * h.inv_t;
-    float sum[TB], bias[TB];
-    int cls[TB];  // in the piece
+    const RowsOut<T, 32 * TA> out{turn, lane};
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
-      cls[j] = at.lane(j) + (lane & 31);
-      bias[j] = h.bias && cls[j] < g.b_ext ? h.bias[h.v0 + cls[j]] : 0.0f;
-      sum[j] = 0.0f;
-    }
+      const int cls = at.lane(j) + (lane & 31);  // in the piece
+      if (h.bias) {
+        const float bias = cls < g.b_ext ? h.bias[h.v0 + cls] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < TA; ++i) {
-      const int a = at.reg(i), loc = a - at.a0;
-      // a row's target lies in few of the blocks: the others compare nothing
-      bool hit[TB];
-      const int tg = h.teacher ? INT32_MIN / 2 : side.target[loc + (lane & 31)];
+        for (int i = 0; i < TA; ++i)
 #pragma unroll
-      for (int j = 0; j < TB; ++j) hit[j] = __ballot((unsigned)(tg - at.lane(j)) < 32u) != 0;
+          for (int r = 0; r < 16; ++r) acc[i][j][r] += bias;
+      }
+      float sum = 0.0f;
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        f32x4_t m[2], sc[2];
+      for (int i = 0; i < TA; ++i) {
+        const int loc = at.reg(i) - at.a0;
+        // a row's target lies in few of the blocks: the others compare nothing
+        const int tg = h.teacher ? INT32_MIN / 2 : side.target[loc + (lane & 31)];
+        const bool hit = __ballot((unsigned)(tg - at.lane(j)) < 32u) != 0;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          m[u] = *reinterpret_cast<const f32x4_t *>(side.m + (loc + 16 * p + 8 * u + 4 * lh));
-          sc[u] = *reinterpret_cast<const f32x4_t *>(side.scale + (loc + 16 * p + 8 * u + 4 * lh));
-        }
+        for (int q = 0; q < 4; ++q) {
+          const int n = loc + 8 * q + 4 * lh;
+          const f32x4_t m = *reinterpret_cast<const f32x4_t *>(side.m + n);
+          const f32x4_t sc = *reinterpret_cast<const f32x4_t *>(side.scale + n);
+          float v[4];
 #pragma unroll
-        for (int j = 0; j < TB; ++j) {
-          float v[8];
+          for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_exp2f((acc[i][j][4 * q + e] - m[e]) * c) * sc[e];
+          if (hit) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            v[e] = __builtin_amdgcn_exp2f((acc[i][j][8 * p + e] + bias[j] - m[e >> 2][e & 3]) * c) * sc[e >> 2][e & 3];
-          if (hit[j]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int n = loc + 16 * p + 8 * (e >> 2) + 4 * lh + (e & 3);
-              v[e] -= side.target[n] == cls[j] ? side.coef[n] : 0.0f;
-            }
+            for (int e = 0; e < 4; ++e) v[e] -= side.target[n + e] == cls ? side.coef[n + e] : 0.0f;
           }
-          if (h.db_part) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[j] += v[e];
-          }
-          T *o = gt + (int64_t)cls[j] * h.rows_pad + a + 16 * p;
-          if constexpr (sizeof(T) == 2) {
-            float w[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[e]), __float_as_uint(v[4 + e]), false, false);
-              w[e] = __uint_as_float(s2[0]);
-              w[4 + e] = __uint_as_float(s2[1]);
-            }
-            const int n = 8 * lh;
-            if (cls[j] < g.b_ext && a + 16 * p + n < h.rows_pad)
-              *reinterpret_cast<uint4 *>(o + n) =
-                  make_uint4(f2bf2(w[0], w[1]), f2bf2(w[2], w[3]), f2bf2(w[4], w[5]), f2bf2(w[6], w[7]));
-          } else {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const int n = 8 * u + 4 * lh;
-              if (cls[j] < g.b_ext && a + 16 * p + n < h.rows_pad)
-                *reinterpret_cast<float4 *>(o + n) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
-            }
-          }
+          if (h.db_part) sum += (v[0] + v[1]) + (v[2] + v[3]);
+          out.put(i, q, v[0], v[1], v[2], v[3]);
         }
       }
-    }
-    if (h.db_part) {
-#pragma unroll
-      for (int j = 0; j < TB; ++j) {
-        sum[j] += __shfl_xor(sum[j], 32, 64);
-        if (lh == 0 && cls[j] < g.b_ext) h.db_part[(int64_t)at.part * h.classes + h.v0 + cls[j]] = sum[j];
+      out.rows([&](int row, int col, const uint4 &v) {
+        const int r = at.lane(j) + row, n = at.reg(0) + col;
+        if (r < g.b_ext && n < h.rows_pad) *reinterpret_cast<uint4 *>(gt + (int64_t)r * h.rows_pad + n) = v;
+      });
+      if (h.db_part) {
+        sum += __shfl_xor(sum, 32, 64);
+        if (lh == 0 && cls < g.b_ext) h.db_part[(int64_t)at.part * h.classes + h.v0 + cls] = sum;
       }
     }
   }
   if constexpr (EPI == E_DX) {
-    float *out = h.dx_part + (int64_t)split * h.rows * h.dx_pad;
+    float *o = h.dx_part + (int64_t)split * h.rows * h.dx_pad;
+    const RowsOut<float, 32 * TA> out{turn, lane};
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
-      const int row = at.lane(j) + (lane & 31);
-      if (row >= g.b_ext) continue;
 #pragma unroll
       for (int i = 0; i < TA; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int a = at.reg(i) + 8 * q + 4 * lh;
-          if (a >= h.dx_pad) continue;
-          float4 *p = reinterpret_cast<float4 *>(out + (int64_t)row * h.dx_pad + a);
-          float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-          if (!h.first) {
-            const float4 u = *p;
-            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
-          }
-          *p = v;
+        for (int q = 0; q < 4; ++q)
+          out.put(i, q, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+      out.rows([&](int row, int col, const uint4 &v) {
+        const int r = at.lane(j) + row, d = at.reg(0) + col;
+        if (r >= g.b_ext || d >= h.dx_pad) return;
+        float4 *p = reinterpret_cast<float4 *>(o + (int64_t)r * h.dx_pad + d);
+        float4 w = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+        if (!h.first) {
+          const float4 u = *p;
+          w.x += u.x; w.y += u.y; w.z += u.z; w.w += u.w;
         }
+        *p = w;
+      });
     }
   }
   if constexpr (EPI == E_DW) {
-    T *out = static_cast<T *>(h.dw);
-    const bool vec = h.dw_ld % (16 / (int)sizeof(T)) == 0 && (uintptr_t)out % 16 == 0;
+    constexpr int V = 16 / (int)sizeof(T);
+    T *o = static_cast<T *>(h.dw) + h.v0 * h.dw_ld;
+    const bool vec = h.dw_ld % V == 0 && (uintptr_t)h.dw % 16 == 0;
+    const RowsOut<T, 32 * TA> out{turn, lane};
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
-      const int cls = at.lane(j) + (lane & 31);
-      const bool live = cls < g.b_ext;
-      T *o = out + (h.v0 + cls) * h.dw_ld;
 #pragma unroll
-      for (int i = 0; i < TA; ++i) {
-        const int a = at.reg(i);
-        if constexpr (sizeof(T) == 2) {
+      for (int i = 0; i < TA; ++i)
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][8 * p + e]),
-                                                               __float_as_uint(acc[i][j][8 * p + 4 + e]), false, false);
-              v[e] = __uint_as_float(s2[0]);
-              v[4 + e] = __uint_as_float(s2[1]);
-            }
-            const int n = a + 16 * p + 8 * lh;
-            if (!live) continue;
-            if (vec && n + 8 <= h.dim) {
-              *reinterpret_cast<uint4 *>(o + n) =
-                  make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (n + e < h.dim) o[n + e] = f2bf(v[e]);
-            }
-          }
+        for (int q = 0; q < 4; ++q)
+          out.put(i, q, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+      out.rows([&](int row, int col, const uint4 &v) {
+        const int r = at.lane(j) + row, d = at.reg(0) + col;
+        if (r >= g.b_ext) return;
+        T *p = o + (int64_t)r * h.dw_ld + d;
+        if (vec && d + V <= h.dim) {
+          *reinterpret_cast<uint4 *>(p) = v;
         } else {
+          T w[V];
+          __builtin_memcpy(w, &v, 16);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int n = a + 8 * q + 4 * lh;
-            if (!live) continue;
-            if (vec && n + 4 <= h.dim) {
-              *reinterpret_cast<float4 *>(o + n) =
-                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (n + e < h.dim) o[n + e] = acc[i][j][4 * q + e];
-            }
-          }
+          for (int e = 0; e < V; ++e)
+            if (d + e < h.dim) p[e] = w[e];
         }
-      }
+      });
     }
   }
 }
@@ -375,6 +358,7 @@ struct RingTile {
   static constexpr int THREADS = 64 * WA * WB, TILE_A = BA, TILE_B = BB;
   static constexpr int SMEM = ST * (BA + BB) * 128;
   typedef SideTable<EPI, BA> Sides;
+  static_assert(RowsOut<float, BA / WA>::BYTES * WA * WB <= SMEM, "the epilogue's rows fit the ring");
   // One barrier a k-tile, ST stages of LDS.
   static __device__ __forceinline__ void run(const Gemm &g, const HeadArgs &h, uint8_t *smem, Sides &side, int bid) {
   constexpr int WAVES = WA * WB, TA = BA / WA / 32, TB = BB / WB / 32;
@@ -385,17 +369,19 @@ struct RingTile {
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wa = wave / WB, wb = wave % WB;
-  const int tiles = g.tiles_a * g.tiles_b;
-  const int split = bid / tiles, tile = bid % tiles;
+  constexpr bool SPLIT = EPI == E_DX;  // k over several workgroups
+  const uint32_t tiles = g.tiles_a * g.tiles_b;
+  const int split = SPLIT ? (int)((uint32_t)bid / tiles) : 0, tile = bid - split * (int)tiles;
   // the smaller side of the grid runs fastest, so the larger one's operand is
   // read by workgroups that run together
-  const int ta = g.tiles_a <= g.tiles_b ? tile % g.tiles_a : tile / g.tiles_b;
-  const int tb = g.tiles_a <= g.tiles_b ? tile / g.tiles_a : tile % g.tiles_b;
+  const int fast = g.tiles_a <= g.tiles_b ? g.tiles_a : g.tiles_b;
+  const int slow_i = (int)((uint32_t)tile / (uint32_t)fast), fast_i = tile - slow_i * fast;
+  const int ta = g.tiles_a <= g.tiles_b ? fast_i : slow_i, tb = g.tiles_a <= g.tiles_b ? slow_i : fast_i;
   const int a0 = ta * BA, b0 = tb * BB;
   const int nkt = (g.k_ext + SA::KT - 1) / SA::KT;
-  const int kt0 = (int)((int64_t)nkt * split / g.splits), kt1 = (int)((int64_t)nkt * (split + 1) / g.splits);
+  const int kt0 = SPLIT ? (int)((uint32_t)(nkt * split) / (uint32_t)g.splits) : 0;
+  const int kt1 = SPLIT ? (int)((uint32_t)(nkt * (split + 1)) / (uint32_t)g.splits) : nkt;
   const int nk = kt1 - kt0;
-  side.template load<THREADS>(g, h, a0, t);
 
   SA sa;
   SB sb;
@@ -431,6 +417,7 @@ struct RingTile {
 
 #pragma unroll
   for (int s = 0; s < ST - 1; ++s) issue();
+  side.template load<THREADS>(g, h, a0, t);  // behind the DMAs: their latencies overlap
   constexpr int PER = SA::LOADS + SB::LOADS;
   for (int kt = 0; kt < nk; ++kt) {
     // this wave's part of the k-tile has landed and its reads of the last one
@@ -471,14 +458,14 @@ struct RingTile {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __syncthreads();
 
-  const Place<32, 32, 64> at = {a0, a0 + wa * TA * 32, b0 + wb * TB * 32, ta * WA + wa};
-  epilogue<T, EPI>(g, h, acc, at, side, split, lane);
+  const Place<32, 64> at = {a0, a0 + wa * TA * 32, b0 + wb * TB * 32, ta * WA + wa};
+  epilogue<T, EPI>(g, h, acc, at, side, smem + wave * (SMEM / WAVES), split, lane);
   }
 };
 
 // The same product on 256 x 256 tiles.  Eight waves, two per SIMD: wave (g, c)
-// owns rows 64 g .. + 63 of both 128-row halves of B and rows 32 c .. + 31 of both
-// halves of A, 128 accumulator registers.  A k-tile is two steps, each a memory
+// owns rows 64 g .. + 63 of both 128-row halves of B and rows 64 c .. + 63 of A, 32 in
+// each of its halves (which take every other 32 rows), 128 accumulator registers.  A k-tile is two steps, each a memory
 // slot (fragments of the next 16 MFMAs out of LDS, DMAs of a later k-tile into
 // it) and a matrix slot, with a barrier after every slot; the two groups g run one
 // slot apart, so one group's MFMAs cover the other's LDS reads.  Two stages of
@@ -496,25 +483,27 @@ struct BigTile {
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  const int tiles = g.tiles_a * g.tiles_b;
-  const int split = bid / tiles, tile = bid % tiles;
-  const int ta = g.tiles_a <= g.tiles_b ? tile % g.tiles_a : tile / g.tiles_b;
-  const int tb = g.tiles_a <= g.tiles_b ? tile / g.tiles_a : tile % g.tiles_b;
+  constexpr bool SPLIT = EPI == E_DX;  // k over several workgroups
+  const uint32_t tiles = g.tiles_a * g.tiles_b;
+  const int split = SPLIT ? (int)((uint32_t)bid / tiles) : 0, tile = bid - split * (int)tiles;
+  const int fast = g.tiles_a <= g.tiles_b ? g.tiles_a : g.tiles_b;
+  const int slow_i = (int)((uint32_t)tile / (uint32_t)fast), fast_i = tile - slow_i * fast;
+  const int ta = g.tiles_a <= g.tiles_b ? fast_i : slow_i, tb = g.tiles_a <= g.tiles_b ? slow_i : fast_i;
   const int a0 = ta * 256, b0 = tb * 256;
   const int nkt = (g.k_ext + SA::KT - 1) / SA::KT;
-  const int kt0 = (int)((int64_t)nkt * split / g.splits), kt1 = (int)((int64_t)nkt * (split + 1) / g.splits);
+  const int kt0 = SPLIT ? (int)((uint32_t)(nkt * split) / (uint32_t)g.splits) : 0;
+  const int kt1 = SPLIT ? (int)((uint32_t)(nkt * (split + 1)) / (uint32_t)g.splits) : nkt;
   const int nk = kt1 - kt0;
-  side.template load<THREADS>(g, h, a0, t);
 
   SA sa[2];
   SB sb[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    sa[i].init(a0 + 128 * i, g.a_ext, g.a_ld, wave, lane);
+    sa[i].init(a0, g.a_ext, g.a_ld, wave, lane, i);
     sb[i].init(b0 + 128 * i, g.b_ext, g.b_ld, wave, lane);
   }
   const int64_t da = SA::k_step(g.a_ld), db = SB::k_step(g.b_ld);
-  const int64_t ha = SA::row_base(128, g.a_ld), hb = SB::row_base(128, g.b_ld);
+  const int64_t hb = SB::row_base(128, g.b_ld);
   const uint8_t *pa = static_cast<const uint8_t *>(g.a) + SA::row_base(a0, g.a_ld) + kt0 * da;
   const uint8_t *pb = static_cast<const uint8_t *>(g.b) + SB::row_base(b0, g.b_ld) + kt0 * db;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
@@ -529,7 +518,7 @@ struct BigTile {
       k_left = 0;
     }
   };
-  auto issue_a = [&](uint32_t stage, int i) { sa[i].issue(pa + i * ha, lds0 + stage + (2 + i) * HALF, k_left, wave); };
+  auto issue_a = [&](uint32_t stage, int i) { sa[i].issue(pa, lds0 + stage + (2 + i) * HALF, k_left, wave); };
   auto issue_b = [&](uint32_t stage, int i) { sb[i].issue(pb + i * hb, lds0 + stage + i * HALF, k_left, wave); };
 
   Frag fb[2][4], fa0[4], fa1[4];
@@ -583,6 +572,7 @@ struct BigTile {
   issue_b(STAGE, 0);
   issue_a(STAGE, 0);
   issue_a(STAGE, 1);
+  side.template load<THREADS>(g, h, a0, t);  // behind the DMAs: their latencies overlap
   uint32_t st = 0;
   mem_end();
   if (wm == 1) bar();  // the second group runs one slot behind
@@ -605,10 +595,11 @@ struct BigTile {
     st ^= STAGE;
   }
   if (wm == 0) bar();
-  // No DMA may outlive the workgroup's LDS (the last ones read nothing).
+  // The last DMAs (they read nothing) write to LDS that the epilogue uses.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  const Place<128, 32, 128> at = {a0, a0 + wn * 32, b0 + wm * 64, ta * 4 + wn};
-  epilogue<T, EPI>(g, h, acc, at, side, split, lane);
+  if constexpr (EPI != E_STATS) __syncthreads();
+  const Place<32, 128> at = {a0, a0 + wn * 64, b0 + wm * 64, ta * 4 + wn};
+  epilogue<T, EPI>(g, h, acc, at, side, smem + wave * (SMEM / 8), split, lane);
   }
 };
 
