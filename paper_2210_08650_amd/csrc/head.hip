@@ -250,7 +250,7 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
         for (int r = 0; r < 16; ++r) s[j] += __builtin_amdgcn_exp2f((acc[i][j][r] - mm) * c);
       s[j] += __shfl_xor(s[j], 32, 64);
       const int row = at.lane(j) + (lane & 31);
-      if (lh == 0 && row < g.b_ext) h.part[(int64_t)at.part * h.rows + row] = make_float2(m[j], s[j]);
+      if (lh == 0 && row < g.b_ext && at.part < h.parts) h.part[(int64_t)at.part * h.rows + row] = make_float2(m[j], s[j]);
     }
   }
   if constexpr (EPI == E_DLOGITS) {
@@ -296,7 +296,7 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
       });
       if (h.db_part) {
         sum += __shfl_xor(sum, 32, 64);
-        if (lh == 0 && cls < g.b_ext) h.db_part[(int64_t)at.part * h.classes + h.v0 + cls] = sum;
+        if (lh == 0 && cls < g.b_ext && at.part < h.db_parts) h.db_part[(int64_t)at.part * h.classes + h.v0 + cls] = sum;
       }
     }
   }
@@ -895,36 +895,109 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
   if (lane == 0) h.info[n] = info;
 }
 
-// Distillation's entries of dz^T: coefficient p less the weights of the row's
-// entries of this class (entries of one class write equal values).
+// Distillation, 256 threads a block.  Blocks [0, nt): the targets' entries of dz^T,
+// coefficient p less the weights of the row's entries of this class (entries of one
+// class write equal values).  The others (first piece, with a bias): what the
+// targets take off dbias, 128 classes and one slice of the entries each, as further
+// parts behind the row parts of db_part.  A block goes through its slice, 2048 a
+// round, keeps the entries of its classes in a list in a fixed order, and two
+// threads a class each take every other entry of the list.  (One block for all
+// entries of its classes: 63 us for 131,072 entries and 32,000 classes, of which
+// the sums are 15; in slices SLICEDUS.)
+constexpr int kBiasClasses = 128, kBiasRound = 2048;
 template <typename T>
-__global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= h.rows * h.top) return;
-  const int id = h.id32[i];
-  if (id < h.v0 || id >= h.v0 + h.piece) return;
-  const int64_t n = i / h.top;
-  const float2 info = h.info[n];
-  float v = __builtin_amdgcn_exp2f((h.picked[i] - info.x) * h.inv_t * kLog2e) * info.y;
-  for (int k = 0; k < h.top; ++k)
-    if (h.id32[n * h.top + k] == id) v -= h.cq[n * h.top + k];
-  put(static_cast<T *>(h.gt) + (id - h.v0) * h.rows_pad + n, v);
-}
-
-// dx[n][d] = the splits' partial sums in order, 0 in rows that do not count; in
-// blocks [0, nx) of the launch.  dbias, in the others, 128 classes a block: the row
-// parts' sums of dz's softmax part in order (dz whole for cross entropy), and for
-// distillation less the targets' weights: the block goes through all entries,
-// 8192 a round, keeps those of its classes in a list in a fixed order, and eight
-// threads a class each take every eighth entry of the list.  Fixed orders, so
-// results do not vary.
-constexpr int kReduceThreads = 1024, kBiasClasses = 128, kBiasRound = 8 * kReduceThreads;
-template <typename T>
-__global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h, int nx) {
-  __shared__ float sums[8][kBiasClasses];
-  __shared__ int cnt[16];
+__global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
+  __shared__ int cnt[4];
   __shared__ uint8_t list_c[kBiasRound];
   __shared__ float list_v[kBiasRound];
+  __shared__ float half_s[kBiasClasses];
+  const int t = threadIdx.x;
+  if ((int)blockIdx.x < nt) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + t;
+    if (i >= h.rows * h.top) return;
+    const int id = h.id32[i];
+    if (id < h.v0 || id >= h.v0 + h.piece) return;
+    const int64_t n = i / h.top;
+    const float2 info = h.info[n];
+    float v = __builtin_amdgcn_exp2f((h.picked[i] - info.x) * h.inv_t * kLog2e) * info.y;
+    for (int k = 0; k < h.top; ++k)
+      if (h.id32[n * h.top + k] == id) v -= h.cq[n * h.top + k];
+    put(static_cast<T *>(h.gt) + (id - h.v0) * h.rows_pad + n, v);
+    return;
+  }
+  const int lane = t & 63, wave = t >> 6;
+  const int b = blockIdx.x - nt, slice = b % kBiasSlices;
+  const int c0 = b / kBiasSlices * kBiasClasses;
+  const int mine = t % kBiasClasses, second = t / kBiasClasses;
+  const int64_t total = h.rows * h.top;
+  const int64_t per = (total + kBiasSlices * 4 - 1) / (kBiasSlices * 4) * 4;  // whole 16 bytes
+  const int64_t lo = slice * per, hi = lo + per < total ? lo + per : total;
+  float sum = 0.0f;
+  int4 nx[2];
+  auto fetch = [&](int64_t i0) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t i = i0 + u * (kBiasRound / 2) + 4 * t;
+      if (i + 4 <= hi) {
+        nx[u] = *reinterpret_cast<const int4 *>(h.id32 + i);
+      } else {
+        int v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = i + k < hi ? h.id32[i + k] : -1;
+        nx[u] = make_int4(v[0], v[1], v[2], v[3]);
+      }
+    }
+  };
+  fetch(lo);
+  for (int64_t i0 = lo; i0 < hi; i0 += kBiasRound) {
+    const int id[8] = {nx[0].x - c0, nx[0].y - c0, nx[0].z - c0, nx[0].w - c0,
+                       nx[1].x - c0, nx[1].y - c0, nx[1].z - c0, nx[1].w - c0};
+    fetch(i0 + kBiasRound);
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) n += (unsigned)id[k] < (unsigned)kBiasClasses;
+    int before = n;  // entries up to this lane's
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(before, o, 64);
+      if (lane >= o) before += u;
+    }
+    if (lane == 63) cnt[wave] = before;
+    __syncthreads();
+    int at = before - n, all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) at += cnt[w];
+      all += cnt[w];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if ((unsigned)id[k] < (unsigned)kBiasClasses) {
+        list_c[at] = (uint8_t)id[k];
+        list_v[at] = h.cq[i0 + (k >> 2) * (kBiasRound / 2) + 4 * t + (k & 3)];
+        ++at;
+      }
+    __syncthreads();
+    for (int k = second; k < all; k += 2)
+      if (list_c[k] == mine) sum -= list_v[k];
+    // the next round's counts are written before its first barrier and its list
+    // behind it, this round's counts read before the last barrier
+  }
+  __syncthreads();
+  if (second) half_s[mine] = sum;
+  __syncthreads();
+  if (!second && c0 + mine < h.classes)
+    h.db_part[(int64_t)(h.db_parts + slice) * h.classes + c0 + mine] = sum + half_s[mine];
+}
+
+// In blocks [0, nx) of the launch: dx[n][d] = the splits' partial sums in order, 0 in
+// rows that do not count.  In the others dbias, 128 classes a block: the sums of its
+// parts (the rows', and for distillation the targets'), four threads a class, in
+// order, so that results do not vary.
+constexpr int kReduceThreads = 512;
+template <typename T>
+__global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h, int nx) {
+  __shared__ float sums[4][kBiasClasses];
   const int t = threadIdx.x;
   if ((int)blockIdx.x < nx) {
     const int per = (h.dim + 3) / 4;
@@ -946,73 +1019,16 @@ __global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h,
     }
     return;
   }
-  const int lane = t & 63, wave = t >> 6;
   const int64_t c0 = (int64_t)(blockIdx.x - nx) * kBiasClasses;
   const int slice = t / kBiasClasses, mine = t % kBiasClasses;
+  const int parts = h.db_parts + (h.teacher ? kBiasSlices : 0);
   float sum = 0.0f;
   if (c0 + mine < h.classes)
-    for (int p = slice; p < h.db_parts; p += 8) sum += h.db_part[(int64_t)p * h.classes + c0 + mine];
-  const int64_t total = h.teacher ? h.rows * h.top : 0;
-  // entries 4 t .. + 3 of each half of a round; a round's are loaded during the last one's
-  int4 nx4[2];
-  auto fetch = [&](int64_t i0) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t i = i0 + u * (kBiasRound / 2) + 4 * t;
-      if (i + 4 <= total) {
-        nx4[u] = *reinterpret_cast<const int4 *>(h.id32 + i);
-      } else {
-        int v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = i + k < total ? h.id32[i + k] : -1;
-        nx4[u] = make_int4(v[0], v[1], v[2], v[3]);
-      }
-    }
-  };
-  fetch(0);
-  for (int64_t i0 = 0; i0 < total; i0 += kBiasRound) {
-    const int c = (int)c0;
-    const int id[8] = {nx4[0].x - c, nx4[0].y - c, nx4[0].z - c, nx4[0].w - c,
-                       nx4[1].x - c, nx4[1].y - c, nx4[1].z - c, nx4[1].w - c};
-    fetch(i0 + kBiasRound);
-    int n = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) n += (unsigned)id[k] < (unsigned)kBiasClasses;
-    int before = n;  // entries up to this lane's
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(before, o, 64);
-      if (lane >= o) before += u;
-    }
-    if (lane == 63) cnt[wave] = before;
-    __syncthreads();
-    int at = before - n, all = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      if (w < wave) at += cnt[w];
-      all += cnt[w];
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if ((unsigned)id[k] < (unsigned)kBiasClasses) {
-        list_c[at] = (uint8_t)id[k];
-        list_v[at] = h.cq[i0 + (k >> 2) * (kBiasRound / 2) + 4 * t + (k & 3)];
-        ++at;
-      }
-    __syncthreads();
-    for (int k = slice; k < all; k += 8)
-      if (list_c[k] == mine) sum -= list_v[k];
-    // the next round's counts are written before its first barrier, read after
-    // it; its list is written after it
-  }
+    for (int p = slice; p < parts; p += 4) sum += h.db_part[(int64_t)p * h.classes + c0 + mine];
   sums[slice][mine] = sum;
   __syncthreads();
-  if (slice == 0 && c0 + mine < h.classes) {
-    float v = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v += sums[k][mine];
-    h.dbias[c0 + mine] = v;
-  }
+  if (slice == 0 && c0 + mine < h.classes)
+    h.dbias[c0 + mine] = (sums[0][mine] + sums[1][mine]) + (sums[2][mine] + sums[3][mine]);
 }
 
 int grid_for(int64_t n, int per) {
@@ -1102,13 +1118,41 @@ hipError_t product(Variant v, const Gemm &g, const HeadArgs &a, hipStream_t s) {
   }
 }
 
+// The classes that 256 x 256 tiles take, the others going to 128 x 128 tiles in a
+// launch of their own: whole rounds of the large ones, where what is left of a
+// round costs more in them (1000 x 520 x 50,021, 784 tiles: 81 us, 768 of them and
+// 80 smaller ones ROUNDUS).  A part is 64 classes (or rows, for dbias) in either.
+int64_t big_classes(int64_t rows, int64_t classes) {
+  const int64_t rt = ceil_div(rows, 256), tiles = rt * ceil_div(classes, 256);
+  const int64_t whole = tiles / kCus * kCus / rt * 256;  // classes of the whole rounds
+  if (whole == 0 || whole >= classes) return classes;
+  const int64_t mid = ceil_div(rows, 128) * ceil_div(classes - whole, 128);
+  // rounds as in variant(): 19 us for 512 of them, 27.5 for 256 large ones
+  const double tm = 19.0 * (double)(mid / (2 * kCus)) + (mid % (2 * kCus) <= kCus ? 12.0 : 19.0);
+  return tm + 3.0 < 27.5 * (double)(ceil_div(tiles, kCus) - tiles / kCus) ? whole : classes;
+}
+
 template <typename T>
-hipError_t forward(const HeadArgs &a, hipStream_t s) {
+hipError_t forward(HeadArgs a, hipStream_t s) {
   Gemm g{};
   g.a = a.w; g.a_ld = a.w_ld; g.a_ext = (int)a.classes;
   g.b = a.x; g.b_ld = a.x_ld; g.b_ext = (int)a.rows;
   g.k_ext = a.dim; g.splits = 1;
-  return product<T, E_STATS>(variant(sizeof(T) == 2, a.rows, a.classes), g, a, s);
+  const Variant v = variant(sizeof(T) == 2, a.rows, a.classes);
+  if (v == BIG && sizeof(T) == 2) {
+    const int64_t c = big_classes(a.rows, a.classes);
+    if (c < a.classes) {
+      g.a_ext = (int)c;
+      const hipError_t e = product<T, E_STATS>(BIG, g, a, s);
+      if (e != hipSuccess) return e;
+      g.a = static_cast<const T *>(a.w) + c * a.w_ld;
+      g.a_ext = (int)(a.classes - c);
+      if (a.bias) a.bias += c;
+      a.part += c / 64 * a.rows;
+      return product<T, E_STATS>(MID, g, a, s);
+    }
+  }
+  return product<T, E_STATS>(v, g, a, s);
 }
 template <typename T>
 hipError_t dlogits(const HeadArgs &a, hipStream_t s) {
@@ -1117,9 +1161,23 @@ hipError_t dlogits(const HeadArgs &a, hipStream_t s) {
   g.a = a.x; g.a_ld = a.x_ld; g.a_ext = (int)a.rows;
   g.b = static_cast<const T *>(a.w) + a.v0 * a.w_ld; g.b_ld = a.w_ld; g.b_ext = (int)a.piece;
   g.k_ext = a.dim; g.splits = 1;
-  const hipError_t e = product<T, E_DLOGITS>(variant(sizeof(T) == 2, a.rows, a.classes), g, a, s);
+  const Variant v = variant(sizeof(T) == 2, a.rows, a.classes);
+  const int64_t c = v == BIG && sizeof(T) == 2 ? big_classes(a.rows, a.piece) : a.piece;
+  g.b_ext = (int)c;
+  hipError_t e = product<T, E_DLOGITS>(v, g, a, s);
+  if (e == hipSuccess && c < a.piece) {
+    HeadArgs rest = a;
+    rest.v0 += c;
+    rest.gt = static_cast<T *>(a.gt) + c * a.rows_pad;
+    g.b = static_cast<const T *>(g.b) + c * a.w_ld;
+    g.b_ext = (int)(a.piece - c);
+    e = product<T, E_DLOGITS>(MID, g, rest, s);
+  }
   if (e != hipSuccess || !a.teacher) return e;
-  hapi_launch(head_targets_kernel<T>, dim3((uint32_t)((a.rows * a.top + 255) / 256)), dim3(256), 0, s, a);
+  const int64_t nt = ceil_div(a.rows * a.top, 256);
+  const int64_t nb = a.db_part && a.first ? ceil_div(a.classes, kBiasClasses) * kBiasSlices : 0;
+  if (nt + nb > 0x7fffffff) return hipErrorInvalidValue;
+  hapi_launch(head_targets_kernel<T>, dim3((uint32_t)(nt + nb)), dim3(256), 0, s, a, (int)nt);
   return hipGetLastError();
 }
 template <typename T>
@@ -1146,7 +1204,7 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
 
 int head_parts(bool bf16, int64_t rows, int64_t classes) {
   switch (variant(bf16, rows, classes)) {
-    case BIG: return (int)ceil_div(classes, 256) * 4;
+    case BIG:  // a tile's parts past these are empty, and not written
     case MID: return (int)ceil_div(classes, 128) * 2;
     case SMALL: return (int)ceil_div(classes, 64) * 2;
     case TINY: return (int)ceil_div(classes, 32);
@@ -1155,7 +1213,7 @@ int head_parts(bool bf16, int64_t rows, int64_t classes) {
 }
 int head_db_parts(bool bf16, int64_t rows, int64_t classes) {
   switch (variant(bf16, rows, classes)) {
-    case BIG: return (int)ceil_div(rows, 256) * 4;
+    case BIG:
     case MID: return (int)ceil_div(rows, 128) * 2;
     case SMALL: return (int)ceil_div(rows, 64) * 2;
     default: return (int)ceil_div(rows, 32);

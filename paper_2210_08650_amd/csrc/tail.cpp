@@ -160,7 +160,7 @@ int read_head(const hapi_head_desc *d, Head &h) {
   h.o_id = take(d->rows * a.top * 4);
   h.o_cq = take(d->rows * a.top * 4);
   h.o_gt = take(h.piece * a.rows_pad * h.esz);
-  h.o_db = take((int64_t)a.db_parts * d->classes * 4);
+  h.o_db = take((int64_t)(a.db_parts + kBiasSlices) * d->classes * 4);
   h.o_dx = take((int64_t)a.splits * d->rows * a.dx_pad * 4);
   h.bytes_bwd = o;
   return HAPI_OK;

@@ -67,6 +67,7 @@ struct HeadArgs {
 int head_parts(bool bf16, int64_t rows, int64_t classes);
 int head_db_parts(bool bf16, int64_t rows, int64_t classes);
 int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece);
+constexpr int kBiasSlices = 8;  // distillation: parts of dbias for what the targets take off
 constexpr int kHeadRowPad = 64;
 constexpr int kHeadPiece = 256;  // pieces are multiples of this many classes
 

@@ -292,6 +292,13 @@ def test_several_pieces_of_the_classes(top):
     _head_check(c, _head_run(c))
 
 
+@pytest.mark.parametrize("rows,classes,top", [(1000, 50021, 0), (600, 33000, 3), (1300, 22100, 0)])
+def test_last_round_in_smaller_tiles(rows, classes, top):
+    """A few 256 x 256 tiles more than whole rounds of the CUs."""
+    c = _head_case(rows, rows, 64, classes, BF, bias=True, top=top)
+    _head_check(c, _head_run(c))
+
+
 def test_pieces_in_float32():
     c = _head_case(4, 1100, 40, 60100, F32, bias=False)
     _head_check(c, _head_run(c))
