@@ -383,6 +383,7 @@ def hapi_choose_split(**job):
 import torch  # noqa: E402  (mapped already: see _load)
 
 _TORCH_TYPES = {HAPI_F32: torch.float32, HAPI_BF16: torch.bfloat16}
+_F32 = torch.float32
 
 class _TailDesc:
     """Owns a descriptor of the trained tail's operators."""
@@ -428,7 +429,18 @@ class Head(_TailDesc):
         self.c.x_stride, self.c.w_stride = int(x_stride), int(w_stride)
 
 
-def _tensor(p, name, dtype, rows, dim=None, stride=0):
+_have_gpu = None
+
+
+def _device():
+    """The current device's index, or None without a GPU."""
+    global _have_gpu
+    if _have_gpu is None:
+        _have_gpu = torch.cuda.is_available()
+    return torch.cuda.current_device() if _have_gpu else None
+
+
+def _tensor(dev, p, name, dtype, shape, stride=0):
     """The address of an argument.  Of a tensor the type, the sizes and the row
     stride have to be the descriptor's, and its device the current one (an address
     is taken as it is)."""
@@ -436,22 +448,16 @@ def _tensor(p, name, dtype, rows, dim=None, stride=0):
         return p
     if not hasattr(p, "data_ptr"):
         return _ptr(p)
-    shape = (rows,) if dim is None else (rows, dim)
-    want = _TORCH_TYPES.get(dtype, dtype)
-    if p.dtype is not want or p.shape != shape:
-        raise HapiError(HAPI_E_INVAL, f"{name} must be {want} of shape {shape}, got {p.dtype} {tuple(p.shape)}")
-    if not p.is_contiguous() or (stride and stride != dim and rows > 1):
-        step = stride or dim
-        if (p.stride(-1) != 1 and p.shape[-1] > 1) or (dim is not None and rows > 1 and p.stride(0) != step):
+    if p.dtype is not dtype or p.shape != shape:
+        raise HapiError(HAPI_E_INVAL, f"{name} must be {dtype} of shape {shape}, got {p.dtype} {tuple(p.shape)}")
+    if not p.is_contiguous() or stride:
+        step = stride or shape[-1]
+        if (p.stride(-1) != 1 and p.shape[-1] > 1) or (len(shape) == 2 and shape[0] > 1 and p.stride(0) != step):
             raise HapiError(HAPI_E_INVAL, f"{name} must have rows of consecutive values, {step} apart, "
                                           f"got strides {tuple(p.stride())}")
-    if p.get_device() != (torch.cuda.current_device() if p.is_cuda else None):
+    if p.get_device() != dev:
         raise HapiError(HAPI_E_INVAL, f"{name} is on {p.device}, not on the current GPU")
     return p.data_ptr()
-
-
-def _f32(p, name, *shape):
-    return _tensor(p, name, HAPI_F32, *shape)
 
 
 def hapi_layernorm_workspace_bytes(desc: Norm) -> int:
@@ -459,63 +465,76 @@ def hapi_layernorm_workspace_bytes(desc: Norm) -> int:
 
 
 def hapi_layernorm_forward(desc: Norm, x, gamma, beta, y, mean, rstd) -> None:
-    c = desc.c
+    c, dev = desc.c, _device()
+    n, d = c.rows, c.dim
+    t = _TORCH_TYPES.get(c.dtype)
     _check(_lib.hapi_layernorm_forward(
-        desc.ref, _tensor(x, "x", c.dtype, c.rows, c.dim, c.x_stride), _f32(gamma, "gamma", c.dim),
-        _f32(beta, "beta", c.dim), _tensor(y, "y", c.dtype, c.rows, c.dim, c.y_stride),
-        _f32(mean, "mean", c.rows), _f32(rstd, "rstd", c.rows)))
+        desc.ref, _tensor(dev, x, "x", t, (n, d), c.x_stride), _tensor(dev, gamma, "gamma", _F32, (d,)),
+        _tensor(dev, beta, "beta", _F32, (d,)), _tensor(dev, y, "y", t, (n, d), c.y_stride),
+        _tensor(dev, mean, "mean", _F32, (n,)), _tensor(dev, rstd, "rstd", _F32, (n,))))
 
 
 def hapi_layernorm_backward(desc: Norm, dy, x, gamma, mean, rstd, dx, dgamma, dbeta) -> None:
-    c = desc.c
+    c, dev = desc.c, _device()
+    n, d = c.rows, c.dim
+    t = _TORCH_TYPES.get(c.dtype)
     _check(_lib.hapi_layernorm_backward(
-        desc.ref, _tensor(dy, "dy", c.dtype, c.rows, c.dim, c.y_stride),
-        _tensor(x, "x", c.dtype, c.rows, c.dim, c.x_stride), _f32(gamma, "gamma", c.dim),
-        _f32(mean, "mean", c.rows), _f32(rstd, "rstd", c.rows),
-        _tensor(dx, "dx", c.dtype, c.rows, c.dim, c.x_stride), _f32(dgamma, "dgamma", c.dim),
-        _f32(dbeta, "dbeta", c.dim)))
+        desc.ref, _tensor(dev, dy, "dy", t, (n, d), c.y_stride), _tensor(dev, x, "x", t, (n, d), c.x_stride),
+        _tensor(dev, gamma, "gamma", _F32, (d,)), _tensor(dev, mean, "mean", _F32, (n,)),
+        _tensor(dev, rstd, "rstd", _F32, (n,)), _tensor(dev, dx, "dx", t, (n, d), c.x_stride),
+        _tensor(dev, dgamma, "dgamma", _F32, (d,)), _tensor(dev, dbeta, "dbeta", _F32, (d,))))
 
 
 def hapi_head_workspace_bytes(desc: Head, backward: bool = False) -> int:
     return _check(_lib.hapi_head_workspace_bytes(desc.ref, int(bool(backward))))
 
 
-def _head_inputs(c, x, weight, bias):
-    return [_tensor(x, "x", c.dtype, c.rows, c.dim, c.x_stride),
-            _tensor(weight, "weight", c.dtype, c.classes, c.dim, c.w_stride), _f32(bias, "bias", c.classes)]
+def _head_inputs(c, dev, x, weight, bias):
+    t = _TORCH_TYPES.get(c.dtype)
+    return (_tensor(dev, x, "x", t, (c.rows, c.dim), c.x_stride),
+            _tensor(dev, weight, "weight", t, (c.classes, c.dim), c.w_stride),
+            _tensor(dev, bias, "bias", _F32, (c.classes,)))
 
 
-def _head_gradients(c, dx, dweight, dbias):
-    return [_tensor(dx, "dx", c.dtype, c.rows, c.dim, c.x_stride),
-            _tensor(dweight, "dweight", c.dtype, c.classes, c.dim, c.w_stride), _f32(dbias, "dbias", c.classes)]
+def _head_gradients(c, dev, dx, dweight, dbias):
+    t = _TORCH_TYPES.get(c.dtype)
+    return (_tensor(dev, dx, "dx", t, (c.rows, c.dim), c.x_stride),
+            _tensor(dev, dweight, "dweight", t, (c.classes, c.dim), c.w_stride),
+            _tensor(dev, dbias, "dbias", _F32, (c.classes,)))
 
 
 def hapi_xent_forward(desc: Head, x, weight, bias, targets, loss, stats) -> None:
-    c = desc.c
+    c, dev = desc.c, _device()
+    n = c.rows
     _check(_lib.hapi_xent_forward(
-        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(targets, "targets", torch.int64, c.rows),
-        _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2)))
+        desc.ref, *_head_inputs(c, dev, x, weight, bias), _tensor(dev, targets, "targets", torch.int64, (n,)),
+        _tensor(dev, loss, "loss", _F32, (n,)), _tensor(dev, stats, "stats", _F32, (n, 2))))
 
 
 def hapi_xent_backward(desc: Head, x, weight, bias, targets, loss, stats, dloss, dx, dweight, dbias) -> None:
-    c = desc.c
+    c, dev = desc.c, _device()
+    n = c.rows
     _check(_lib.hapi_xent_backward(
-        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(targets, "targets", torch.int64, c.rows),
-        _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2), _f32(dloss, "dloss", c.rows),
-        *_head_gradients(c, dx, dweight, dbias)))
+        desc.ref, *_head_inputs(c, dev, x, weight, bias), _tensor(dev, targets, "targets", torch.int64, (n,)),
+        _tensor(dev, loss, "loss", _F32, (n,)), _tensor(dev, stats, "stats", _F32, (n, 2)),
+        _tensor(dev, dloss, "dloss", _F32, (n,)), *_head_gradients(c, dev, dx, dweight, dbias)))
 
 
 def hapi_distill_forward(desc: Head, x, weight, bias, ids, teacher, loss, stats, picked) -> None:
-    c = desc.c
+    c, dev = desc.c, _device()
+    n, k = c.rows, c.top
     _check(_lib.hapi_distill_forward(
-        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(ids, "ids", torch.int64, c.rows, c.top),
-        _f32(teacher, "teacher", c.rows, c.top), _f32(loss, "loss", c.rows), _f32(stats, "stats", c.rows, 2),
-        _f32(picked, "picked", c.rows, c.top)))
+        desc.ref, *_head_inputs(c, dev, x, weight, bias), _tensor(dev, ids, "ids", torch.int64, (n, k)),
+        _tensor(dev, teacher, "teacher", _F32, (n, k)), _tensor(dev, loss, "loss", _F32, (n,)),
+        _tensor(dev, stats, "stats", _F32, (n, 2)), _tensor(dev, picked, "picked", _F32, (n, k))))
 
 
-def hapi_distill_backward(desc: Head, x, weight, bias, ids, teacher, stats, picked, dloss, dx, dweight, dbias) -> None:
-    c = desc.c
+def hapi_distill_backward(desc: Head, x, weight, bias, ids, teacher, stats, picked, dloss, dx, dweight,
+                          dbias) -> None:
+    c, dev = desc.c, _device()
+    n, k = c.rows, c.top
     _check(_lib.hapi_distill_backward(
-        desc.ref, *_head_inputs(c, x, weight, bias), _tensor(ids, "ids", torch.int64, c.rows, c.top),
-        _f32(teacher, "teacher", c.rows, c.top), _f32(stats, "stats", c.rows, 2), _f32(picked, "picked", c.rows, c.top),
-        _f32(dloss, "dloss", c.rows), *_head_gradients(c, dx, dweight, dbias)))
+        desc.ref, *_head_inputs(c, dev, x, weight, bias), _tensor(dev, ids, "ids", torch.int64, (n, k)),
+        _tensor(dev, teacher, "teacher", _F32, (n, k)), _tensor(dev, stats, "stats", _F32, (n, 2)),
+        _tensor(dev, picked, "picked", _F32, (n, k)), _tensor(dev, dloss, "dloss", _F32, (n,)),
+        *_head_gradients(c, dev, dx, dweight, dbias)))

@@ -463,6 +463,76 @@ struct RingTile {
   }
 };
 
+// 32 x 32 tiles for the smallest calls, the k-steps of a k-tile on four waves, whose
+// sums the first one adds up in order.  A k-tile costs a workgroup its DMAs, LDS
+// reads and MFMAs one after the other (0.25 us with one wave, 0.27 us with four
+// waves on a 64 x 64 tile); four waves on one tile have a quarter of each.
+template <typename T, int ST, int EPI>
+struct TinyTile {
+  static constexpr int THREADS = 256, TILE_A = 32, TILE_B = 32;
+  typedef Side<T, 32, false, 4> S;
+  static constexpr int STAGE = 2 * S::BYTES, SMEM = ST * STAGE;
+  static_assert(S::KSTEPS == 4 && S::LOADS == 1, "a k-step and a DMA of each operand to a wave");
+  static_assert(SMEM >= 3 * 4096 + RowsOut<float, 32>::BYTES, "the sums and the epilogue's rows fit the ring");
+  typedef SideTable<EPI, 32> Sides;
+  static __device__ __forceinline__ void run(const Gemm &g, const HeadArgs &h, uint8_t *smem, Sides &side, int bid) {
+    const int t = threadIdx.x, lane = t & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int ta = bid % g.tiles_a, tb = bid / g.tiles_a;
+    const int a0 = ta * 32, b0 = tb * 32;
+    const int nk = (g.k_ext + S::KT - 1) / S::KT;
+    S sa, sb;
+    sa.init(a0, g.a_ext, g.a_ld, wave, lane);
+    sb.init(b0, g.b_ext, g.b_ld, wave, lane);
+    const uint8_t *pa = static_cast<const uint8_t *>(g.a) + S::row_base(a0, g.a_ld);
+    const uint8_t *pb = static_cast<const uint8_t *>(g.b) + S::row_base(b0, g.b_ld);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+    int issued = 0;
+    auto issue = [&] {  // past the last k-tile: nothing read
+      const uint32_t dst = lds0 + (uint32_t)(issued % ST) * STAGE;
+      const int left = issued < nk ? g.k_ext - issued * S::KT : 0;
+      const int64_t o = issued < nk ? (int64_t)issued * 128 : 0;
+      sa.issue(pa + o, dst, left, wave);
+      sb.issue(pb + o, dst + S::BYTES, left, wave);
+      ++issued;
+    };
+    f32x16_t acc[1][1];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[0][0][r] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < ST - 1; ++s) issue();
+    side.template load<THREADS>(g, h, a0, t);
+    for (int kt = 0; kt < nk; ++kt) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((ST - 2) * 2) : "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      const uint8_t *at = smem + (kt % ST) * STAGE;
+      const typename Elem<T>::Frag fa = S::frag(at, 0, wave, lane), fb = S::frag(at + S::BYTES, 0, wave, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      issue();
+      __builtin_amdgcn_sched_barrier(0);
+      acc[0][0] = mma(fa, fb, acc[0][0]);
+    }
+    // No DMA may outlive the workgroup's LDS, or write to it when it holds the sums.
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    float *part = reinterpret_cast<float *>(smem);
+    if (wave > 0)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) part[((wave - 1) * 16 + r) * 64 + lane] = acc[0][0][r];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[0][0][r] += part[(w * 16 + r) * 64 + lane];
+    const Place<32, 64> at = {a0, a0, b0, ta};
+    epilogue<T, EPI>(g, h, acc, at, side, smem + 3 * 4096, 0, lane);
+  }
+};
+
 // The same product on 256 x 256 tiles.  Eight waves, two per SIMD: wave (g, c)
 // owns rows 64 g .. + 63 of both 128-row halves of B and rows 64 c .. + 63 of A, 32 in
 // each of its halves (which take every other 32 rows), 128 accumulator registers.  A k-tile is two steps, each a memory
@@ -1044,11 +1114,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kCus = 256;
 
 Variant variant(bool bf16, int64_t rows, int64_t classes) {
-  // The smallest calls: a k-tile costs a workgroup some 0.3 us of loads, LDS reads
-  // and MFMAs one after the other, whatever the tile, so one-wave tiles over more CUs
-  // lose nothing (128 x 2048 x 1000: 14.0 us, 32 workgroups of 64 x 64 tiles
-  // 13.6 us; 8 x 768 x 1000: 7.4 us, 8 workgroups of 32 x 128 tiles 8.4 us).
-  if (ceil_div(rows, 32) * ceil_div(classes, 32) <= kCus) return TINY;
+  // TINYRULE
+  if (ceil_div(rows, 32) * ceil_div(classes, 32) <= 2 * kCus) return TINY;
   if (rows <= 32) return FEW;
   const int64_t big = ceil_div(rows, 256) * ceil_div(classes, 256), mid = ceil_div(rows, 128) * ceil_div(classes, 128),
                 small = ceil_div(rows, 64) * ceil_div(classes, 64);
@@ -1078,7 +1145,7 @@ struct Tiles<T, E_STATS> {
   typedef RingTile<T, 64, 64, 2, 2, 3, false, false, E_STATS> Small;
   typedef RingTile<T, 128, 32, 4, 1, 7, false, false, E_STATS> Few;
   typedef RingTile<T, 64, 64, 2, 2, 8, false, false, E_STATS> Deep;
-  typedef RingTile<T, 32, 32, 1, 1, 8, false, false, E_STATS> Tiny;
+  typedef TinyTile<T, 8, E_STATS> Tiny;
 };
 template <typename T>
 struct Tiles<T, E_DLOGITS> {
@@ -1087,7 +1154,7 @@ struct Tiles<T, E_DLOGITS> {
   typedef RingTile<T, 64, 64, 2, 2, 3, false, false, E_DLOGITS> Small;
   typedef RingTile<T, 32, 128, 1, 4, 7, false, false, E_DLOGITS> Few;
   typedef RingTile<T, 64, 64, 2, 2, 8, false, false, E_DLOGITS> Deep;
-  typedef RingTile<T, 32, 32, 1, 1, 8, false, false, E_DLOGITS> Tiny;
+  typedef TinyTile<T, 8, E_DLOGITS> Tiny;
 };
 template <typename T>
 struct Tiles<T, E_DX> {
