@@ -327,6 +327,7 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
     constexpr int V = 16 / (int)sizeof(T);
     T *o = static_cast<T *>(h.dw) + h.v0 * h.dw_ld;
     const bool vec = h.dw_ld % V == 0 && (uintptr_t)h.dw % 16 == 0;
+    const float unit = h.rows > 0 ? *h.unit : 0.0f;
     const RowsOut<T, 32 * TA> out{turn, lane};
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
@@ -334,7 +335,8 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
       for (int i = 0; i < TA; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          out.put(i, q, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+          out.put(i, q, acc[i][j][4 * q] * unit, acc[i][j][4 * q + 1] * unit, acc[i][j][4 * q + 2] * unit,
+                  acc[i][j][4 * q + 3] * unit);
       out.rows([&](int row, int col, const uint4 &v) {
         const int r = at.lane(j) + row, d = at.reg(0) + col;
         if (r >= g.b_ext) return;
@@ -911,7 +913,16 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
   float2 info = make_float2(INFINITY, 0.0f);
   if (n < h.rows) {
     const int64_t *ids = h.ids + n * h.top;
-    float coef = h.dloss[n] * h.t;
+    // The first row's coefficient's significand, which every coefficient is divided
+    // by and the gradients are multiplied by in float32: where all rows have the same
+    // dloss (a mean's), a target's entry of dz is then a power of two times p - 1, and
+    // not off by the rounding of dloss to 16 bits in every row alike (up to 2^-8 of
+    // the whole gradient: 0.004 at 8192 x 2048 x 131072, PRECUS without).  Its
+    // value is of no importance else: coefficients stay within a factor of two.
+    const float c0 = fabsf(h.dloss[0] * h.t);
+    const float unit = c0 > 0.0f && c0 < INFINITY ? __uint_as_float((__float_as_uint(c0) & 0x7fffffu) | 0x3f800000u) : 1.0f;
+    if (n == 0 && lane == 0) *h.unit = unit;
+    float coef = h.dloss[n] * h.t / unit;
     float bad = 0.0f;
     bool none;
     float tm = -INFINITY, ts = 1.0f;
@@ -980,7 +991,7 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
   __shared__ int cnt[4];
   __shared__ uint8_t list_c[kBiasRound];
   __shared__ float list_v[kBiasRound];
-  __shared__ float half_s[kBiasClasses];
+  __shared__ double half_s[kBiasClasses];
   const int t = threadIdx.x;
   if ((int)blockIdx.x < nt) {
     const int64_t i = (int64_t)blockIdx.x * 256 + t;
@@ -1002,7 +1013,7 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
   const int64_t total = h.rows * h.top;
   const int64_t per = (total + kBiasSlices * 4 - 1) / (kBiasSlices * 4) * 4;  // whole 16 bytes
   const int64_t lo = slice * per, hi = lo + per < total ? lo + per : total;
-  float sum = 0.0f;
+  double sum = 0.0;
   int4 nx[2];
   auto fetch = [&](int64_t i0) {
 #pragma unroll
@@ -1057,18 +1068,19 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
   if (second) half_s[mine] = sum;
   __syncthreads();
   if (!second && c0 + mine < h.classes)
-    h.db_part[(int64_t)(h.db_parts + slice) * h.classes + c0 + mine] = sum + half_s[mine];
+    h.db_part[(int64_t)(h.db_parts + slice) * h.classes + c0 + mine] = (float)(sum + half_s[mine]);
 }
 
 // In blocks [0, nx) of the launch: dx[n][d] = the splits' partial sums in order, 0 in
 // rows that do not count.  In the others dbias, 128 classes a block: the sums of its
-// parts (the rows', and for distillation the targets'), four threads a class, in
-// order, so that results do not vary.
+// parts (the rows', and for distillation the targets', which cancel much of them: in
+// 64 bits), four threads a class, in order, so that results do not vary.
 constexpr int kReduceThreads = 512;
 template <typename T>
 __global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h, int nx) {
-  __shared__ float sums[4][kBiasClasses];
+  __shared__ double sums[4][kBiasClasses];
   const int t = threadIdx.x;
+  const float unit = h.rows > 0 ? *h.unit : 0.0f;
   if ((int)blockIdx.x < nx) {
     const int per = (h.dim + 3) / 4;
     const int64_t total = h.rows * per;
@@ -1085,20 +1097,20 @@ __global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h,
       T *o = dx + n * h.dx_ld + d;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (d + j < h.dim) put(o + j, v[j]);
+        if (d + j < h.dim) put(o + j, v[j] * unit);
     }
     return;
   }
   const int64_t c0 = (int64_t)(blockIdx.x - nx) * kBiasClasses;
   const int slice = t / kBiasClasses, mine = t % kBiasClasses;
   const int parts = h.db_parts + (h.teacher ? kBiasSlices : 0);
-  float sum = 0.0f;
+  double sum = 0.0;
   if (c0 + mine < h.classes)
     for (int p = slice; p < parts; p += 4) sum += h.db_part[(int64_t)p * h.classes + c0 + mine];
   sums[slice][mine] = sum;
   __syncthreads();
   if (slice == 0 && c0 + mine < h.classes)
-    h.dbias[c0 + mine] = (sums[0][mine] + sums[1][mine]) + (sums[2][mine] + sums[3][mine]);
+    h.dbias[c0 + mine] = (float)(((sums[0][mine] + sums[1][mine]) + (sums[2][mine] + sums[3][mine])) * (double)unit);
 }
 
 int grid_for(int64_t n, int per) {

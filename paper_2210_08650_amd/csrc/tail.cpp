@@ -95,7 +95,7 @@ struct Head {
   int64_t piece;     // classes of a piece
   int64_t bytes_fwd, bytes_bwd;
   // byte offsets into the workspace
-  int64_t o_part, o_xs, o_ws, o_info, o_id, o_cq, o_gt, o_db, o_dx;
+  int64_t o_part, o_xs, o_ws, o_info, o_unit, o_id, o_cq, o_gt, o_db, o_dx;
 };
 
 int read_head(const hapi_head_desc *d, Head &h) {
@@ -157,6 +157,7 @@ int read_head(const hapi_head_desc *d, Head &h) {
   o = h.o_xs;
   take(xs);
   h.o_info = take(a.rows_pad * 8);
+  h.o_unit = take(4);
   h.o_id = take(d->rows * a.top * 4);
   h.o_cq = take(d->rows * a.top * 4);
   h.o_gt = take(h.piece * a.rows_pad * h.esz);
@@ -237,6 +238,7 @@ int head_backward(const hapi_head_desc *d, Head &h, const void *x, const void *w
   a.picked = const_cast<float *>(picked);
   a.dloss = dloss;
   a.info = reinterpret_cast<float2 *>(base + h.o_info);
+  a.unit = reinterpret_cast<float *>(base + h.o_unit);
   a.id32 = reinterpret_cast<int32_t *>(base + h.o_id);
   a.cq = reinterpret_cast<float *>(base + h.o_cq);
   a.gt = base + h.o_gt;

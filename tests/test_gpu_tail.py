@@ -10,7 +10,7 @@ import torch
 import paper_2210_08650_amd as H
 from paper_2210_08650_amd import models as PM
 from tests import tail_reference as R
-from tests.hip_harness import SENTINEL, Guarded
+from tests.hip_harness import Guarded
 
 pytestmark = pytest.mark.gpu
 
@@ -434,6 +434,20 @@ def test_distillation_entries():
         keep = torch.arange(8, device="cuda") != 5
         assert math.isnan(float(b["loss"][5])) and bool(torch.isnan(b["dx"][5]).all()), what
         assert torch.equal(b["loss"][keep], got["loss"][keep]) and torch.equal(b["dx"][keep], got["dx"][keep])
+
+
+@pytest.mark.parametrize("rows,classes", [(20, 900), (300, 5003), (700, 33000)])
+def test_a_mean_keeps_its_targets_whole(rows, classes):
+    """With one dloss for all rows a target's entry of dz is -1 + p of a power of
+    two, so dz's rounding to 16 bits takes at most 2^-9 of p there, not up to 2^-8
+    of the whole gradient: what is left is the gradients' own rounding, 2^-8 / sqrt 3
+    of their length at most, and the small entries'."""
+    c = _head_case(50, rows, 96, classes, BF, bias=False, spread=1.0)
+    c["dloss"].fill_(1.0 / 7782)  # a significand of 1.0527: 16 bits would put 1.0547
+    got = _head_run(c)
+    want = R.head(c["x"], c["w"], None, c["ids"], None, 1.0, c["dloss"])
+    for name in ("dx", "dw"):
+        R.check(name, got[name], want[name], 1.1 * 2.0 ** -8 / math.sqrt(3))
 
 
 @pytest.mark.parametrize("top", [0, 3])
