@@ -44,6 +44,20 @@ struct Gemm {
   int splits;               // of k, over workgroups: whole k-tiles
 };
 
+// Tile `tile` of the grid: panels of 8 tiles of its smaller side, each along the whole
+// larger one, so that the 32 workgroups an XCD runs at once are 8 x 4 tiles and
+// share their operands' k-tiles in its L2 (8192 x 2048 x 131072 forward, one panel
+// of all 32: half the requests miss).  PANELUS
+__device__ __forceinline__ void place_tile(const Gemm &g, int tile, int &ta, int &tb) {
+  const bool a_small = g.tiles_a <= g.tiles_b;
+  const int few = a_small ? g.tiles_a : g.tiles_b, many = a_small ? g.tiles_b : g.tiles_a;
+  const int p = (int)((uint32_t)tile / (uint32_t)(8 * many));
+  const int w = few - 8 * p < 8 ? few - 8 * p : 8;
+  const int i = tile - p * 8 * many, m = (int)((uint32_t)i / (uint32_t)w), f = 8 * p + i - m * w;
+  ta = a_small ? f : m;
+  tb = a_small ? m : f;
+}
+
 enum Epi { E_STATS, E_DLOGITS, E_DX, E_DW };
 
 template <typename T>
@@ -374,11 +388,8 @@ struct RingTile {
   constexpr bool SPLIT = EPI == E_DX;  // k over several workgroups
   const uint32_t tiles = g.tiles_a * g.tiles_b;
   const int split = SPLIT ? (int)((uint32_t)bid / tiles) : 0, tile = bid - split * (int)tiles;
-  // the smaller side of the grid runs fastest, so the larger one's operand is
-  // read by workgroups that run together
-  const int fast = g.tiles_a <= g.tiles_b ? g.tiles_a : g.tiles_b;
-  const int slow_i = (int)((uint32_t)tile / (uint32_t)fast), fast_i = tile - slow_i * fast;
-  const int ta = g.tiles_a <= g.tiles_b ? fast_i : slow_i, tb = g.tiles_a <= g.tiles_b ? slow_i : fast_i;
+  int ta, tb;
+  place_tile(g, tile, ta, tb);
   const int a0 = ta * BA, b0 = tb * BB;
   const int nkt = (g.k_ext + SA::KT - 1) / SA::KT;
   const int kt0 = SPLIT ? (int)((uint32_t)(nkt * split) / (uint32_t)g.splits) : 0;
@@ -558,9 +569,8 @@ struct BigTile {
   constexpr bool SPLIT = EPI == E_DX;  // k over several workgroups
   const uint32_t tiles = g.tiles_a * g.tiles_b;
   const int split = SPLIT ? (int)((uint32_t)bid / tiles) : 0, tile = bid - split * (int)tiles;
-  const int fast = g.tiles_a <= g.tiles_b ? g.tiles_a : g.tiles_b;
-  const int slow_i = (int)((uint32_t)tile / (uint32_t)fast), fast_i = tile - slow_i * fast;
-  const int ta = g.tiles_a <= g.tiles_b ? fast_i : slow_i, tb = g.tiles_a <= g.tiles_b ? slow_i : fast_i;
+  int ta, tb;
+  place_tile(g, tile, ta, tb);
   const int a0 = ta * 256, b0 = tb * 256;
   const int nkt = (g.k_ext + SA::KT - 1) / SA::KT;
   const int kt0 = SPLIT ? (int)((uint32_t)(nkt * split) / (uint32_t)g.splits) : 0;
