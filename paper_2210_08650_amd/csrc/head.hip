@@ -923,14 +923,16 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
   float2 info = make_float2(INFINITY, 0.0f);
   if (n < h.rows) {
     const int64_t *ids = h.ids + n * h.top;
-    // The first row's coefficient's significand, which every coefficient is divided
-    // by and the gradients are multiplied by in float32: where all rows have the same
+    // The significand of a coefficient (of the first row that counts, among 64), which
+    // every coefficient is divided by and the gradients are multiplied by in float32: where all rows have the same
     // dloss (a mean's), a target's entry of dz is then a power of two times p - 1, and
     // not off by the rounding of dloss to 16 bits in every row alike (up to 2^-8 of
     // the whole gradient: 0.004 at 8192 x 2048 x 131072, PRECUS without).  Its
     // value is of no importance else: coefficients stay within a factor of two.
-    const float c0 = fabsf(h.dloss[0] * h.t);
-    const float unit = c0 > 0.0f && c0 < INFINITY ? __uint_as_float((__float_as_uint(c0) & 0x7fffffu) | 0x3f800000u) : 1.0f;
+    const float c0 = fabsf(lane < h.rows ? h.dloss[lane] * h.t : 0.0f);
+    const uint64_t some = __ballot(c0 > 0.0f && c0 < INFINITY && h.ids[lane < h.rows ? lane * (int64_t)h.top : 0] >= 0);
+    const uint32_t bits = __shfl(__float_as_uint(c0), some ? __ffsll((unsigned long long)some) - 1 : 0, 64);
+    const float unit = some ? __uint_as_float((bits & 0x7fffffu) | 0x3f800000u) : 1.0f;
     if (n == 0 && lane == 0) *h.unit = unit;
     float coef = h.dloss[n] * h.t / unit;
     float bad = 0.0f;
@@ -1130,34 +1132,6 @@ int grid_for(int64_t n, int per) {
 
 // ---------------------------------------------------------------- variants
 
-// Tiles of the products.  FEW: up to 32 rows, the weights stream past.
-enum Variant { BIG, MID, SMALL, FEW, TINY };
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int64_t kCus = 256;
-
-Variant variant(bool bf16, int64_t rows, int64_t classes) {
-  // TINYRULE
-  if (ceil_div(rows, 32) * ceil_div(classes, 32) <= 2 * kCus) return TINY;
-  if (rows <= 32) return FEW;
-  const int64_t big = ceil_div(rows, 256) * ceil_div(classes, 256), mid = ceil_div(rows, 128) * ceil_div(classes, 128),
-                small = ceil_div(rows, 64) * ceil_div(classes, 64);
-  double tb, tm, ts;
-  if (bf16) {
-    // 27.5, 19 and 10.3 us a round of 256, 512 and 768 workgroups at 768 features
-    // (4096 x 768 x 32000); the last round less when it holds one to a CU.
-    tb = 27.5 * (double)ceil_div(big, kCus);
-    tm = 19.0 * (double)(mid / (2 * kCus)) + (mid % (2 * kCus) == 0 ? 0.0 : mid % (2 * kCus) <= kCus ? 12.0 : 19.0);
-    const int64_t r = small % (3 * kCus);
-    ts = 10.3 * (double)(small / (3 * kCus)) + (r == 0 ? 0.0 : r <= kCus ? 5.0 : r <= 2 * kCus ? 7.5 : 10.3);
-  } else {
-    // the matrix pipes are the bound: a CU's workgroups take turns on them
-    tb = 16.0 * (double)ceil_div(big, kCus);
-    tm = 4.25 * (double)ceil_div(mid, kCus);
-    ts = 1.06 * (double)ceil_div(small, kCus);
-  }
-  return tb <= tm && tb <= ts ? BIG : tm <= ts ? MID : SMALL;
-}
-
 template <typename T, int EPI>
 struct Tiles;
 template <typename T>
@@ -1207,29 +1181,15 @@ hipError_t product(Variant v, const Gemm &g, const HeadArgs &a, hipStream_t s) {
   }
 }
 
-// The classes that 256 x 256 tiles take, the others going to 128 x 128 tiles in a
-// launch of their own: whole rounds of the large ones, where what is left of a
-// round costs more in them (1000 x 520 x 50,021, 784 tiles: 81 us, 768 of them and
-// 80 smaller ones ROUNDUS).  A part is 64 classes (or rows, for dbias) in either.
-int64_t big_classes(int64_t rows, int64_t classes) {
-  const int64_t rt = ceil_div(rows, 256), tiles = rt * ceil_div(classes, 256);
-  const int64_t whole = tiles / kCus * kCus / rt * 256;  // classes of the whole rounds
-  if (whole == 0 || whole >= classes) return classes;
-  const int64_t mid = ceil_div(rows, 128) * ceil_div(classes - whole, 128);
-  // rounds as in variant(): 19 us for 512 of them, 27.5 for 256 large ones
-  const double tm = 19.0 * (double)(mid / (2 * kCus)) + (mid % (2 * kCus) <= kCus ? 12.0 : 19.0);
-  return tm + 3.0 < 27.5 * (double)(ceil_div(tiles, kCus) - tiles / kCus) ? whole : classes;
-}
-
 template <typename T>
 hipError_t forward(HeadArgs a, hipStream_t s) {
   Gemm g{};
   g.a = a.w; g.a_ld = a.w_ld; g.a_ext = (int)a.classes;
   g.b = a.x; g.b_ld = a.x_ld; g.b_ext = (int)a.rows;
   g.k_ext = a.dim; g.splits = 1;
-  const Variant v = variant(sizeof(T) == 2, a.rows, a.classes);
+  const Variant v = head_variant(sizeof(T) == 2, a.rows, a.classes);
   if (v == BIG && sizeof(T) == 2) {
-    const int64_t c = big_classes(a.rows, a.classes);
+    const int64_t c = head_big_classes(a.rows, a.classes);
     if (c < a.classes) {
       g.a_ext = (int)c;
       const hipError_t e = product<T, E_STATS>(BIG, g, a, s);
@@ -1250,8 +1210,8 @@ hipError_t dlogits(const HeadArgs &a, hipStream_t s) {
   g.a = a.x; g.a_ld = a.x_ld; g.a_ext = (int)a.rows;
   g.b = static_cast<const T *>(a.w) + a.v0 * a.w_ld; g.b_ld = a.w_ld; g.b_ext = (int)a.piece;
   g.k_ext = a.dim; g.splits = 1;
-  const Variant v = variant(sizeof(T) == 2, a.rows, a.classes);
-  const int64_t c = v == BIG && sizeof(T) == 2 ? big_classes(a.rows, a.piece) : a.piece;
+  const Variant v = head_variant(sizeof(T) == 2, a.rows, a.classes);
+  const int64_t c = v == BIG && sizeof(T) == 2 ? head_big_classes(a.rows, a.piece) : a.piece;
   g.b_ext = (int)c;
   hipError_t e = product<T, E_DLOGITS>(v, g, a, s);
   if (e == hipSuccess && c < a.piece) {
@@ -1280,7 +1240,7 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
   w.k_ext = (int)a.rows; w.splits = 1;
   typedef Tiles<T, E_DX> X;
   typedef Tiles<T, E_DW> W;
-  Variant v = variant(sizeof(T) == 2, a.rows, a.classes);
+  Variant v = head_variant(sizeof(T) == 2, a.rows, a.classes);
   if (v == TINY) v = a.rows <= 32 ? FEW : SMALL;
   switch (v) {
     case BIG: return launch_grads<typename X::Big, typename W::Big>(x, w, a, s);
@@ -1290,63 +1250,6 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
   }
 }
 }  // namespace
-
-int head_parts(bool bf16, int64_t rows, int64_t classes) {
-  switch (variant(bf16, rows, classes)) {
-    case BIG:  // a tile's parts past these are empty, and not written
-    case MID: return (int)ceil_div(classes, 128) * 2;
-    case SMALL: return (int)ceil_div(classes, 64) * 2;
-    case TINY: return (int)ceil_div(classes, 32);
-    default: return (int)ceil_div(classes, 128) * 4;
-  }
-}
-int head_db_parts(bool bf16, int64_t rows, int64_t classes) {
-  switch (variant(bf16, rows, classes)) {
-    case BIG:
-    case MID: return (int)ceil_div(rows, 128) * 2;
-    case SMALL: return (int)ceil_div(rows, 64) * 2;
-    default: return (int)ceil_div(rows, 32);
-  }
-}
-int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece) {
-  Variant v = variant(bf16, rows, classes);
-  if (v == TINY) v = rows <= 32 ? FEW : SMALL;
-  const int64_t br = v == BIG ? 256 : v == MID ? 128 : v == SMALL ? 64 : 32, ba = v == BIG ? 256 : v == SMALL ? 64 : 128;
-  const int64_t bc = v == BIG ? 256 : v == MID ? 128 : 64;
-  const int64_t nx = ceil_div(rows, br) * ceil_div(dim, ba), nw = ceil_div(piece, bc) * ceil_div(dim, v == FEW ? 64 : ba);
-  if (nx == 0) return 1;
-  const int64_t kt = bf16 ? 64 : 32;
-  const double kx = (double)ceil_div(piece, kt), kw = (double)ceil_div(rows, kt) + 4.0;
-  // The launch's time in k-tiles of one workgroup per CU: dx's rounds, then dW's on
-  // the CUs as they come free; and the partial sums' way through memory.
-  const int64_t cus = kCus;
-  double best = 0.0;
-  int64_t pick = 1;
-  for (int64_t s = 1; s <= 64 && s * 4 <= (int64_t)kx + 3; ++s) {
-    const double lx = kx / (double)s + 4.0;
-    const int64_t n = nx * s, full = n / cus, rest = n % cus;
-    const double t0 = (double)full * lx, t1 = t0 + lx;
-    // earliest time by which the CUs have run all of dW's workgroups: the early
-    // CUs' k-th round of them, with what the late ones have done by then
-    double end = rest ? t1 : t0;
-    if (nw > 0)
-      for (int64_t k = std::max<int64_t>(1, (int64_t)((double)nw / cus) - 1);; ++k) {
-        const double t = t0 + (double)k * kw;
-        const int64_t late = t > t1 ? (int64_t)((t - t1) / kw) : 0;
-        if ((cus - rest) * k + rest * late < nw) continue;
-        end = std::max(end, t);
-        break;
-      }
-    const double bytes = (double)s * (double)rows * (double)dim * 8.0;
-    const double ktile_bytes = v == BIG ? 8.0e6 : v == MID ? 3.0e6 : 1.0e6;  // memory traffic in a k-tile's time
-    const double cost = end + bytes / ktile_bytes;
-    if (s == 1 || cost < best) {
-      best = cost;
-      pick = s;
-    }
-  }
-  return (int)pick;
-}
 
 hipError_t launch_head_stage(bool bf16, const void *in, int64_t ld_in, void *out, int64_t ld_out, int64_t rows, int dim,
                              hipStream_t s) {

@@ -6,6 +6,103 @@
 #include "tail.h"
 
 namespace hapi {
+
+// ------------------------------------------------------------------ tile rules
+
+Variant head_variant(bool bf16, int64_t rows, int64_t classes) {
+  // TINYRULE
+  if (ceil_div(rows, 32) * ceil_div(classes, 32) <= 2 * kCus) return TINY;
+  if (rows <= 32) return FEW;
+  const int64_t big = ceil_div(rows, 256) * ceil_div(classes, 256), mid = ceil_div(rows, 128) * ceil_div(classes, 128),
+                small = ceil_div(rows, 64) * ceil_div(classes, 64);
+  double tb, tm, ts;
+  if (bf16) {
+    // 27.5, 19 and 10.3 us a round of 256, 512 and 768 workgroups at 768 features
+    // (4096 x 768 x 32000); the last round less when it holds one to a CU.
+    tb = 27.5 * (double)ceil_div(big, kCus);
+    tm = 19.0 * (double)(mid / (2 * kCus)) + (mid % (2 * kCus) == 0 ? 0.0 : mid % (2 * kCus) <= kCus ? 12.0 : 19.0);
+    const int64_t r = small % (3 * kCus);
+    ts = 10.3 * (double)(small / (3 * kCus)) + (r == 0 ? 0.0 : r <= kCus ? 5.0 : r <= 2 * kCus ? 7.5 : 10.3);
+  } else {
+    // the matrix pipes are the bound: a CU's workgroups take turns on them
+    tb = 16.0 * (double)ceil_div(big, kCus);
+    tm = 4.25 * (double)ceil_div(mid, kCus);
+    ts = 1.06 * (double)ceil_div(small, kCus);
+  }
+  return tb <= tm && tb <= ts ? BIG : tm <= ts ? MID : SMALL;
+}
+
+// The classes that 256 x 256 tiles take, the others going to 128 x 128 tiles in a
+// launch of their own: whole rounds of the large ones, where what is left of a
+// round costs more in them (1000 x 520 x 50,021, 784 tiles: 81 us, 768 of them and
+// 80 smaller ones ROUNDUS).  A part is 64 classes (or rows, for dbias) in either.
+int64_t head_big_classes(int64_t rows, int64_t classes) {
+  const int64_t rt = ceil_div(rows, 256), tiles = rt * ceil_div(classes, 256);
+  const int64_t whole = tiles / kCus * kCus / rt * 256;  // classes of the whole rounds
+  if (whole == 0 || whole >= classes) return classes;
+  const int64_t mid = ceil_div(rows, 128) * ceil_div(classes - whole, 128);
+  // rounds as in head_variant(): 19 us for 512 of them, 27.5 for 256 large ones
+  const double tm = 19.0 * (double)(mid / (2 * kCus)) + (mid % (2 * kCus) <= kCus ? 12.0 : 19.0);
+  return tm + 3.0 < 27.5 * (double)(ceil_div(tiles, kCus) - tiles / kCus) ? whole : classes;
+}
+
+int head_parts(bool bf16, int64_t rows, int64_t classes) {
+  switch (head_variant(bf16, rows, classes)) {
+    case BIG:  // a tile's parts past these are empty, and not written
+    case MID: return (int)ceil_div(classes, 128) * 2;
+    case SMALL: return (int)ceil_div(classes, 64) * 2;
+    case TINY: return (int)ceil_div(classes, 32);
+    default: return (int)ceil_div(classes, 128) * 4;
+  }
+}
+int head_db_parts(bool bf16, int64_t rows, int64_t classes) {
+  switch (head_variant(bf16, rows, classes)) {
+    case BIG:
+    case MID: return (int)ceil_div(rows, 128) * 2;
+    case SMALL: return (int)ceil_div(rows, 64) * 2;
+    default: return (int)ceil_div(rows, 32);
+  }
+}
+int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece) {
+  Variant v = head_variant(bf16, rows, classes);
+  if (v == TINY) v = rows <= 32 ? FEW : SMALL;
+  const int64_t br = v == BIG ? 256 : v == MID ? 128 : v == SMALL ? 64 : 32, ba = v == BIG ? 256 : v == SMALL ? 64 : 128;
+  const int64_t bc = v == BIG ? 256 : v == MID ? 128 : 64;
+  const int64_t nx = ceil_div(rows, br) * ceil_div(dim, ba), nw = ceil_div(piece, bc) * ceil_div(dim, v == FEW ? 64 : ba);
+  if (nx == 0) return 1;
+  const int64_t kt = bf16 ? 64 : 32;
+  const double kx = (double)ceil_div(piece, kt), kw = (double)ceil_div(rows, kt) + 4.0;
+  // The launch's time in k-tiles of one workgroup per CU: dx's rounds, then dW's on
+  // the CUs as they come free; and the partial sums' way through memory.
+  const int64_t cus = kCus;
+  double best = 0.0;
+  int64_t pick = 1;
+  for (int64_t s = 1; s <= 64 && s * 4 <= (int64_t)kx + 3; ++s) {
+    const double lx = kx / (double)s + 4.0;
+    const int64_t n = nx * s, full = n / cus, rest = n % cus;
+    const double t0 = (double)full * lx, t1 = t0 + lx;
+    // earliest time by which the CUs have run all of dW's workgroups: the early
+    // CUs' k-th round of them, with what the late ones have done by then
+    double end = rest ? t1 : t0;
+    if (nw > 0)
+      for (int64_t k = std::max<int64_t>(1, (int64_t)((double)nw / cus) - 1);; ++k) {
+        const double t = t0 + (double)k * kw;
+        const int64_t late = t > t1 ? (int64_t)((t - t1) / kw) : 0;
+        if ((cus - rest) * k + rest * late < nw) continue;
+        end = std::max(end, t);
+        break;
+      }
+    const double bytes = (double)s * (double)rows * (double)dim * 8.0;
+    const double ktile_bytes = v == BIG ? 8.0e6 : v == MID ? 3.0e6 : 1.0e6;  // memory traffic in a k-tile's time
+    const double cost = end + bytes / ktile_bytes;
+    if (s == 1 || cost < best) {
+      best = cost;
+      pick = s;
+    }
+  }
+  return (int)pick;
+}
+
 namespace {
 
 #define HIP_TRY(expr)                                                                  \

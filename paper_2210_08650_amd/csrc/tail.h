@@ -63,8 +63,16 @@ struct HeadArgs {
   float *dbias;
 };
 
-// The parts launch_head_forward writes for this many classes and rows, and the
-// row parts and splits of the backward pass: functions of the sizes only.
+// Tiles of the products, out of a rule on the sizes: 256 x 256, 128 x 128, 64 x 64,
+// 32 rows by 128 classes (the weights stream past), 32 x 32.
+enum Variant { BIG, MID, SMALL, FEW, TINY };
+constexpr int64_t kCus = 256;  // compute units the rules count on
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+Variant head_variant(bool bf16, int64_t rows, int64_t classes);
+// BIG: the classes that 256 x 256 tiles take; 128 x 128 ones take the others.
+int64_t head_big_classes(int64_t rows, int64_t classes);
+// The parts the forward product writes of a row, dz's of a class, and the splits of
+// dx's product.
 int head_parts(bool bf16, int64_t rows, int64_t classes);
 int head_db_parts(bool bf16, int64_t rows, int64_t classes);
 int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece);

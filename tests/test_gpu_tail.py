@@ -253,11 +253,9 @@ def _head_run(c, backward=True, stream=None):
 
 def _head_check(c, got):
     want = R.head(c["x"], c["w"], c["bias"], c["ids"], c["teacher"], c["temp"], c["dloss"] if "dx" in got else None)
-    # two independent roundings of half a step, uniform within it: 2^-8 sqrt(2 / 3) of
-    # the length; float32 from the logits' roundings
-    l2 = 2.0 ** -8 if c["x"].dtype == BF else 4e-5
     for name, t in got.items():
-        R.check(name, t, want[name], l2 if name in ("dx", "dw") else None)
+        # float32: a logit's rounding, 4e-5 at the largest spread here
+        R.check(name, t, want[name], 4e-5 if name in ("dx", "dw") and t.dtype == F32 else None)
     counts = c["ids"] >= 0 if c["teacher"] is None else (c["ids"] >= 0).any(1)
     assert bool((got["loss"][~counts] == 0).all())
     if "dx" in got:
