@@ -314,47 +314,61 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
       }
     }
   }
-  if constexpr (EPI == E_DX) {
-    float *o = h.dx_part + (int64_t)split * h.rows * h.dx_pad;
-    const RowsOut<float, 32 * TA> out{turn, lane};
+  if constexpr (EPI == E_DX || EPI == E_DW) {
+    // out[row][feature], whole or as one of the float32 partial sums of a split k
+    const bool whole = EPI == E_DX ? h.dx_whole : h.w_splits == 1;
+    if (!whole) {
+      float *o = EPI == E_DX ? h.dx_part + (int64_t)split * h.rows * h.dx_pad
+                             : h.dw_part + (int64_t)split * h.piece * h.dx_pad;
+      const bool add = EPI == E_DX && !h.first;
+      const RowsOut<float, 32 * TA> out{turn, lane};
 #pragma unroll
-    for (int j = 0; j < TB; ++j) {
+      for (int j = 0; j < TB; ++j) {
 #pragma unroll
-      for (int i = 0; i < TA; ++i)
+        for (int i = 0; i < TA; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          out.put(i, q, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-      out.rows([&](int row, int col, const uint4 &v) {
-        const int r = at.lane(j) + row, d = at.reg(0) + col;
-        if (r >= g.b_ext || d >= h.dx_pad) return;
-        float4 *p = reinterpret_cast<float4 *>(o + (int64_t)r * h.dx_pad + d);
-        float4 w = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
-        if (!h.first) {
-          const float4 u = *p;
-          w.x += u.x; w.y += u.y; w.z += u.z; w.w += u.w;
-        }
-        *p = w;
-      });
+          for (int q = 0; q < 4; ++q)
+            out.put(i, q, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        out.rows([&](int row, int col, const uint4 &v) {
+          const int r = at.lane(j) + row, d = at.reg(0) + col;
+          if (r >= g.b_ext || d >= h.dx_pad) return;
+          float4 *p = reinterpret_cast<float4 *>(o + (int64_t)r * h.dx_pad + d);
+          float4 w = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+          if (add) {
+            const float4 u = *p;
+            w.x += u.x; w.y += u.y; w.z += u.z; w.w += u.w;
+          }
+          *p = w;
+        });
+      }
+      return;
     }
-  }
-  if constexpr (EPI == E_DW) {
     constexpr int V = 16 / (int)sizeof(T);
-    T *o = static_cast<T *>(h.dw) + h.v0 * h.dw_ld;
-    const bool vec = h.dw_ld % V == 0 && (uintptr_t)h.dw % 16 == 0;
+    T *o = EPI == E_DX ? static_cast<T *>(h.dx) : static_cast<T *>(h.dw) + h.v0 * h.dw_ld;
+    const int64_t ld = EPI == E_DX ? h.dx_ld : h.dw_ld;
+    const bool vec = ld % V == 0 && (uintptr_t)o % 16 == 0;
     const float unit = h.rows > 0 ? *h.unit : 0.0f;
     const RowsOut<T, 32 * TA> out{turn, lane};
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
+      bool none = false;  // a row that does not count: zeros, whatever the weights hold
+      if constexpr (EPI == E_DX) {
+        const int r = at.lane(j) + (lane & 31);
+        none = r >= g.b_ext || h.info[r].y == 0.0f;
+      }
 #pragma unroll
       for (int i = 0; i < TA; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          out.put(i, q, acc[i][j][4 * q] * unit, acc[i][j][4 * q + 1] * unit, acc[i][j][4 * q + 2] * unit,
-                  acc[i][j][4 * q + 3] * unit);
+        for (int q = 0; q < 4; ++q) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = EPI == E_DX && none ? 0.0f : acc[i][j][4 * q + e] * unit;
+          out.put(i, q, v[0], v[1], v[2], v[3]);
+        }
       out.rows([&](int row, int col, const uint4 &v) {
         const int r = at.lane(j) + row, d = at.reg(0) + col;
         if (r >= g.b_ext) return;
-        T *p = o + (int64_t)r * h.dw_ld + d;
+        T *p = o + (int64_t)r * ld + d;
         if (vec && d + V <= h.dim) {
           *reinterpret_cast<uint4 *>(p) = v;
         } else {
@@ -385,7 +399,7 @@ struct RingTile {
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wa = wave / WB, wb = wave % WB;
-  constexpr bool SPLIT = EPI == E_DX;  // k over several workgroups
+  constexpr bool SPLIT = EPI == E_DX || EPI == E_DW;  // k over several workgroups
   const uint32_t tiles = g.tiles_a * g.tiles_b;
   const int split = SPLIT ? (int)((uint32_t)bid / tiles) : 0, tile = bid - split * (int)tiles;
   int ta, tb;
@@ -566,7 +580,7 @@ struct BigTile {
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  constexpr bool SPLIT = EPI == E_DX;  // k over several workgroups
+  constexpr bool SPLIT = EPI == E_DX || EPI == E_DW;  // k over several workgroups
   const uint32_t tiles = g.tiles_a * g.tiles_b;
   const int split = SPLIT ? (int)((uint32_t)bid / tiles) : 0, tile = bid - split * (int)tiles;
   int ta, tb;
@@ -824,9 +838,13 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
     m = mx;
   };
   if (row < h.rows)
-    for (int p = t >> 4; p < h.parts; p += 64) {
-      const float2 v = h.part[(int64_t)p * h.rows + row];
-      merge(v.x, v.y);
+    for (int p0 = t >> 4; p0 < h.parts; p0 += 64 * 8) {  // eight parts' loads at a time
+      float2 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        v[i] = p0 + 64 * i < h.parts ? h.part[(int64_t)(p0 + 64 * i) * h.rows + row] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) merge(v[i].x, v[i].y);
     }
 #pragma unroll
   for (int o = 16; o <= 32; o <<= 1) {
@@ -997,7 +1015,7 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
 // threads a class each take every other entry of the list.  (One block for all
 // entries of its classes: 63 us for 131,072 entries and 32,000 classes, of which
 // the sums are 15; in slices SLICEDUS.)
-constexpr int kBiasClasses = 128, kBiasRound = 2048;
+constexpr int kBiasRound = 2048;
 template <typename T>
 __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
   __shared__ int cnt[4];
@@ -1019,11 +1037,11 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
     return;
   }
   const int lane = t & 63, wave = t >> 6;
-  const int b = blockIdx.x - nt, slice = b % kBiasSlices;
-  const int c0 = b / kBiasSlices * kBiasClasses;
+  const int b = blockIdx.x - nt, slice = b % h.bias_slices;
+  const int c0 = b / h.bias_slices * kBiasClasses;
   const int mine = t % kBiasClasses, second = t / kBiasClasses;
   const int64_t total = h.rows * h.top;
-  const int64_t per = (total + kBiasSlices * 4 - 1) / (kBiasSlices * 4) * 4;  // whole 16 bytes
+  const int64_t per = (total + h.bias_slices * 4 - 1) / (h.bias_slices * 4) * 4;  // whole 16 bytes
   const int64_t lo = slice * per, hi = lo + per < total ? lo + per : total;
   double sum = 0.0;
   int4 nx[2];
@@ -1071,6 +1089,7 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
         ++at;
       }
     __syncthreads();
+#pragma unroll 4
     for (int k = second; k < all; k += 2)
       if (list_c[k] == mine) sum -= list_v[k];
     // the next round's counts are written before its first barrier and its list
@@ -1083,39 +1102,51 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
     h.db_part[(int64_t)(h.db_parts + slice) * h.classes + c0 + mine] = (float)(sum + half_s[mine]);
 }
 
-// In blocks [0, nx) of the launch: dx[n][d] = the splits' partial sums in order, 0 in
-// rows that do not count.  In the others dbias, 128 classes a block: the sums of its
-// parts (the rows', and for distillation the targets', which cancel much of them: in
-// 64 bits), four threads a class, in order, so that results do not vary.
+// out[r][d] = unit times the splits' partial sums in order, 0 in rows that do not
+// count (info, if given); block b of nb.
 constexpr int kReduceThreads = 512;
 template <typename T>
-__global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h, int nx) {
-  __shared__ double sums[4][kBiasClasses];
-  const int t = threadIdx.x;
-  const float unit = h.rows > 0 ? *h.unit : 0.0f;
-  if ((int)blockIdx.x < nx) {
-    const int per = (h.dim + 3) / 4;
-    const int64_t total = h.rows * per;
-    T *dx = static_cast<T *>(h.dx);
-    for (int64_t i = (int64_t)blockIdx.x * kReduceThreads + t; i < total; i += (int64_t)nx * kReduceThreads) {
-      const int64_t n = i / per;
-      const int d = (int)(i - n * per) * 4;
-      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (h.info[n].y != 0.0f)
-        for (int s = 0; s < h.splits; ++s) {
-          const float4 u = *reinterpret_cast<const float4 *>(h.dx_part + ((int64_t)s * h.rows + n) * h.dx_pad + d);
-          v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
-        }
-      T *o = dx + n * h.dx_ld + d;
+__device__ __forceinline__ void reduce_rows(const float *part, int splits, int64_t rows, int dim, int pad, T *out, int64_t ld,
+                                            float unit, const float2 *info, int b, int nb) {
+  const int per = (dim + 3) / 4;
+  const int64_t total = rows * per;
+  for (int64_t i = (int64_t)b * kReduceThreads + threadIdx.x; i < total; i += (int64_t)nb * kReduceThreads) {
+    const int64_t n = i / per;
+    const int d = (int)(i - n * per) * 4;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (!info || info[n].y != 0.0f)
+      for (int s = 0; s < splits; ++s) {
+        const float4 u = *reinterpret_cast<const float4 *>(part + ((int64_t)s * rows + n) * pad + d);
+        v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+      }
+    T *o = out + n * ld + d;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (d + j < h.dim) put(o + j, v[j] * unit);
-    }
+    for (int j = 0; j < 4; ++j)
+      if (d + j < dim) put(o + j, v[j] * unit);
+  }
+}
+
+// In blocks [0, nx) of the launch dx from its partial sums, in [nx, nx + nw) dW from
+// its (where there are any).  In the others dbias, 128 classes a block: the sums of
+// its parts (the rows', and for distillation the targets', which cancel much of them:
+// in 64 bits), four threads a class, in order, so that results do not vary.
+template <typename T>
+__global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h, int nx, int nw) {
+  __shared__ double sums[4][kBiasClasses];
+  const int t = threadIdx.x, b = blockIdx.x;
+  const float unit = h.rows > 0 ? *h.unit : 0.0f;
+  if (b < nx) {
+    reduce_rows(h.dx_part, h.splits, h.rows, h.dim, h.dx_pad, static_cast<T *>(h.dx), h.dx_ld, unit, h.info, b, nx);
     return;
   }
-  const int64_t c0 = (int64_t)(blockIdx.x - nx) * kBiasClasses;
+  if (b < nx + nw) {
+    reduce_rows(h.dw_part, h.w_splits, h.classes, h.dim, h.dx_pad, static_cast<T *>(h.dw), h.dw_ld, unit,
+                (const float2 *)nullptr, b - nx, nw);
+    return;
+  }
+  const int64_t c0 = (int64_t)(b - nx - nw) * kBiasClasses;
   const int slice = t / kBiasClasses, mine = t % kBiasClasses;
-  const int parts = h.db_parts + (h.teacher ? kBiasSlices : 0);
+  const int parts = h.db_parts + (h.teacher ? h.bias_slices : 0);
   double sum = 0.0;
   if (c0 + mine < h.classes)
     for (int p = slice; p < parts; p += 4) sum += h.db_part[(int64_t)p * h.classes + c0 + mine];
@@ -1224,7 +1255,7 @@ hipError_t dlogits(const HeadArgs &a, hipStream_t s) {
   }
   if (e != hipSuccess || !a.teacher) return e;
   const int64_t nt = ceil_div(a.rows * a.top, 256);
-  const int64_t nb = a.db_part && a.first ? ceil_div(a.classes, kBiasClasses) * kBiasSlices : 0;
+  const int64_t nb = a.db_part && a.first ? ceil_div(a.classes, kBiasClasses) * a.bias_slices : 0;
   if (nt + nb > 0x7fffffff) return hipErrorInvalidValue;
   hapi_launch(head_targets_kernel<T>, dim3((uint32_t)(nt + nb)), dim3(256), 0, s, a, (int)nt);
   return hipGetLastError();
@@ -1237,7 +1268,7 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
   x.k_ext = (int)a.piece; x.splits = a.splits;
   w.a = a.x; w.a_ld = a.x_ld; w.a_ext = a.dx_pad;
   w.b = a.gt; w.b_ld = a.rows_pad; w.b_ext = (int)a.piece;
-  w.k_ext = (int)a.rows; w.splits = 1;
+  w.k_ext = (int)a.rows; w.splits = a.w_splits;
   typedef Tiles<T, E_DX> X;
   typedef Tiles<T, E_DW> W;
   Variant v = head_variant(sizeof(T) == 2, a.rows, a.classes);
@@ -1246,7 +1277,15 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
     case BIG: return launch_grads<typename X::Big, typename W::Big>(x, w, a, s);
     case MID: return launch_grads<typename X::Mid, typename W::Mid>(x, w, a, s);
     case SMALL: return launch_grads<typename X::Small, typename W::Small>(x, w, a, s);
-    default: return launch_grads<typename X::Few, typename W::Small>(x, w, a, s);
+    default:
+      // Many tiles of dW: in a launch of their own, where more of them fit a CU
+      // (8 x 4096 x 131072: 1279 us in one launch, 82 KB of LDS each, FEWUS apart).
+      if (ceil_div(w.a_ext, 64) * ceil_div(w.b_ext, 64) <= 4 * kCus)
+        return launch_grads<typename X::Few, typename W::Small>(x, w, a, s);
+      {
+        const hipError_t e = launch_product<typename X::Few>(x, a, s);
+        return e != hipSuccess ? e : launch_product<typename W::Mid>(w, a, s);
+      }
   }
 }
 }  // namespace
@@ -1293,12 +1332,14 @@ hipError_t launch_head_grads(bool bf16, const HeadArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_head_reduce(bool bf16, const HeadArgs &a, hipStream_t s) {
-  const int64_t n = a.rows * ((a.dim + 3) / 4);
-  const int nx = a.rows > 0 ? (int)std::min<int64_t>(ceil_div(n, kReduceThreads), 2048) : 0;
+  auto blocks = [&](int64_t rows) { return (int)std::min<int64_t>(ceil_div(rows * ((a.dim + 3) / 4), kReduceThreads), 2048); };
+  const int nx = a.rows > 0 && !a.dx_whole ? blocks(a.rows) : 0;
+  const int nw = a.w_splits > 1 ? blocks(a.classes) : 0;
   const int nb = a.dbias ? (int)ceil_div(a.classes, kBiasClasses) : 0;
-  if (nx + nb == 0) return hipSuccess;
-  if (bf16) hapi_launch(head_reduce_kernel<uint16_t>, dim3(nx + nb), dim3(kReduceThreads), 0, s, a, nx);
-  else hapi_launch(head_reduce_kernel<float>, dim3(nx + nb), dim3(kReduceThreads), 0, s, a, nx);
+  if (nx + nw + nb == 0) return hipSuccess;
+  const dim3 grid((uint32_t)(nx + nw + nb));
+  if (bf16) hapi_launch(head_reduce_kernel<uint16_t>, grid, dim3(kReduceThreads), 0, s, a, nx, nw);
+  else hapi_launch(head_reduce_kernel<float>, grid, dim3(kReduceThreads), 0, s, a, nx, nw);
   return hipGetLastError();
 }
 

@@ -63,15 +63,45 @@ int head_db_parts(bool bf16, int64_t rows, int64_t classes) {
     default: return (int)ceil_div(rows, 32);
   }
 }
-int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece) {
-  Variant v = head_variant(bf16, rows, classes);
-  if (v == TINY) v = rows <= 32 ? FEW : SMALL;
-  const int64_t br = v == BIG ? 256 : v == MID ? 128 : v == SMALL ? 64 : 32, ba = v == BIG ? 256 : v == SMALL ? 64 : 128;
-  const int64_t bc = v == BIG ? 256 : v == MID ? 128 : 64;
-  const int64_t nx = ceil_div(rows, br) * ceil_div(dim, ba), nw = ceil_div(piece, bc) * ceil_div(dim, v == FEW ? 64 : ba);
+namespace {
+struct GradTiles {
+  Variant v;
+  int64_t nx, nw;  // tiles of dx and of dW
+};
+GradTiles grad_tiles(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece) {
+  GradTiles t;
+  t.v = head_variant(bf16, rows, classes);
+  if (t.v == TINY) t.v = rows <= 32 ? FEW : SMALL;
+  const int64_t br = t.v == BIG ? 256 : t.v == MID ? 128 : t.v == SMALL ? 64 : 32;
+  const int64_t ba = t.v == BIG ? 256 : t.v == SMALL ? 64 : 128, bc = t.v == BIG ? 256 : t.v == MID ? 128 : 64;
+  t.nx = ceil_div(rows, br) * ceil_div(dim, ba);
+  t.nw = ceil_div(piece, bc) * ceil_div(dim, t.v == FEW ? 64 : ba);
+  return t;
+}
+}  // namespace
+
+// dW's rows split over workgroups where its tiles leave CUs idle (few classes, many
+// rows), at least 8 k-tiles to each; its partial sums are of all classes, so with one
+// piece of them only.
+int head_w_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece) {
+  if (piece < classes) return 1;
+  const GradTiles t = grad_tiles(bf16, rows, dim, classes, piece);
+  const int64_t most = ceil_div(rows, bf16 ? 64 : 32) / 8, want = 2 * kCus / std::max<int64_t>(t.nw, 1);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(most, want), 16));
+}
+
+// Slices of the entries: 512 blocks or more, of 128 classes and one slice each.
+int head_bias_slices(int64_t classes) {
+  return (int)std::max<int64_t>(8, std::min<int64_t>(64, 512 / ceil_div(classes, kBiasClasses)));
+}
+
+int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece, int w_splits) {
+  const GradTiles tiles = grad_tiles(bf16, rows, dim, classes, piece);
+  const Variant v = tiles.v;
+  const int64_t nx = tiles.nx, nw = tiles.nw * w_splits;
   if (nx == 0) return 1;
   const int64_t kt = bf16 ? 64 : 32;
-  const double kx = (double)ceil_div(piece, kt), kw = (double)ceil_div(rows, kt) + 4.0;
+  const double kx = (double)ceil_div(piece, kt), kw = (double)ceil_div(rows, kt) / w_splits + 4.0;
   // The launch's time in k-tiles of one workgroup per CU: dx's rounds, then dW's on
   // the CUs as they come free; and the partial sums' way through memory.
   const int64_t cus = kCus;
@@ -92,7 +122,8 @@ int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece
         end = std::max(end, t);
         break;
       }
-    const double bytes = (double)s * (double)rows * (double)dim * 8.0;
+    // one split of one piece is stored whole
+    const double bytes = s == 1 && piece >= classes ? 0.0 : (double)s * (double)rows * (double)dim * 8.0;
     const double ktile_bytes = v == BIG ? 8.0e6 : v == MID ? 3.0e6 : 1.0e6;  // memory traffic in a k-tile's time
     const double cost = end + bytes / ktile_bytes;
     if (s == 1 || cost < best) {
@@ -192,7 +223,7 @@ struct Head {
   int64_t piece;     // classes of a piece
   int64_t bytes_fwd, bytes_bwd;
   // byte offsets into the workspace
-  int64_t o_part, o_xs, o_ws, o_info, o_unit, o_id, o_cq, o_gt, o_db, o_dx;
+  int64_t o_part, o_xs, o_ws, o_info, o_unit, o_id, o_cq, o_gt, o_db, o_dx, o_dw;
 };
 
 int read_head(const hapi_head_desc *d, Head &h) {
@@ -238,7 +269,10 @@ int read_head(const hapi_head_desc *d, Head &h) {
   const int64_t pieces = (d->classes + most - 1) / most;
   h.piece = std::min(up((d->classes + pieces - 1) / pieces, kHeadPiece), up(d->classes, kHeadPiece));
   a.db_parts = head_db_parts(h.bf16, d->rows, d->classes);
-  a.splits = head_splits(h.bf16, d->rows, d->dim, d->classes, h.piece);
+  a.w_splits = head_w_splits(h.bf16, d->rows, d->dim, d->classes, h.piece);
+  a.splits = head_splits(h.bf16, d->rows, d->dim, d->classes, h.piece, a.w_splits);
+  a.dx_whole = a.splits == 1 && h.piece >= d->classes;
+  a.bias_slices = head_bias_slices(d->classes);
 
   const int64_t xs = up(d->rows * a.dx_pad * h.esz, kAlign), ws = up(d->classes * a.dx_pad * h.esz, kAlign);
   int64_t o = 0;
@@ -258,8 +292,9 @@ int read_head(const hapi_head_desc *d, Head &h) {
   h.o_id = take(d->rows * a.top * 4);
   h.o_cq = take(d->rows * a.top * 4);
   h.o_gt = take(h.piece * a.rows_pad * h.esz);
-  h.o_db = take((int64_t)(a.db_parts + kBiasSlices) * d->classes * 4);
-  h.o_dx = take((int64_t)a.splits * d->rows * a.dx_pad * 4);
+  h.o_db = take((int64_t)(a.db_parts + (d->top > 0 ? a.bias_slices : 0)) * d->classes * 4);
+  h.o_dx = take(a.dx_whole ? 0 : (int64_t)a.splits * d->rows * a.dx_pad * 4);
+  h.o_dw = take(a.w_splits > 1 ? (int64_t)a.w_splits * d->classes * a.dx_pad * 4 : 0);
   h.bytes_bwd = o;
   return HAPI_OK;
 }
@@ -341,6 +376,7 @@ int head_backward(const hapi_head_desc *d, Head &h, const void *x, const void *w
   a.gt = base + h.o_gt;
   a.db_part = dbias ? reinterpret_cast<float *>(base + h.o_db) : nullptr;
   a.dx_part = reinterpret_cast<float *>(base + h.o_dx);
+  a.dw_part = reinterpret_cast<float *>(base + h.o_dw);
   a.dx = dx;
   a.dw = dw;
   a.dx_ld = a.x_in_ld;
@@ -352,7 +388,6 @@ int head_backward(const hapi_head_desc *d, Head &h, const void *x, const void *w
     a.v0 = v0;
     a.piece = std::min(h.piece, a.classes - v0);
     a.first = v0 == 0;
-    a.last = v0 + a.piece == a.classes;
     HIP_TRY(launch_head_dlogits(h.bf16, a, s));
     HIP_TRY(launch_head_grads(h.bf16, a, s));
   }

@@ -57,7 +57,11 @@ struct HeadArgs {
   int db_parts;
   float *dx_part;           // [splits][rows][dx_pad]
   int splits, dx_pad;
-  bool first, last;         // first / last piece
+  bool first;               // first piece
+  bool dx_whole;            // one split and one piece: no partial sums
+  float *dw_part;           // [w_splits][classes][dx_pad], one piece only
+  int w_splits;
+  int bias_slices;          // distillation: parts of dbias for what the targets take off
   void *dx, *dw;
   int64_t dx_ld, dw_ld;
   float *dbias;
@@ -75,8 +79,10 @@ int64_t head_big_classes(int64_t rows, int64_t classes);
 // dx's product.
 int head_parts(bool bf16, int64_t rows, int64_t classes);
 int head_db_parts(bool bf16, int64_t rows, int64_t classes);
-int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece);
-constexpr int kBiasSlices = 8;  // distillation: parts of dbias for what the targets take off
+int head_w_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece);
+int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece, int w_splits);
+constexpr int kBiasClasses = 128;  // classes of a block that sums dbias
+int head_bias_slices(int64_t classes);
 constexpr int kHeadRowPad = 64;
 constexpr int kHeadPiece = 256;  // pieces are multiples of this many classes
 

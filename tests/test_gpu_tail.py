@@ -262,7 +262,7 @@ def _head_check(c, got):
         assert bool((got["dx"][~counts] == 0).all())
 
 
-HEAD_SHAPES = [(1, 1, 1), (1, 8, 2), (2, 16, 1), (1, 64, 1000), (3, 7, 5), (8, 768, 1000), (31, 72, 127), (32, 64, 128),
+HEAD_SHAPES = [(8192, 64, 100), (4096, 40, 1000), (2000, 130, 300), (20, 520, 9000), (1, 1, 1), (1, 8, 2), (2, 16, 1), (1, 64, 1000), (3, 7, 5), (8, 768, 1000), (31, 72, 127), (32, 64, 128),
                (33, 96, 129), (64, 200, 255), (65, 64, 257), (128, 512, 1000), (129, 777, 300), (200, 520, 5003),
                (257, 128, 1024), (1000, 64, 333), (300, 1030, 2000), (515, 2048, 700)]
 
@@ -277,7 +277,7 @@ def test_cross_entropy(rows, dim, classes, dtype):
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("rows,dim,classes,top", [(1, 8, 3, 1), (1, 64, 1000, 7), (5, 7, 4, 9), (32, 512, 1000, 10),
                                                   (33, 100, 129, 3), (66, 96, 255, 64), (130, 777, 1003, 5),
-                                                  (257, 256, 5003, 32), (40, 64, 300, 200)])
+                                                  (257, 256, 5003, 32), (40, 64, 300, 200), (3000, 64, 130, 20)])
 def test_distillation(rows, dim, classes, top, dtype):
     c = _head_case(rows + dim + classes + top, rows, dim, classes, dtype, bias=rows % 2 == 1, top=top)
     _head_check(c, _head_run(c))
