@@ -1280,7 +1280,7 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
     default:
       // Many tiles of dW: in a launch of their own, where more of them fit a CU
       // (8 x 4096 x 131072: 1279 us in one launch, 82 KB of LDS each, FEWUS apart).
-      if (ceil_div(w.a_ext, 64) * ceil_div(w.b_ext, 64) <= 4 * kCus)
+      if (!head_few_apart(a.dim, a.piece))
         return launch_grads<typename X::Few, typename W::Small>(x, w, a, s);
       {
         const hipError_t e = launch_product<typename X::Few>(x, a, s);

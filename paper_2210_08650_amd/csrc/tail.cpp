@@ -80,6 +80,8 @@ GradTiles grad_tiles(bool bf16, int64_t rows, int dim, int64_t classes, int64_t 
 }
 }  // namespace
 
+bool head_few_apart(int dim, int64_t piece) { return ceil_div(dim, 64) * ceil_div(piece, 64) > 4 * kCus; }
+
 // dW's rows split over workgroups where its tiles leave CUs idle (few classes, many
 // rows), at least 8 k-tiles to each; its partial sums are of all classes, so with one
 // piece of them only.
@@ -98,21 +100,23 @@ int head_bias_slices(int64_t classes) {
 int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece, int w_splits) {
   const GradTiles tiles = grad_tiles(bf16, rows, dim, classes, piece);
   const Variant v = tiles.v;
-  const int64_t nx = tiles.nx, nw = tiles.nw * w_splits;
+  // few rows: dW has a launch of its own where it has many tiles
+  const int64_t nx = tiles.nx, nw = v == FEW && head_few_apart(dim, piece) ? 0 : tiles.nw * w_splits;
   if (nx == 0) return 1;
   const int64_t kt = bf16 ? 64 : 32;
   const double kx = (double)ceil_div(piece, kt), kw = (double)ceil_div(rows, kt) / w_splits + 4.0;
-  // The launch's time in k-tiles of one workgroup per CU: dx's rounds, then dW's on
-  // the CUs as they come free; and the partial sums' way through memory.
-  const int64_t cus = kCus;
+  // The launch's time in a workgroup's k-tiles: dx's rounds over as many workgroups as
+  // run at once, then dW's as places come free; and the partial sums' way through
+  // memory.
+  const int64_t cus = kCus * (v == MID ? 2 : v == SMALL ? 3 : 1);
   double best = 0.0;
   int64_t pick = 1;
   for (int64_t s = 1; s <= 64 && s * 4 <= (int64_t)kx + 3; ++s) {
     const double lx = kx / (double)s + 4.0;
     const int64_t n = nx * s, full = n / cus, rest = n % cus;
     const double t0 = (double)full * lx, t1 = t0 + lx;
-    // earliest time by which the CUs have run all of dW's workgroups: the early
-    // CUs' k-th round of them, with what the late ones have done by then
+    // earliest time by which the places have run all of dW's workgroups: the early
+    // ones' k-th round of them, with what the late ones have done by then
     double end = rest ? t1 : t0;
     if (nw > 0)
       for (int64_t k = std::max<int64_t>(1, (int64_t)((double)nw / cus) - 1);; ++k) {

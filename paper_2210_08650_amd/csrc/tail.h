@@ -79,6 +79,8 @@ int64_t head_big_classes(int64_t rows, int64_t classes);
 // dx's product.
 int head_parts(bool bf16, int64_t rows, int64_t classes);
 int head_db_parts(bool bf16, int64_t rows, int64_t classes);
+// FEW: whether dx and dW are launches of their own.
+bool head_few_apart(int dim, int64_t piece);
 int head_w_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece);
 int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece, int w_splits);
 constexpr int kBiasClasses = 128;  // classes of a block that sums dbias
