@@ -516,7 +516,7 @@ int hapi_xent_forward(const hapi_head_desc *desc, const void *x, const void *wei
 
 /* Gradients of sum(dloss * loss): with dz = dloss (softmax(z) - onehot(target)),
  *   dx = dz weight [rows, dim], dweight = dz^T x [classes, dim], in desc->dtype,
- *   dbias = sum over rows of dz, float32 [classes], or NULL.
+ *   dbias = sum over rows of dz, float32 [classes], or NULL (it must be without a bias).
  * loss and stats are the forward pass's.  Rows that do not count, and rows whose
  * dloss is 0, get dx = 0 and add nothing.  Between its two products dz is held
  * in desc->dtype.  rows = 0: dweight and dbias are zeros.  Errors as forward. */

@@ -10,18 +10,27 @@
 //   forward    a = class, b = row:  epilogue = (max, sum of exp) of a row over the
 //              tile's classes; a second kernel joins these and forms the loss.
 //   dz^T       a = row, b = class:  the same product again, epilogue
-//              g exp(z - m) / sum, stored transposed, one piece of the classes at a
-//              time: a lane owns a class, so the bias's gradient is a sum of its
-//              own registers.  The targets' entries are put in by a small kernel.
+//              g exp(z - m) / sum less the target's entry, stored transposed, one
+//              piece of the classes at a time: a lane owns a class, so the bias's
+//              gradient is a sum of its own registers, joined over the rows in 64
+//              bits.  A teacher's entries are put in by a small kernel of their own.
 //   dx         a = feature, b = row, k = class: dz^T and the weights as they lie,
 //              the piece's classes split over workgroups, float32 partial sums.
-//   dW         a = feature, b = class, k = row: dz^T and x as they lie.
+//   dW         a = feature, b = class, k = row: dz^T and x as they lie; one launch
+//              with dx.
 //
 // float32 uses v_mfma_f32_32x32x2_f32 in the same tiles (128 bytes of k).
 // dz is rounded to the operands' type before its two products (the matrix
 // cores' bf16 operands; 2^-8 of each entry at most, against 2^-8 of the
 // outputs' own rounding); sums, softmax statistics and the bias's gradient are
-// float32 throughout.
+// float32 or wider throughout.
+//
+// Four products of 2 N D V operations in a step, one more than with the logits kept,
+// which would be 2 or 4 bytes a logit, written once and read twice.  Bound by the
+// matrix pipes: at 8192 x 2048 x 131072 they are busy 78% of the forward product's
+// time, 66% of dz's and 74% of the gradients' (their clock, under this load 1.6 to
+// 1.9 GHz, included in neither); the k-loop of a 256 x 256 tile takes 2.08k cycles a
+// k-tile, its MFMAs 2048.
 #include <algorithm>
 
 #include "gemm_util.h"
@@ -47,7 +56,7 @@ struct Gemm {
 // Tile `tile` of the grid: panels of 8 tiles of its smaller side, each along the whole
 // larger one, so that the 32 workgroups an XCD runs at once are 8 x 4 tiles and
 // share their operands' k-tiles in its L2 (8192 x 2048 x 131072 forward, one panel
-// of all 32: half the requests miss).  PANELUS
+// of all 32: half the L2's requests miss, in panels 19%; the step 14.15 -> 13.79 ms).
 __device__ __forceinline__ void place_tile(const Gemm &g, int tile, int &ta, int &tb) {
   const bool a_small = g.tiles_a <= g.tiles_b;
   const int few = a_small ? g.tiles_a : g.tiles_b, many = a_small ? g.tiles_b : g.tiles_a;
@@ -205,7 +214,7 @@ struct Place {
 // 8 q + 4 lh .. + 3 of block b of the lane's row; rows(f) calls f(row, column, 16
 // bytes) with consecutive lanes on consecutive columns.  Stores of the lanes' own
 // values would write 32 bytes of 32 rows each, and the L2 takes a request for every
-// such piece (dz of 8192 x 2048 x 16384: 525 us, turned TURNEDUS).
+// such piece (dz of 8192 x 2048 x 16384: 525 us, turned 479).
 template <typename O, int L>
 struct RowsOut {
   static constexpr int PITCH = L * (int)sizeof(O) + 16, V = 16 / (int)sizeof(O), PER = L / V, RPS = 64 / PER;
@@ -383,6 +392,10 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
   }
 }
 
+// A tile of BA x BB on WA x WB waves.  Two or three stages leave room for more
+// workgroups on a CU, whose waves cover each other's waits: 128 x 128 in two stages,
+// two workgroups, 302 us for the forward product of 4096 x 768 x 32000; in three
+// stages, one workgroup, 371; all of a k-tile's fragments read ahead 486.
 template <typename T, int BA, int BB, int WA, int WB, int ST, bool KRA, bool KRB, int EPI>
 struct RingTile {
   static constexpr int THREADS = 64 * WA * WB, TILE_A = BA, TILE_B = BB;
@@ -562,11 +575,15 @@ struct TinyTile {
 
 // The same product on 256 x 256 tiles.  Eight waves, two per SIMD: wave (g, c)
 // owns rows 64 g .. + 63 of both 128-row halves of B and rows 64 c .. + 63 of A, 32 in
-// each of its halves (which take every other 32 rows), 128 accumulator registers.  A k-tile is two steps, each a memory
-// slot (fragments of the next 16 MFMAs out of LDS, DMAs of a later k-tile into
-// it) and a matrix slot, with a barrier after every slot; the two groups g run one
-// slot apart, so one group's MFMAs cover the other's LDS reads.  Two stages of
-// 64 KB; half a stage is loaded again as soon as both groups have read it.
+// each of its halves (which take every other 32 rows), 128 accumulator registers.  A
+// k-tile is two steps, each a memory slot (fragments of the next 16 MFMAs out of LDS,
+// DMAs of a later k-tile into it) and a matrix slot, with a barrier after every slot;
+// the two groups g run one slot apart, so one group's MFMAs cover the other's LDS
+// reads.  Two stages of 64 KB; half a stage is loaded again as soon as both groups
+// have read it.
+// Not faster: workgroups that stay and take the next tile with its loads in flight
+// during the epilogue (4096 x 768 x 32000: forward 212 us against 216, gradients 395
+// against 372); 128 x 256 tiles, two workgroups to a CU (forward 320 us and more).
 template <typename T, bool KRA, bool KRB, int EPI>
 struct BigTile {
   static constexpr int THREADS = 512, TILE_A = 256, TILE_B = 256;
@@ -942,11 +959,12 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
   if (n < h.rows) {
     const int64_t *ids = h.ids + n * h.top;
     // The significand of a coefficient (of the first row that counts, among 64), which
-    // every coefficient is divided by and the gradients are multiplied by in float32: where all rows have the same
-    // dloss (a mean's), a target's entry of dz is then a power of two times p - 1, and
+    // every coefficient is divided by and the gradients are multiplied by in float32:
+    // where all rows have the same dloss (a mean's), a target's entry of dz is then a power of two times p - 1, and
     // not off by the rounding of dloss to 16 bits in every row alike (up to 2^-8 of
-    // the whole gradient: 0.004 at 8192 x 2048 x 131072, PRECUS without).  Its
-    // value is of no importance else: coefficients stay within a factor of two.
+    // the whole gradient: at 8192 x 2048 x 131072 it was off by 0.0040 of its length,
+    // and is by 0.0017, its own rounding).  Its value is of no importance else:
+    // coefficients stay within a factor of two.
     const float c0 = fabsf(lane < h.rows ? h.dloss[lane] * h.t : 0.0f);
     const uint64_t some = __ballot(c0 > 0.0f && c0 < INFINITY && h.ids[lane < h.rows ? lane * (int64_t)h.top : 0] >= 0);
     const uint32_t bits = __shfl(__float_as_uint(c0), some ? __ffsll((unsigned long long)some) - 1 : 0, 64);
@@ -1013,8 +1031,8 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
 // parts behind the row parts of db_part.  A block goes through its slice, 2048 a
 // round, keeps the entries of its classes in a list in a fixed order, and two
 // threads a class each take every other entry of the list.  (One block for all
-// entries of its classes: 63 us for 131,072 entries and 32,000 classes, of which
-// the sums are 15; in slices SLICEDUS.)
+// entries of its classes: 63 us for 131,072 entries and 32,000 classes with dx's
+// reduction, targets' entries 12; in eight slices 18 and 36.)
 constexpr int kBiasRound = 2048;
 template <typename T>
 __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
@@ -1163,13 +1181,18 @@ int grid_for(int64_t n, int per) {
 
 // ---------------------------------------------------------------- variants
 
+// Stages of the 64 x 64 tiles: three, and three workgroups to a CU; float32, bound by
+// its MFMAs, is better with four workgroups of two stages (512 x 1024 x 10,007 step
+// 367 us against 380; bf16 1000 x 1024 x 5000 112 us against 93 the other way round).
+template <typename T>
+constexpr int kSmallStages = sizeof(T) == 2 ? 3 : 2;
 template <typename T, int EPI>
 struct Tiles;
 template <typename T>
 struct Tiles<T, E_STATS> {
   typedef BigTile<T, false, false, E_STATS> Big;
   typedef RingTile<T, 128, 128, 2, 2, 2, false, false, E_STATS> Mid;
-  typedef RingTile<T, 64, 64, 2, 2, 3, false, false, E_STATS> Small;
+  typedef RingTile<T, 64, 64, 2, 2, kSmallStages<T>, false, false, E_STATS> Small;
   typedef RingTile<T, 128, 32, 4, 1, 7, false, false, E_STATS> Few;
   typedef RingTile<T, 64, 64, 2, 2, 8, false, false, E_STATS> Deep;
   typedef TinyTile<T, 8, E_STATS> Tiny;
@@ -1178,7 +1201,7 @@ template <typename T>
 struct Tiles<T, E_DLOGITS> {
   typedef BigTile<T, false, false, E_DLOGITS> Big;
   typedef RingTile<T, 128, 128, 2, 2, 2, false, false, E_DLOGITS> Mid;
-  typedef RingTile<T, 64, 64, 2, 2, 3, false, false, E_DLOGITS> Small;
+  typedef RingTile<T, 64, 64, 2, 2, kSmallStages<T>, false, false, E_DLOGITS> Small;
   typedef RingTile<T, 32, 128, 1, 4, 7, false, false, E_DLOGITS> Few;
   typedef RingTile<T, 64, 64, 2, 2, 8, false, false, E_DLOGITS> Deep;
   typedef TinyTile<T, 8, E_DLOGITS> Tiny;
@@ -1187,14 +1210,14 @@ template <typename T>
 struct Tiles<T, E_DX> {
   typedef BigTile<T, true, true, E_DX> Big;
   typedef RingTile<T, 128, 128, 2, 2, 2, true, true, E_DX> Mid;
-  typedef RingTile<T, 64, 64, 2, 2, 3, true, true, E_DX> Small;
+  typedef RingTile<T, 64, 64, 2, 2, kSmallStages<T>, true, true, E_DX> Small;
   typedef RingTile<T, 128, 32, 4, 1, 4, true, true, E_DX> Few;
 };
 template <typename T>
 struct Tiles<T, E_DW> {
   typedef BigTile<T, true, false, E_DW> Big;
   typedef RingTile<T, 128, 128, 2, 2, 2, true, false, E_DW> Mid;
-  typedef RingTile<T, 64, 64, 2, 2, 3, true, false, E_DW> Small;
+  typedef RingTile<T, 64, 64, 2, 2, kSmallStages<T>, true, false, E_DW> Small;
 };
 
 template <typename T, int EPI>
@@ -1279,7 +1302,7 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
     case SMALL: return launch_grads<typename X::Small, typename W::Small>(x, w, a, s);
     default:
       // Many tiles of dW: in a launch of their own, where more of them fit a CU
-      // (8 x 4096 x 131072: 1279 us in one launch, 82 KB of LDS each, FEWUS apart).
+      // (8 x 4096 x 131072: 1279 us in one launch, 82 KB of LDS each; apart dW takes 324).
       if (!head_few_apart(a.dim, a.piece))
         return launch_grads<typename X::Few, typename W::Small>(x, w, a, s);
       {
