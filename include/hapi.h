@@ -519,7 +519,7 @@ int hapi_xent_forward(const hapi_head_desc *desc, const void *x, const void *wei
  *   dbias = sum over rows of dz, float32 [classes], or NULL (it must be without a bias).
  * loss and stats are the forward pass's.  Rows that do not count, and rows whose
  * dloss is 0, get dx = 0 and add nothing.  Between its two products dz is held
- * in desc->dtype.  rows = 0: dweight and dbias are zeros.  Errors as forward. */
+ * in desc->dtype (up to 32 rows, with what that rounding leaves).  rows = 0: dweight and dbias are zeros.  Errors as forward. */
 int hapi_xent_backward(const hapi_head_desc *desc, const void *x, const void *weight, const float *bias,
                        const int64_t *targets, const float *loss, const float *stats, const float *dloss, void *dx,
                        void *dweight, float *dbias);

@@ -23,7 +23,12 @@
 // dz is rounded to the operands' type before its two products (the matrix
 // cores' bf16 operands; 2^-8 of each entry at most, against 2^-8 of the
 // outputs' own rounding); sums, softmax statistics and the bias's gradient are
-// float32 or wider throughout.
+// float32 or wider throughout.  Up to 32 rows (FEW), where one row's rounding can be
+// all of a gradient's, bf16 dz is a sum of two, the second one what the first leaves:
+// columns 32 .. 63 of dz^T, further 32 rows to dx's product and further 32 k to dW's,
+// whose k-tile holds 64 (a step of 32 x 2048 x 1000 33.5 -> 35.6 us, of 16 x 1024 x
+// 32000 81.5 -> 82.5, of 8 x 4096 x 131072 no longer; one row's dW off by 2.6e-4 of its
+// length, not 3.8e-4).
 //
 // Four products of 2 N D V operations in a step, one more than with the logits kept,
 // which would be 2 or 4 bytes a logit, written once and read twice.  Bound by the
@@ -32,6 +37,7 @@
 // 1.9 GHz, included in neither); the k-loop of a 256 x 256 tile takes 2.08k cycles a
 // k-tile, its MFMAs 2048.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_util.h"
 #include "tail.h"
@@ -65,6 +71,12 @@ __device__ __forceinline__ void place_tile(const Gemm &g, int tile, int &ta, int
   const int i = tile - p * 8 * many, m = (int)((uint32_t)i / (uint32_t)w), f = 8 * p + i - m * w;
   ta = a_small ? f : m;
   tb = a_small ? m : f;
+}
+
+// What rounding v to bf16 leaves of it (0 where it rounds to inf or NaN).
+__device__ __forceinline__ float bf16_rest(float v) {
+  const float r = bf2f(f2bf(v));
+  return fabsf(r) < INFINITY ? v - r : 0.0f;
 }
 
 enum Epi { E_STATS, E_DLOGITS, E_DX, E_DW };
@@ -236,7 +248,8 @@ struct RowsOut {
   }
 };
 
-template <typename T, int EPI, int TA, int TB, typename P, typename S>
+// REGS: values of the tile's reg side.
+template <typename T, int EPI, int REGS, int TA, int TB, typename P, typename S>
 __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x16_t (&acc)[TA][TB], const P &at,
                                          const S &side, uint8_t *turn, int split, int lane) {
   const int lh = lane >> 5;
@@ -280,6 +293,7 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
     T *gt = static_cast<T *>(h.gt);
     const float c = kLog2e * h.inv_t;
     const RowsOut<T, 32 * TA> out{turn, lane};
+    constexpr bool kPair = sizeof(T) == 2 && REGS == 32;  // tiles that few rows may take
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
       const int cls = at.lane(j) + (lane & 31);  // in the piece
@@ -311,12 +325,25 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
           }
           if (h.db_part) sum += (v[0] + v[1]) + (v[2] + v[3]);
           out.put(i, q, v[0], v[1], v[2], v[3]);
+          if constexpr (kPair)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = bf16_rest(v[e]);
         }
       }
-      out.rows([&](int row, int col, const uint4 &v) {
-        const int r = at.lane(j) + row, n = at.reg(0) + col;
-        if (r < g.b_ext && n < h.rows_pad) *reinterpret_cast<uint4 *>(gt + (int64_t)r * h.rows_pad + n) = v;
-      });
+      auto store = [&](int to) {
+        out.rows([&](int row, int col, const uint4 &v) {
+          const int r = at.lane(j) + row, n = at.reg(0) + col + to;
+          if (r < g.b_ext && n < h.rows_pad) *reinterpret_cast<uint4 *>(gt + (int64_t)r * h.rows_pad + n) = v;
+        });
+      };
+      store(0);
+      if constexpr (kPair)
+        if (h.rows <= kFewRows) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            out.put(0, q, acc[0][j][4 * q], acc[0][j][4 * q + 1], acc[0][j][4 * q + 2], acc[0][j][4 * q + 3]);
+          store(kFewRows);
+        }
       if (h.db_part) {
         sum += __shfl_xor(sum, 32, 64);
         if (lh == 0 && cls < g.b_ext && at.part < h.db_parts) h.db_part[(int64_t)at.part * h.classes + h.v0 + cls] = sum;
@@ -396,7 +423,9 @@ __device__ __forceinline__ void epilogue(const Gemm &g, const HeadArgs &h, f32x1
 // workgroups on a CU, whose waves cover each other's waits: 128 x 128 in two stages,
 // two workgroups, 302 us for the forward product of 4096 x 768 x 32000; in three
 // stages, one workgroup, 371; all of a k-tile's fragments read ahead 486.
-template <typename T, int BA, int BB, int WA, int WB, int ST, bool KRA, bool KRB, int EPI>
+// FOLD: B's second 32 rows are what the first ones leave of their values; the sums of
+// the two are one.
+template <typename T, int BA, int BB, int WA, int WB, int ST, bool KRA, bool KRB, int EPI, bool FOLD = false>
 struct RingTile {
   static constexpr int THREADS = 64 * WA * WB, TILE_A = BA, TILE_B = BB;
   static constexpr int SMEM = ST * (BA + BB) * 128;
@@ -499,7 +528,20 @@ struct RingTile {
   __syncthreads();
 
   const Place<32, 64> at = {a0, a0 + wa * TA * 32, b0 + wb * TB * 32, ta * WA + wa};
-  epilogue<T, EPI>(g, h, acc, at, side, smem + wave * (SMEM / WAVES), split, lane);
+  uint8_t *turn = smem + wave * (SMEM / WAVES);
+  if constexpr (FOLD) {
+    static_assert(BB == 64 && WB == 1, "a wave has both halves");
+    f32x16_t sum[TA][1];
+#pragma unroll
+    for (int i = 0; i < TA; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[i][0][r] = acc[i][0][r] + acc[i][1][r];
+    Gemm one = g;
+    one.b_ext = (int)h.rows;
+    epilogue<T, EPI, BA>(one, h, sum, at, side, turn, split, lane);
+  } else {
+    epilogue<T, EPI, BA>(g, h, acc, at, side, turn, split, lane);
+  }
   }
 };
 
@@ -569,7 +611,7 @@ struct TinyTile {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[0][0][r] += part[(w * 16 + r) * 64 + lane];
     const Place<32, 64> at = {a0, a0, b0, ta};
-    epilogue<T, EPI>(g, h, acc, at, side, smem + 3 * 4096, 0, lane);
+    epilogue<T, EPI, 32>(g, h, acc, at, side, smem + 3 * 4096, 0, lane);
   }
 };
 
@@ -712,7 +754,7 @@ struct BigTile {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if constexpr (EPI != E_STATS) __syncthreads();
   const Place<32, 128> at = {a0, a0 + wn * 64, b0 + wm * 64, ta * 4 + wn};
-  epilogue<T, EPI>(g, h, acc, at, side, smem + wave * (SMEM / 8), split, lane);
+  epilogue<T, EPI, 256>(g, h, acc, at, side, smem + wave * (SMEM / 8), split, lane);
   }
 };
 
@@ -949,6 +991,7 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
 // times it, or (inf, 0) for a row that does not count; the targets as 32-bit
 // classes (-1: none) with the weight to take off there; and a copy of x whose rows
 // that do not count are zero, so that nothing they hold reaches a sum.
+// Few rows of 16 bits: x and zeros up to row 32, then the same again.
 template <typename T>
 __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__restrict__ xs, int64_t xs_ld) {
   constexpr int V = 16 / (int)sizeof(T);
@@ -956,6 +999,12 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
   const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (n >= h.rows_pad) return;
   float2 info = make_float2(INFINITY, 0.0f);
+  const bool pair = sizeof(T) == 2 && h.rows <= kFewRows;
+  if (pair && n >= h.rows && n < kFewRows)
+    for (int d = lane * V; d < xs_ld; d += 64 * V) {
+      *reinterpret_cast<uint4 *>(xs + n * xs_ld + d) = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4 *>(xs + (n + kFewRows) * xs_ld + d) = make_uint4(0, 0, 0, 0);
+    }
   if (n < h.rows) {
     const int64_t *ids = h.ids + n * h.top;
     // The significand of a coefficient (of the first row that counts, among 64), which
@@ -1019,6 +1068,7 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
       uint4 q;
       __builtin_memcpy(&q, v, 16);
       *reinterpret_cast<uint4 *>(xs + n * xs_ld + d) = q;
+      if (pair) *reinterpret_cast<uint4 *>(xs + (n + kFewRows) * xs_ld + d) = q;
     }
   }
   if (lane == 0) h.info[n] = info;
@@ -1051,7 +1101,9 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
     float v = __builtin_amdgcn_exp2f((h.picked[i] - info.x) * h.inv_t * kLog2e) * info.y;
     for (int k = 0; k < h.top; ++k)
       if (h.id32[n * h.top + k] == id) v -= h.cq[n * h.top + k];
-    put(static_cast<T *>(h.gt) + (id - h.v0) * h.rows_pad + n, v);
+    T *p = static_cast<T *>(h.gt) + (id - h.v0) * h.rows_pad + n;
+    put(p, v);
+    if (sizeof(T) == 2 && h.rows <= kFewRows) put(p + kFewRows, bf16_rest(v));
     return;
   }
   const int lane = t & 63, wave = t >> 6;
@@ -1211,7 +1263,8 @@ struct Tiles<T, E_DX> {
   typedef BigTile<T, true, true, E_DX> Big;
   typedef RingTile<T, 128, 128, 2, 2, 2, true, true, E_DX> Mid;
   typedef RingTile<T, 64, 64, 2, 2, kSmallStages<T>, true, true, E_DX> Small;
-  typedef RingTile<T, 128, 32, 4, 1, 4, true, true, E_DX> Few;
+  typedef std::conditional_t<sizeof(T) == 2, RingTile<T, 128, 64, 4, 1, 3, true, true, E_DX, true>,
+                             RingTile<T, 128, 32, 4, 1, 4, true, true, E_DX>> Few;
 };
 template <typename T>
 struct Tiles<T, E_DW> {
@@ -1292,10 +1345,14 @@ hipError_t grads(const HeadArgs &a, hipStream_t s) {
   w.a = a.x; w.a_ld = a.x_ld; w.a_ext = a.dx_pad;
   w.b = a.gt; w.b_ld = a.rows_pad; w.b_ext = (int)a.piece;
   w.k_ext = (int)a.rows; w.splits = a.w_splits;
+  if (sizeof(T) == 2 && a.rows > 0 && a.rows <= kFewRows) {  // dz's second halves
+    x.b_ext = 2 * kFewRows;
+    w.k_ext = 2 * kFewRows;
+  }
   typedef Tiles<T, E_DX> X;
   typedef Tiles<T, E_DW> W;
   Variant v = head_variant(sizeof(T) == 2, a.rows, a.classes);
-  if (v == TINY) v = a.rows <= 32 ? FEW : SMALL;
+  if (v == TINY) v = a.rows <= kFewRows ? FEW : SMALL;
   switch (v) {
     case BIG: return launch_grads<typename X::Big, typename W::Big>(x, w, a, s);
     case MID: return launch_grads<typename X::Mid, typename W::Mid>(x, w, a, s);

@@ -14,7 +14,7 @@ Variant head_variant(bool bf16, int64_t rows, int64_t classes) {
   // (forward product of 128 x 2048 x 1000 7.9 us, in 64 x 64 tiles 13.6; of
   // 8 x 768 x 1000 5.4 us, in 32 x 128 tiles 8.4).
   if (ceil_div(rows, 32) * ceil_div(classes, 32) <= 2 * kCus) return TINY;
-  if (rows <= 32) return FEW;
+  if (rows <= kFewRows) return FEW;
   const int64_t big = ceil_div(rows, 256) * ceil_div(classes, 256), mid = ceil_div(rows, 128) * ceil_div(classes, 128),
                 small = ceil_div(rows, 64) * ceil_div(classes, 64);
   double tb, tm, ts;
@@ -73,7 +73,7 @@ struct GradTiles {
 GradTiles grad_tiles(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece) {
   GradTiles t;
   t.v = head_variant(bf16, rows, classes);
-  if (t.v == TINY) t.v = rows <= 32 ? FEW : SMALL;
+  if (t.v == TINY) t.v = rows <= kFewRows ? FEW : SMALL;
   const int64_t br = t.v == BIG ? 256 : t.v == MID ? 128 : t.v == SMALL ? 64 : 32;
   const int64_t ba = t.v == BIG ? 256 : t.v == SMALL ? 64 : 128, bc = t.v == BIG ? 256 : t.v == MID ? 128 : 64;
   t.nx = ceil_div(rows, br) * ceil_div(dim, ba);
@@ -292,7 +292,8 @@ int read_head(const hapi_head_desc *d, Head &h) {
   h.o_part = take((int64_t)a.parts * d->rows * 8);
   h.bytes_fwd = o;
   o = h.o_xs;
-  take(xs);
+  // up to kFewRows rows of 16 bits: x twice
+  take(h.bf16 && d->rows > 0 && d->rows <= kFewRows ? up((int64_t)2 * kFewRows * a.dx_pad * h.esz, kAlign) : xs);
   h.o_info = take(a.rows_pad * 8);
   h.o_unit = take(4);
   h.o_id = take(d->rows * a.top * 4);

@@ -86,6 +86,10 @@ int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece
 constexpr int kBiasClasses = 128;  // classes of a block that sums dbias
 int head_bias_slices(int64_t classes);
 constexpr int kHeadRowPad = 64;
+// FEW, and what calls of so few rows do more: bf16 dz has a second half that the first
+// one's rounding left, in columns [kFewRows, 2 kFewRows) of dz^T.
+constexpr int kFewRows = 32;
+static_assert(2 * kFewRows <= kHeadRowPad, "both halves in the padded rows");
 constexpr int kHeadPiece = 256;  // pieces are multiples of this many classes
 
 // rows of T values from ld_in to a padded, aligned [rows][ld_out], zero from dim on.

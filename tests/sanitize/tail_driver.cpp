@@ -100,6 +100,10 @@ hipError_t launch_head_finish(bool, const HeadArgs &a, hipStream_t) {
 hipError_t launch_head_prepare(bool bf16, const HeadArgs &a, void *xs, int64_t xs_ld, hipStream_t) {
   EXPECT(xs == a.x && xs_ld == a.x_ld && a.rows_pad >= a.rows && a.rows_pad % kHeadRowPad == 0);
   check_operands(bf16, a);
+  if (bf16 && a.rows > 0 && a.rows <= kFewRows) {  // x twice
+    g_regions.pop_back();
+    region("x", a.x, 2 * kFewRows * a.x_ld * 2);
+  }
   region("info", a.info, a.rows_pad * 8);
   region("unit", a.unit, 4);
   region("id32", a.id32, a.rows * a.top * 4);
