@@ -878,17 +878,18 @@ __device__ __forceinline__ void wave_dots(const T *x, const T *w, int64_t ld, co
     for (int k = 0; k < K; ++k) s[k] += __shfl_xor(s[k], o, 64);
 }
 
-// Joins a row's partial statistics and forms its loss: 16 rows a block, 64
-// threads on a row's parts, then a wave per row for the logits at its targets.
+// Joins a row's partial statistics and forms its loss: R rows a block, 1024 / R
+// threads on a row's parts, then 16 / R waves on the logits at its targets.
 // Merging two (max, sum) pairs rescales the smaller one's sum.
-constexpr int kFinishRows = 16;
-template <typename T>
+template <typename T, int R>
 __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
-  __shared__ float2 ms[16][kFinishRows];
+  constexpr int SLICES = 1024 / R, W = 16 / R;
+  __shared__ float2 ms[16][R];
+  __shared__ float sums[16];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int64_t r0 = (int64_t)blockIdx.x * kFinishRows;
+  const int64_t r0 = (int64_t)blockIdx.x * R;
   const float c = kLog2e * h.inv_t;
-  const int64_t row = r0 + (t & 15);
+  const int64_t row = r0 + t % R;
   float m = -INFINITY, s = 0.0f;
   auto merge = [&](float m2, float s2) {
     const float mx = fmaxf(m, m2);
@@ -897,37 +898,39 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
     m = mx;
   };
   if (row < h.rows)
-    for (int p0 = t >> 4; p0 < h.parts; p0 += 64 * 8) {  // eight parts' loads at a time
+    for (int p0 = t / R; p0 < h.parts; p0 += SLICES * 8) {  // eight parts' loads at a time
       float2 v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        v[i] = p0 + 64 * i < h.parts ? h.part[(int64_t)(p0 + 64 * i) * h.rows + row] : make_float2(-INFINITY, 0.0f);
+        v[i] = p0 + SLICES * i < h.parts ? h.part[(int64_t)(p0 + SLICES * i) * h.rows + row] : make_float2(-INFINITY, 0.0f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) merge(v[i].x, v[i].y);
     }
 #pragma unroll
-  for (int o = 16; o <= 32; o <<= 1) {
+  for (int o = R; o <= 32; o <<= 1) {
     const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
     merge(m2, s2);
   }
-  if (lane < 16) ms[wave][lane] = make_float2(m, s);
+  if (lane < R) ms[wave][lane] = make_float2(m, s);
   __syncthreads();
-  // wave w: row w
-  const int64_t n = r0 + wave;
-  if (n >= h.rows) return;
-  m = ms[lane & 15][wave].x;
-  s = ms[lane & 15][wave].y;
+  // waves W r .. W r + W - 1: row r
+  const int part = wave % W;
+  const int64_t n = r0 + wave / W;
+  const bool live = n < h.rows;
+  m = ms[lane & 15][wave / W].x;
+  s = ms[lane & 15][wave / W].y;
 #pragma unroll
   for (int o = 1; o <= 8; o <<= 1) {
     const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
     merge(m2, s2);
   }
   const float l = logf(s);
-  if (lane == 0) h.stats[n] = make_float2(m, l);
+  if (live && part == 0 && lane == 0) h.stats[n] = make_float2(m, l);
 
   const T *x = static_cast<const T *>(h.x_in) + n * h.x_in_ld;
   const T *w = static_cast<const T *>(h.w_in);
   if (!h.teacher) {
+    if (!live || part > 0) return;
     const int64_t id = h.ids[n];
     float loss = 0.0f;
     if (id >= h.classes) {
@@ -945,45 +948,52 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
   // q = softmax(teacher / T) over the entries that count
   const int64_t *ids = h.ids + n * h.top;
   const float *te = h.teacher + n * h.top;
-  float tm = -INFINITY, bad = 0.0f;
-  for (int k = lane; k < h.top; k += 64)
-    if (ids[k] >= 0) {
-      tm = fmaxf(tm, te[k]);
-      if (ids[k] >= h.classes || !(te[k] < INFINITY)) bad = 1.0f;
-    }
-  tm = wave_max(tm);
-  bad = wave_max(bad);
-  const bool none = tm == -INFINITY;
-  float ts = 0.0f;
-  for (int k = lane; k < h.top; k += 64)
-    if (ids[k] >= 0 && !none) ts += __builtin_amdgcn_exp2f((te[k] - tm) * c);
-  ts = wave_sum(ts);
-  const float lts = logf(ts);
-  float loss = 0.0f;
-  constexpr int KB = 8;
-  for (int k0 = 0; k0 < h.top; k0 += KB) {
-    int64_t id[KB];
-    float z[KB];
-#pragma unroll
-    for (int k = 0; k < KB; ++k) {
-      const int64_t v = k0 + k < h.top ? ids[k0 + k] : -1;
-      id[k] = v < h.classes ? v : -1;
-    }
-    wave_dots<T, KB>(x, w, h.w_in_ld, id, h.dim, lane, z);
-#pragma unroll
-    for (int k = 0; k < KB; ++k) {
-      if (k0 + k >= h.top) continue;
-      if (id[k] >= 0) {
-        if (h.bias) z[k] += h.bias[id[k]];
-        const float u = (te[k0 + k] - tm) * h.inv_t;
-        const float q = __builtin_amdgcn_exp2f(u * kLog2e) / ts;
-        // an entry without weight adds nothing, whatever its logit
-        if (q > 0.0f) loss += q * ((u - lts) + ((m - z[k]) * h.inv_t + l));
+  float tm = -INFINITY, bad = 0.0f, loss = 0.0f;
+  if (live) {
+    for (int k = lane; k < h.top; k += 64)
+      if (ids[k] >= 0) {
+        tm = fmaxf(tm, te[k]);
+        if (ids[k] >= h.classes || !(te[k] < INFINITY)) bad = 1.0f;
       }
-      if (lane == 0) h.picked[n * h.top + k0 + k] = id[k] >= 0 ? z[k] : 0.0f;
+    tm = wave_max(tm);
+    bad = wave_max(bad);
+    float ts = 0.0f;
+    for (int k = lane; k < h.top; k += 64)
+      if (ids[k] >= 0 && tm != -INFINITY) ts += __builtin_amdgcn_exp2f((te[k] - tm) * c);
+    ts = wave_sum(ts);
+    const float lts = logf(ts);
+    constexpr int KB = R == 16 ? 8 : R == 4 ? 4 : 2;
+    for (int k0 = part * KB; k0 < h.top; k0 += W * KB) {
+      int64_t id[KB];
+      float z[KB];
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        const int64_t v = k0 + k < h.top ? ids[k0 + k] : -1;
+        id[k] = v < h.classes ? v : -1;
+      }
+      wave_dots<T, KB>(x, w, h.w_in_ld, id, h.dim, lane, z);
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        if (k0 + k >= h.top) continue;
+        if (id[k] >= 0) {
+          if (h.bias) z[k] += h.bias[id[k]];
+          const float u = (te[k0 + k] - tm) * h.inv_t;
+          const float q = __builtin_amdgcn_exp2f(u * kLog2e) / ts;
+          // an entry without weight adds nothing, whatever its logit
+          if (q > 0.0f) loss += q * ((u - lts) + ((m - z[k]) * h.inv_t + l));
+        }
+        if (lane == 0) h.picked[n * h.top + k0 + k] = id[k] >= 0 ? z[k] : 0.0f;
+      }
     }
   }
-  if (lane == 0) h.loss[n] = bad != 0.0f ? NAN : none ? 0.0f : h.t * h.t * loss;
+  if (W > 1) {
+    if (lane == 0) sums[wave] = loss;
+    __syncthreads();
+    loss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) loss += sums[wave / W * W + i];
+  }
+  if (live && part == 0 && lane == 0) h.loss[n] = bad != 0.0f ? NAN : tm == -INFINITY ? 0.0f : h.t * h.t * loss;
 }
 
 // What the backward pass needs of a row, a wave per row: its largest logit m and
@@ -1311,6 +1321,18 @@ hipError_t forward(HeadArgs a, hipStream_t s) {
   return product<T, E_STATS>(v, g, a, s);
 }
 template <typename T>
+hipError_t finish(const HeadArgs &a, hipStream_t s) {
+  // As many waves to a row as leave a block to every CU: its entries' dots are what takes
+  // the time (256 x 1024 x 32000, 32 entries a row: 9.5 us with a row a block, 15.2 with
+  // four, 39.8 with sixteen; 1000 rows 23.8, 19.5 and 39.9; 4096 rows 98, 79 and 64: the
+  // more rows to a block, the wider are the reads of the parts).
+  const dim3 block(1024);
+  if (a.rows <= kCus) hapi_launch((head_finish_kernel<T, 1>), dim3((uint32_t)a.rows), block, 0, s, a);
+  else if (a.rows <= 4 * kCus) hapi_launch((head_finish_kernel<T, 4>), dim3((uint32_t)ceil_div(a.rows, 4)), block, 0, s, a);
+  else hapi_launch((head_finish_kernel<T, 16>), dim3((uint32_t)ceil_div(a.rows, 16)), block, 0, s, a);
+  return hipGetLastError();
+}
+template <typename T>
 hipError_t dlogits(const HeadArgs &a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   Gemm g{};
@@ -1389,10 +1411,7 @@ hipError_t launch_head_forward(bool bf16, const HeadArgs &a, hipStream_t s) {
 
 hipError_t launch_head_finish(bool bf16, const HeadArgs &a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  const dim3 grid((uint32_t)((a.rows + kFinishRows - 1) / kFinishRows));
-  if (bf16) hapi_launch(head_finish_kernel<uint16_t>, grid, dim3(1024), 0, s, a);
-  else hapi_launch(head_finish_kernel<float>, grid, dim3(1024), 0, s, a);
-  return hipGetLastError();
+  return bf16 ? finish<uint16_t>(a, s) : finish<float>(a, s);
 }
 
 hipError_t launch_head_prepare(bool bf16, const HeadArgs &a, void *xs, int64_t xs_ld, hipStream_t s) {
