@@ -137,6 +137,18 @@ def test_norm_row_strides(rows, dim, xs, ys, dtype):
     R.check("dbeta", db, want[2])
 
 
+def test_norm_offsets_past_32_bits():
+    """2.3e9 elements from the first row to the last."""
+    x, dy, gamma, beta = _norm_case(6, 2200, 50, BF, 2 ** 20 - 50)
+    want = R.norm_forward(x, gamma, beta, 1e-6)
+    got = _norm_forward(x, gamma, beta)
+    for name, t, w in zip(("y", "mean", "rstd"), got, want):
+        R.check(name, t, w)
+    back = _norm_backward(dy, x, gamma, got[1], got[2], 2 ** 20 - 50)
+    for name, t, w in zip(("dx", "dgamma", "dbeta"), back, R.norm_backward(dy, x, gamma, got[1], got[2])):
+        R.check(name, t, w)
+
+
 def test_norm_unaligned_start():
     """A tensor that starts one element into its allocation."""
     for dtype in (BF, F32):
@@ -299,6 +311,30 @@ def test_last_round_in_smaller_tiles(rows, classes, top):
 
 def test_pieces_in_float32():
     c = _head_case(4, 1100, 40, 60100, F32, bias=False)
+    _head_check(c, _head_run(c))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,dim,classes,top", [(256, 40, 90, 5), (1023, 32, 60, 40), (1025, 16, 33, 3)])
+def test_distillation_waves_to_a_row(rows, dim, classes, top, dtype):
+    c = _head_case(rows + top, rows, dim, classes, dtype, bias=True, top=top)
+    _head_check(c, _head_run(c))
+
+
+@pytest.mark.parametrize("rows,dim,classes,top", [(2, 16, 2100001, 0), (3, 24, 2100001, 3), (5, 66000, 70, 0),
+                                                  (40, 20000, 130, 2), (70001, 24, 11, 2)])
+def test_far_ends_of_the_sizes(rows, dim, classes, top):
+    """Few rows and several pieces of the classes, many features, many rows."""
+    c = _head_case(rows + top, rows, dim, classes, BF, bias=True, top=top)
+    _head_check(c, _head_run(c))
+
+
+@pytest.mark.parametrize("which", ["x", "w"])
+def test_offsets_past_32_bits(which):
+    """The longest row stride: 2.3e9 elements from the first row to the last."""
+    rows, classes = (2200, 100) if which == "x" else (100, 2200)
+    c = _head_case(5, rows, 64, classes, BF)
+    c[which] = _strided(c[which], 2 ** 20 - 64)
     _head_check(c, _head_run(c))
 
 
