@@ -90,7 +90,7 @@ bool head_few_apart(int dim, int64_t piece) { return ceil_div(dim, 64) * ceil_di
 int head_w_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece) {
   if (piece < classes) return 1;
   const GradTiles t = grad_tiles(bf16, rows, dim, classes, piece);
-  const int64_t most = ceil_div(rows, bf16 ? 64 : 32) / 8, want = 2 * kCus / std::max<int64_t>(t.nw, 1);
+  const int64_t most = ceil_div(rows, bf16 ? 64 : 32) / 8, want = (t.v == BIG ? 1 : 2) * kCus / std::max<int64_t>(t.nw, 1);
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(most, want), 16));
 }
 
