@@ -856,10 +856,21 @@ __device__ __forceinline__ void wave_dots(const T *x, const T *w, int64_t ld, co
   for (int k = 0; k < K; ++k) s[k] = 0.0f;
   for (int d = lane * V; d < dim; d += 64 * V) {
     T a[V], b[K][V];
-    if (d + V <= dim) {
-      __builtin_memcpy(a, x + d, 16);
+    if (dim >= V) {
+      // the last values come with some of the ones before, which the lane there has
+      const int at = d + V <= dim ? d : dim - V;
+      __builtin_memcpy(a, x + at, 16);
 #pragma unroll
-      for (int k = 0; k < K; ++k) __builtin_memcpy(b[k], w + (id[k] < 0 ? 0 : id[k]) * ld + d, 16);
+      for (int k = 0; k < K; ++k) __builtin_memcpy(b[k], w + (id[k] < 0 ? 0 : id[k]) * ld + at, 16);
+      if (at < d) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          if (at + j >= d) continue;
+          a[j] = 0;
+#pragma unroll
+          for (int k = 0; k < K; ++k) b[k][j] = 0;
+        }
+      }
 #pragma unroll
       for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -867,9 +878,7 @@ __device__ __forceinline__ void wave_dots(const T *x, const T *w, int64_t ld, co
     } else {
 #pragma unroll
       for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (d + j < dim) s[k] = fmaf(to_f(x[d + j]), to_f(w[(id[k] < 0 ? 0 : id[k]) * ld + d + j]), s[k]);
+        for (int j = 0; j < dim; ++j) s[k] = fmaf(to_f(x[j]), to_f(w[(id[k] < 0 ? 0 : id[k]) * ld + j]), s[k]);
     }
   }
 #pragma unroll
@@ -962,7 +971,9 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
       if (ids[k] >= 0 && tm != -INFINITY) ts += __builtin_amdgcn_exp2f((te[k] - tm) * c);
     ts = wave_sum(ts);
     const float lts = logf(ts);
-    constexpr int KB = R == 16 ? 8 : R == 4 ? 4 : 2;
+    // rows of W in flight to a wave (eight leave no registers: 5000 x 300 x 3000, 32
+    // entries a row, 86 us against 59)
+    constexpr int KB = R == 1 ? 2 : 4;
     for (int k0 = part * KB; k0 < h.top; k0 += W * KB) {
       int64_t id[KB];
       float z[KB];
