@@ -1237,7 +1237,7 @@ __global__ __launch_bounds__(kReduceThreads) void head_reduce_kernel(HeadArgs h,
   }
   const int64_t c0 = (int64_t)(b - nx - nw) * kBiasClasses;
   const int slice = t / kBiasClasses, mine = t % kBiasClasses;
-  const int parts = h.db_parts + (h.teacher ? h.bias_slices : 0);
+  const int parts = h.db_parts + h.bias_slices;
   double sum = 0.0;
   if (c0 + mine < h.classes)
     for (int p = slice; p < parts; p += 4) sum += h.db_part[(int64_t)p * h.classes + c0 + mine];

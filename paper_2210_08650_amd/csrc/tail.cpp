@@ -279,7 +279,7 @@ int read_head(const hapi_head_desc *d, Head &h) {
   a.w_splits = head_w_splits(h.bf16, d->rows, d->dim, d->classes, h.piece);
   a.splits = head_splits(h.bf16, d->rows, d->dim, d->classes, h.piece, a.w_splits);
   a.dx_whole = a.splits == 1 && h.piece >= d->classes;
-  a.bias_slices = head_bias_slices(d->classes);
+  a.bias_slices = d->top > 0 && d->rows > 0 ? head_bias_slices(d->classes) : 0;  // without rows nothing writes them
 
   const int64_t xs = up(d->rows * a.dx_pad * h.esz, kAlign), ws = up(d->classes * a.dx_pad * h.esz, kAlign);
   int64_t o = 0;
@@ -300,7 +300,7 @@ int read_head(const hapi_head_desc *d, Head &h) {
   h.o_id = take(d->rows * a.top * 4);
   h.o_cq = take(d->rows * a.top * 4);
   h.o_gt = take(h.piece * a.rows_pad * h.esz);
-  h.o_db = take((int64_t)(a.db_parts + (d->top > 0 ? a.bias_slices : 0)) * d->classes * 4);
+  h.o_db = take((int64_t)(a.db_parts + a.bias_slices) * d->classes * 4);
   h.o_dx = take(a.dx_whole ? 0 : (int64_t)a.splits * d->rows * a.dx_pad * 4);
   h.o_dw = take(a.w_splits > 1 ? (int64_t)a.w_splits * d->classes * a.dx_pad * 4 : 0);
   h.bytes_bwd = o;

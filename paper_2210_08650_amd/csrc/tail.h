@@ -61,7 +61,7 @@ struct HeadArgs {
   bool dx_whole;            // one split and one piece: no partial sums
   float *dw_part;           // [w_splits][classes][dx_pad], one piece only
   int w_splits;
-  int bias_slices;          // distillation: parts of dbias for what the targets take off
+  int bias_slices;          // distillation of any rows: parts of dbias for what the targets take off; else 0
   void *dx, *dw;
   int64_t dx_ld, dw_ld;
   float *dbias;
