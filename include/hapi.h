@@ -528,14 +528,15 @@ int hapi_xent_backward(const hapi_head_desc *desc, const void *x, const void *we
  * row's top entries and p = softmax(z / T) over all classes,
  *   loss = T^2 sum_k q_k (log q_k - log p[ids_k])   (the divergence KL(q | p))
  *   ids     [rows, top] int64: the classes of the teacher's logits, in any order.
- *           An id < 0 or a logit of -inf is no entry; a row without entries does
- *           not count (as a negative target).  A class named twice has both
- *           entries' weight.  An id >= classes, or a logit of NaN or +inf of an
- *           entry: the loss and the gradients it reaches are NaN.
+ *           An id < 0 or a logit of -inf is no entry, whatever stands beside it; a
+ *           row without entries does not count (as a negative target).  A class
+ *           named twice has both entries' weight.  An entry whose id is >= classes
+ *           or whose logit is NaN or +inf: the loss and the gradients it reaches
+ *           are NaN.
  *   teacher [rows, top] float32
  *   loss [rows], stats [rows, 2] (m, the largest logit, and
  *           l = log sum exp((z - m) / T)), picked [rows, top] (the classifier's
- *           logits z at the ids, 0 where there is none) float32 outputs
+ *           logits z at the ids that are classes, 0 at others) float32 outputs
  * Everything else as in the cross entropy. */
 int hapi_distill_forward(const hapi_head_desc *desc, const void *x, const void *weight, const float *bias,
                          const int64_t *ids, const float *teacher, float *loss, float *stats, float *picked);

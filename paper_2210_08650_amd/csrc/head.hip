@@ -887,6 +887,9 @@ __device__ __forceinline__ void wave_dots(const T *x, const T *w, int64_t ld, co
     for (int k = 0; k < K; ++k) s[k] += __shfl_xor(s[k], o, 64);
 }
 
+// Whether a teacher's logit beside an id is an entry.  One of NaN is, with an error in it.
+__device__ __forceinline__ bool is_entry(int64_t id, float logit) { return id >= 0 && logit != -INFINITY; }
+
 // Joins a row's partial statistics and forms its loss: R rows a block, 1024 / R
 // threads on a row's parts, then 16 / R waves on the logits at its targets.
 // Merging two (max, sum) pairs rescales the smaller one's sum.
@@ -960,7 +963,7 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
   float tm = -INFINITY, bad = 0.0f, loss = 0.0f;
   if (live) {
     for (int k = lane; k < h.top; k += 64)
-      if (ids[k] >= 0) {
+      if (is_entry(ids[k], te[k])) {
         tm = fmaxf(tm, te[k]);
         if (ids[k] >= h.classes || !(te[k] < INFINITY)) bad = 1.0f;
       }
@@ -1050,7 +1053,7 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
     } else {
       const float *te = h.teacher + n * h.top;
       for (int k = lane; k < h.top; k += 64)
-        if (ids[k] >= 0) {
+        if (is_entry(ids[k], te[k])) {
           tm = fmaxf(tm, te[k]);
           if (ids[k] >= h.classes || !(te[k] < INFINITY)) bad = 1.0f;
         }
@@ -1069,9 +1072,10 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
       info = make_float2(st.x, coef * __builtin_amdgcn_exp2f(-st.y * kLog2e));
     }
     for (int k = lane; k < h.top; k += 64) {
-      const bool entry = counts && ids[k] >= 0 && ids[k] < h.classes;
+      const float te = h.teacher ? h.teacher[n * h.top + k] : 0.0f;
+      const bool entry = counts && is_entry(ids[k], te) && ids[k] < h.classes;
       h.id32[n * h.top + k] = entry ? (int)ids[k] : -1;
-      const float q = h.teacher ? __builtin_amdgcn_exp2f((h.teacher[n * h.top + k] - tm) * kLog2e * h.inv_t) / ts : 1.0f;
+      const float q = h.teacher ? __builtin_amdgcn_exp2f((te - tm) * kLog2e * h.inv_t) / ts : 1.0f;
       h.cq[n * h.top + k] = entry ? coef * q : 0.0f;
     }
     const T *p = static_cast<const T *>(h.x_in) + n * h.x_in_ld;

@@ -1,12 +1,12 @@
 """The trained tail at the edges of what its header allows: no rows with real
-addresses."""
+addresses, entries without weight."""
 import math
 
 import pytest
 import torch
 
 import paper_2210_08650_amd as H
-from tests.test_gpu_tail import BF, CODE, F32
+from tests.test_gpu_tail import BF, CODE, F32, _gen, _head_case, _head_run
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +33,26 @@ def test_no_rows_with_addresses(top, dtype):
     torch.cuda.synchronize()
     assert bool((dw == 0).all()) and bool((db == 0).all())
     assert bool(torch.isnan(some).all()), "wrote to a row that is not there"
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [20, 150])
+@pytest.mark.parametrize("pad", [-1, 5, 200, 2 ** 40])
+def test_entries_without_weight_may_name_anything(pad, rows, dtype):
+    """A teacher's logit of -inf is no entry, whatever id stands beside it: the results
+    are those of the id -1.  A row of nothing else does not count."""
+    c = _head_case(61, rows, 72, 200, dtype, top=4)
+    out = torch.rand(rows, 4, generator=_gen(62), device="cuda") < 0.3
+    out[3] = True
+    c["teacher"][out] = -math.inf
+    c["ids"] = c["ids"].masked_fill(out, -1)
+    want = {k: v.clone() for k, v in _head_run(c).items()}
+    c["ids"] = c["ids"].masked_fill(out, pad)
+    got = _head_run(c)
+    for name in ("loss", "stats", "dx", "dw", "db"):
+        assert torch.equal(got[name], want[name]), name
+    assert float(got["loss"][3]) == 0 and bool((got["dx"][3] == 0).all())
+    # picked holds a logit wherever the id is a class
+    assert torch.equal(got["picked"][~out], want["picked"][~out])
+    if not 0 <= pad < 200:
+        assert bool((got["picked"][out] == 0).all())
