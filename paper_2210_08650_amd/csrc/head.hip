@@ -186,7 +186,7 @@ struct Side {
 // What the epilogue needs of the tile's reg side, in LDS.  Forward: the bias of
 // its classes, -inf past the last one.  dz: its rows' largest logit and scale, and
 // for cross entropy the target class (in the piece; far off if none) and the
-// coefficient to take off there.
+// coefficient to take off there, both over the coefficients' unit.
 template <int EPI, int BA>
 struct SideTable {
   static constexpr int N = EPI == E_STATS || EPI == E_DLOGITS ? BA : 4;
@@ -200,13 +200,14 @@ struct SideTable {
     if constexpr (EPI == E_DLOGITS)
       for (int i = t; i < BA; i += THREADS) {
         const int n = a0 + i;
+        const float unit = *h.unit;
         const float2 in = n < h.rows_pad ? h.info[n] : make_float2(INFINITY, 0.0f);
         m[i] = in.x;
-        scale[i] = in.y;
+        scale[i] = in.y / unit;
         if (!h.teacher) {
           const int id = n < h.rows ? h.id32[n] : -1;
           target[i] = id >= 0 ? id - (int)h.v0 : INT32_MIN / 2;
-          coef[i] = n < h.rows ? h.cq[n] : 0.0f;
+          coef[i] = n < h.rows ? h.cq[n] / unit : 0.0f;
         }
       }
   }
@@ -1010,17 +1011,66 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs h) {
   if (live && part == 0 && lane == 0) h.loss[n] = bad != 0.0f ? NAN : tm == -INFINITY ? 0.0f : h.t * h.t * loss;
 }
 
+// The significand of a coefficient dloss T, of the first entry of a row that counts (1
+// if there is none), by the 256 threads of one block, 4096 entries a round.  dz^T holds
+// the coefficients over it, and the gradients are multiplied by it in float32: where all
+// rows have the same dloss (a mean's), a target's entry of dz is then a power of two
+// times p - 1, and not off by the rounding of dloss to 16 bits in every row alike (up
+// to 2^-8 of the whole gradient: at 8192 x 2048 x 131072 it was off by 0.0040 of its
+// length, and is by 0.0017, its own rounding).  Where they differ any value does as
+// well as another: coefficients stay within a factor of two.  Padding in front is
+// common (a masked prompt), so the search goes on until it finds a row, while the other
+// blocks prepare theirs (2048 of 4096 rows of 32 entries masked: the step 967 -> 975 us;
+// no row masked, no longer).
+__device__ __forceinline__ void find_unit(const HeadArgs &h) {
+  constexpr int U = 16, NONE = INT32_MAX;
+  __shared__ int found[2][4];
+  const int t = threadIdx.x, total = (int)(h.rows * h.top);  // at most 2^30
+  auto coefficient = [&](int i) { return fabsf(h.dloss[(uint32_t)i / (uint32_t)h.top] * h.t); };
+  int first = NONE, flip = 0;
+  for (int i0 = 0; i0 < total; i0 += 256 * U) {
+    // all loads in flight together: past the last entry that one again
+    auto entry = [&](int u) { return min(i0 + 256 * u + t, total - 1); };
+    int64_t id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = h.ids[entry(u)];
+    uint32_t named = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) named |= (uint32_t)(id[u] >= 0) << u;
+    for (; named && first == NONE; named &= named - 1) {
+      const int i = entry(__ffs(named) - 1);
+      const float c = coefficient(i);
+      if (c > 0.0f && c < INFINITY && (!h.teacher || is_entry(0, h.teacher[i]))) first = i;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) first = min(first, __shfl_xor(first, o, 64));
+    if ((t & 63) == 0) found[flip][t >> 6] = first;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) first = min(first, found[flip][w]);
+    if (first != NONE) break;
+    flip ^= 1;  // one barrier a round
+  }
+  if (t == 0)
+    *h.unit = first != NONE ? __uint_as_float((__float_as_uint(coefficient(first)) & 0x7fffffu) | 0x3f800000u) : 1.0f;
+}
+
 // What the backward pass needs of a row, a wave per row: its largest logit m and
 // the coefficient over the sum of exp((z - m) / T), so that dz = exp((z - m) / T)
 // times it, or (inf, 0) for a row that does not count; the targets as 32-bit
 // classes (-1: none) with the weight to take off there; and a copy of x whose rows
 // that do not count are zero, so that nothing they hold reaches a sum.
 // Few rows of 16 bits: x and zeros up to row 32, then the same again.
+// The first block finds the coefficients' unit.
 template <typename T>
 __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__restrict__ xs, int64_t xs_ld) {
   constexpr int V = 16 / (int)sizeof(T);
+  if (blockIdx.x == 0) {
+    find_unit(h);
+    return;
+  }
   const int lane = threadIdx.x & 63;
-  const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t n = (int64_t)(blockIdx.x - 1) * 4 + (threadIdx.x >> 6);
   if (n >= h.rows_pad) return;
   float2 info = make_float2(INFINITY, 0.0f);
   const bool pair = sizeof(T) == 2 && h.rows <= kFewRows;
@@ -1031,19 +1081,7 @@ __global__ __launch_bounds__(256) void head_prepare_kernel(HeadArgs h, T *__rest
     }
   if (n < h.rows) {
     const int64_t *ids = h.ids + n * h.top;
-    // The significand of a coefficient (of the first row that counts, among 64), which
-    // every coefficient is divided by and the gradients are multiplied by in float32:
-    // where all rows have the same dloss (a mean's), a target's entry of dz is then a power of two times p - 1, and
-    // not off by the rounding of dloss to 16 bits in every row alike (up to 2^-8 of
-    // the whole gradient: at 8192 x 2048 x 131072 it was off by 0.0040 of its length,
-    // and is by 0.0017, its own rounding).  Its value is of no importance else:
-    // coefficients stay within a factor of two.
-    const float c0 = fabsf(lane < h.rows ? h.dloss[lane] * h.t : 0.0f);
-    const uint64_t some = __ballot(c0 > 0.0f && c0 < INFINITY && h.ids[lane < h.rows ? lane * (int64_t)h.top : 0] >= 0);
-    const uint32_t bits = __shfl(__float_as_uint(c0), some ? __ffsll((unsigned long long)some) - 1 : 0, 64);
-    const float unit = some ? __uint_as_float((bits & 0x7fffffu) | 0x3f800000u) : 1.0f;
-    if (n == 0 && lane == 0) *h.unit = unit;
-    float coef = h.dloss[n] * h.t / unit;
+    float coef = h.dloss[n] * h.t;
     float bad = 0.0f;
     bool none;
     float tm = -INFINITY, ts = 1.0f;
@@ -1126,6 +1164,7 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
     float v = __builtin_amdgcn_exp2f((h.picked[i] - info.x) * h.inv_t * kLog2e) * info.y;
     for (int k = 0; k < h.top; ++k)
       if (h.id32[n * h.top + k] == id) v -= h.cq[n * h.top + k];
+    v /= *h.unit;
     T *p = static_cast<T *>(h.gt) + (id - h.v0) * h.rows_pad + n;
     put(p, v);
     if (sizeof(T) == 2 && h.rows <= kFewRows) put(p + kFewRows, bf16_rest(v));
@@ -1194,7 +1233,7 @@ __global__ __launch_bounds__(256) void head_targets_kernel(HeadArgs h, int nt) {
   if (second) half_s[mine] = sum;
   __syncthreads();
   if (!second && c0 + mine < h.classes)
-    h.db_part[(int64_t)(h.db_parts + slice) * h.classes + c0 + mine] = (float)(sum + half_s[mine]);
+    h.db_part[(int64_t)(h.db_parts + slice) * h.classes + c0 + mine] = (float)((sum + half_s[mine]) / (double)*h.unit);
 }
 
 // out[r][d] = unit times the splits' partial sums in order, 0 in rows that do not
@@ -1431,7 +1470,7 @@ hipError_t launch_head_finish(bool bf16, const HeadArgs &a, hipStream_t s) {
 
 hipError_t launch_head_prepare(bool bf16, const HeadArgs &a, void *xs, int64_t xs_ld, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  const dim3 grid((uint32_t)((a.rows_pad + 3) / 4));
+  const dim3 grid((uint32_t)((a.rows_pad + 3) / 4) + 1);
   if (bf16) hapi_launch(head_prepare_kernel<uint16_t>, grid, dim3(256), 0, s, a, (uint16_t *)xs, xs_ld);
   else hapi_launch(head_prepare_kernel<float>, grid, dim3(256), 0, s, a, (float *)xs, xs_ld);
   return hipGetLastError();

@@ -48,7 +48,7 @@ struct HeadArgs {
   // backward
   const float *dloss;
   float2 *info;             // [rows_pad] (m, coefficient / sum of exp); rows that do not count: (inf, 0)
-  float *unit;              // what all coefficients are divided by, in [1, 2)
+  float *unit;              // what dz^T's coefficients are divided by, in [1, 2)
   int32_t *id32;            // [rows][top] the targets' classes, -1: none
   float *cq;                // [rows][top] what they take off dz: coefficient times weight
   void *gt;                 // [piece][rows_pad] dz^T of one piece of the classes

@@ -1,11 +1,12 @@
 """The trained tail at the edges of what its header allows: no rows with real
-addresses, entries without weight."""
+addresses, entries without weight, counting rows that begin late."""
 import math
 
 import pytest
 import torch
 
 import paper_2210_08650_amd as H
+from tests import tail_reference as R
 from tests.test_gpu_tail import BF, CODE, F32, _gen, _head_case, _head_run
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +57,29 @@ def test_entries_without_weight_may_name_anything(pad, rows, dtype):
     assert torch.equal(got["picked"][~out], want["picked"][~out])
     if not 0 <= pad < 200:
         assert bool((got["picked"][out] == 0).all())
+
+
+@pytest.mark.parametrize("rows,classes,first,top", [
+    (300, 5003, 64, 0), (700, 33000, 64, 0), (700, 33000, 650, 0), (5000, 700, 4700, 0), (70001, 200, 69000, 0),
+    (300, 5003, 0, 2), (300, 5003, 65, 2), (5000, 700, 4700, 2), (300, 600, 290, 1024)])
+def test_a_mean_keeps_its_targets_whole_wherever_it_begins(rows, classes, first, top):
+    """The rows that count begin behind `first` others (a masked prompt, padding in
+    front), and a teacher's one entry is the last of its row.  1 / 4080 has a
+    significand of 1.0039, half a step of 16 bits from either neighbour: were dloss
+    rounded, every target's entry and so the whole gradient would be off by 2^-8.
+    The bound is the gradients' own rounding, 2^-8 / sqrt 3 of their length at most,
+    and a tenth for the small entries' (p, of a 16-bit step of its own)."""
+    c = _head_case(70, rows, 96, classes, BF, bias=False, spread=1.0)
+    ids = c["ids"].clamp(min=0)
+    ids[:first] = -1
+    c["dloss"].fill_(1.0 / 4080)
+    c["dloss"][:first] = 0.7
+    c["ids"] = ids
+    want = R.head(c["x"], c["w"], None, ids, None, 1.0, c["dloss"])
+    if top:
+        c["ids"] = torch.full((rows, top), -1, device="cuda")
+        c["ids"][:, -1] = ids
+        c["teacher"] = torch.zeros(rows, top, device="cuda")
+    got = _head_run(c)
+    for name in ("dx", "dw"):
+        R.check(name, got[name], want[name], 1.1 * 2.0 ** -8 / math.sqrt(3))
