@@ -1353,26 +1353,24 @@ hipError_t product(Variant v, const Gemm &g, const HeadArgs &a, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t forward(HeadArgs a, hipStream_t s) {
+hipError_t forward(const HeadArgs &a, hipStream_t s) {
   Gemm g{};
-  g.a = a.w; g.a_ld = a.w_ld; g.a_ext = (int)a.classes;
+  g.a_ld = a.w_ld;
   g.b = a.x; g.b_ld = a.x_ld; g.b_ext = (int)a.rows;
   g.k_ext = a.dim; g.splits = 1;
-  const Variant v = head_variant(sizeof(T) == 2, a.rows, a.classes);
-  if (v == BIG && sizeof(T) == 2) {
-    const int64_t c = head_big_classes(a.rows, a.classes);
-    if (c < a.classes) {
-      g.a_ext = (int)c;
-      const hipError_t e = product<T, E_STATS>(BIG, g, a, s);
-      if (e != hipSuccess) return e;
-      g.a = static_cast<const T *>(a.w) + c * a.w_ld;
-      g.a_ext = (int)(a.classes - c);
-      if (a.bias) a.bias += c;
-      a.part += c / 64 * a.rows;
-      return product<T, E_STATS>(MID, g, a, s);
-    }
+  for (int64_t c0 = 0; c0 < a.classes;) {
+    const HeadLaunch l = head_forward_launch(sizeof(T) == 2, a.rows, a.classes, c0);
+    g.a = static_cast<const T *>(a.w) + c0 * a.w_ld;
+    g.a_ext = (int)l.classes;
+    HeadArgs h = a;
+    if (a.bias) h.bias += c0;
+    h.part += (int64_t)l.part * a.rows;
+    h.parts = l.parts;
+    const hipError_t e = product<T, E_STATS>(l.v, g, h, s);
+    if (e != hipSuccess) return e;
+    c0 += l.classes;
   }
-  return product<T, E_STATS>(v, g, a, s);
+  return hipSuccess;
 }
 template <typename T>
 hipError_t finish(const HeadArgs &a, hipStream_t s) {

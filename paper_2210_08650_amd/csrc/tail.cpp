@@ -57,6 +57,20 @@ int head_parts(bool bf16, int64_t rows, int64_t classes) {
     default: return (int)ceil_div(classes, 128) * 4;
   }
 }
+HeadLaunch head_forward_launch(bool bf16, int64_t rows, int64_t classes, int64_t c0) {
+  HeadLaunch l;
+  l.v = head_variant(bf16, rows, classes);
+  int64_t end = classes;
+  if (l.v == BIG && bf16) {
+    const int64_t big = head_big_classes(rows, classes);
+    if (c0 < big) end = big;
+    else l.v = MID;
+  }
+  l.classes = end - c0;
+  l.part = (int)(c0 / (l.v == BIG || l.v == MID ? 64 : 32));
+  l.parts = head_parts(bf16, rows, classes) - l.part;
+  return l;
+}
 int head_db_parts(bool bf16, int64_t rows, int64_t classes) {
   switch (head_variant(bf16, rows, classes)) {
     case BIG:

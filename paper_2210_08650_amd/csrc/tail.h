@@ -75,11 +75,18 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 Variant head_variant(bool bf16, int64_t rows, int64_t classes);
 // BIG: the classes that 256 x 256 tiles take; 128 x 128 ones take the others.
 int64_t head_big_classes(int64_t rows, int64_t classes);
-// The parts the forward product writes of a row, dz's of a class, and the splits of
-// dx's product.
+// The parts the forward product writes of a row, and dz's of a class.
 int head_parts(bool bf16, int64_t rows, int64_t classes);
 int head_db_parts(bool bf16, int64_t rows, int64_t classes);
-// FEW: whether dx and dW are launches of their own.
+// The forward product's launch that begins at class c0: its tiles and classes, its first
+// part, and the parts there are from that one on.
+struct HeadLaunch {
+  Variant v;
+  int64_t classes;
+  int part, parts;
+};
+HeadLaunch head_forward_launch(bool bf16, int64_t rows, int64_t classes, int64_t c0);
+// FEW: whether dx and dW are launches of their own; the splits of either product's k.
 bool head_few_apart(int dim, int64_t piece);
 int head_w_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece);
 int head_splits(bool bf16, int64_t rows, int dim, int64_t classes, int64_t piece, int w_splits);
