@@ -791,7 +791,7 @@ template <typename Tile>
 hipError_t launch_product(Gemm g, const HeadArgs &h, hipStream_t s) {
   const int64_t blocks = count_tiles<Tile>(g);
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (blocks > kMaxLaunchThreads / Tile::THREADS) return hipErrorInvalidValue;
   hapi_launch(head_product_kernel<Tile>, dim3((uint32_t)blocks), dim3(Tile::THREADS), 0, s, g, h);
   return hipGetLastError();
 }
@@ -799,7 +799,7 @@ hipError_t launch_product(Gemm g, const HeadArgs &h, hipStream_t s) {
 template <typename DX, typename DW>
 hipError_t launch_grads(Gemm gx, Gemm gw, const HeadArgs &h, hipStream_t s) {
   const int64_t nx = count_tiles<DX>(gx), nw = count_tiles<DW>(gw);
-  if (nx + nw > 0x7fffffff) return hipErrorInvalidValue;
+  if (nx + nw > kMaxLaunchThreads / DX::THREADS) return hipErrorInvalidValue;
   hapi_launch((head_grads_kernel<DX, DW>), dim3((uint32_t)(nx + nw)), dim3(DX::THREADS), 0, s, gx, gw, (int)nx, h);
   return hipGetLastError();
 }
@@ -1406,7 +1406,7 @@ hipError_t dlogits(const HeadArgs &a, hipStream_t s) {
   if (e != hipSuccess || !a.teacher) return e;
   const int64_t nt = ceil_div(a.rows * a.top, 256);
   const int64_t nb = a.db_part && a.first ? ceil_div(a.classes, kBiasClasses) * a.bias_slices : 0;
-  if (nt + nb > 0x7fffffff) return hipErrorInvalidValue;
+  if (nt + nb > kMaxLaunchThreads / 256) return hipErrorInvalidValue;
   hapi_launch(head_targets_kernel<T>, dim3((uint32_t)(nt + nb)), dim3(256), 0, s, a, (int)nt);
   return hipGetLastError();
 }

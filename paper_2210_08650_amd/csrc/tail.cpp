@@ -66,7 +66,12 @@ HeadLaunch head_forward_launch(bool bf16, int64_t rows, int64_t classes, int64_t
     if (c0 < big) end = big;
     else l.v = MID;
   }
-  l.classes = end - c0;
+  // No more threads than a launch takes: 131,072 rows of 4,194,304 classes, 2^23 tiles
+  // of 512 threads, are two.
+  const int64_t threads = l.v == BIG ? 512 : 256, tile_rows = l.v == BIG ? 256 : l.v == MID ? 128 : l.v == SMALL ? 64 : 32,
+                tile_classes = l.v == BIG ? 256 : l.v == MID || l.v == FEW ? 128 : l.v == SMALL ? 64 : 32;
+  const int64_t most = kMaxLaunchThreads / threads / std::max<int64_t>(ceil_div(rows, tile_rows), 1) * tile_classes;
+  l.classes = std::min(end - c0, most);
   l.part = (int)(c0 / (l.v == BIG || l.v == MID ? 64 : 32));
   l.parts = head_parts(bf16, rows, classes) - l.part;
   return l;

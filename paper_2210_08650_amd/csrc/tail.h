@@ -71,6 +71,7 @@ struct HeadArgs {
 // 32 rows by 128 classes (the weights stream past), 32 x 32.
 enum Variant { BIG, MID, SMALL, FEW, TINY };
 constexpr int64_t kCus = 256;  // compute units the rules count on
+constexpr int64_t kMaxLaunchThreads = UINT32_MAX;  // the threads of a launch are a 32-bit number
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 Variant head_variant(bool bf16, int64_t rows, int64_t classes);
 // BIG: the classes that 256 x 256 tiles take; 128 x 128 ones take the others.

@@ -1,7 +1,7 @@
 // Walks the launches that the forward product of the trained tail's classifier is made
 // of, from one row and class to the largest sizes: they cover the classes once, and
 // their parts lie within the partial statistics to the last one, with no more room
-// than there is.  Host code only.  Prints "OK <launches>".
+// than there is, and each is a launch that the device takes.  Host code only.  Prints "OK <launches>".
 #include <cstdio>
 #include <cstdlib>
 #include <initializer_list>
@@ -61,6 +61,8 @@ static void walk(bool bf16, int64_t rows, int64_t classes) {
     const Tile t = tile(l.v);
     EXPECT(l.classes > 0 && c0 + l.classes <= classes);
     const bool last = c0 + l.classes == classes;
+    // a launch's threads are a 32-bit number
+    EXPECT(ceil_div(l.classes, t.classes) * ceil_div(rows, t.rows) * t.threads <= (int64_t)UINT32_MAX);
     EXPECT(last || l.classes % t.classes == 0);  // whole tiles, so whole parts
     EXPECT(l.part == next_part && l.parts == parts - l.part && l.parts > 0);
     // parts that the launch's tiles have classes for: all of what is left by the last one

@@ -83,3 +83,27 @@ def test_a_mean_keeps_its_targets_whole_wherever_it_begins(rows, classes, first,
     got = _head_run(c)
     for name in ("dx", "dw"):
         R.check(name, got[name], want[name], 1.1 * 2.0 ** -8 / math.sqrt(3))
+
+
+def test_more_tiles_than_a_launch_takes():
+    """512 x 16,385 tiles of 512 threads, 2^32 threads and more: two launches of the
+    forward product.  Eight rows over and over, each as the eight alone."""
+    rows, dim, classes = 131072, 16, 4194304 + 5
+    d = H.Head(H.HAPI_BF16, rows, dim, classes, stream=torch.cuda.current_stream())
+    need = H.hapi_head_workspace_bytes(d, False)
+    if torch.cuda.mem_get_info()[0] < need + (8 << 30):
+        pytest.skip(f"{need} bytes of workspace")
+    g = _gen(90)
+    x8, w = torch.randn(8, dim, generator=g, device="cuda").to(BF), torch.randn(classes, dim, generator=g, device="cuda").to(BF)
+    bias = torch.randn(classes, generator=g, device="cuda")
+    ids8 = torch.tensor([0, classes - 1, -1, 255, 4194303, 4194304, 2 ** 21, 77777], device="cuda")
+    x, ids = x8.repeat(rows // 8, 1), ids8.repeat(rows // 8)
+    loss, stats = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    d.set(workspace=torch.empty(need, dtype=torch.uint8, device="cuda"), workspace_bytes=need)
+    H.hapi_xent_forward(d, x, w, bias, ids, loss, stats)
+    torch.cuda.synchronize()
+    want = R.head(x8, w, bias, ids8)
+    R.check("loss", loss.view(-1, 8), want["loss"])
+    R.check("stats", stats.view(-1, 8, 2), want["stats"])
+    del d
+    torch.cuda.empty_cache()  # 64 GB
