@@ -323,13 +323,7 @@ hipError_t launch_one(const NormArgs &a, hipStream_t s) {
     hapi_launch(norm_reduce_kernel, dim3((2 * a.dim + 15) / 16), dim3(1024), 0, s, (const float *)a.part, blocks, a.dim,
                 a.dgamma, a.dbeta);
   } else {
-    // As many rows to every block, up to four: gamma and beta are read once, and
-    // there are blocks enough for the CUs (25,216 x 768: 15.2 us with one, 14.8 with
-    // two, 15.3 with four, 17.0 with eight).
-    int64_t iters = want / 1536;
-    iters = iters < 1 ? 1 : iters > 4 ? 4 : iters;
-    const int64_t blocks = (want + iters - 1) / iters;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t blocks = norm_forward_blocks(want, block_of(TPR));
     if (blocks > 0) hapi_launch((norm_forward_kernel<T, TPR, CH>), dim3((uint32_t)blocks), dim3(block_of(TPR)), 0, s, a);
   }
   return hipGetLastError();

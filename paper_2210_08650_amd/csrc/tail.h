@@ -6,6 +6,9 @@
 
 namespace hapi {
 
+constexpr int64_t kMaxLaunchThreads = UINT32_MAX;  // the threads of a launch are a 32-bit number
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 // ---------------------------------------------------------------- layer norm
 
 constexpr int kNormMaxDim = 16384;
@@ -22,6 +25,9 @@ struct NormArgs {
   int dim;
   float eps;
 };
+// Blocks of the forward kernel, which walk the rows in a stride of the grid, for `want`
+// blocks' rows.
+int64_t norm_forward_blocks(int64_t want, int threads);
 hipError_t launch_norm_forward(bool bf16, const NormArgs &a, hipStream_t s);
 hipError_t launch_norm_backward(bool bf16, const NormArgs &a, hipStream_t s);
 
@@ -71,8 +77,6 @@ struct HeadArgs {
 // 32 rows by 128 classes (the weights stream past), 32 x 32.
 enum Variant { BIG, MID, SMALL, FEW, TINY };
 constexpr int64_t kCus = 256;  // compute units the rules count on
-constexpr int64_t kMaxLaunchThreads = UINT32_MAX;  // the threads of a launch are a 32-bit number
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 Variant head_variant(bool bf16, int64_t rows, int64_t classes);
 // BIG: the classes that 256 x 256 tiles take; 128 x 128 ones take the others.
 int64_t head_big_classes(int64_t rows, int64_t classes);

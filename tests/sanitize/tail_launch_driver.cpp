@@ -1,7 +1,8 @@
-// Walks the launches that the forward product of the trained tail's classifier is made
-// of, from one row and class to the largest sizes: they cover the classes once, and
-// their parts lie within the partial statistics to the last one, with no more room
-// than there is, and each is a launch that the device takes.  Host code only.  Prints "OK <launches>".
+// Walks layer norm's grids, and the launches that the forward product of the trained
+// tail's classifier is made of, from one row and class to the largest sizes: these
+// cover the classes once, and their parts lie within the partial statistics to the last
+// one, with no more room than there is; all are launches that the device takes.  Host
+// code only.  Prints "OK <launches>".
 #include <cstdio>
 #include <cstdlib>
 #include <initializer_list>
@@ -84,6 +85,16 @@ int main() {
     for (int64_t rows = 1; rows < 3000; rows += 37)
       for (int64_t classes = 1; classes < 200000; classes += 1 + classes / 9) walk(bf16, rows, classes);
   }
+  // Layer norm's forward grid: threads a launch takes, and no block without rows.
+  g_classes = 0;
+  for (int threads : {256, 512})
+    for (int64_t want : {(int64_t)1, (int64_t)2, (int64_t)1535, (int64_t)6145, (int64_t)1 << 26, ((int64_t)1 << 26) + 5,
+                         (int64_t)1 << 40, (int64_t)1 << 60}) {
+      g_rows = want;
+      const int64_t blocks = norm_forward_blocks(want, threads);
+      EXPECT(blocks >= 1 && blocks <= want && blocks * threads <= (int64_t)UINT32_MAX);
+      ++g_launches;
+    }
   std::printf("OK %ld\n", g_launches);
   return 0;
 }

@@ -1,5 +1,6 @@
 """The trained tail at the edges of what its header allows: no rows with real
-addresses, entries without weight, counting rows that begin late."""
+addresses, entries without weight, counting rows that begin late, more tiles and rows
+than one launch takes."""
 import math
 
 import pytest
@@ -107,3 +108,27 @@ def test_more_tiles_than_a_launch_takes():
     R.check("stats", stats.view(-1, 8, 2), want["stats"])
     del d
     torch.cuda.empty_cache()  # 64 GB
+
+
+def test_norm_of_more_rows_than_a_launch_takes():
+    """2^30 + 37 rows, 64 to a block of 256 threads, would be 2^32 threads and more.  The same
+    2^20 rows over and over, each time with the same bits."""
+    rows, dim, some = 2 ** 30 + 37, 2, 2 ** 20
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("24 GB of tensors")
+    g = _gen(91)
+    gamma, beta = torch.rand(dim, generator=g, device="cuda") + 0.5, torch.randn(dim, generator=g, device="cuda")
+    few = (torch.randn(some, dim, generator=g, device="cuda") * 1.5 + 0.3).to(BF)
+    x = torch.empty(rows, dim, dtype=BF, device="cuda")
+    for r in range(0, rows, some):
+        x[r:r + some] = few[:rows - r]
+    y, mean, rstd = torch.full_like(x, 9.0), torch.full((rows,), 9.0, device="cuda"), torch.full((rows,), 9.0, device="cuda")
+    H.hapi_layernorm_forward(H.Norm(H.HAPI_BF16, rows, dim, stream=torch.cuda.current_stream()), x, gamma, beta, y, mean, rstd)
+    torch.cuda.synchronize()
+    for name, t, w in zip(("y", "mean", "rstd"), (y, mean, rstd), R.norm_forward(few, gamma, beta, 1e-6)):
+        R.check(name, t[:some], w)
+    for t in (y, mean, rstd):
+        for r in range(some, rows, some):
+            assert torch.equal(t[r:r + some], t[:min(some, rows - r)]), r
+    del x, y, mean, rstd, t
+    torch.cuda.empty_cache()
