@@ -484,7 +484,7 @@ typedef struct {
   int64_t x_stride;         /* elements between rows of x and dx; 0 = dim; <= 2^20 */
   int64_t w_stride;         /* elements between rows of weight and dweight; 0 = dim; <= 2^20 */
   int32_t top;              /* distillation: the teacher's entries per row, 1 .. 1024; cross entropy: 0 */
-  float temperature;        /* distillation: T > 0; cross entropy: 1 */
+  float temperature;        /* distillation: T, 2^-60 .. 2^60; cross entropy: 1 */
   void *stream;             /* hipStream_t; NULL = the null stream */
   void *workspace;          /* device scratch, 256-byte aligned */
   size_t workspace_bytes;
@@ -527,6 +527,8 @@ int hapi_xent_backward(const hapi_head_desc *desc, const void *x, const void *we
 /* Distillation from a teacher's top logits: with q = softmax(teacher / T) over a
  * row's top entries and p = softmax(z / T) over all classes,
  *   loss = T^2 sum_k q_k (log q_k - log p[ids_k])   (the divergence KL(q | p))
+ * (held in float32, so off by some T^2 times the rounding of log sum exp(z / T): about
+ * 1e-6 T^2; the gradients are not)
  *   ids     [rows, top] int64: the classes of the teacher's logits, in any order.
  *           An id < 0 or a logit of -inf is no entry, whatever stands beside it; a
  *           row without entries does not count (as a negative target).  A class

@@ -182,6 +182,7 @@ constexpr int64_t kMaxRows = (int64_t)1 << 20;
 constexpr int64_t kMaxLd = (int64_t)1 << 20;     // a tile's rows lie within 2^31 bytes of its first
 constexpr int64_t kMaxClasses = (int64_t)1 << 24;
 constexpr int kMaxTop = 1024;
+constexpr float kMinTemperature = 0x1p-60f;  // T^2, 1 / T and the exponent's log2(e) / T stay normal numbers
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;  // of dz^T: one piece of the classes
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -266,8 +267,8 @@ int read_head(const hapi_head_desc *d, Head &h) {
   if (d->rows < 0) return fail(HAPI_E_INVAL, "rows must be >= 0");
   if (d->dim < 1 || d->classes < 1) return fail(HAPI_E_INVAL, "dim and classes must be >= 1");
   if (d->top < 0) return fail(HAPI_E_INVAL, "top must be >= 0");
-  if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !std::isfinite(1.0f / d->temperature))
-    return fail(HAPI_E_INVAL, "temperature must be finite and > 0");
+  if (!(d->temperature >= kMinTemperature && d->temperature <= 1.0f / kMinTemperature))
+    return fail(HAPI_E_INVAL, "temperature must be in [2^-60, 2^60]");
   if (d->top == 0 && d->temperature != 1.0f) return fail(HAPI_E_INVAL, "cross entropy has temperature 1");
   if ((d->x_stride != 0 && d->x_stride < d->dim) || (d->w_stride != 0 && d->w_stride < d->dim))
     return fail(HAPI_E_INVAL, "a row stride must be 0 or >= dim");

@@ -1,6 +1,6 @@
 """The trained tail at the edges of what its header allows: no rows with real
 addresses, entries without weight, counting rows that begin late, more tiles and rows
-than one launch takes."""
+than one launch takes, the ends of the temperatures."""
 import math
 
 import pytest
@@ -132,3 +132,15 @@ def test_norm_of_more_rows_than_a_launch_takes():
             assert torch.equal(t[r:r + some], t[:min(some, rows - r)]), r
     del x, y, mean, rstd, t
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("power", [-60, -8, 10, 60])
+def test_temperatures_at_the_ends_of_their_range(power, dtype):
+    c = _head_case(95, 40, 64, 300, dtype, top=3)
+    c["temp"] = 2.0 ** power
+    got = _head_run(c)
+    want = R.head(c["x"], c["w"], c["bias"], c["ids"], c["teacher"], c["temp"], c["dloss"])
+    for name, t in got.items():
+        R.check(name, t, want[name])
+        assert bool(torch.isfinite(t).all()), name
