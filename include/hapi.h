@@ -517,9 +517,13 @@ int hapi_xent_forward(const hapi_head_desc *desc, const void *x, const void *wei
 /* Gradients of sum(dloss * loss): with dz = dloss (softmax(z) - onehot(target)),
  *   dx = dz weight [rows, dim], dweight = dz^T x [classes, dim], in desc->dtype,
  *   dbias = sum over rows of dz, float32 [classes], or NULL (it must be without a bias).
- * loss and stats are the forward pass's.  Rows that do not count, and rows whose
- * dloss is 0, get dx = 0 and add nothing.  Between its two products dz is held
- * in desc->dtype (up to 32 rows, with what that rounding leaves).  rows = 0: dweight and dbias are zeros.  Errors as forward. */
+ * stats are the forward pass's; so is loss, which must be given but is not read.
+ * Rows that do not count, and rows without an error in their data whose dloss is 0,
+ * get dx = 0 and add nothing.  dweight and dbias of a class whose weights or bias are
+ * NaN or infinite (but for a bias of -inf) are NaN, even where no row counts.  Between
+ * its two products dz is held in desc->dtype (up to 32 rows, with what that rounding
+ * leaves).
+ * rows = 0: dweight and dbias are zeros.  Errors as forward. */
 int hapi_xent_backward(const hapi_head_desc *desc, const void *x, const void *weight, const float *bias,
                        const int64_t *targets, const float *loss, const float *stats, const float *dloss, void *dx,
                        void *dweight, float *dbias);

@@ -376,8 +376,8 @@ int head_forward(const hapi_head_desc *d, Head &h, const void *x, const void *w,
 }
 
 int head_backward(const hapi_head_desc *d, Head &h, const void *x, const void *w, const float *bias, const int64_t *ids,
-                  const float *teacher, const float *loss, const float *stats, const float *picked, const float *dloss,
-                  void *dx, void *dw, float *dbias) {
+                  const float *teacher, const float *stats, const float *picked, const float *dloss, void *dx, void *dw,
+                  float *dbias) {
   if (d->rows > 0) {
     TRY(check_ptr(stats, 8, "stats"));
     TRY(check_ptr(dloss, 4, "dloss"));
@@ -401,7 +401,6 @@ int head_backward(const hapi_head_desc *d, Head &h, const void *x, const void *w
   a.bias = bias;
   a.ids = ids;
   a.teacher = teacher;
-  a.loss = const_cast<float *>(loss);
   a.stats = reinterpret_cast<float2 *>(const_cast<float *>(stats));
   a.picked = const_cast<float *>(picked);
   a.dloss = dloss;
@@ -517,8 +516,8 @@ int hapi_xent_backward(const hapi_head_desc *desc, const void *x, const void *we
   TRY(read_head(desc, h));
   if (desc->top != 0) return fail(HAPI_E_INVAL, "cross entropy needs top = 0");
   TRY(check_head_inputs(desc, h, x, weight, bias, targets, "targets"));
-  if (desc->rows > 0) TRY(check_ptr(loss, 4, "loss"));
-  return head_backward(desc, h, x, weight, bias, targets, nullptr, loss, stats, nullptr, dloss, dx, dweight, dbias);
+  if (desc->rows > 0) TRY(check_ptr(loss, 4, "loss"));  // of the interface, not read
+  return head_backward(desc, h, x, weight, bias, targets, nullptr, stats, nullptr, dloss, dx, dweight, dbias);
 }
 
 int hapi_distill_forward(const hapi_head_desc *desc, const void *x, const void *weight, const float *bias,
@@ -545,7 +544,7 @@ int hapi_distill_backward(const hapi_head_desc *desc, const void *x, const void 
     TRY(check_ptr(teacher, 4, "teacher"));
     TRY(check_ptr(picked, 4, "picked"));
   }
-  return head_backward(desc, h, x, weight, bias, ids, teacher, nullptr, stats, picked, dloss, dx, dweight, dbias);
+  return head_backward(desc, h, x, weight, bias, ids, teacher, stats, picked, dloss, dx, dweight, dbias);
 }
 
 }  // extern "C"

@@ -144,3 +144,16 @@ def test_temperatures_at_the_ends_of_their_range(power, dtype):
     for name, t in got.items():
         R.check(name, t, want[name])
         assert bool(torch.isfinite(t).all()), name
+
+
+def test_backward_does_not_read_the_loss():
+    c = _head_case(97, 70, 64, 300, BF)
+    want = {k: v.clone() for k, v in _head_run(c).items()}
+    d = H.Head(H.HAPI_BF16, 70, 64, 300, stream=torch.cuda.current_stream())
+    need = H.hapi_head_workspace_bytes(d, True)
+    d.set(workspace=torch.empty(need, dtype=torch.uint8, device="cuda"), workspace_bytes=need)
+    dx, dw, db = (torch.empty_like(t) for t in (c["x"], c["w"], c["bias"]))
+    H.hapi_xent_backward(d, c["x"], c["w"], c["bias"], c["ids"], torch.full((70,), math.nan, device="cuda"), want["stats"],
+                         c["dloss"], dx, dw, db)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, want["dx"]) and torch.equal(dw, want["dw"]) and torch.equal(db, want["db"])
