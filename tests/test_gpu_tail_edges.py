@@ -8,7 +8,7 @@ import torch
 
 import paper_2210_08650_amd as H
 from tests import tail_reference as R
-from tests.test_gpu_tail import BF, CODE, F32, _gen, _head_case, _head_run
+from tests.test_gpu_tail import BF, CODE, F32, _gen, _head_case, _head_check, _head_run
 
 pytestmark = pytest.mark.gpu
 
@@ -157,3 +157,35 @@ def test_backward_does_not_read_the_loss():
                          c["dloss"], dx, dw, db)
     torch.cuda.synchronize()
     assert torch.equal(dx, want["dx"]) and torch.equal(dw, want["dw"]) and torch.equal(db, want["db"])
+
+
+@pytest.mark.parametrize("rows,dim,classes,top", [(2048, 72, 8192, 0), (2047, 100, 8190, 3), (4096, 1030, 4096, 0)])
+def test_float32_on_the_largest_tiles(rows, dim, classes, top):
+    """A whole round of 256 x 256 tiles, or nearly."""
+    c = _head_case(rows + dim, rows, dim, classes, F32, bias=True, top=top)
+    _head_check(c, _head_run(c))
+
+
+@pytest.mark.parametrize("rows,dim,classes,top", [(2, 16, 2100001, 0), (3, 24, 1100001, 3), (5, 66000, 70, 0),
+                                                  (40, 20000, 130, 2), (70001, 24, 11, 2)])
+def test_far_ends_of_the_sizes_in_float32(rows, dim, classes, top):
+    c = _head_case(rows + top, rows, dim, classes, F32, bias=True, top=top)
+    _head_check(c, _head_run(c))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,top", [(8, 0), (8, 3), (300, 0), (300, 3)])
+def test_a_bias_without_its_gradient(rows, top, dtype):
+    c = _head_case(98, rows, 64, 500, dtype, top=top)
+    want = {k: v.clone() for k, v in _head_run(c).items()}
+    d = H.Head(CODE[dtype], rows, 64, 500, top=top, temperature=c["temp"], stream=torch.cuda.current_stream())
+    need = H.hapi_head_workspace_bytes(d, True)
+    d.set(workspace=torch.empty(need, dtype=torch.uint8, device="cuda"), workspace_bytes=need)
+    dx, dw = torch.empty_like(c["x"]), torch.empty_like(c["w"])
+    if top:
+        H.hapi_distill_backward(d, c["x"], c["w"], c["bias"], c["ids"], c["teacher"], want["stats"], want["picked"],
+                                c["dloss"], dx, dw, None)
+    else:
+        H.hapi_xent_backward(d, c["x"], c["w"], c["bias"], c["ids"], want["loss"], want["stats"], c["dloss"], dx, dw, None)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, want["dx"]) and torch.equal(dw, want["dw"])
