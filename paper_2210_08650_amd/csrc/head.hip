@@ -33,7 +33,7 @@
 // Four products of 2 N D V operations in a step, one more than with the logits kept,
 // which would be 2 or 4 bytes a logit, written once and read twice.  Bound by the
 // matrix pipes: at 8192 x 2048 x 131072 they are busy 78% of the forward product's
-// time, 66% of dz's and 74% of the gradients' (their clock, under this load 1.6 to
+// time, 69% of dz's and 76% of the gradients' (their clock, under this load 1.6 to
 // 1.9 GHz, included in neither); the k-loop of a 256 x 256 tile takes 2.08k cycles a
 // k-tile, its MFMAs 2048.
 #include <algorithm>

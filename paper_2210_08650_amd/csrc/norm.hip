@@ -9,9 +9,10 @@
 // Statistics, sums and gradients are float32; y and dx are rounded once.
 //
 // Bound by memory: x read and y written, backward x and dy read and dx written.
-// 25,216 x 768 bf16: forward 14.4 us (5.4 TB/s; a copy of as many bytes 11.6), backward
-// with both launches 30.2 us (3.8 TB/s); 8191 x 1111 float32 backward, rows with no
-// alignment, 34.9 us (3.1 TB/s); 197 x 768 is one launch's 6 us.
+// 25,216 x 768 bf16: forward 14.8 us (5.2 TB/s; a copy of as many bytes 11.6), backward
+// with both launches 30.1 us (3.9 TB/s); 8191 x 1111 float32 backward, rows with no
+// alignment, 34.7 us (3.1 TB/s; 2.3 requests to the L2 for each 128 bytes, where aligned
+// bf16 rows have 1.4); 197 x 768 is one launch's 6 us.
 #include "tail.h"
 
 namespace hapi {

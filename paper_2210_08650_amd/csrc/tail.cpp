@@ -28,7 +28,8 @@ Variant head_variant(bool bf16, int64_t rows, int64_t classes) {
   double tb, tm, ts;
   if (bf16) {
     // 27.5, 19 and 10.3 us a round of 256, 512 and 768 workgroups at 768 features
-    // (4096 x 768 x 32000); the last round less when it holds one to a CU.
+    // (4096 x 768 x 32000); the last round less when it holds one to a CU.  The rule
+    // takes their ratios for every width.
     tb = 27.5 * (double)ceil_div(big, kCus);
     tm = 19.0 * (double)(mid / (2 * kCus)) + (mid % (2 * kCus) == 0 ? 0.0 : mid % (2 * kCus) <= kCus ? 12.0 : 19.0);
     const int64_t r = small % (3 * kCus);
@@ -183,7 +184,9 @@ constexpr int64_t kMaxLd = (int64_t)1 << 20;     // a tile's rows lie within 2^3
 constexpr int64_t kMaxClasses = (int64_t)1 << 24;
 constexpr int kMaxTop = 1024;
 constexpr float kMinTemperature = 0x1p-60f;  // T^2, 1 / T and the exponent's log2(e) / T stay normal numbers
-constexpr int64_t kPieceBytes = (int64_t)256 << 20;  // of dz^T: one piece of the classes
+// Of dz^T: one piece of the classes, or kHeadPiece classes where those are more (1 GiB at
+// 2^20 rows in float32).
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
