@@ -553,6 +553,99 @@ int hapi_distill_backward(const hapi_head_desc *desc, const void *x, const void 
                           const int64_t *ids, const float *teacher, const float *stats, const float *picked,
                           const float *dloss, void *dx, void *dweight, float *dbias);
 
+/* ---------------------------------------------------------------------------
+ * The trained block.  Between the extracted tokens and the classifier the compute
+ * tier may train a block of its own (an attentive probe, a decoder that attends to
+ * the image's tokens).  These are its operators: rotary positions with the heads'
+ * norm, cross attention, and the norm and clipping of the step's gradients.  What
+ * is said of the trained tail's operators holds for these. */
+
+/* Rotary positions on several axes, with the heads' RMS norm in the same pass.  For a
+ * vector x of head_dim values, one head of one token of q or of k:
+ *   h = x r gamma, r = 1 / sqrt(mean(x^2) + eps)   (norm = 1; else h = x)
+ *   y = h, but for each pair i of values (a, b): (a cos t - b sin t, b cos t + a sin t),
+ *       t = position[axis of i] freq[i]
+ * The first sections[0] pairs turn by the position on axis 0, the next sections[1] by
+ * that on axis 1, ...; P pairs in all.  Pair i is the values (i, P + i), or with
+ * neighbours = 1 (2 i, 2 i + 1); values from 2 P on are not rotated.  axes = 0 is the norm
+ * alone.  Angles are formed in float64 (off by |t| 2^-52 or so), the rest is float32. */
+typedef struct {
+  int32_t dtype;              /* hapi_dtype of q, k, their outputs and gradients */
+  int32_t head_dim;           /* 1 .. 256 */
+  int32_t heads, kv_heads;    /* of q and of k; 0: there is no q (no k), its pointers are NULL */
+  int32_t axes;               /* 0 .. 4 */
+  int32_t sections[4];        /* pairs of each axis, >= 1; 0 past the last axis; 2 P <= head_dim */
+  int32_t neighbours;         /* 0: pairs of the two halves, 1: of neighbours */
+  int32_t norm;               /* 0 or 1 */
+  int32_t reserved;           /* must be 0 */
+  float eps;                  /* >= 0 */
+  int64_t batch, length;      /* tokens; batch * length * (heads + kv_heads) < 2^31 */
+  /* Elements between batch entries, tokens and heads (the values of a head are
+   * consecutive); three zeros: contiguous [batch, length, heads, head_dim].  x: q and k, and
+   * dq and dk; out: q_out and k_out, and dq_out and dk_out.  Tensors that are written must
+   * not overlap themselves; those that are read may (a stride of 0). */
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
+  void *stream;               /* hipStream_t; NULL = the null stream */
+  void *workspace;            /* backward with a norm only: device scratch, 256-byte aligned */
+  size_t workspace_bytes;
+} hapi_rotary_desc;
+
+/* Bytes of workspace hapi_rotary_backward needs, or < 0 on error.  Host only. */
+int64_t hapi_rotary_workspace_bytes(const hapi_rotary_desc *desc);
+
+/*   q, k       [batch, length, heads or kv_heads, head_dim], element-aligned
+ *   q_gamma, k_gamma  [head_dim] float32, NULL without a norm (or without heads)
+ *   positions  [axes, batch, length] int64, contiguous; any values (past 2^31 the angle's
+ *              float64 rounding shows); NULL with axes = 0
+ *   freq       [P] float64: radians a step
+ *   lens       [batch] int64 or NULL: tokens from lens[b] on are padding: they are not
+ *              read (they may be NaN), and their outputs are 0
+ *   q_out, k_out  outputs; each may be q or k itself where their strides are the same
+ * Errors: HAPI_E_INVAL, HAPI_E_UNSUPPORTED, HAPI_E_DEVICE. */
+int hapi_rotary_forward(const hapi_rotary_desc *desc, const void *q, const void *k, const float *q_gamma, const float *k_gamma,
+                        const int64_t *positions, const double *freq, const int64_t *lens, void *q_out, void *k_out);
+
+/* dq, dk (of the strides of q and k; 0 for padding), and float32 [head_dim] dq_gamma and
+ * dk_gamma, sums over batch, tokens and heads (NULL without a norm; zeros of no tokens).
+ * q and k are the forward pass's inputs (not read without a norm).  dq may be dq_out
+ * itself where their strides are the same.  Errors as forward; HAPI_E_NOMEM. */
+int hapi_rotary_backward(const hapi_rotary_desc *desc, const void *dq_out, const void *dk_out, const void *q, const void *k,
+                         const float *q_gamma, const float *k_gamma, const int64_t *positions, const double *freq,
+                         const int64_t *lens, void *dq, void *dk, float *dq_gamma, float *dk_gamma);
+
+/* The global norm of many gradients, n = sqrt(sum over all tensors of g^2), and
+ * their clipping, g min(1, max_norm / n).  Squares and sums are float64. */
+typedef struct {
+  int32_t count;              /* tensors, 0 .. 2^20 */
+  int32_t reserved;           /* must be 0 */
+  const void *const *grads;   /* host [count]: device addresses, element-aligned, of
+                                 consecutive values; not read where sizes[i] = 0 */
+  void *const *out;           /* host [count], of hapi_gradient_clip: a tensor of its own, or
+                                 grads[i] itself; NULL: every one grads[i] itself */
+  const int64_t *sizes;       /* host [count]: values, 0 .. 2^38 */
+  const int32_t *dtypes;      /* host [count]: hapi_dtype */
+  float max_norm;             /* finite, > 0; hapi_gradient_norm does not use it */
+  void *stream;               /* hipStream_t; NULL = the null stream */
+  void *workspace;            /* device scratch, 256-byte aligned */
+  size_t workspace_bytes;
+} hapi_gradient_desc;
+
+/* Bytes of workspace of either call, or < 0 on error.  Host only. */
+int64_t hapi_gradient_workspace_bytes(const hapi_gradient_desc *desc);
+
+/* norm [1] float32 (inf where n is past float32's range).  The host arrays are read
+ * before the call returns.  No tensors: 0.
+ * Errors: HAPI_E_INVAL, HAPI_E_UNSUPPORTED, HAPI_E_NOMEM, HAPI_E_DEVICE. */
+int hapi_gradient_norm(const hapi_gradient_desc *desc, float *norm);
+
+/* The norm, and out = g min(1, max_norm / n), formed in 64 bits and rounded through
+ * float32 to the tensor's type.  Where n <= max_norm every g keeps its bits.  So it
+ * does where n is not a finite number (a gradient holds a NaN or an infinity): norm
+ * tells, and the caller leaves the step out.  Tensors that are written must not
+ * overlap each other or other tensors that are read (HAPI_E_INVAL), so none may be
+ * listed twice.  Errors: as hapi_gradient_norm. */
+int hapi_gradient_clip(const hapi_gradient_desc *desc, float *norm);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *hapi_last_error(void);
 

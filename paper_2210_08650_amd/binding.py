@@ -33,7 +33,9 @@ __all__ = ["HapiError", "Desc", "hapi_layer", "hapi_model_desc", "hapi_kernel_st
            "hapi_extract_noalloc", "HAPI_NOALLOC_SCRATCH_BYTES", "hapi_profile_layers", "hapi_profile_memory",
            "hapi_stats_enable", "hapi_stats_collect", "hapi_last_error", "hapi_split_job", "hapi_split_estimate", "hapi_split_choice", "hapi_choose_split",
            "Norm", "Head", "hapi_norm_desc", "hapi_head_desc", "hapi_layernorm_workspace_bytes", "hapi_layernorm_forward", "hapi_layernorm_backward",
-           "hapi_head_workspace_bytes", "hapi_xent_forward", "hapi_xent_backward", "hapi_distill_forward", "hapi_distill_backward"]
+           "hapi_head_workspace_bytes", "hapi_xent_forward", "hapi_xent_backward", "hapi_distill_forward", "hapi_distill_backward",
+           "Gradients", "hapi_gradient_desc", "hapi_gradient_workspace_bytes", "hapi_gradient_norm", "hapi_gradient_clip",
+           "Rotary", "hapi_rotary_desc", "hapi_rotary_workspace_bytes", "hapi_rotary_forward", "hapi_rotary_backward"]
 
 _STATUS = {HAPI_E_INVAL: "HAPI_E_INVAL", HAPI_E_UNSUPPORTED: "HAPI_E_UNSUPPORTED",
            HAPI_E_NOMEM: "HAPI_E_NOMEM", HAPI_E_DEVICE: "HAPI_E_DEVICE"}
@@ -116,6 +118,25 @@ class hapi_head_desc(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class hapi_gradient_desc(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("grads", ctypes.POINTER(ctypes.c_void_p)), ("out", ctypes.POINTER(ctypes.c_void_p)),
+                ("sizes", ctypes.POINTER(ctypes.c_int64)), ("dtypes", ctypes.POINTER(ctypes.c_int32)),
+                ("max_norm", ctypes.c_float), ("stream", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class hapi_rotary_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4),
+                ("neighbours", ctypes.c_int32), ("norm", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("batch", ctypes.c_int64), ("length", ctypes.c_int64),
+                ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
+                ("q_out_stride", ctypes.c_int64 * 3), ("k_out_stride", ctypes.c_int64 * 3),
+                ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 def _hip_runtimes():
     try:
         with open("/proc/self/maps") as f:
@@ -169,6 +190,15 @@ def _load():
         "hapi_distill_forward": (ctypes.c_int, [T] + [vp] * 8),
         "hapi_distill_backward": (ctypes.c_int, [T] + [vp] * 11),
     })
+    G, R = ctypes.POINTER(hapi_gradient_desc), ctypes.POINTER(hapi_rotary_desc)
+    sig.update({
+        "hapi_gradient_workspace_bytes": (i64, [G]),
+        "hapi_gradient_norm": (ctypes.c_int, [G, vp]),
+        "hapi_gradient_clip": (ctypes.c_int, [G, vp]),
+        "hapi_rotary_workspace_bytes": (i64, [R]),
+        "hapi_rotary_forward": (ctypes.c_int, [R] + [vp] * 9),
+        "hapi_rotary_backward": (ctypes.c_int, [R] + [vp] * 13),
+    })
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
         f.restype, f.argtypes = res, args
@@ -181,7 +211,9 @@ EXPORTED = ("hapi_raw_weight_count", "hapi_packed_weight_bytes", "hapi_pack_weig
             "hapi_workspace_guards", "hapi_extract_range", "hapi_extract_noalloc", "hapi_profile_layers", "hapi_profile_memory",
             "hapi_stats_enable", "hapi_stats_collect", "hapi_last_error", "hapi_choose_split",
             "hapi_layernorm_workspace_bytes", "hapi_layernorm_forward", "hapi_layernorm_backward", "hapi_head_workspace_bytes",
-            "hapi_xent_forward", "hapi_xent_backward", "hapi_distill_forward", "hapi_distill_backward")
+            "hapi_xent_forward", "hapi_xent_backward", "hapi_distill_forward", "hapi_distill_backward",
+            "hapi_gradient_workspace_bytes", "hapi_gradient_norm", "hapi_gradient_clip",
+            "hapi_rotary_workspace_bytes", "hapi_rotary_forward", "hapi_rotary_backward")
 
 
 def _ptr(p):
@@ -538,3 +570,164 @@ def hapi_distill_backward(desc: Head, x, weight, bias, ids, teacher, stats, pick
         _tensor(dev, teacher, "teacher", _F32, (n, k)), _tensor(dev, stats, "stats", _F32, (n, 2)),
         _tensor(dev, picked, "picked", _F32, (n, k)), _tensor(dev, dloss, "dloss", _F32, (n,)),
         *_head_gradients(c, dev, dx, dweight, dbias)))
+
+
+# ----------------------------------------------------------- the trained block
+
+_CODES = {torch.float32: HAPI_F32, torch.bfloat16: HAPI_BF16}
+
+
+class Gradients(_TailDesc):
+    """Owns a ``hapi_gradient_desc`` of tensors whose values are consecutive in memory
+    (in any order of their dimensions).  The addresses are read here: after a
+    gradient was allocated anew, a new descriptor is needed.  ``out``: the clipped
+    gradients, tensors of the same types and sizes; None: in place."""
+    _struct = hapi_gradient_desc
+
+    def __init__(self, tensors, max_norm=1.0, out=None, **kw):
+        super().__init__(**kw)
+        self.tensors = list(tensors)
+        self.out = None if out is None else list(out)
+        n = len(self.tensors)
+        if self.out is not None and len(self.out) != n:
+            raise HapiError(HAPI_E_INVAL, f"{len(self.out)} outputs for {n} gradients")
+        for i, t in enumerate(self.tensors + (self.out or [])):
+            name = f"grads[{i}]" if i < n else f"out[{i - n}]"
+            if t.dtype not in _CODES:
+                raise HapiError(HAPI_E_INVAL, f"{name} must be float32 or bfloat16, got {t.dtype}")
+            if not _dense(t):
+                raise HapiError(HAPI_E_INVAL, f"{name} must hold consecutive values, got strides {tuple(t.stride())}")
+            if i >= n:
+                g = self.tensors[i - n]
+                if t.dtype is not g.dtype or t.shape != g.shape or (t.stride() != g.stride() and not (t.is_contiguous() and g.is_contiguous())):
+                    raise HapiError(HAPI_E_INVAL, f"{name} must be {g.dtype} of shape {tuple(g.shape)} and lie as its gradient")
+        self._grads = (ctypes.c_void_p * max(n, 1))(*[t.data_ptr() for t in self.tensors])
+        self._sizes = (ctypes.c_int64 * max(n, 1))(*[t.numel() for t in self.tensors])
+        self._dtypes = (ctypes.c_int32 * max(n, 1))(*[_CODES[t.dtype] for t in self.tensors])
+        c = self.c
+        c.count, c.max_norm = n, float(max_norm)
+        c.grads = ctypes.cast(self._grads, ctypes.POINTER(ctypes.c_void_p))
+        c.sizes = ctypes.cast(self._sizes, ctypes.POINTER(ctypes.c_int64))
+        c.dtypes = ctypes.cast(self._dtypes, ctypes.POINTER(ctypes.c_int32))
+        if self.out is not None:
+            self._out = (ctypes.c_void_p * max(n, 1))(*[t.data_ptr() for t in self.out])
+            c.out = ctypes.cast(self._out, ctypes.POINTER(ctypes.c_void_p))
+        self._devices = {t.get_device() for t in self.tensors + (self.out or []) if t.numel()}
+
+
+def _dense(t):
+    """Whether t's values are consecutive in memory, in some order of its dimensions."""
+    step = 1
+    for size, stride in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda x: x[1]):
+        if stride != step and t.numel():
+            return False
+        step *= size
+    return True
+
+
+def _on_current(dev, desc):
+    if any(d != dev for d in desc._devices):
+        raise HapiError(HAPI_E_INVAL, "a gradient is not on the current GPU")
+
+
+def hapi_gradient_workspace_bytes(desc: Gradients) -> int:
+    return _check(_lib.hapi_gradient_workspace_bytes(desc.ref))
+
+
+def hapi_gradient_norm(desc: Gradients, norm) -> None:
+    dev = _device()
+    _on_current(dev, desc)
+    _check(_lib.hapi_gradient_norm(desc.ref, _tensor(dev, norm, "norm", _F32, (1,))))
+
+
+def hapi_gradient_clip(desc: Gradients, norm) -> None:
+    dev = _device()
+    _on_current(dev, desc)
+    _check(_lib.hapi_gradient_clip(desc.ref, _tensor(dev, norm, "norm", _F32, (1,))))
+
+
+def _strides(field, given):
+    if given:
+        if len(given) != 3:
+            raise ValueError(f"three strides (batch, token, head), got {tuple(given)}")
+        field[:] = [int(x) for x in given]
+
+
+def _contiguous(length, heads, dim):
+    return (length * heads * dim, heads * dim, dim)
+
+
+def _heads(dev, p, name, dtype, shape, field):
+    """The address of a [batch, tokens, heads, head_dim] argument; of a tensor the
+    type, sizes, strides and device have to be the descriptor's and the current ones."""
+    if p is None or type(p) is int:
+        return p
+    if not hasattr(p, "data_ptr"):
+        return _ptr(p)
+    if p.dtype is not dtype or p.shape != shape:
+        raise HapiError(HAPI_E_INVAL, f"{name} must be {dtype} of shape {shape}, got {p.dtype} {tuple(p.shape)}")
+    want = tuple(field) if any(field) else _contiguous(*shape[1:])
+    if p.numel() and any(n > 1 and a != b for n, a, b in zip(shape, p.stride(), want + (1,))):
+        raise HapiError(HAPI_E_INVAL, f"{name} must have strides {want + (1,)}, got {tuple(p.stride())}")
+    if p.get_device() != dev:
+        raise HapiError(HAPI_E_INVAL, f"{name} is on {p.device}, not on the current GPU")
+    return p.data_ptr()
+
+
+def _flat(dev, p, name, dtype, shape):
+    """The address of an argument that must be contiguous."""
+    if hasattr(p, "is_contiguous") and not p.is_contiguous():
+        raise HapiError(HAPI_E_INVAL, f"{name} must be contiguous, got strides {tuple(p.stride())}")
+    return _tensor(dev, p, name, dtype, shape)
+
+
+class Rotary(_TailDesc):
+    """Owns a ``hapi_rotary_desc``.  ``sections``: the pairs of each axis.  Strides are
+    (batch, token, head), in elements; empty: contiguous."""
+    _struct = hapi_rotary_desc
+
+    def __init__(self, dtype, batch, length, heads, kv_heads, head_dim, sections=(), neighbours=False, norm=True, eps=1e-6,
+                 q_stride=(), k_stride=(), q_out_stride=(), k_out_stride=(), **kw):
+        super().__init__(**kw)
+        c = self.c
+        c.dtype, c.batch, c.length, c.heads, c.kv_heads = dtype, int(batch), int(length), int(heads), int(kv_heads)
+        c.head_dim, c.axes, c.neighbours, c.norm, c.eps = int(head_dim), len(sections), int(neighbours), int(norm), float(eps)
+        if len(sections) > 4:
+            raise HapiError(HAPI_E_INVAL, f"at most 4 axes, got {len(sections)}")
+        for i, n in enumerate(sections):
+            c.sections[i] = int(n)
+        _strides(c.q_stride, q_stride)
+        _strides(c.k_stride, k_stride)
+        _strides(c.q_out_stride, q_out_stride)
+        _strides(c.k_out_stride, k_out_stride)
+
+
+def hapi_rotary_workspace_bytes(desc: Rotary) -> int:
+    return _check(_lib.hapi_rotary_workspace_bytes(desc.ref))
+
+
+def _rotary_common(c, dev, q_gamma, k_gamma, positions, freq, lens):
+    return (_tensor(dev, q_gamma, "q_gamma", _F32, (c.head_dim,)), _tensor(dev, k_gamma, "k_gamma", _F32, (c.head_dim,)),
+            _flat(dev, positions, "positions", torch.int64, (c.axes, c.batch, c.length)),
+            _flat(dev, freq, "freq", torch.float64, (sum(c.sections),)), _flat(dev, lens, "lens", torch.int64, (c.batch,)))
+
+
+def hapi_rotary_forward(desc: Rotary, q, k, q_gamma, k_gamma, positions, freq, lens, q_out, k_out) -> None:
+    c, dev = desc.c, _device()
+    t, qs, ks = _TORCH_TYPES.get(c.dtype), (c.batch, c.length, c.heads, c.head_dim), (c.batch, c.length, c.kv_heads, c.head_dim)
+    _check(_lib.hapi_rotary_forward(
+        desc.ref, _heads(dev, q, "q", t, qs, c.q_stride), _heads(dev, k, "k", t, ks, c.k_stride),
+        *_rotary_common(c, dev, q_gamma, k_gamma, positions, freq, lens),
+        _heads(dev, q_out, "q_out", t, qs, c.q_out_stride), _heads(dev, k_out, "k_out", t, ks, c.k_out_stride)))
+
+
+def hapi_rotary_backward(desc: Rotary, dq_out, dk_out, q, k, q_gamma, k_gamma, positions, freq, lens, dq, dk, dq_gamma,
+                         dk_gamma) -> None:
+    c, dev = desc.c, _device()
+    t, qs, ks = _TORCH_TYPES.get(c.dtype), (c.batch, c.length, c.heads, c.head_dim), (c.batch, c.length, c.kv_heads, c.head_dim)
+    _check(_lib.hapi_rotary_backward(
+        desc.ref, _heads(dev, dq_out, "dq_out", t, qs, c.q_out_stride), _heads(dev, dk_out, "dk_out", t, ks, c.k_out_stride),
+        _heads(dev, q, "q", t, qs, c.q_stride), _heads(dev, k, "k", t, ks, c.k_stride),
+        *_rotary_common(c, dev, q_gamma, k_gamma, positions, freq, lens),
+        _heads(dev, dq, "dq", t, qs, c.q_stride), _heads(dev, dk, "dk", t, ks, c.k_stride),
+        _tensor(dev, dq_gamma, "dq_gamma", _F32, (c.head_dim,)), _tensor(dev, dk_gamma, "dk_gamma", _F32, (c.head_dim,))))

@@ -1,0 +1,363 @@
+// Entry points of the trained block: argument checks, workspace layout and the
+// launches of the gradients' norm and clipping, of the rotary positions and of the
+// cross attention.  Declared in hapi.h.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "block.h"
+#include "host_checks.h"
+
+namespace hapi {
+namespace {
+
+// ----------------------------------------------------------------- gradients
+
+constexpr int kMaxTensors = 1 << 20;
+constexpr int64_t kMaxTensorSize = (int64_t)1 << 38;  // a launch's segments are a 32-bit number
+
+int check_gradients(const hapi_gradient_desc *d) {
+  if (!d) return fail(HAPI_E_INVAL, "desc is NULL");
+  if (d->reserved) return fail(HAPI_E_INVAL, "reserved must be 0");
+  if (d->count < 0) return fail(HAPI_E_INVAL, "count must be >= 0");
+  if (d->count > kMaxTensors) return fail(HAPI_E_UNSUPPORTED, "%d tensors (at most 2^20)", d->count);
+  if (!(d->max_norm > 0.0f) || !std::isfinite(d->max_norm)) return fail(HAPI_E_INVAL, "max_norm must be finite and > 0");
+  if (d->count == 0) return HAPI_OK;
+  if (!d->grads || !d->sizes || !d->dtypes) return fail(HAPI_E_INVAL, "grads, sizes or dtypes is NULL");
+  for (int i = 0; i < d->count; ++i) {
+    if (d->dtypes[i] != HAPI_F32 && d->dtypes[i] != HAPI_BF16) return fail(HAPI_E_INVAL, "unknown dtype %d of tensor %d", d->dtypes[i], i);
+    if (d->sizes[i] < 0) return fail(HAPI_E_INVAL, "size of tensor %d must be >= 0", i);
+    if (d->sizes[i] > kMaxTensorSize) return fail(HAPI_E_UNSUPPORTED, "tensor %d has more than 2^38 values", i);
+    if (d->sizes[i] == 0) continue;
+    const uintptr_t align = d->dtypes[i] == HAPI_BF16 ? 2 : 4;
+    if (!d->grads[i]) return fail(HAPI_E_INVAL, "grads[%d] is NULL", i);
+    if ((uintptr_t)d->grads[i] % align) return fail(HAPI_E_INVAL, "grads[%d] must be %d-byte aligned", i, (int)align);
+    if (d->out && !d->out[i]) return fail(HAPI_E_INVAL, "out[%d] is NULL", i);
+    if (d->out && (uintptr_t)d->out[i] % align) return fail(HAPI_E_INVAL, "out[%d] must be %d-byte aligned", i, (int)align);
+  }
+  return HAPI_OK;
+}
+
+struct Range {
+  uintptr_t lo, hi;
+};
+
+// No value is written twice, or read after it was written as another tensor's: a
+// tensor listed twice would be scaled twice, and by blocks that race.
+int check_outputs_apart(const hapi_gradient_desc *d) {
+  std::vector<Range> out;
+  out.reserve(d->count);
+  auto range = [&](const void *p, int i) {
+    const uintptr_t lo = (uintptr_t)p;
+    return Range{lo, lo + (uintptr_t)d->sizes[i] * (d->dtypes[i] == HAPI_BF16 ? 2 : 4)};
+  };
+  for (int i = 0; i < d->count; ++i)
+    if (d->sizes[i] > 0) out.push_back(range(d->out ? d->out[i] : d->grads[i], i));
+  const auto below = [](const Range &a, const Range &b) { return a.lo < b.lo; };
+  if (!std::is_sorted(out.begin(), out.end(), below)) std::sort(out.begin(), out.end(), below);
+  for (size_t i = 1; i < out.size(); ++i)
+    if (out[i].lo < out[i - 1].hi) return fail(HAPI_E_INVAL, "two of the tensors that are written overlap");
+  for (int i = 0; d->out && i < d->count; ++i) {
+    if (d->sizes[i] == 0 || d->out[i] == d->grads[i]) continue;
+    const Range g = range(d->grads[i], i);
+    auto next = std::upper_bound(out.begin(), out.end(), g, below);  // the first that starts behind g's start
+    if ((next != out.end() && next->lo < g.hi) || (next != out.begin() && (next - 1)->hi > g.lo))
+      return fail(HAPI_E_INVAL, "grads[%d] overlaps a tensor that is written", i);
+  }
+  return HAPI_OK;
+}
+
+int64_t gradient_workspace(const hapi_gradient_desc *d) {
+  const int64_t launches = std::max<int64_t>(1, ceil_div(d->count, kGradTensors));
+  return up((launches + 1) * kGradBlocks * (int64_t)sizeof(double), kAlign);
+}
+
+// The next launch's tensors from i on (those without values left out); its blocks, 0: none.
+int next_gradients(const hapi_gradient_desc *d, int &i, GradArgs &a) {
+  a.count = 0;
+  for (uint32_t &f : a.f32) f = 0;
+  int64_t total = 0;
+  for (; i < d->count && a.count < kGradTensors; ++i) {
+    if (d->sizes[i] == 0) continue;
+    a.in[a.count] = d->grads[i];
+    a.out[a.count] = d->out ? d->out[i] : const_cast<void *>(d->grads[i]);
+    a.size[a.count] = d->sizes[i];
+    if (d->dtypes[i] == HAPI_F32) a.f32[a.count >> 5] |= 1u << (a.count & 31);
+    total += d->sizes[i];
+    ++a.count;
+  }
+  // Segments that fill the blocks, of 2048 to 32,768 values: a block's first loads
+  // wait for its search of the tensor.
+  a.seg_size = 32768;
+  while (a.seg_size > 2048 && total / a.seg_size < 2 * kGradBlocks) a.seg_size /= 2;
+  int64_t seg = 0;
+  for (int t = 0; t < a.count; ++t) {
+    a.seg[t] = (int32_t)seg;
+    seg += ceil_div(a.size[t], a.seg_size);
+  }
+  a.seg[a.count] = (int32_t)seg;
+  return (int)std::min<int64_t>(seg, kGradBlocks);
+}
+
+int run_gradients(const hapi_gradient_desc *d, float *norm, bool clip) {
+  TRY(check_gradients(d));
+  TRY(check_ptr(norm, 4, "norm"));
+  if (clip) TRY(check_outputs_apart(d));
+  TRY(check_workspace(d->workspace, d->workspace_bytes, gradient_workspace(d)));
+  TRY(check_stream(d->stream));
+  hipStream_t s = static_cast<hipStream_t>(d->stream);
+  double *part = static_cast<double *>(d->workspace);
+  GradArgs a;
+  a.max_norm = d->max_norm;
+  int64_t parts = 0;
+  int launches = 0;
+  for (int i = 0; i < d->count;) {
+    const int blocks = next_gradients(d, i, a);
+    if (blocks == 0) break;
+    a.part = part + parts;
+    a.parts = 0;
+    a.norm = nullptr;
+    HIP_TRY(launch_grad_squares(a, blocks, s));
+    parts += blocks;
+    ++launches;
+  }
+  if (launches > kGradSumLaunches) {
+    double *joined = part + (int64_t)ceil_div(d->count, kGradTensors) * kGradBlocks;
+    HIP_TRY(launch_grad_join(part, parts, joined, s));
+    part = joined;
+    parts = std::min<int64_t>(parts, kGradBlocks);
+  }
+  if (!clip || launches == 0) {
+    HIP_TRY(launch_grad_norm(part, parts, norm, s));
+    return HAPI_OK;
+  }
+  for (int i = 0; i < d->count;) {
+    const int blocks = next_gradients(d, i, a);
+    if (blocks == 0) break;
+    a.part = part;
+    a.parts = parts;
+    a.norm = norm;
+    norm = nullptr;
+    HIP_TRY(launch_grad_clip(a, blocks, s));
+  }
+  return HAPI_OK;
+}
+
+// ------------------------------------------------------------------- layouts
+
+constexpr int64_t kMaxExtent = (int64_t)1 << 31;
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
+
+// Elements between batch entries, tokens and heads; three zeros: [batch, tokens, heads, dim].
+int read_strides(const int64_t *in, int64_t tokens, int64_t heads, int64_t dim, const char *name, int64_t *out) {
+  if (in[0] == 0 && in[1] == 0 && in[2] == 0) {
+    out[2] = dim;
+    out[1] = heads * dim;
+    out[0] = tokens * out[1];
+    return HAPI_OK;
+  }
+  for (int i = 0; i < 3; ++i) {
+    if (in[i] < 0) return fail(HAPI_E_INVAL, "strides of %s must be >= 0", name);
+    if (in[i] > kMaxStride) return fail(HAPI_E_UNSUPPORTED, "strides of %s must be <= 2^40", name);
+    out[i] = in[i];
+  }
+  return HAPI_OK;
+}
+
+// Whether no two values of a tensor share a place, as one that is written must.
+int check_apart(const int64_t *stride, int64_t batch, int64_t tokens, int64_t heads, int64_t dim, const char *name) {
+  struct {
+    int64_t stride, extent;
+  } d[3] = {{stride[0], batch}, {stride[1], tokens}, {stride[2], heads}};
+  std::sort(d, d + 3, [](const auto &a, const auto &b) { return a.stride < b.stride; });
+  if (batch == 0 || tokens == 0 || heads == 0) return HAPI_OK;
+  __int128 span = dim;
+  for (const auto &x : d) {
+    if (x.extent == 1) continue;
+    if (x.stride < span) return fail(HAPI_E_INVAL, "strides of %s let its values overlap", name);
+    span += (__int128)x.stride * (x.extent - 1);
+  }
+  return HAPI_OK;
+}
+
+// -------------------------------------------------------------------- rotary
+
+struct Rotary {
+  bool bf16;
+  int esz, v;
+  RotaryArgs a;
+  int64_t batch;
+};
+
+int read_rotary(const hapi_rotary_desc *d, Rotary &r) {
+  if (!d) return fail(HAPI_E_INVAL, "desc is NULL");
+  if (d->dtype != HAPI_F32 && d->dtype != HAPI_BF16) return fail(HAPI_E_INVAL, "unknown dtype %d", d->dtype);
+  if (d->reserved) return fail(HAPI_E_INVAL, "reserved must be 0");
+  if (d->head_dim < 1) return fail(HAPI_E_INVAL, "head_dim must be >= 1");
+  if (d->head_dim > kRotaryMaxDim) return fail(HAPI_E_UNSUPPORTED, "head_dim %d (at most %d)", d->head_dim, kRotaryMaxDim);
+  if (d->heads < 0 || d->kv_heads < 0 || d->heads + (int64_t)d->kv_heads < 1)
+    return fail(HAPI_E_INVAL, "heads and kv_heads must be >= 0, one of them >= 1");
+  if (d->batch < 0 || d->length < 0) return fail(HAPI_E_INVAL, "batch and length must be >= 0");
+  if (d->axes < 0 || d->axes > kRotaryAxes) return fail(HAPI_E_INVAL, "axes must be in [0, %d]", kRotaryAxes);
+  if (d->neighbours != 0 && d->neighbours != 1) return fail(HAPI_E_INVAL, "neighbours must be 0 or 1");
+  if (d->norm != 0 && d->norm != 1) return fail(HAPI_E_INVAL, "norm must be 0 or 1");
+  if (!(d->eps >= 0.0f) || !std::isfinite(d->eps)) return fail(HAPI_E_INVAL, "eps must be finite and >= 0");
+  r = Rotary{};
+  RotaryArgs &a = r.a;
+  int64_t pairs = 0;
+  for (int i = 0; i < kRotaryAxes; ++i) {
+    if (i >= d->axes ? d->sections[i] != 0 : d->sections[i] < 1)
+      return fail(HAPI_E_INVAL, "sections must be >= 1 on each axis, and 0 past the last one");
+    a.first[i] = (int32_t)std::min<int64_t>(pairs, kRotaryMaxDim);
+    pairs += d->sections[i];
+  }
+  if (2 * pairs > d->head_dim) return fail(HAPI_E_INVAL, "the sections' %lld pairs exceed head_dim", (long long)pairs);
+  if (d->batch >= kMaxExtent || d->length >= kMaxExtent || d->heads >= 1 << 20 || d->kv_heads >= 1 << 20 ||
+      (__int128)d->batch * d->length * (d->heads + d->kv_heads) >= kMaxExtent)
+    return fail(HAPI_E_UNSUPPORTED, "batch * length * (heads + kv_heads) must be below 2^31");
+  r.bf16 = d->dtype == HAPI_BF16;
+  r.esz = r.bf16 ? 2 : 4;
+  r.batch = d->batch;
+  a.heads[0] = d->heads;
+  a.heads[1] = d->kv_heads;
+  a.tokens = d->batch * d->length;
+  a.len = (int32_t)d->length;
+  a.dim = d->head_dim;
+  a.pairs = (int32_t)pairs;
+  a.axes = d->axes;
+  a.eps = d->eps;
+  a.inv_dim = 1.0f / (float)d->head_dim;
+  a.norm = d->norm;
+  a.neighbours = d->neighbours;
+  TRY(read_strides(d->q_stride, d->length, d->heads, d->head_dim, "q", a.x_st[0]));
+  TRY(read_strides(d->k_stride, d->length, d->kv_heads, d->head_dim, "k", a.x_st[1]));
+  TRY(read_strides(d->q_out_stride, d->length, d->heads, d->head_dim, "q_out", a.y_st[0]));
+  TRY(read_strides(d->k_out_stride, d->length, d->kv_heads, d->head_dim, "k_out", a.y_st[1]));
+  // as many values at once as the pairs and what is not rotated divide into
+  r.v = r.bf16 ? 8 : 4;
+  while (r.v > 1 && (pairs % r.v != 0 || (d->head_dim - 2 * pairs) % (2 * r.v) != 0)) r.v /= 2;
+  // Up to 8 heads a lane, so that it forms sines and cosines once for them, as long as
+  // the CUs' 2048 lanes each are filled.
+  int lanes = 4;
+  while (lanes < 64 && lanes * 2 * r.v < d->head_dim) lanes *= 2;
+  const int64_t heads = (int64_t)d->heads + d->kv_heads;
+  const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, a.tokens * heads * lanes / (kCus * 2048)));
+  a.head_groups = (int32_t)ceil_div(heads, each);
+  return HAPI_OK;
+}
+
+int64_t rotary_workspace(const Rotary &r) { return r.a.norm ? up((int64_t)kRotaryParts * 2 * r.a.dim * 4, kAlign) : 0; }
+
+// The inputs that both directions read, and the gammas.
+int check_rotary_inputs(const hapi_rotary_desc *d, Rotary &r, const float *q_gamma, const float *k_gamma,
+                        const int64_t *positions, const double *freq, const int64_t *lens) {
+  const float *gamma[2] = {q_gamma, k_gamma};
+  static const char *const names[2] = {"q_gamma", "k_gamma"};
+  for (int w = 0; w < 2; ++w) {
+    if (r.a.norm && r.a.heads[w] > 0) TRY(check_ptr(gamma[w], 4, names[w]));
+    else if (gamma[w]) return fail(HAPI_E_INVAL, "%s is given, and not used", names[w]);
+    r.a.gamma[w] = gamma[w];
+  }
+  if (d->axes > 0) {
+    TRY(check_ptr(freq, 8, "freq"));
+    if (r.a.tokens > 0) TRY(check_ptr(positions, 8, "positions"));
+  }
+  if (lens && (uintptr_t)lens % 8) return fail(HAPI_E_INVAL, "lens must be 8-byte aligned");
+  r.a.positions = positions;
+  r.a.freq = freq;
+  r.a.lens = lens;
+  return HAPI_OK;
+}
+
+// Tensors of q and k, which must be there where there are heads of them.
+int check_both(const Rotary &r, const void *q, const void *k, const char *q_name, const char *k_name) {
+  if (r.a.heads[0] > 0) TRY(check_ptr(q, r.esz, q_name));
+  else if (q) return fail(HAPI_E_INVAL, "%s without heads", q_name);
+  if (r.a.heads[1] > 0) TRY(check_ptr(k, r.esz, k_name));
+  else if (k) return fail(HAPI_E_INVAL, "%s without kv_heads", k_name);
+  return HAPI_OK;
+}
+
+}  // namespace
+}  // namespace hapi
+
+using namespace hapi;
+
+extern "C" {
+
+int64_t hapi_gradient_workspace_bytes(const hapi_gradient_desc *desc) {
+  TRY(check_gradients(desc));
+  return gradient_workspace(desc);
+}
+
+int hapi_gradient_norm(const hapi_gradient_desc *desc, float *norm) { return run_gradients(desc, norm, false); }
+
+int hapi_gradient_clip(const hapi_gradient_desc *desc, float *norm) {
+  try {
+    return run_gradients(desc, norm, true);
+  } catch (const std::bad_alloc &) {
+    return fail(HAPI_E_NOMEM, "no host memory to compare the tensors' addresses");
+  }
+}
+
+int64_t hapi_rotary_workspace_bytes(const hapi_rotary_desc *desc) {
+  Rotary r;
+  TRY(read_rotary(desc, r));
+  return rotary_workspace(r);
+}
+
+int hapi_rotary_forward(const hapi_rotary_desc *desc, const void *q, const void *k, const float *q_gamma, const float *k_gamma,
+                        const int64_t *positions, const double *freq, const int64_t *lens, void *q_out, void *k_out) {
+  Rotary r;
+  TRY(read_rotary(desc, r));
+  TRY(check_rotary_inputs(desc, r, q_gamma, k_gamma, positions, freq, lens));
+  if (r.a.tokens == 0) return HAPI_OK;
+  TRY(check_both(r, q, k, "q", "k"));
+  TRY(check_both(r, q_out, k_out, "q_out", "k_out"));
+  TRY(check_apart(r.a.y_st[0], r.batch, r.a.len, r.a.heads[0], r.a.dim, "q_out"));
+  TRY(check_apart(r.a.y_st[1], r.batch, r.a.len, r.a.heads[1], r.a.dim, "k_out"));
+  TRY(check_stream(desc->stream));
+  r.a.x[0] = q;
+  r.a.x[1] = k;
+  r.a.y[0] = q_out;
+  r.a.y[1] = k_out;
+  HIP_TRY(launch_rotary_forward(r.bf16, r.v, r.a, static_cast<hipStream_t>(desc->stream)));
+  return HAPI_OK;
+}
+
+int hapi_rotary_backward(const hapi_rotary_desc *desc, const void *dq_out, const void *dk_out, const void *q, const void *k,
+                         const float *q_gamma, const float *k_gamma, const int64_t *positions, const double *freq,
+                         const int64_t *lens, void *dq, void *dk, float *dq_gamma, float *dk_gamma) {
+  Rotary r;
+  TRY(read_rotary(desc, r));
+  TRY(check_rotary_inputs(desc, r, q_gamma, k_gamma, positions, freq, lens));
+  if (r.a.tokens > 0) {
+    TRY(check_both(r, dq_out, dk_out, "dq_out", "dk_out"));
+    TRY(check_both(r, dq, dk, "dq", "dk"));
+    if (r.a.norm) TRY(check_both(r, q, k, "q", "k"));
+    TRY(check_apart(r.a.x_st[0], r.batch, r.a.len, r.a.heads[0], r.a.dim, "dq"));
+    TRY(check_apart(r.a.x_st[1], r.batch, r.a.len, r.a.heads[1], r.a.dim, "dk"));
+  }
+  float *const dgamma[2] = {dq_gamma, dk_gamma};
+  static const char *const names[2] = {"dq_gamma", "dk_gamma"};
+  for (int w = 0; w < 2; ++w) {
+    if (r.a.norm && r.a.heads[w] > 0) TRY(check_ptr(dgamma[w], 4, names[w]));
+    else if (dgamma[w]) return fail(HAPI_E_INVAL, "%s is given, and nothing to write", names[w]);
+    r.a.dgamma[w] = dgamma[w];
+  }
+  TRY(check_workspace(desc->workspace, desc->workspace_bytes, rotary_workspace(r)));
+  TRY(check_stream(desc->stream));
+  r.a.x[0] = q;
+  r.a.x[1] = k;
+  r.a.dy[0] = dq_out;
+  r.a.dy[1] = dk_out;
+  r.a.y[0] = dq;
+  r.a.y[1] = dk;
+  r.a.part = static_cast<float *>(desc->workspace);
+  if (r.a.tokens == 0 && !r.a.norm) return HAPI_OK;
+  HIP_TRY(launch_rotary_backward(r.bf16, r.v, r.a, static_cast<hipStream_t>(desc->stream)));
+  return HAPI_OK;
+}
+
+}  // extern "C"
