@@ -613,6 +613,56 @@ int hapi_rotary_backward(const hapi_rotary_desc *desc, const void *dq_out, const
                          const float *q_gamma, const float *k_gamma, const int64_t *positions, const double *freq,
                          const int64_t *lens, void *dq, void *dk, float *dq_gamma, float *dk_gamma);
 
+/* Cross attention: queries attend to an encoder's states of another length.  Per query
+ * head h, with the key head h / (heads / kv_heads), over the keys that take part:
+ *   o = softmax(scale q k^T) v */
+typedef struct {
+  int32_t dtype;              /* hapi_dtype of q, k, v, o and their gradients */
+  int32_t head_dim;           /* 1 .. 128 */
+  int32_t heads, kv_heads;    /* heads a multiple of kv_heads, at most 512 times */
+  int64_t batch, q_len, kv_len;  /* >= 0; at most 2^24 tiles of 32 to 128 queries or keys */
+  /* Elements between batch entries, tokens and heads, as in hapi_rotary_desc; three
+   * zeros: contiguous [batch, tokens, heads, head_dim].  q: q and dq; k: k and dk; v: v and
+   * dv; o: o and dout. */
+  int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+  float scale;                /* > 0; 0 = 1 / sqrt(head_dim) */
+  int32_t reserved;           /* must be 0 */
+  void *stream;               /* hipStream_t; NULL = the null stream */
+  void *workspace;            /* device scratch, 256-byte aligned */
+  size_t workspace_bytes;
+} hapi_attention_desc;
+
+/* Bytes of workspace of a forward call (backward = 0), or of either direction (backward
+ * != 0); < 0 on error.  Widths or strides that are no whole 16-byte multiples, token
+ * strides past 2^20 elements and groups of heads that lie 2^30 bytes apart cost an aligned
+ * copy of the tensor in it.  Host only. */
+int64_t hapi_cross_attention_workspace_bytes(const hapi_attention_desc *desc, int32_t backward);
+
+/*   q [batch, q_len, heads, head_dim], k, v [batch, kv_len, kv_heads, head_dim], 16-byte
+ *             aligned when head_dim and the strides are whole 16-byte multiples, else
+ *             element-aligned
+ *   q_lens    [batch] int64 or NULL: tokens from q_lens[b] on are padding (values are
+ *             taken into 0 .. q_len)
+ *   kv_lens   [batch] int64 or NULL: keys from kv_lens[b] on take no part
+ *   mask      [batch, kv_len] bytes or NULL: keys whose byte is 0 take no part
+ *   o         [batch, q_len, heads, head_dim] output, element-aligned
+ *   stats     [batch, q_len, heads, 2] float32 output, 8-byte aligned: m, the row's largest
+ *             q k^T (before the scale), and l = log sum exp(scale (q k^T - m)), which the
+ *             backward pass reads (apart, so that a row of large scores keeps its l)
+ * Keys that take no part and padding are not read as numbers: they may be NaN.  A row
+ * without a key (or whose every score is -inf), and padding, has o = 0 and m = l = -inf.
+ * Errors: HAPI_E_INVAL, HAPI_E_UNSUPPORTED, HAPI_E_NOMEM, HAPI_E_DEVICE. */
+int hapi_cross_attention_forward(const hapi_attention_desc *desc, const void *q, const void *k, const void *v,
+                                 const int64_t *q_lens, const int64_t *kv_lens, const uint8_t *mask, void *o, float *stats);
+
+/* Gradients of sum(dout o); o and stats are the forward pass's.  dq of padding and of rows
+ * without a key, and dk and dv of keys that take no part, are 0; dk and dv of a key head
+ * are sums over its query heads.  Tensors that share memory between batch entries or heads
+ * (a stride of 0) have no gradient here (HAPI_E_INVAL).  Errors as forward. */
+int hapi_cross_attention_backward(const hapi_attention_desc *desc, const void *q, const void *k, const void *v,
+                                  const int64_t *q_lens, const int64_t *kv_lens, const uint8_t *mask, const void *o,
+                                  const float *stats, const void *dout, void *dq, void *dk, void *dv);
+
 /* The global norm of many gradients, n = sqrt(sum over all tensors of g^2), and
  * their clipping, g min(1, max_norm / n).  Squares and sums are float64. */
 typedef struct {

@@ -35,7 +35,9 @@ __all__ = ["HapiError", "Desc", "hapi_layer", "hapi_model_desc", "hapi_kernel_st
            "Norm", "Head", "hapi_norm_desc", "hapi_head_desc", "hapi_layernorm_workspace_bytes", "hapi_layernorm_forward", "hapi_layernorm_backward",
            "hapi_head_workspace_bytes", "hapi_xent_forward", "hapi_xent_backward", "hapi_distill_forward", "hapi_distill_backward",
            "Gradients", "hapi_gradient_desc", "hapi_gradient_workspace_bytes", "hapi_gradient_norm", "hapi_gradient_clip",
-           "Rotary", "hapi_rotary_desc", "hapi_rotary_workspace_bytes", "hapi_rotary_forward", "hapi_rotary_backward"]
+           "Rotary", "hapi_rotary_desc", "hapi_rotary_workspace_bytes", "hapi_rotary_forward", "hapi_rotary_backward",
+           "Attention", "hapi_attention_desc", "hapi_cross_attention_workspace_bytes", "hapi_cross_attention_forward",
+           "hapi_cross_attention_backward"]
 
 _STATUS = {HAPI_E_INVAL: "HAPI_E_INVAL", HAPI_E_UNSUPPORTED: "HAPI_E_UNSUPPORTED",
            HAPI_E_NOMEM: "HAPI_E_NOMEM", HAPI_E_DEVICE: "HAPI_E_DEVICE"}
@@ -137,6 +139,15 @@ class hapi_rotary_desc(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class hapi_attention_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("batch", ctypes.c_int64), ("q_len", ctypes.c_int64),
+                ("kv_len", ctypes.c_int64), ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3), ("scale", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 def _hip_runtimes():
     try:
         with open("/proc/self/maps") as f:
@@ -190,7 +201,7 @@ def _load():
         "hapi_distill_forward": (ctypes.c_int, [T] + [vp] * 8),
         "hapi_distill_backward": (ctypes.c_int, [T] + [vp] * 11),
     })
-    G, R = ctypes.POINTER(hapi_gradient_desc), ctypes.POINTER(hapi_rotary_desc)
+    G, R, A = ctypes.POINTER(hapi_gradient_desc), ctypes.POINTER(hapi_rotary_desc), ctypes.POINTER(hapi_attention_desc)
     sig.update({
         "hapi_gradient_workspace_bytes": (i64, [G]),
         "hapi_gradient_norm": (ctypes.c_int, [G, vp]),
@@ -198,6 +209,9 @@ def _load():
         "hapi_rotary_workspace_bytes": (i64, [R]),
         "hapi_rotary_forward": (ctypes.c_int, [R] + [vp] * 9),
         "hapi_rotary_backward": (ctypes.c_int, [R] + [vp] * 13),
+        "hapi_cross_attention_workspace_bytes": (i64, [A, i32]),
+        "hapi_cross_attention_forward": (ctypes.c_int, [A] + [vp] * 8),
+        "hapi_cross_attention_backward": (ctypes.c_int, [A] + [vp] * 12),
     })
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -213,7 +227,8 @@ EXPORTED = ("hapi_raw_weight_count", "hapi_packed_weight_bytes", "hapi_pack_weig
             "hapi_layernorm_workspace_bytes", "hapi_layernorm_forward", "hapi_layernorm_backward", "hapi_head_workspace_bytes",
             "hapi_xent_forward", "hapi_xent_backward", "hapi_distill_forward", "hapi_distill_backward",
             "hapi_gradient_workspace_bytes", "hapi_gradient_norm", "hapi_gradient_clip",
-            "hapi_rotary_workspace_bytes", "hapi_rotary_forward", "hapi_rotary_backward")
+            "hapi_rotary_workspace_bytes", "hapi_rotary_forward", "hapi_rotary_backward",
+            "hapi_cross_attention_workspace_bytes", "hapi_cross_attention_forward", "hapi_cross_attention_backward")
 
 
 def _ptr(p):
@@ -731,3 +746,50 @@ def hapi_rotary_backward(desc: Rotary, dq_out, dk_out, q, k, q_gamma, k_gamma, p
         *_rotary_common(c, dev, q_gamma, k_gamma, positions, freq, lens),
         _heads(dev, dq, "dq", t, qs, c.q_stride), _heads(dev, dk, "dk", t, ks, c.k_stride),
         _tensor(dev, dq_gamma, "dq_gamma", _F32, (c.head_dim,)), _tensor(dev, dk_gamma, "dk_gamma", _F32, (c.head_dim,))))
+
+
+class Attention(_TailDesc):
+    """Owns a ``hapi_attention_desc``.  Strides are (batch, token, head), in elements;
+    empty: contiguous.  ``scale = 0`` is 1 / sqrt(head_dim)."""
+    _struct = hapi_attention_desc
+
+    def __init__(self, dtype, batch, q_len, kv_len, heads, kv_heads, head_dim, scale=0.0, q_stride=(), k_stride=(),
+                 v_stride=(), o_stride=(), **kw):
+        super().__init__(**kw)
+        c = self.c
+        c.dtype, c.batch, c.q_len, c.kv_len = dtype, int(batch), int(q_len), int(kv_len)
+        c.heads, c.kv_heads, c.head_dim, c.scale = int(heads), int(kv_heads), int(head_dim), float(scale)
+        _strides(c.q_stride, q_stride)
+        _strides(c.k_stride, k_stride)
+        _strides(c.v_stride, v_stride)
+        _strides(c.o_stride, o_stride)
+
+
+def hapi_cross_attention_workspace_bytes(desc: Attention, backward: bool = False) -> int:
+    return _check(_lib.hapi_cross_attention_workspace_bytes(desc.ref, int(bool(backward))))
+
+
+def _attention_inputs(c, dev, q, k, v, q_lens, kv_lens, mask):
+    t, ks = _TORCH_TYPES.get(c.dtype), (c.batch, c.kv_len, c.kv_heads, c.head_dim)
+    byte = mask.dtype if getattr(mask, "dtype", None) in (torch.bool, torch.uint8) else torch.bool
+    return (_heads(dev, q, "q", t, (c.batch, c.q_len, c.heads, c.head_dim), c.q_stride),
+            _heads(dev, k, "k", t, ks, c.k_stride), _heads(dev, v, "v", t, ks, c.v_stride),
+            _flat(dev, q_lens, "q_lens", torch.int64, (c.batch,)), _flat(dev, kv_lens, "kv_lens", torch.int64, (c.batch,)),
+            _flat(dev, mask, "mask", byte, (c.batch, c.kv_len)))
+
+
+def hapi_cross_attention_forward(desc: Attention, q, k, v, q_lens, kv_lens, mask, o, stats) -> None:
+    c, dev = desc.c, _device()
+    t, qs = _TORCH_TYPES.get(c.dtype), (c.batch, c.q_len, c.heads, c.head_dim)
+    _check(_lib.hapi_cross_attention_forward(
+        desc.ref, *_attention_inputs(c, dev, q, k, v, q_lens, kv_lens, mask), _heads(dev, o, "o", t, qs, c.o_stride),
+        _flat(dev, stats, "stats", _F32, qs[:3] + (2,))))
+
+
+def hapi_cross_attention_backward(desc: Attention, q, k, v, q_lens, kv_lens, mask, o, stats, dout, dq, dk, dv) -> None:
+    c, dev = desc.c, _device()
+    t, qs, ks = _TORCH_TYPES.get(c.dtype), (c.batch, c.q_len, c.heads, c.head_dim), (c.batch, c.kv_len, c.kv_heads, c.head_dim)
+    _check(_lib.hapi_cross_attention_backward(
+        desc.ref, *_attention_inputs(c, dev, q, k, v, q_lens, kv_lens, mask), _heads(dev, o, "o", t, qs, c.o_stride),
+        _flat(dev, stats, "stats", _F32, qs[:3] + (2,)), _heads(dev, dout, "dout", t, qs, c.o_stride),
+        _heads(dev, dq, "dq", t, qs, c.q_stride), _heads(dev, dk, "dk", t, ks, c.k_stride), _heads(dev, dv, "dv", t, ks, c.v_stride)))

@@ -279,7 +279,171 @@ int check_both(const Rotary &r, const void *q, const void *k, const char *q_name
   return HAPI_OK;
 }
 
+// ----------------------------------------------------------- cross attention
+
+struct Attend {
+  bool bf16;
+  int esz, v;  // bytes of a value, values of 16 bytes
+  AttendArgs a;
+  int64_t batch;
+  bool stage_q, stage_k, stage_v, stage_o;  // copied to aligned rows; dout lies as o does
+  int64_t ld;                               // of those
+  int fwd_splits, fwd_parts, dkv_splits;
+  int64_t bytes_fwd, bytes_bwd;
+  int64_t o_q, o_k, o_v, o_o, o_g, o_part, o_ml, o_delta;  // byte offsets into the workspace
+};
+
+int read_attend(const hapi_attention_desc *d, Attend &t) {
+  if (!d) return fail(HAPI_E_INVAL, "desc is NULL");
+  if (d->dtype != HAPI_F32 && d->dtype != HAPI_BF16) return fail(HAPI_E_INVAL, "unknown dtype %d", d->dtype);
+  if (d->reserved) return fail(HAPI_E_INVAL, "reserved must be 0");
+  if (d->head_dim < 1) return fail(HAPI_E_INVAL, "head_dim must be >= 1");
+  if (d->head_dim > kAttendMaxDim) return fail(HAPI_E_UNSUPPORTED, "head_dim %d (at most %d)", d->head_dim, kAttendMaxDim);
+  if (d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads)
+    return fail(HAPI_E_INVAL, "heads must be a multiple of kv_heads, both >= 1");
+  if (d->heads / d->kv_heads > kAttendMaxGroup)
+    return fail(HAPI_E_UNSUPPORTED, "%d heads share a key head (at most %d)", d->heads / d->kv_heads, kAttendMaxGroup);
+  if (d->batch < 0 || d->q_len < 0 || d->kv_len < 0) return fail(HAPI_E_INVAL, "batch, q_len and kv_len must be >= 0");
+  if (!(d->scale >= 0.0f) || !std::isfinite(d->scale)) return fail(HAPI_E_INVAL, "scale must be finite and > 0, or 0");
+  t = Attend{};
+  AttendArgs &a = t.a;
+  constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxTiles = (int64_t)1 << 24;  // 2^32 threads are too many for a launch
+  const int64_t group = d->heads / d->kv_heads;
+  if (d->batch > kMaxRows || d->q_len > kMaxRows || d->kv_len > kMaxRows || d->q_len * group > kMaxRows)
+    return fail(HAPI_E_UNSUPPORTED, "batch, kv_len and q_len times heads / kv_heads must be at most 2^30");
+  const int64_t pairs = d->batch * d->kv_heads, rows = d->q_len * group;
+  const int rw = attend_row_waves(rows);
+  if (pairs >= kMaxTiles || ceil_div(rows, 32 * rw) * pairs >= kMaxTiles || ceil_div(d->kv_len, 128) * pairs >= kMaxTiles)
+    return fail(HAPI_E_UNSUPPORTED, "more than 2^24 tiles of queries or keys");
+  t.bf16 = d->dtype == HAPI_BF16;
+  t.esz = t.bf16 ? 2 : 4;
+  t.v = 16 / t.esz;
+  t.batch = d->batch;
+  a.q_len = (int32_t)d->q_len;
+  a.kv_len = (int32_t)d->kv_len;
+  a.heads = d->heads;
+  a.kv_heads = d->kv_heads;
+  a.group = (int32_t)group;
+  a.dim = d->head_dim;
+  a.dim4 = (int32_t)up(d->head_dim, 4);
+  a.pairs = (int32_t)pairs;
+  a.scale = d->scale != 0.0f ? d->scale : 1.0f / std::sqrt((float)d->head_dim);
+  a.c = (float)((double)a.scale * 1.4426950408889634);
+  TRY(read_strides(d->q_stride, d->q_len, d->heads, d->head_dim, "q", a.q_st));
+  TRY(read_strides(d->k_stride, d->kv_len, d->kv_heads, d->head_dim, "k", a.k_st));
+  TRY(read_strides(d->v_stride, d->kv_len, d->kv_heads, d->head_dim, "v", a.v_st));
+  TRY(read_strides(d->o_stride, d->q_len, d->heads, d->head_dim, "o", a.o_st));
+  // The kernels read whole 16-byte slots, at 32-bit offsets from a tile's first token.
+  const auto staged = [&](const int64_t *st, int64_t heads) {
+    return d->head_dim % t.v != 0 || st[0] % t.v != 0 || st[1] % t.v != 0 || st[2] % t.v != 0 || st[1] > 1 << 20 ||
+           st[2] * heads * t.esz >= (int64_t)1 << 30;
+  };
+  t.stage_q = staged(a.q_st, group);
+  t.stage_k = staged(a.k_st, 1);
+  t.stage_v = staged(a.v_st, 1);
+  t.stage_o = staged(a.o_st, group);
+  t.ld = up(d->head_dim, t.v);
+
+  // Few rows: the keys over as many workgroups as fill the CUs, some tiles to each wave.
+  const int kw = attend_key_waves(t.bf16, d->head_dim, rw), bn = attend_tile_keys(t.bf16, d->head_dim, kw);
+  const int64_t wgs = ceil_div(rows, 32 * rw) * pairs, want = rw == 4 ? 2 * kCus : kCus;
+  const int64_t key_tiles = ceil_div(d->kv_len, bn);
+  t.fwd_splits = wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, key_tiles / (4 * kw), 64}));
+  t.fwd_parts = t.fwd_splits * kw;
+  const int64_t kwgs = ceil_div(d->kv_len, 128) * pairs, row_tiles = ceil_div(rows, t.bf16 ? 64 : 32);
+  t.dkv_splits = kwgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({2 * kCus / kwgs, row_tiles / 4, 64}));
+
+  const int64_t all = pairs * rows, keys = pairs * d->kv_len;
+  int64_t o = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t at = o;
+    o += up(bytes, kAlign);
+    return at;
+  };
+  t.o_q = take(t.stage_q ? all * t.ld * t.esz : 0);
+  t.o_k = take(t.stage_k ? keys * t.ld * t.esz : 0);
+  t.o_v = take(t.stage_v ? keys * t.ld * t.esz : 0);
+  const int64_t shared = o;
+  t.o_ml = take(t.fwd_parts > 1 ? t.fwd_parts * all * 8 : 0);
+  take(t.fwd_parts > 1 ? t.fwd_parts * all * a.dim4 * 4 : 0);
+  t.bytes_fwd = o;
+  o = shared;
+  t.o_o = take(t.stage_o ? all * t.ld * t.esz : 0);
+  t.o_g = take(t.stage_o ? all * t.ld * t.esz : 0);
+  t.o_delta = take(all * 4);
+  t.o_part = o;  // dq's, then dk's and dv's
+  take(std::max<int64_t>(t.fwd_parts > 1 ? t.fwd_parts * all * a.dim4 * 4 : 0, t.dkv_splits > 1 ? t.dkv_splits * 2 * keys * a.dim4 * 4 : 0));
+  t.bytes_bwd = o;
+  return HAPI_OK;
+}
+
+int check_attend_inputs(const Attend &t, const void *q, const void *k, const void *v, const int64_t *q_lens,
+                        const int64_t *kv_lens, const uint8_t *mask) {
+  if (t.a.q_len > 0) TRY(check_ptr(q, t.stage_q ? t.esz : 16, "q"));
+  if (t.a.kv_len > 0) {
+    TRY(check_ptr(k, t.stage_k ? t.esz : 16, "k"));
+    TRY(check_ptr(v, t.stage_v ? t.esz : 16, "v"));
+  }
+  if ((uintptr_t)q_lens % 8) return fail(HAPI_E_INVAL, "q_lens must be 8-byte aligned");
+  if ((uintptr_t)kv_lens % 8) return fail(HAPI_E_INVAL, "kv_lens must be 8-byte aligned");
+  return HAPI_OK;
+}
+
+// Whether four values of every row can be stored at once.
+bool vec4(const Attend &t, const void *p, const int64_t *st) {
+  return t.a.dim % 4 == 0 && st[0] % 4 == 0 && st[1] % 4 == 0 && st[2] % 4 == 0 && (uintptr_t)p % (4 * t.esz) == 0;
+}
+
+// A copy of in, [batch][tokens][heads], with aligned rows, and its strides.
+int stage_rows(const Attend &t, const void *in, int64_t *st, int64_t tokens, int64_t heads, void *out, hipStream_t s) {
+  StageArgs g;
+  g.in = in;
+  g.out = out;
+  for (int i = 0; i < 3; ++i) g.st[i] = st[i];
+  g.count = t.batch * tokens * heads;
+  g.tokens = (int32_t)tokens;
+  g.heads = (int32_t)heads;
+  g.dim = t.a.dim;
+  g.ld = (int32_t)t.ld;
+  HIP_TRY(launch_attend_stage(t.bf16, g, s));
+  st[2] = t.ld;
+  st[1] = heads * t.ld;
+  st[0] = tokens * st[1];
+  return HAPI_OK;
+}
+
+int stage_inputs(Attend &t, const void *q, const void *k, const void *v, uint8_t *base, hipStream_t s) {
+  AttendArgs &a = t.a;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  if (t.stage_q) {
+    a.q = base + t.o_q;
+    TRY(stage_rows(t, q, a.q_st, a.q_len, a.heads, base + t.o_q, s));
+  }
+  if (t.stage_k) {
+    a.k = base + t.o_k;
+    TRY(stage_rows(t, k, a.k_st, a.kv_len, a.kv_heads, base + t.o_k, s));
+  }
+  if (t.stage_v) {
+    a.v = base + t.o_v;
+    TRY(stage_rows(t, v, a.v_st, a.kv_len, a.kv_heads, base + t.o_v, s));
+  }
+  return HAPI_OK;
+}
+
 }  // namespace
+
+int attend_row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+int attend_key_waves(bool bf16, int dim, int row_waves) {
+  // as many as two stages of their tiles leave room for in the LDS
+  return row_waves == 4 ? 1 : row_waves == 2 ? 2 : !bf16 && dim > 64 ? 2 : 4;
+}
+int attend_tile_keys(bool bf16, int dim, int key_waves) {
+  const int padded = (int)up(dim, 32);
+  return bf16 && key_waves * 4 * 64 * padded * 2 <= 128 * 1024 ? 64 : 32;
+}
+
 }  // namespace hapi
 
 using namespace hapi;
@@ -357,6 +521,106 @@ int hapi_rotary_backward(const hapi_rotary_desc *desc, const void *dq_out, const
   r.a.part = static_cast<float *>(desc->workspace);
   if (r.a.tokens == 0 && !r.a.norm) return HAPI_OK;
   HIP_TRY(launch_rotary_backward(r.bf16, r.v, r.a, static_cast<hipStream_t>(desc->stream)));
+  return HAPI_OK;
+}
+
+int64_t hapi_cross_attention_workspace_bytes(const hapi_attention_desc *desc, int32_t backward) {
+  Attend t;
+  TRY(read_attend(desc, t));
+  return backward ? std::max(t.bytes_fwd, t.bytes_bwd) : t.bytes_fwd;
+}
+
+int hapi_cross_attention_forward(const hapi_attention_desc *desc, const void *q, const void *k, const void *v,
+                                 const int64_t *q_lens, const int64_t *kv_lens, const uint8_t *mask, void *o, float *stats) {
+  Attend t;
+  TRY(read_attend(desc, t));
+  if (t.batch == 0 || t.a.q_len == 0) return HAPI_OK;
+  AttendArgs &a = t.a;
+  TRY(check_attend_inputs(t, q, k, v, q_lens, kv_lens, mask));
+  TRY(check_ptr(o, t.esz, "o"));
+  TRY(check_ptr(stats, 8, "stats"));
+  TRY(check_apart(a.o_st, t.batch, a.q_len, a.heads, a.dim, "o"));
+  TRY(check_workspace(desc->workspace, desc->workspace_bytes, t.bytes_fwd));
+  TRY(check_stream(desc->stream));
+  hipStream_t s = static_cast<hipStream_t>(desc->stream);
+  uint8_t *base = static_cast<uint8_t *>(desc->workspace);
+  TRY(stage_inputs(t, q, k, v, base, s));
+  a.q_lens = q_lens;
+  a.kv_lens = kv_lens;
+  a.mask = mask;
+  a.y = o;
+  for (int i = 0; i < 3; ++i) a.y_st[i] = a.o_st[i];
+  a.y_vec = vec4(t, o, a.o_st);
+  a.stats = reinterpret_cast<float2 *>(stats);
+  a.splits = t.fwd_splits;
+  a.parts = t.fwd_parts;
+  a.part_ml = reinterpret_cast<float2 *>(base + t.o_ml);
+  a.part = reinterpret_cast<float *>(base + t.o_ml + up((int64_t)t.fwd_parts * a.pairs * a.q_len * a.group * 8, kAlign));
+  HIP_TRY(launch_attend_forward(t.bf16, a, s));
+  return HAPI_OK;
+}
+
+int hapi_cross_attention_backward(const hapi_attention_desc *desc, const void *q, const void *k, const void *v,
+                                  const int64_t *q_lens, const int64_t *kv_lens, const uint8_t *mask, const void *o,
+                                  const float *stats, const void *dout, void *dq, void *dk, void *dv) {
+  Attend t;
+  TRY(read_attend(desc, t));
+  AttendArgs &a = t.a;
+  if (t.batch == 0 || (a.q_len == 0 && a.kv_len == 0)) return HAPI_OK;
+  TRY(check_attend_inputs(t, q, k, v, q_lens, kv_lens, mask));
+  if (a.q_len > 0) {
+    TRY(check_ptr(o, t.stage_o ? t.esz : 16, "o"));
+    TRY(check_ptr(stats, 8, "stats"));
+    TRY(check_ptr(dout, t.stage_o ? t.esz : 16, "dout"));
+    TRY(check_ptr(dq, t.esz, "dq"));
+    TRY(check_apart(a.q_st, t.batch, a.q_len, a.heads, a.dim, "dq"));
+  }
+  if (a.kv_len > 0) {
+    TRY(check_ptr(dk, t.esz, "dk"));
+    TRY(check_ptr(dv, t.esz, "dv"));
+    TRY(check_apart(a.k_st, t.batch, a.kv_len, a.kv_heads, a.dim, "dk"));
+    TRY(check_apart(a.v_st, t.batch, a.kv_len, a.kv_heads, a.dim, "dv"));
+  }
+  TRY(check_workspace(desc->workspace, desc->workspace_bytes, t.bytes_bwd));
+  TRY(check_stream(desc->stream));
+  hipStream_t s = static_cast<hipStream_t>(desc->stream);
+  uint8_t *base = static_cast<uint8_t *>(desc->workspace);
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  for (int i = 0; i < 3; ++i) {
+    a.dq_st[i] = a.q_st[i];
+    a.dk_st[i] = a.k_st[i];
+    a.dv_st[i] = a.v_st[i];
+    a.g_st[i] = a.o_st[i];
+  }
+  a.dq_vec = vec4(t, dq, a.dq_st);
+  a.dk_vec = vec4(t, dk, a.dk_st);
+  a.dv_vec = vec4(t, dv, a.dv_st);
+  TRY(stage_inputs(t, q, k, v, base, s));
+  a.o = o;
+  a.dout = dout;
+  if (t.stage_o && a.q_len > 0) {
+    a.o = base + t.o_o;
+    a.dout = base + t.o_g;
+    TRY(stage_rows(t, o, a.o_st, a.q_len, a.heads, base + t.o_o, s));
+    TRY(stage_rows(t, dout, a.g_st, a.q_len, a.heads, base + t.o_g, s));
+  }
+  a.q_lens = q_lens;
+  a.kv_lens = kv_lens;
+  a.mask = mask;
+  a.stats = reinterpret_cast<float2 *>(const_cast<float *>(stats));
+  a.delta = reinterpret_cast<float *>(base + t.o_delta);
+  a.part = reinterpret_cast<float *>(base + t.o_part);
+  if (a.q_len > 0) {
+    a.splits = t.fwd_splits;
+    a.parts = t.fwd_parts;
+    HIP_TRY(launch_attend_dq(t.bf16, a, s));
+  }
+  if (a.kv_len > 0) {
+    a.splits = a.parts = t.dkv_splits;
+    HIP_TRY(launch_attend_dkv(t.bf16, a, s));
+  }
   return HAPI_OK;
 }
 

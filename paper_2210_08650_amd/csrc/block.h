@@ -61,4 +61,47 @@ struct RotaryArgs {
 hipError_t launch_rotary_forward(bool bf16, int v, const RotaryArgs &a, hipStream_t s);
 hipError_t launch_rotary_backward(bool bf16, int v, const RotaryArgs &a, hipStream_t s);
 
+// ----------------------------------------------------------- cross attention
+
+constexpr int kAttendMaxDim = 128;
+constexpr int kAttendMaxGroup = 512;  // query heads of a key head
+
+// The rows of one key head's problem are its query heads' tokens: row r is token
+// r / group, head r % group of the group.
+struct AttendArgs {
+  const void *q, *k, *v, *o, *dout;  // as the kernels read them: 16-byte aligned rows
+  int64_t q_st[3], k_st[3], v_st[3], o_st[3], g_st[3];  // elements; g: of dout
+  void *y, *dq, *dk, *dv;            // y: o as it is written
+  int64_t y_st[3], dq_st[3], dk_st[3], dv_st[3];
+  bool y_vec, dq_vec, dk_vec, dv_vec;  // four values can be stored at once
+  float2 *stats;                     // [batch][q_len][heads] (largest score, log of the sum)
+  const int64_t *q_lens, *kv_lens;
+  const uint8_t *mask;               // [batch][kv_len] or null
+  int32_t q_len, kv_len, heads, kv_heads, group, dim;
+  int32_t pairs;                     // batch * kv_heads
+  float scale, c;                    // c = scale log2(e)
+  int32_t splits, parts;             // of the keys (dk, dv: of the rows); parts: with the waves that share rows
+  float *part;                       // [parts][pairs][rows][dim4]; dk, dv: [parts][2][pairs][kv_len][dim4]
+  float2 *part_ml;                   // [parts][pairs][rows] (reference score, sum)
+  int32_t dim4;                      // dim up to a multiple of 4
+  float *delta;                      // [pairs][rows] sum of dout o
+};
+
+// Rows to a workgroup's waves: 4 x 32, 2 x 32 (two waves take other keys), 32 (all do).
+int attend_row_waves(int64_t rows);
+int attend_key_waves(bool bf16, int dim, int row_waves);
+int attend_tile_keys(bool bf16, int dim, int key_waves);
+// Rows from any layout to [batch][tokens][heads][ld], zeros from dim on.
+struct StageArgs {
+  const void *in;
+  void *out;
+  int64_t st[3];
+  int64_t count;  // rows
+  int32_t tokens, heads, dim, ld;
+};
+hipError_t launch_attend_stage(bool bf16, const StageArgs &a, hipStream_t s);
+hipError_t launch_attend_forward(bool bf16, const AttendArgs &a, hipStream_t s);
+hipError_t launch_attend_dq(bool bf16, const AttendArgs &a, hipStream_t s);   // delta, too
+hipError_t launch_attend_dkv(bool bf16, const AttendArgs &a, hipStream_t s);
+
 }  // namespace hapi

@@ -1,0 +1,265 @@
+// Cross attention, forward: o = softmax(scale q k^T) v over the keys that take part.
+//
+// The query heads that share a key head are the rows of one problem (row r: token
+// r / group, head r % group), so keys and values are read once for all of them and a
+// single token's heads fill a tile together.  A wave owns 32 rows, its queries in
+// registers; keys and values pass through LDS in tiles that the waves of a workgroup
+// share (several waves on 32 rows: each takes other tiles).  Scores are formed
+// transposed, S^T = K Q^T, so that a lane owns one row's: the softmax needs its own
+// registers and one exchange with the other half-wave, and the probabilities are the
+// next product's operand as they are, o^T = V^T P^T, with V^T read transposed from LDS.
+//
+// One pass with a running maximum and sum.  The maximum is taken of the scores
+// themselves and the difference is formed before the scale: (s - m) c has no
+// rounding of m c in it.  Scores, statistics and sums are float32; probabilities are
+// rounded to the operands' type for the matrix cores (2^-8 of each in bf16, the sum is
+// of the unrounded ones), the output once.
+//
+// Keys that take no part are zeros in LDS, whatever memory holds, and their scores are
+// -inf, so NaN in padding reaches nothing.  Where rows are few, the keys are split over
+// workgroups and a second kernel joins the parts.
+#include "attend.h"
+
+namespace hapi {
+namespace {
+
+template <typename T, int DP, int RW, int KW, int BN>
+__global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_kernel(AttendArgs a) {
+  typedef hapi::Tile<T, DP, BN> Tile;
+  typedef Loader<T, DP, BN, RW> Load;
+  typedef typename Elem<T>::Frag Frag;
+  constexpr int KS = DP / 16, DB = DP / 32, NT = BN / 32, STAGE = 2 * Tile::BYTES;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[KW * 2 * STAGE];
+
+  const int t = threadIdx.x, lane = t & 63, col = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wr = wave % RW, wk = wave / RW;
+  const int rows = a.q_len * a.group, tiles = (rows + 32 * RW - 1) / (32 * RW);
+  const Place at = place(a, tiles);
+  const int tile = at.tile, split = at.split, pair = at.pair, b = at.b, kh = at.kh;
+  const int q_valid = clamped(a.q_lens, b, a.q_len), kv_valid = clamped(a.kv_lens, b, a.kv_len);
+
+  // this lane's row
+  const int r = (tile * RW + wr) * 32 + col;
+  const int qi = r / a.group, qg = r - qi * a.group;
+  const bool counts = qi < q_valid;
+  const T *qp = static_cast<const T *>(a.q) + (int64_t)b * a.q_st[0] + (int64_t)qi * a.q_st[1] + (int64_t)(kh * a.group + qg) * a.q_st[2];
+  Frag qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = row_frag<T>(qp, ks, lh, a.dim, counts);
+
+  // the split's tiles of keys; wave wk takes every KW-th
+  const int key_tiles = tile * RW * 32 < q_valid * a.group ? (kv_valid + BN - 1) / BN : 0;
+  const int t0 = (int)((int64_t)key_tiles * split / a.splits), t1 = (int)((int64_t)key_tiles * (split + 1) / a.splits);
+  const int steps = (t1 - t0 + KW - 1) / KW;
+  Load lk, lv;
+  lk.init(a.k_st[1], a.dim, wr, lane);
+  lv.init(a.v_st[1], a.dim, wr, lane);
+  const T *kp = static_cast<const T *>(a.k) + (int64_t)b * a.k_st[0] + (int64_t)kh * a.k_st[2];
+  const T *vp = static_cast<const T *>(a.v) + (int64_t)b * a.v_st[0] + (int64_t)kh * a.v_st[2];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem + wk * 2 * STAGE;
+
+  uint64_t keep = 0;  // of the tile in flight
+  auto issue = [&](int step) {
+    const int kt = t0 + step * KW + wk;
+    keep = kt < t1 ? key_bits(kv_valid - (int64_t)kt * BN) : 0;
+    if (keep && a.mask) {
+      const bool in = (keep >> lane) & 1;
+      keep &= __ballot(in && a.mask[(int64_t)b * a.kv_len + (int64_t)kt * BN + (in ? lane : 0)] != 0);
+    }
+    if (kt >= t1) return;
+    const uint32_t at = lds0 + (step & 1) * STAGE;
+    lk.issue(kp + (int64_t)kt * BN * a.k_st[1], at, keep, wr);
+    lv.issue(vp + (int64_t)kt * BN * a.v_st[1], at + Tile::BYTES, keep, wr);
+  };
+
+  f32x16_t o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) o[d] = zeros();
+  float m = -INFINITY, sum = 0.0f;  // sum: of this half-wave's keys
+  constexpr uint64_t ALL = BN == 64 ? ~0ull : (1ull << BN) - 1;
+
+  if (steps > 0) issue(0);
+  for (int step = 0; step < steps; ++step) {
+    // this wave's DMAs have landed and its reads of the last tile are done; after the
+    // barrier, everyone's
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (RW > 1) __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    const uint64_t now = keep;
+    if (step + 1 < steps) issue(step + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    if (now == 0) continue;  // the same for all waves of wk
+    const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE, *vt = kt + Tile::BYTES;
+    f32x16_t s[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s[n] = zeros();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], s[n]);
+    if (now != ALL) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uint32_t bits = (uint32_t)(now >> (32 * n)) >> (4 * lh);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1)) s[n][i] = -INFINITY;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float mn = fmaxf(m, mx);
+    const float ref = mn == -INFINITY ? 0.0f : mn;  // no key yet: sums of 0, not NaN
+    const float alpha = __builtin_amdgcn_exp2f((m - ref) * a.c);
+    m = mn;
+    sum *= alpha;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[n][i] = __builtin_amdgcn_exp2f((s[n][i] - ref) * a.c);
+        sum += s[n][i];
+      }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const Frag p = operand<T>(s[n], j);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = mma(Tile::by_column(vt, 32 * n + 16 * j, 32 * d, lane), p, o[d]);
+      }
+  }
+  sum += __shfl_xor(sum, 32, 64);
+  if (r >= rows) return;
+  if (!counts) {  // padding between rows that count: as a row without keys
+    m = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = zeros();
+  }
+  if (a.parts > 1) {
+    const int64_t at = ((int64_t)(split * KW + wk) * a.pairs + pair) * rows + r;
+    float *p = a.part + at * a.dim4;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int e = 32 * d + 8 * q + 4 * lh;
+        if (e < a.dim4) *reinterpret_cast<float4 *>(p + e) = make_float4(o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]);
+      }
+    if (lh == 0) a.part_ml[at] = make_float2(m, sum);
+    return;
+  }
+  const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+  const int64_t h = kh * a.group + qg;
+  T *y = static_cast<T *>(a.y) + (int64_t)b * a.y_st[0] + (int64_t)qi * a.y_st[1] + h * a.y_st[2];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      store4<T>(y, 32 * d + 8 * q + 4 * lh, a.dim, a.y_vec, o[d][4 * q] * inv, o[d][4 * q + 1] * inv, o[d][4 * q + 2] * inv,
+                o[d][4 * q + 3] * inv);
+  if (lh == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = make_float2(m, logf(sum));
+}
+
+// Joins a row's parts: a thread has four of its values.
+template <typename T>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+  const int per = a.dim4 / 4;
+  const int64_t rows = (int64_t)a.q_len * a.group, all = rows * a.pairs;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = i / per;
+  if (row >= all) return;
+  const int d = (int)(i - row * per) * 4;
+  float m = -INFINITY;
+  for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.part_ml[p * all + row].x);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float sum = 0.0f, o[4] = {};
+  for (int p = 0; p < a.parts; ++p) {
+    const float2 ml = a.part_ml[p * all + row];
+    const float4 v = *reinterpret_cast<const float4 *>(a.part + (p * all + row) * a.dim4 + d);
+    const float w = __builtin_amdgcn_exp2f((ml.x - ref) * a.c);
+    sum = fmaf(ml.y, w, sum);
+    o[0] = fmaf(v.x, w, o[0]);
+    o[1] = fmaf(v.y, w, o[1]);
+    o[2] = fmaf(v.z, w, o[2]);
+    o[3] = fmaf(v.w, w, o[3]);
+  }
+  const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+  const int pair = (int)(row / rows), r = (int)(row - pair * rows), qi = r / a.group;
+  const int b = pair / a.kv_heads;
+  const int64_t h = (int64_t)(pair - b * a.kv_heads) * a.group + (r - qi * a.group);
+  T *y = static_cast<T *>(a.y) + (int64_t)b * a.y_st[0] + (int64_t)qi * a.y_st[1] + h * a.y_st[2];
+  store4<T>(y, d, a.dim, a.y_vec, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  if (d == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = make_float2(m, logf(sum));
+}
+
+// Rows of any layout to 16-byte aligned ones, a slot of 16 bytes a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void attend_stage_kernel(StageArgs a) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const int per = a.ld / V;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.count * per; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per;
+    const int d = (int)(i - row * per) * V;
+    const int64_t tok = row / a.heads, b = tok / a.tokens;
+    const T *p = static_cast<const T *>(a.in) + b * a.st[0] + (tok - b * a.tokens) * a.st[1] + (row - tok * a.heads) * a.st[2];
+    T v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = d + e < a.dim ? p[d + e] : T{};
+    __builtin_memcpy(static_cast<T *>(a.out) + row * a.ld + d, v, 16);
+  }
+}
+
+template <typename T, int DP, int RW, int KW>
+hipError_t forward(const AttendArgs &a, hipStream_t s) {
+  constexpr int BN = sizeof(T) == 2 && KW * 4 * 64 * DP * 2 <= 128 * 1024 ? 64 : 32;
+  const int64_t rows = (int64_t)a.q_len * a.group, tiles = ceil_div(rows, 32 * RW);
+  hapi_launch(attend_forward_kernel<T, DP, RW, KW, BN>, dim3((uint32_t)(tiles * a.splits * a.pairs)), dim3(64 * RW * KW), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  hapi_launch(attend_join_kernel<T>, dim3((uint32_t)ceil_div(rows * a.pairs * (a.dim4 / 4), 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t forward_rows(const AttendArgs &a, hipStream_t s) {
+  const int rw = attend_row_waves((int64_t)a.q_len * a.group);
+  if (rw == 4) return forward<T, DP, 4, 1>(a, s);
+  if (rw == 2) return forward<T, DP, 2, 2>(a, s);
+  return forward<T, DP, 1, (sizeof(T) == 4 && DP > 64) ? 2 : 4>(a, s);
+}
+
+template <typename T>
+hipError_t forward_dim(const AttendArgs &a, hipStream_t s) {
+  if (a.dim <= 32) return forward_rows<T, 32>(a, s);
+  if (a.dim <= 64) return forward_rows<T, 64>(a, s);
+  if (a.dim <= 96) return forward_rows<T, 96>(a, s);
+  return forward_rows<T, 128>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_attend_forward(bool bf16, const AttendArgs &a, hipStream_t s) {
+  return bf16 ? forward_dim<uint16_t>(a, s) : forward_dim<float>(a, s);
+}
+
+hipError_t launch_attend_stage(bool bf16, const StageArgs &a, hipStream_t s) {
+  const int64_t slots = a.count * (a.ld / (bf16 ? 8 : 4)), want = ceil_div(slots, 256);
+  if (want == 0) return hipSuccess;
+  const dim3 grid((uint32_t)(want < 16384 ? want : 16384)), block(256);
+  if (bf16) hapi_launch(attend_stage_kernel<uint16_t>, grid, block, 0, s, a);
+  else hapi_launch(attend_stage_kernel<float>, grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace hapi

@@ -1,0 +1,391 @@
+// Cross attention, backward, in two kernels without atomics, so that results do not
+// vary.  With p = exp(scale (s - m) - l) from the forward pass's statistics:
+//   dv = p^T dout, dp = dout v^T, ds = p (dp - delta), delta = sum of dout o,
+//   dq = scale ds k, dk = scale ds^T q.
+//
+// dq: rows and waves as in the forward pass.  A wave keeps its rows' q and dout in
+// registers and forms S^T and dP^T of each tile of keys; dS^T is the operand of
+// dq^T = K^T dS^T as it is, K^T read transposed from LDS.  It also forms delta.
+// dk, dv: a wave keeps 32 keys, k and v in registers, and walks the rows of all query
+// heads that share them (their sum is that of its registers): S = Q K^T and dP = dout
+// V^T own a key in a lane, so P and dS are the operands of dv^T = dout^T P and
+// dk^T = Q^T dS as they are.
+//
+// Scores and dP are formed in both kernels, seven products where five would do if the
+// parts of dq could be added by atomics or went through memory (4 bytes of each value
+// for every 128 keys).  P and dS are rounded to the operands' type for the matrix
+// cores; all sums are float32.
+#include "attend.h"
+
+namespace hapi {
+namespace {
+
+template <typename T, int DP, int RW, int KW, int BN>
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 && RW == 4 && DP <= 96 ? 2 : 1) void attend_dq_kernel(AttendArgs a) {
+  typedef hapi::Tile<T, DP, BN> Tile;
+  typedef Loader<T, DP, BN, RW> Load;
+  typedef typename Elem<T>::Frag Frag;
+  constexpr int KS = DP / 16, DB = DP / 32, NT = BN / 32, STAGE = 2 * Tile::BYTES;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[KW * 2 * STAGE];
+
+  const int t = threadIdx.x, lane = t & 63, col = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wr = wave % RW, wk = wave / RW;
+  const int rows = a.q_len * a.group, tiles = (rows + 32 * RW - 1) / (32 * RW);
+  const Place at = place(a, tiles);
+  const int tile = at.tile, split = at.split, pair = at.pair, b = at.b, kh = at.kh;
+  const int q_valid = clamped(a.q_lens, b, a.q_len), kv_valid = clamped(a.kv_lens, b, a.kv_len);
+
+  const int r = (tile * RW + wr) * 32 + col;
+  const int qi = r / a.group, qg = r - qi * a.group;
+  const bool counts = qi < q_valid;
+  const int64_t h = kh * a.group + qg;
+  const T *qp = static_cast<const T *>(a.q) + (int64_t)b * a.q_st[0] + (int64_t)qi * a.q_st[1] + h * a.q_st[2];
+  const T *gp = static_cast<const T *>(a.dout) + (int64_t)b * a.g_st[0] + (int64_t)qi * a.g_st[1] + h * a.g_st[2];
+  const T *op = static_cast<const T *>(a.o) + (int64_t)b * a.o_st[0] + (int64_t)qi * a.o_st[1] + h * a.o_st[2];
+  Frag qf[KS], gf[KS];
+  float delta = 0.0f;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    qf[ks] = row_frag<T>(qp, ks, lh, a.dim, counts);
+    gf[ks] = row_frag<T>(gp, ks, lh, a.dim, counts);
+    const Frag of = row_frag<T>(op, ks, lh, a.dim, counts);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[e], delta);
+  }
+  delta += __shfl_xor(delta, 32, 64);
+  if (split == 0 && wk == 0 && r < rows && lh == 0) a.delta[(int64_t)pair * rows + r] = delta;
+  // a row without a key has m = l = -inf: its p are to be 0
+  float m = INFINITY, l2 = 0.0f;
+  if (counts) {
+    const float2 st = a.stats[((int64_t)b * a.q_len + qi) * a.heads + h];
+    if (st.x != -INFINITY) m = st.x, l2 = st.y * kLog2e;
+  }
+
+  const int key_tiles = tile * RW * 32 < q_valid * a.group ? (kv_valid + BN - 1) / BN : 0;
+  const int t0 = (int)((int64_t)key_tiles * split / a.splits), t1 = (int)((int64_t)key_tiles * (split + 1) / a.splits);
+  const int steps = (t1 - t0 + KW - 1) / KW;
+  Load lk, lv;
+  lk.init(a.k_st[1], a.dim, wr, lane);
+  lv.init(a.v_st[1], a.dim, wr, lane);
+  const T *kp = static_cast<const T *>(a.k) + (int64_t)b * a.k_st[0] + (int64_t)kh * a.k_st[2];
+  const T *vp = static_cast<const T *>(a.v) + (int64_t)b * a.v_st[0] + (int64_t)kh * a.v_st[2];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem + wk * 2 * STAGE;
+
+  uint64_t keep = 0;
+  auto issue = [&](int step) {
+    const int kt = t0 + step * KW + wk;
+    keep = kt < t1 ? key_bits(kv_valid - (int64_t)kt * BN) : 0;
+    if (keep && a.mask) {
+      const bool in = (keep >> lane) & 1;
+      keep &= __ballot(in && a.mask[(int64_t)b * a.kv_len + (int64_t)kt * BN + (in ? lane : 0)] != 0);
+    }
+    if (kt >= t1) return;
+    const uint32_t at = lds0 + (step & 1) * STAGE;
+    lk.issue(kp + (int64_t)kt * BN * a.k_st[1], at, keep, wr);
+    lv.issue(vp + (int64_t)kt * BN * a.v_st[1], at + Tile::BYTES, keep, wr);
+  };
+  constexpr uint64_t ALL = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
+
+  f32x16_t dq[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) dq[d] = zeros();
+  if (steps > 0) issue(0);
+  for (int step = 0; step < steps; ++step) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (RW > 1) __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    const uint64_t now = keep;
+    if (step + 1 < steps) issue(step + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    if (now == 0) continue;
+    const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE, *vt = kt + Tile::BYTES;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      f32x16_t s = zeros(), dp = zeros();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], s);
+        dp = mma(Tile::by_row(vt, 32 * n, ks, lane), gf[ks], dp);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - m) * a.c - l2) * (dp[i] - delta);
+      if (now != ALL) {
+        const uint32_t bits = (uint32_t)(now >> (32 * n)) >> (4 * lh);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1)) s[i] = 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const Frag ds = operand<T>(s, j);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) dq[d] = mma(Tile::by_column(kt, 32 * n + 16 * j, 32 * d, lane), ds, dq[d]);
+      }
+    }
+  }
+  if (r >= rows) return;
+  if (a.parts > 1) {
+    float *p = a.part + (((int64_t)(split * KW + wk) * a.pairs + pair) * rows + r) * a.dim4;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int e = 32 * d + 8 * q + 4 * lh;
+        if (e < a.dim4) *reinterpret_cast<float4 *>(p + e) = make_float4(dq[d][4 * q], dq[d][4 * q + 1], dq[d][4 * q + 2], dq[d][4 * q + 3]);
+      }
+    return;
+  }
+  T *y = static_cast<T *>(a.dq) + (int64_t)b * a.dq_st[0] + (int64_t)qi * a.dq_st[1] + h * a.dq_st[2];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      store4<T>(y, 32 * d + 8 * q + 4 * lh, a.dim, a.dq_vec, dq[d][4 * q] * a.scale, dq[d][4 * q + 1] * a.scale,
+                dq[d][4 * q + 2] * a.scale, dq[d][4 * q + 3] * a.scale);
+}
+
+// BM rows at a time past 4 x 32 keys.
+template <typename T, int DP, int BM>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attend_dkv_kernel(AttendArgs a) {
+  typedef hapi::Tile<T, DP, BM> Tile;
+  typedef typename Elem<T>::Frag Frag;
+  constexpr int KS = DP / 16, DB = DP / 32, STAGE = 2 * Tile::BYTES, LOADS = Tile::DMAS / 4;
+  static_assert(LOADS * 4 == Tile::DMAS && BM <= 64, "as many DMAs to every wave");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE];
+  __shared__ __attribute__((aligned(16))) float side[2][3][BM];  // m, l log2(e), delta
+
+  const int t = threadIdx.x, lane = t & 63, col = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int rows = a.q_len * a.group, tiles = (a.kv_len + 127) / 128;
+  const Place at = place(a, tiles);
+  const int tile = at.tile, split = at.split, pair = at.pair, b = at.b, kh = at.kh;
+  const int q_valid = clamped(a.q_lens, b, a.q_len), kv_valid = clamped(a.kv_lens, b, a.kv_len);
+
+  // this lane's key
+  const int key = tile * 128 + wave * 32 + col;
+  bool counts = key < kv_valid;
+  if (a.mask && counts) counts = a.mask[(int64_t)b * a.kv_len + key] != 0;
+  const T *kp = static_cast<const T *>(a.k) + (int64_t)b * a.k_st[0] + (int64_t)key * a.k_st[1] + (int64_t)kh * a.k_st[2];
+  const T *vp = static_cast<const T *>(a.v) + (int64_t)b * a.v_st[0] + (int64_t)key * a.v_st[1] + (int64_t)kh * a.v_st[2];
+  Frag kf[KS], vf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    kf[ks] = row_frag<T>(kp, ks, lh, a.dim, counts);
+    vf[ks] = row_frag<T>(vp, ks, lh, a.dim, counts);
+  }
+
+  const int valid = tile * 128 < kv_valid ? q_valid * a.group : 0, row_tiles = (valid + BM - 1) / BM;
+  const int t0 = (int)((int64_t)row_tiles * split / a.splits), t1 = (int)((int64_t)row_tiles * (split + 1) / a.splits);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+  const T *qb = static_cast<const T *>(a.q) + (int64_t)b * a.q_st[0] + (int64_t)kh * a.group * a.q_st[2];
+  const T *gb = static_cast<const T *>(a.dout) + (int64_t)b * a.g_st[0] + (int64_t)kh * a.group * a.g_st[2];
+  const uint32_t magic = (1u << 20) / (uint32_t)a.group + 1;  // n / group of n < group + 64 <= 576 as n * magic >> 20
+  // byte offsets of this lane's slots from the first token of the row tile
+  auto issue = [&](int rt, int buf) {
+    const int r0 = rt * BM, i0 = __builtin_amdgcn_readfirstlane(r0 / a.group), g0 = r0 - i0 * a.group;
+    const u32x4_t qs = make_srd(qb + (int64_t)i0 * a.q_st[1]), gs = make_srd(gb + (int64_t)i0 * a.g_st[1]);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + wave * LOADS * 1024);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int slot = (wave * LOADS + i) * 64 + lane, lr = slot / Tile::CPR;
+      const int d = ((slot % Tile::CPR) ^ Tile::swz(lr)) * Tile::V;
+      const uint32_t n = (uint32_t)(g0 + lr), di = (n * magic) >> 20, dg = n - di * a.group;
+      const bool in = r0 + lr < valid && d < a.dim;
+      const uint32_t qo = (uint32_t)((di * a.q_st[1] + dg * a.q_st[2] + d) * (int64_t)sizeof(T));
+      const uint32_t go = (uint32_t)((di * a.g_st[1] + dg * a.g_st[2] + d) * (int64_t)sizeof(T));
+      lds_dma16(qs, lds + i * 1024, in ? qo : kOob, 0);
+      lds_dma16(gs, lds + Tile::BYTES + i * 1024, in ? go : kOob, 0);
+    }
+  };
+  // rows that do not count, and those without a key (m = l = -inf), have p = 0
+  float sm, sl, sd;
+  auto load_side = [&](int rt) {
+    sm = INFINITY, sl = 0.0f, sd = 0.0f;
+    const int r = rt * BM + t;
+    if (t < BM && r < valid) {
+      const int qi = r / a.group;
+      const float2 st = a.stats[((int64_t)b * a.q_len + qi) * a.heads + kh * a.group + (r - qi * a.group)];
+      if (st.x != -INFINITY) sm = st.x, sl = st.y * kLog2e;
+      sd = a.delta[(int64_t)pair * rows + r];
+    }
+  };
+  auto store_side = [&](int buf) {
+    if (t < BM) side[buf][0][t] = sm, side[buf][1][t] = sl, side[buf][2][t] = sd;
+  };
+
+  f32x16_t dk[DB], dv[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
+  if (t0 < t1) {
+    load_side(t0);
+    issue(t0, 0);
+    store_side(0);
+  }
+  for (int rt = t0; rt < t1; ++rt) {
+    const int buf = (rt - t0) & 1;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (rt + 1 < t1) {
+      load_side(rt + 1);
+      issue(rt + 1, buf ^ 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES;
+#pragma unroll
+    for (int n = 0; n < BM / 32; ++n) {
+      f32x16_t s = zeros(), dp = zeros();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mma(Tile::by_row(qt, 32 * n, ks, lane), kf[ks], s);
+        dp = mma(Tile::by_row(gt, 32 * n, ks, lane), vf[ks], dp);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        typedef float f32x4_t __attribute__((ext_vector_type(4)));
+        const int at = 32 * n + 8 * q + 4 * lh;
+        const f32x4_t m = *reinterpret_cast<const f32x4_t *>(&side[buf][0][at]);
+        const f32x4_t l2 = *reinterpret_cast<const f32x4_t *>(&side[buf][1][at]);
+        const f32x4_t delta = *reinterpret_cast<const f32x4_t *>(&side[buf][2][at]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * q + e;
+          const float p = counts ? __builtin_amdgcn_exp2f((s[i] - m[e]) * a.c - l2[e]) : 0.0f;
+          s[i] = p;
+          dp[i] = p * (dp[i] - delta[e]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const Frag p = operand<T>(s, j), ds = operand<T>(dp, j);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          dv[d] = mma(Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane), p, dv[d]);
+          dk[d] = mma(Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane), ds, dk[d]);
+        }
+      }
+    }
+    if (rt + 1 < t1) store_side(buf ^ 1);
+  }
+  if (key >= a.kv_len) return;
+  if (!counts) {  // whatever the rows hold (0 times NaN)
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
+  }
+  if (a.parts > 1) {
+    const int64_t all = (int64_t)a.pairs * a.kv_len;
+    float *p = a.part + (((int64_t)split * 2) * all + (int64_t)pair * a.kv_len + key) * a.dim4;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int e = 32 * d + 8 * q + 4 * lh;
+        if (e >= a.dim4) continue;
+        *reinterpret_cast<float4 *>(p + e) = make_float4(dk[d][4 * q], dk[d][4 * q + 1], dk[d][4 * q + 2], dk[d][4 * q + 3]);
+        *reinterpret_cast<float4 *>(p + all * a.dim4 + e) = make_float4(dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
+      }
+    return;
+  }
+  T *yk = static_cast<T *>(a.dk) + (int64_t)b * a.dk_st[0] + (int64_t)key * a.dk_st[1] + (int64_t)kh * a.dk_st[2];
+  T *yv = static_cast<T *>(a.dv) + (int64_t)b * a.dv_st[0] + (int64_t)key * a.dv_st[1] + (int64_t)kh * a.dv_st[2];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int e = 32 * d + 8 * q + 4 * lh;
+      store4<T>(yk, e, a.dim, a.dk_vec, dk[d][4 * q] * a.scale, dk[d][4 * q + 1] * a.scale, dk[d][4 * q + 2] * a.scale, dk[d][4 * q + 3] * a.scale);
+      store4<T>(yv, e, a.dim, a.dv_vec, dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
+    }
+}
+
+// Adds the parts: a thread has four values of a row of dq, or of a key's dk (blockIdx.y
+// = 0) or dv.
+template <typename T, bool DQ>
+__global__ __launch_bounds__(256) void attend_sum_kernel(AttendArgs a) {
+  const int per = a.dim4 / 4;
+  const int64_t rows = DQ ? (int64_t)a.q_len * a.group : a.kv_len, all = rows * a.pairs;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = i / per;
+  if (row >= all) return;
+  const int d = (int)(i - row * per) * 4;
+  const int which = blockIdx.y, each = DQ ? 1 : 2;
+  float o[4] = {};
+  for (int p = 0; p < a.parts; ++p) {
+    const float4 v = *reinterpret_cast<const float4 *>(a.part + ((p * each + which) * all + row) * a.dim4 + d);
+    o[0] += v.x;
+    o[1] += v.y;
+    o[2] += v.z;
+    o[3] += v.w;
+  }
+  const float scale = DQ || which == 0 ? a.scale : 1.0f;
+  const int pair = (int)(row / rows), r = (int)(row - pair * rows), b = pair / a.kv_heads, kh = pair - b * a.kv_heads;
+  T *y;
+  bool vec;
+  if (DQ) {
+    const int qi = r / a.group;
+    y = static_cast<T *>(a.dq) + (int64_t)b * a.dq_st[0] + (int64_t)qi * a.dq_st[1] + (int64_t)(kh * a.group + r - qi * a.group) * a.dq_st[2];
+    vec = a.dq_vec;
+  } else {
+    const int64_t *st = which ? a.dv_st : a.dk_st;
+    y = static_cast<T *>(which ? a.dv : a.dk) + (int64_t)b * st[0] + (int64_t)r * st[1] + (int64_t)kh * st[2];
+    vec = which ? a.dv_vec : a.dk_vec;
+  }
+  store4<T>(y, d, a.dim, vec, o[0] * scale, o[1] * scale, o[2] * scale, o[3] * scale);
+}
+
+template <typename T, int DP, int RW, int KW>
+hipError_t dq(const AttendArgs &a, hipStream_t s) {
+  constexpr int BN = sizeof(T) == 2 && KW * 4 * 64 * DP * 2 <= 128 * 1024 ? 64 : 32;
+  const int64_t rows = (int64_t)a.q_len * a.group, tiles = ceil_div(rows, 32 * RW);
+  hapi_launch(attend_dq_kernel<T, DP, RW, KW, BN>, dim3((uint32_t)(tiles * a.splits * a.pairs)), dim3(64 * RW * KW), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  hapi_launch(attend_sum_kernel<T, true>, dim3((uint32_t)ceil_div(rows * a.pairs * (a.dim4 / 4), 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T, int DP>
+hipError_t dq_rows(const AttendArgs &a, hipStream_t s) {
+  const int rw = attend_row_waves((int64_t)a.q_len * a.group);
+  if (rw == 4) return dq<T, DP, 4, 1>(a, s);
+  if (rw == 2) return dq<T, DP, 2, 2>(a, s);
+  return dq<T, DP, 1, (sizeof(T) == 4 && DP > 64) ? 2 : 4>(a, s);
+}
+template <typename T>
+hipError_t dq_dim(const AttendArgs &a, hipStream_t s) {
+  if (a.dim <= 32) return dq_rows<T, 32>(a, s);
+  if (a.dim <= 64) return dq_rows<T, 64>(a, s);
+  if (a.dim <= 96) return dq_rows<T, 96>(a, s);
+  return dq_rows<T, 128>(a, s);
+}
+
+template <typename T, int DP>
+hipError_t dkv(const AttendArgs &a, hipStream_t s) {
+  constexpr int BM = sizeof(T) == 2 ? 64 : 32;
+  hapi_launch(attend_dkv_kernel<T, DP, BM>, dim3((uint32_t)(ceil_div(a.kv_len, 128) * a.splits * a.pairs)), dim3(256), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  hapi_launch(attend_sum_kernel<T, false>, dim3((uint32_t)ceil_div((int64_t)a.kv_len * a.pairs * (a.dim4 / 4), 256), 2), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t dkv_dim(const AttendArgs &a, hipStream_t s) {
+  if (a.dim <= 32) return dkv<T, 32>(a, s);
+  if (a.dim <= 64) return dkv<T, 64>(a, s);
+  if (a.dim <= 96) return dkv<T, 96>(a, s);
+  return dkv<T, 128>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_attend_dq(bool bf16, const AttendArgs &a, hipStream_t s) {
+  return bf16 ? dq_dim<uint16_t>(a, s) : dq_dim<float>(a, s);
+}
+hipError_t launch_attend_dkv(bool bf16, const AttendArgs &a, hipStream_t s) {
+  return bf16 ? dkv_dim<uint16_t>(a, s) : dkv_dim<float>(a, s);
+}
+
+}  // namespace hapi

@@ -213,3 +213,84 @@ def test_rotary_tensors_must_fit_the_descriptor():
     pos = torch.zeros(2, 2, 6, dtype=torch.int64)[:, :, :3]
     assert "contiguous" in _raises(H.HAPI_E_INVAL, H.hapi_rotary_forward, d, P, P, P, P, pos, P, None, P, P)
     assert "float64" in _raises(H.HAPI_E_INVAL, H.hapi_rotary_forward, d, P, P, P, P, P, torch.zeros(32), None, P, P)
+
+
+# ----------------------------------------------------------- cross attention
+
+def _attend(batch=2, q_len=3, kv_len=5, heads=4, kv_heads=2, dim=64, dtype=BF, **kw):
+    return _ready(H.Attention(dtype, batch, q_len, kv_len, heads, kv_heads, dim, **kw))
+
+
+AF, AB = [P] * 3 + [None] * 3 + [P] * 2, [P] * 3 + [None] * 3 + [P] * 6
+
+
+def test_attention_struct_matches_the_header():
+    assert ctypes.sizeof(H.hapi_attention_desc) == 4 * 4 + 8 * 3 + 8 * 12 + 8 + 8 * 3
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=2), H.HAPI_E_INVAL), (dict(dim=0), H.HAPI_E_INVAL), (dict(dim=129), H.HAPI_E_UNSUPPORTED), (dict(heads=0), H.HAPI_E_INVAL),
+    (dict(kv_heads=0), H.HAPI_E_INVAL), (dict(heads=5), H.HAPI_E_INVAL), (dict(heads=513, kv_heads=1), H.HAPI_E_UNSUPPORTED),
+    (dict(batch=-1), H.HAPI_E_INVAL), (dict(q_len=-1), H.HAPI_E_INVAL), (dict(kv_len=-1), H.HAPI_E_INVAL), (dict(scale=-1.0), H.HAPI_E_INVAL),
+    (dict(scale=float("nan")), H.HAPI_E_INVAL), (dict(scale=float("inf")), H.HAPI_E_INVAL), (dict(q_len=1 << 31), H.HAPI_E_UNSUPPORTED),
+    (dict(kv_len=1 << 31), H.HAPI_E_UNSUPPORTED), (dict(batch=1 << 23), H.HAPI_E_UNSUPPORTED), (dict(batch=1 << 14, kv_len=1 << 20), H.HAPI_E_UNSUPPORTED),
+    (dict(q_stride=(1, 2, -3)), H.HAPI_E_INVAL), (dict(v_stride=(1 << 41, 1, 1)), H.HAPI_E_UNSUPPORTED)])
+def test_attention_descriptor_refusals(kw, code):
+    d = _attend(**kw)
+    _raises(code, H.hapi_cross_attention_workspace_bytes, d, True)
+    _raises(code, H.hapi_cross_attention_forward, d, *AF)
+    _raises(code, H.hapi_cross_attention_backward, d, *AB)
+
+
+def test_attention_pointer_refusals():
+    d = _attend()
+    d.c.reserved = 1
+    _raises(H.HAPI_E_INVAL, H.hapi_cross_attention_forward, d, *AF)
+    for fn, args in ((H.hapi_cross_attention_forward, AF), (H.hapi_cross_attention_backward, AB)):
+        for i, x in enumerate(args):
+            for bad in (None, P + 1):
+                if (x is None and bad is None) or i == 5:  # a mask is bytes, of any address
+                    continue
+                a = list(args)
+                a[i] = bad
+                _raises(H.HAPI_E_INVAL, fn, _attend(), *a)
+        for i in range(3):  # whole 16-byte rows are read as they lie
+            a = list(args)
+            a[i] = P + 8
+            assert "16-byte" in _raises(H.HAPI_E_INVAL, fn, _attend(), *a)
+        need = H.hapi_cross_attention_workspace_bytes(_attend(q_len=100), True)
+        assert need >= 2 * 4 * 100 * 4
+        _raises(H.HAPI_E_NOMEM, fn, _attend(kv_len=2000).set(workspace_bytes=64), *args)
+        _raises(H.HAPI_E_INVAL, fn, _attend().set(workspace=P + 128), *args)
+
+
+@pytest.mark.parametrize("stride", [(0, 256, 64), (768, 256, 63), (700, 256, 64), (768, 64, 64)])
+def test_attention_outputs_must_not_overlap(stride):
+    assert "o let" in _raises(H.HAPI_E_INVAL, H.hapi_cross_attention_forward, _attend(o_stride=stride), *AF)
+    assert "dq let" in _raises(H.HAPI_E_INVAL, H.hapi_cross_attention_backward, _attend(q_stride=stride), *AB)
+    for name in ("k", "v"):
+        d = _attend(kv_heads=4, kv_len=3, **{name + "_stride": stride})
+        assert f"d{name} let" in _raises(H.HAPI_E_INVAL, H.hapi_cross_attention_backward, d, *AB)
+
+
+def test_attention_tensors_must_fit_the_descriptor():
+    d = _attend()
+    q, k = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 5, 2, 64, dtype=torch.bfloat16)
+    call = lambda *a: _raises(H.HAPI_E_INVAL, H.hapi_cross_attention_forward, d, *(list(a) + AF[len(a):]))
+    assert "bfloat16" in call(q.float())
+    assert "(2, 5, 2, 64)" in call(P, q)
+    assert "strides" in call(P, P, k.transpose(0, 1).contiguous().transpose(0, 1))
+    assert "int64" in call(P, P, P, torch.zeros(2))
+    assert "(2, 5)" in call(P, P, P, None, None, torch.zeros(2, 4, dtype=torch.bool))
+    assert "bool" in call(P, P, P, None, None, torch.zeros(2, 5))
+    assert "contiguous" in call(P, P, P, None, None, torch.zeros(2, 10, dtype=torch.bool)[:, ::2])
+    assert "current GPU" in call(P, k)
+
+
+def test_attention_workspace():
+    w = H.hapi_cross_attention_workspace_bytes
+    assert w(_attend(q_len=4096, kv_len=4096, heads=16), False) == 0  # rows enough: nothing is split
+    few = _attend(q_len=1, kv_len=8192)
+    _raises(H.HAPI_E_NOMEM, H.hapi_cross_attention_forward, few.set(workspace_bytes=w(few, False) - 1), *AF)
+    # odd widths cost aligned copies
+    assert w(_attend(q_len=300, kv_len=300, dim=63), False) >= 2 * 300 * (4 + 2 + 2) * 64 * 2
