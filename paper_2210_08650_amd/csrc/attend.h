@@ -37,12 +37,15 @@ __device__ __forceinline__ f32x16_t mma(f32x8_t a, f32x8_t b, f32x16_t c) {
   for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
   return c;
 }
-__device__ __forceinline__ f32x16_t zeros() {
+// A block of one value: a product's accumulator may start from it, which subtracts a
+// row's number without an instruction of its own.
+__device__ __forceinline__ f32x16_t block_of(float v) {
   f32x16_t z;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) z[r] = 0.0f;
+  for (int r = 0; r < 16; ++r) z[r] = v;
   return z;
 }
+__device__ __forceinline__ f32x16_t zeros() { return block_of(0.0f); }
 // Registers 8 j .. 8 j + 7 of a block as an operand of 16 k, rounded to T.
 template <typename T>
 __device__ __forceinline__ typename Elem<T>::Frag operand(const f32x16_t &s, int j) {

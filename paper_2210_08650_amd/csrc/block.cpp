@@ -364,7 +364,7 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
   t.o_k = take(t.stage_k ? keys * t.ld * t.esz : 0);
   t.o_v = take(t.stage_v ? keys * t.ld * t.esz : 0);
   const int64_t shared = o;
-  t.o_ml = take(t.fwd_parts > 1 ? t.fwd_parts * all * 8 : 0);
+  t.o_ml = take(t.fwd_parts > 1 ? t.fwd_parts * all * 16 : 0);
   take(t.fwd_parts > 1 ? t.fwd_parts * all * a.dim4 * 4 : 0);
   t.bytes_fwd = o;
   o = shared;
@@ -554,8 +554,8 @@ int hapi_cross_attention_forward(const hapi_attention_desc *desc, const void *q,
   a.stats = reinterpret_cast<float2 *>(stats);
   a.splits = t.fwd_splits;
   a.parts = t.fwd_parts;
-  a.part_ml = reinterpret_cast<float2 *>(base + t.o_ml);
-  a.part = reinterpret_cast<float *>(base + t.o_ml + up((int64_t)t.fwd_parts * a.pairs * a.q_len * a.group * 8, kAlign));
+  a.part_ml = reinterpret_cast<float4 *>(base + t.o_ml);
+  a.part = reinterpret_cast<float *>(base + t.o_ml + up((int64_t)t.fwd_parts * a.pairs * a.q_len * a.group * 16, kAlign));
   HIP_TRY(launch_attend_forward(t.bf16, a, s));
   return HAPI_OK;
 }

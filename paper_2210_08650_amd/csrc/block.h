@@ -82,7 +82,7 @@ struct AttendArgs {
   float scale, c;                    // c = scale log2(e)
   int32_t splits, parts;             // of the keys (dk, dv: of the rows); parts: with the waves that share rows
   float *part;                       // [parts][pairs][rows][dim4]; dk, dv: [parts][2][pairs][kv_len][dim4]
-  float2 *part_ml;                   // [parts][pairs][rows] (reference score, sum)
+  float4 *part_ml;                   // [parts][pairs][rows] (reference score, sum about it, largest score)
   int32_t dim4;                      // dim up to a multiple of 4
   float *delta;                      // [pairs][rows] sum of dout o
 };

@@ -9,9 +9,10 @@
 // registers and one exchange with the other half-wave, and the probabilities are the
 // next product's operand as they are, o^T = V^T P^T, with V^T read transposed from LDS.
 //
-// One pass with a running maximum and sum.  The maximum is taken of the scores
-// themselves and the difference is formed before the scale: (s - m) c has no
-// rounding of m c in it.  Scores, statistics and sums are float32; probabilities are
+// One pass with a running sum about a reference score, which the products' accumulators
+// start from: the difference costs no instruction, and it is formed before the scale,
+// so that no rounding of ref c is in it.  The reference moves, and what is summed is
+// rescaled, only when a tile's largest score goes past it by more than a factor of 2^8.  Scores, statistics and sums are float32; probabilities are
 // rounded to the operands' type for the matrix cores (2^-8 of each in bf16, the sum is
 // of the unrounded ones), the output once.
 //
@@ -22,6 +23,11 @@
 
 namespace hapi {
 namespace {
+
+// (largest score, log of the sum about it) from the sum about ref.
+__device__ __forceinline__ float2 row_stats(float m, float ref, float sum, float scale) {
+  return make_float2(m, m == -INFINITY ? -INFINITY : logf(sum) - (m - ref) * scale);
+}
 
 template <typename T, int DP, int RW, int KW, int BN>
 __global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_kernel(AttendArgs a) {
@@ -75,7 +81,12 @@ __global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_
   f32x16_t o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = zeros();
-  float m = -INFINITY, sum = 0.0f;  // sum: of this half-wave's keys
+  // m: the largest score so far; ref: what is subtracted from the scores, the same until
+  // a tile goes past it by more than 2^8 in the probabilities; sum: of this half-wave's keys
+  float m = -INFINITY, ref = 0.0f, sum = 0.0f;
+  f32x16_t start = zeros();
+  bool first = true;
+  const float slack = 8.0f / a.c;
   constexpr uint64_t ALL = BN == 64 ? ~0ull : (1ull << BN) - 1;
 
   if (steps > 0) issue(0);
@@ -92,13 +103,11 @@ __global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_
     __builtin_amdgcn_sched_barrier(0);
     if (now == 0) continue;  // the same for all waves of wk
     const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE, *vt = kt + Tile::BYTES;
-    f32x16_t s[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) s[n] = zeros();
+    f32x16_t s[NT];  // scores less ref
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], s[n]);
+      for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], ks == 0 ? start : s[n]);
     if (now != ALL) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -114,20 +123,30 @@ __global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float mn = fmaxf(m, mx);
-    const float ref = mn == -INFINITY ? 0.0f : mn;  // no key yet: sums of 0, not NaN
-    const float alpha = __builtin_amdgcn_exp2f((m - ref) * a.c);
-    m = mn;
-    sum *= alpha;
+    m = fmaxf(m, ref + mx);
+    // the first key of a row sets its ref, whatever its size
+    const bool moves = mx > slack || (first && mx > -INFINITY);
+    if (__any(moves)) {
+      const float by = moves ? mx : 0.0f;
+      const float alpha = first ? 1.0f : __builtin_amdgcn_exp2f(-by * a.c);
+      first = first && !moves;
+      ref += by;
+      start = block_of(-ref);
+      sum *= alpha;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+        for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] -= by;
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[n][i] = __builtin_amdgcn_exp2f((s[n][i] - ref) * a.c);
+        s[n][i] = __builtin_amdgcn_exp2f(s[n][i] * a.c);
         sum += s[n][i];
       }
 #pragma unroll
@@ -142,7 +161,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_
   sum += __shfl_xor(sum, 32, 64);
   if (r >= rows) return;
   if (!counts) {  // padding between rows that count: as a row without keys
-    m = -INFINITY, sum = 0.0f;
+    m = -INFINITY, ref = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = zeros();
   }
@@ -156,7 +175,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_
         const int e = 32 * d + 8 * q + 4 * lh;
         if (e < a.dim4) *reinterpret_cast<float4 *>(p + e) = make_float4(o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]);
       }
-    if (lh == 0) a.part_ml[at] = make_float2(m, sum);
+    if (lh == 0) a.part_ml[at] = make_float4(ref, sum, m, 0.0f);
     return;
   }
   const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
@@ -168,7 +187,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_
     for (int q = 0; q < 4; ++q)
       store4<T>(y, 32 * d + 8 * q + 4 * lh, a.dim, a.y_vec, o[d][4 * q] * inv, o[d][4 * q + 1] * inv, o[d][4 * q + 2] * inv,
                 o[d][4 * q + 3] * inv);
-  if (lh == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = make_float2(m, logf(sum));
+  if (lh == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = row_stats(m, ref, sum, a.scale);
 }
 
 // Joins a row's parts: a thread has four of its values.
@@ -180,14 +199,18 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const int64_t row = i / per;
   if (row >= all) return;
   const int d = (int)(i - row * per) * 4;
-  float m = -INFINITY;
-  for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.part_ml[p * all + row].x);
-  const float ref = m == -INFINITY ? 0.0f : m;
+  float m = -INFINITY, ref = -INFINITY;
+  for (int p = 0; p < a.parts; ++p) {
+    const float4 ml = a.part_ml[p * all + row];
+    m = fmaxf(m, ml.z);
+    if (ml.z > -INFINITY) ref = fmaxf(ref, ml.x);
+  }
+  if (ref == -INFINITY) ref = 0.0f;  // no key: sums of 0
   float sum = 0.0f, o[4] = {};
   for (int p = 0; p < a.parts; ++p) {
-    const float2 ml = a.part_ml[p * all + row];
+    const float4 ml = a.part_ml[p * all + row];
     const float4 v = *reinterpret_cast<const float4 *>(a.part + (p * all + row) * a.dim4 + d);
-    const float w = __builtin_amdgcn_exp2f((ml.x - ref) * a.c);
+    const float w = ml.z > -INFINITY ? __builtin_amdgcn_exp2f((ml.x - ref) * a.c) : 0.0f;
     sum = fmaf(ml.y, w, sum);
     o[0] = fmaf(v.x, w, o[0]);
     o[1] = fmaf(v.y, w, o[1]);
@@ -200,7 +223,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const int64_t h = (int64_t)(pair - b * a.kv_heads) * a.group + (r - qi * a.group);
   T *y = static_cast<T *>(a.y) + (int64_t)b * a.y_st[0] + (int64_t)qi * a.y_st[1] + h * a.y_st[2];
   store4<T>(y, d, a.dim, a.y_vec, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-  if (d == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = make_float2(m, logf(sum));
+  if (d == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = row_stats(m, ref, sum, a.scale);
 }
 
 // Rows of any layout to 16-byte aligned ones, a slot of 16 bytes a thread.

@@ -21,7 +21,7 @@ namespace hapi {
 namespace {
 
 template <typename T, int DP, int RW, int KW, int BN>
-__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 && RW == 4 && DP <= 96 ? 2 : 1) void attend_dq_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 && RW == 4 ? 2 : 1) void attend_dq_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BN> Tile;
   typedef Loader<T, DP, BN, RW> Load;
   typedef typename Elem<T>::Frag Frag;
@@ -86,6 +86,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 && RW == 4 && DP <= 96
   };
   constexpr uint64_t ALL = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
 
+  const f32x16_t less_m = block_of(-m), less_delta = block_of(-delta);
   f32x16_t dq[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) dq[d] = zeros();
@@ -103,14 +104,14 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 && RW == 4 && DP <= 96
     const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE, *vt = kt + Tile::BYTES;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      f32x16_t s = zeros(), dp = zeros();
+      f32x16_t s = less_m, dp = less_delta;  // scores less m, dp less delta
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         s = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], s);
         dp = mma(Tile::by_row(vt, 32 * n, ks, lane), gf[ks], dp);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - m) * a.c - l2) * (dp[i] - delta);
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -l2)) * dp[i];
       if (now != ALL) {
         const uint32_t bits = (uint32_t)(now >> (32 * n)) >> (4 * lh);
 #pragma unroll
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
   constexpr int KS = DP / 16, DB = DP / 32, STAGE = 2 * Tile::BYTES, LOADS = Tile::DMAS / 4;
   static_assert(LOADS * 4 == Tile::DMAS && BM <= 64, "as many DMAs to every wave");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE];
-  __shared__ __attribute__((aligned(16))) float side[2][3][BM];  // m, l log2(e), delta
+  __shared__ __attribute__((aligned(16))) float side[2][3][BM];  // less m, l log2(e), delta
 
   const int t = threadIdx.x, lane = t & 63, col = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
     }
   };
   auto store_side = [&](int buf) {
-    if (t < BM) side[buf][0][t] = sm, side[buf][1][t] = sl, side[buf][2][t] = sd;
+    if (t < BM) side[buf][0][t] = -sm, side[buf][1][t] = -sl, side[buf][2][t] = -sd;
   };
 
   f32x16_t dk[DB], dv[DB];
@@ -238,26 +239,26 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
     const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES;
 #pragma unroll
     for (int n = 0; n < BM / 32; ++n) {
-      f32x16_t s = zeros(), dp = zeros();
+      typedef float f32x4_t __attribute__((ext_vector_type(4)));
+      f32x16_t s, dp, l2;  // scores less m, dp less delta
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int at = 32 * n + 8 * q + 4 * lh;
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[buf][0][at]);
+        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(&side[buf][1][at]);
+        const f32x4_t z = *reinterpret_cast<const f32x4_t *>(&side[buf][2][at]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e], l2[4 * q + e] = y[e], dp[4 * q + e] = z[e];
+      }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         s = mma(Tile::by_row(qt, 32 * n, ks, lane), kf[ks], s);
         dp = mma(Tile::by_row(gt, 32 * n, ks, lane), vf[ks], dp);
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        typedef float f32x4_t __attribute__((ext_vector_type(4)));
-        const int at = 32 * n + 8 * q + 4 * lh;
-        const f32x4_t m = *reinterpret_cast<const f32x4_t *>(&side[buf][0][at]);
-        const f32x4_t l2 = *reinterpret_cast<const f32x4_t *>(&side[buf][1][at]);
-        const f32x4_t delta = *reinterpret_cast<const f32x4_t *>(&side[buf][2][at]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 4 * q + e;
-          const float p = counts ? __builtin_amdgcn_exp2f((s[i] - m[e]) * a.c - l2[e]) : 0.0f;
-          s[i] = p;
-          dp[i] = p * (dp[i] - delta[e]);
-        }
+      for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, l2[i]));
+        dp[i] *= s[i];
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
