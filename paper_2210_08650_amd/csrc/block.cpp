@@ -288,7 +288,7 @@ struct Attend {
   int64_t batch;
   bool stage_q, stage_k, stage_v, stage_o;  // copied to aligned rows; dout lies as o does
   int64_t ld;                               // of those
-  int fwd_splits, fwd_parts, dkv_splits;
+  int fwd_splits, dkv_splits;
   int64_t bytes_fwd, bytes_bwd;
   int64_t o_q, o_k, o_v, o_o, o_g, o_part, o_ml, o_delta;  // byte offsets into the workspace
 };
@@ -345,11 +345,10 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
   t.ld = up(d->head_dim, t.v);
 
   // Few rows: the keys over as many workgroups as fill the CUs, some tiles to each wave.
-  const int kw = attend_key_waves(t.bf16, d->head_dim, rw), bn = attend_tile_keys(t.bf16, d->head_dim, kw);
-  const int64_t wgs = ceil_div(rows, 32 * rw) * pairs, want = rw == 4 ? 2 * kCus : kCus;
+  const int padded = (int)up(d->head_dim, 32), kw = attend_key_waves(t.esz, padded, rw), bn = attend_tile_keys(t.esz, padded, kw);
+  const int64_t wgs = ceil_div(rows, 32 * rw) * pairs, want = 2 * kCus;
   const int64_t key_tiles = ceil_div(d->kv_len, bn);
   t.fwd_splits = wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, key_tiles / (4 * kw), 64}));
-  t.fwd_parts = t.fwd_splits * kw;
   const int64_t kwgs = ceil_div(d->kv_len, 128) * pairs, row_tiles = ceil_div(rows, t.bf16 ? 64 : 32);
   t.dkv_splits = kwgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({2 * kCus / kwgs, row_tiles / 4, 64}));
 
@@ -364,15 +363,15 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
   t.o_k = take(t.stage_k ? keys * t.ld * t.esz : 0);
   t.o_v = take(t.stage_v ? keys * t.ld * t.esz : 0);
   const int64_t shared = o;
-  t.o_ml = take(t.fwd_parts > 1 ? t.fwd_parts * all * 16 : 0);
-  take(t.fwd_parts > 1 ? t.fwd_parts * all * a.dim4 * 4 : 0);
+  t.o_ml = take(t.fwd_splits > 1 ? t.fwd_splits * all * 16 : 0);
+  take(t.fwd_splits > 1 ? t.fwd_splits * all * a.dim4 * 4 : 0);
   t.bytes_fwd = o;
   o = shared;
   t.o_o = take(t.stage_o ? all * t.ld * t.esz : 0);
   t.o_g = take(t.stage_o ? all * t.ld * t.esz : 0);
   t.o_delta = take(all * 4);
   t.o_part = o;  // dq's, then dk's and dv's
-  take(std::max<int64_t>(t.fwd_parts > 1 ? t.fwd_parts * all * a.dim4 * 4 : 0, t.dkv_splits > 1 ? t.dkv_splits * 2 * keys * a.dim4 * 4 : 0));
+  take(std::max<int64_t>(t.fwd_splits > 1 ? t.fwd_splits * all * a.dim4 * 4 : 0, t.dkv_splits > 1 ? t.dkv_splits * 2 * keys * a.dim4 * 4 : 0));
   t.bytes_bwd = o;
   return HAPI_OK;
 }
@@ -433,16 +432,6 @@ int stage_inputs(Attend &t, const void *q, const void *k, const void *v, uint8_t
 }
 
 }  // namespace
-
-int attend_row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
-int attend_key_waves(bool bf16, int dim, int row_waves) {
-  // as many as two stages of their tiles leave room for in the LDS
-  return row_waves == 4 ? 1 : row_waves == 2 ? 2 : !bf16 && dim > 64 ? 2 : 4;
-}
-int attend_tile_keys(bool bf16, int dim, int key_waves) {
-  const int padded = (int)up(dim, 32);
-  return bf16 && key_waves * 4 * 64 * padded * 2 <= 128 * 1024 ? 64 : 32;
-}
 
 }  // namespace hapi
 
@@ -553,9 +542,8 @@ int hapi_cross_attention_forward(const hapi_attention_desc *desc, const void *q,
   a.y_vec = vec4(t, o, a.o_st);
   a.stats = reinterpret_cast<float2 *>(stats);
   a.splits = t.fwd_splits;
-  a.parts = t.fwd_parts;
   a.part_ml = reinterpret_cast<float4 *>(base + t.o_ml);
-  a.part = reinterpret_cast<float *>(base + t.o_ml + up((int64_t)t.fwd_parts * a.pairs * a.q_len * a.group * 16, kAlign));
+  a.part = reinterpret_cast<float *>(base + t.o_ml + up((int64_t)t.fwd_splits * a.pairs * a.q_len * a.group * 16, kAlign));
   HIP_TRY(launch_attend_forward(t.bf16, a, s));
   return HAPI_OK;
 }
@@ -614,11 +602,10 @@ int hapi_cross_attention_backward(const hapi_attention_desc *desc, const void *q
   a.part = reinterpret_cast<float *>(base + t.o_part);
   if (a.q_len > 0) {
     a.splits = t.fwd_splits;
-    a.parts = t.fwd_parts;
     HIP_TRY(launch_attend_dq(t.bf16, a, s));
   }
   if (a.kv_len > 0) {
-    a.splits = a.parts = t.dkv_splits;
+    a.splits = t.dkv_splits;
     HIP_TRY(launch_attend_dkv(t.bf16, a, s));
   }
   return HAPI_OK;

@@ -80,17 +80,24 @@ struct AttendArgs {
   int32_t q_len, kv_len, heads, kv_heads, group, dim;
   int32_t pairs;                     // batch * kv_heads
   float scale, c;                    // c = scale log2(e)
-  int32_t splits, parts;             // of the keys (dk, dv: of the rows); parts: with the waves that share rows
-  float *part;                       // [parts][pairs][rows][dim4]; dk, dv: [parts][2][pairs][kv_len][dim4]
-  float4 *part_ml;                   // [parts][pairs][rows] (reference score, sum about it, largest score)
+  int32_t splits;                    // of the keys (dk, dv: of the rows) over workgroups
+  float *part;                       // [splits][pairs][rows][dim4]; dk, dv: [splits][2][pairs][kv_len][dim4]
+  float4 *part_ml;                   // [splits][pairs][rows] (reference score, sum about it, largest score)
   int32_t dim4;                      // dim up to a multiple of 4
   float *delta;                      // [pairs][rows] sum of dout o
 };
 
-// Rows to a workgroup's waves: 4 x 32, 2 x 32 (two waves take other keys), 32 (all do).
-int attend_row_waves(int64_t rows);
-int attend_key_waves(bool bf16, int dim, int row_waves);
-int attend_tile_keys(bool bf16, int dim, int key_waves);
+// A workgroup's waves have 4 x 32, 2 x 32 or 32 rows between them.
+inline int attend_row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+// Up to four waves in all: those that share rows take other keys, in tiles of their own,
+// two of them in flight; 64 KB of the LDS, so that a CU runs two workgroups.
+constexpr int attend_key_waves(int esz, int padded_dim, int row_waves) {
+  const int fit = 65536 / (4 * 32 * padded_dim * esz), most = 4 / row_waves;
+  return fit < 1 ? 1 : fit < most ? (fit == 3 ? 2 : fit) : most;
+}
+constexpr int attend_tile_keys(int esz, int padded_dim, int key_waves) {
+  return esz == 2 && key_waves * 4 * 64 * padded_dim * esz <= 65536 ? 64 : 32;
+}
 // Rows from any layout to [batch][tokens][heads][ld], zeros from dim on.
 struct StageArgs {
   const void *in;

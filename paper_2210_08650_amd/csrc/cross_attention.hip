@@ -30,7 +30,7 @@ __device__ __forceinline__ float2 row_stats(float m, float ref, float sum, float
 }
 
 template <typename T, int DP, int RW, int KW, int BN>
-__global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) void attend_forward_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BN> Tile;
   typedef Loader<T, DP, BN, RW> Load;
   typedef typename Elem<T>::Frag Frag;
@@ -159,14 +159,48 @@ __global__ __launch_bounds__(64 * RW * KW, RW == 4 ? 2 : 1) void attend_forward_
       }
   }
   sum += __shfl_xor(sum, 32, 64);
+  if constexpr (KW > 1) {
+    // the waves that share rows: the others' sums to the first one's, a register of all
+    // lanes after another, in the tiles' place
+    constexpr int REGS = 3 + 16 * DB;
+    static_assert((KW - 1) * RW * REGS * 256 <= KW * 2 * STAGE, "the tiles' place");
+    float *box = reinterpret_cast<float *>(smem);
+    __syncthreads();
+    if (wk > 0) {
+      float *to = box + ((wk - 1) * RW + wr) * REGS * 64 + lane;
+      to[0] = ref, to[64] = sum, to[128] = m;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[(3 + 16 * d + i) * 64] = o[d][i];
+    }
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll
+    for (int w = 0; w < KW - 1; ++w) {
+      const float *from = box + (w * RW + wr) * REGS * 64 + lane;
+      const float ref2 = from[0], sum2 = from[64], m2 = from[128];
+      // a part without a key has no weight, and its ref no say
+      const float both = m == -INFINITY ? ref2 : m2 == -INFINITY ? ref : fmaxf(ref, ref2);
+      const float w1 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ref - both) * a.c);
+      const float w2 = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ref2 - both) * a.c);
+      ref = both;
+      m = fmaxf(m, m2);
+      sum = sum * w1 + sum2 * w2;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * w1 + from[(3 + 16 * d + i) * 64] * w2;
+    }
+  }
   if (r >= rows) return;
   if (!counts) {  // padding between rows that count: as a row without keys
     m = -INFINITY, ref = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = zeros();
   }
-  if (a.parts > 1) {
-    const int64_t at = ((int64_t)(split * KW + wk) * a.pairs + pair) * rows + r;
+  if (a.splits > 1) {
+    const int64_t at = ((int64_t)split * a.pairs + pair) * rows + r;
     float *p = a.part + at * a.dim4;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -200,14 +234,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   if (row >= all) return;
   const int d = (int)(i - row * per) * 4;
   float m = -INFINITY, ref = -INFINITY;
-  for (int p = 0; p < a.parts; ++p) {
+  for (int p = 0; p < a.splits; ++p) {
     const float4 ml = a.part_ml[p * all + row];
     m = fmaxf(m, ml.z);
     if (ml.z > -INFINITY) ref = fmaxf(ref, ml.x);
   }
   if (ref == -INFINITY) ref = 0.0f;  // no key: sums of 0
   float sum = 0.0f, o[4] = {};
-  for (int p = 0; p < a.parts; ++p) {
+  for (int p = 0; p < a.splits; ++p) {
     const float4 ml = a.part_ml[p * all + row];
     const float4 v = *reinterpret_cast<const float4 *>(a.part + (p * all + row) * a.dim4 + d);
     const float w = ml.z > -INFINITY ? __builtin_amdgcn_exp2f((ml.x - ref) * a.c) : 0.0f;
@@ -243,13 +277,13 @@ __global__ __launch_bounds__(256) void attend_stage_kernel(StageArgs a) {
   }
 }
 
-template <typename T, int DP, int RW, int KW>
+template <typename T, int DP, int RW>
 hipError_t forward(const AttendArgs &a, hipStream_t s) {
-  constexpr int BN = sizeof(T) == 2 && KW * 4 * 64 * DP * 2 <= 128 * 1024 ? 64 : 32;
+  constexpr int KW = attend_key_waves(sizeof(T), DP, RW), BN = attend_tile_keys(sizeof(T), DP, KW);
   const int64_t rows = (int64_t)a.q_len * a.group, tiles = ceil_div(rows, 32 * RW);
   hapi_launch(attend_forward_kernel<T, DP, RW, KW, BN>, dim3((uint32_t)(tiles * a.splits * a.pairs)), dim3(64 * RW * KW), 0, s, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.parts == 1) return e;
+  if (e != hipSuccess || a.splits == 1) return e;
   hapi_launch(attend_join_kernel<T>, dim3((uint32_t)ceil_div(rows * a.pairs * (a.dim4 / 4), 256)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -257,9 +291,7 @@ hipError_t forward(const AttendArgs &a, hipStream_t s) {
 template <typename T, int DP>
 hipError_t forward_rows(const AttendArgs &a, hipStream_t s) {
   const int rw = attend_row_waves((int64_t)a.q_len * a.group);
-  if (rw == 4) return forward<T, DP, 4, 1>(a, s);
-  if (rw == 2) return forward<T, DP, 2, 2>(a, s);
-  return forward<T, DP, 1, (sizeof(T) == 4 && DP > 64) ? 2 : 4>(a, s);
+  return rw == 4 ? forward<T, DP, 4>(a, s) : rw == 2 ? forward<T, DP, 2>(a, s) : forward<T, DP, 1>(a, s);
 }
 
 template <typename T>

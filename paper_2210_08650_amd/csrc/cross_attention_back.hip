@@ -21,7 +21,7 @@ namespace hapi {
 namespace {
 
 template <typename T, int DP, int RW, int KW, int BN>
-__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 && RW == 4 ? 2 : 1) void attend_dq_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void attend_dq_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BN> Tile;
   typedef Loader<T, DP, BN, RW> Load;
   typedef typename Elem<T>::Frag Frag;
@@ -126,9 +126,33 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 && RW == 4 ? 2 : 1) vo
       }
     }
   }
+  if constexpr (KW > 1) {
+    // the waves that share rows: the others' sums to the first one, a register of all
+    // lanes after another, in the tiles' place
+    static_assert((KW - 1) * RW * DB * 16 * 256 <= KW * 2 * STAGE, "the tiles' place");
+    float *box = reinterpret_cast<float *>(smem);
+    __syncthreads();
+    if (wk > 0) {
+      float *to = box + ((wk - 1) * RW + wr) * DB * 1024 + lane;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[(16 * d + i) * 64] = dq[d][i];
+    }
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll
+    for (int w = 0; w < KW - 1; ++w) {
+      const float *from = box + (w * RW + wr) * DB * 1024 + lane;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dq[d][i] += from[(16 * d + i) * 64];
+    }
+  }
   if (r >= rows) return;
-  if (a.parts > 1) {
-    float *p = a.part + (((int64_t)(split * KW + wk) * a.pairs + pair) * rows + r) * a.dim4;
+  if (a.splits > 1) {
+    float *p = a.part + (((int64_t)split * a.pairs + pair) * rows + r) * a.dim4;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -148,8 +172,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 && RW == 4 ? 2 : 1) vo
 }
 
 // BM rows at a time past 4 x 32 keys.
-template <typename T, int DP, int BM>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attend_dkv_kernel(AttendArgs a) {
+template <typename T, int DP, int BM, bool DK, bool DV>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dkv_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BM> Tile;
   typedef typename Elem<T>::Frag Frag;
   constexpr int KS = DP / 16, DB = DP / 32, STAGE = 2 * Tile::BYTES, LOADS = Tile::DMAS / 4;
@@ -174,7 +198,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     kf[ks] = row_frag<T>(kp, ks, lh, a.dim, counts);
-    vf[ks] = row_frag<T>(vp, ks, lh, a.dim, counts);
+    if (DK) vf[ks] = row_frag<T>(vp, ks, lh, a.dim, counts);
   }
 
   const int valid = tile * 128 < kv_valid ? q_valid * a.group : 0, row_tiles = (valid + BM - 1) / BM;
@@ -183,21 +207,34 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
   const T *qb = static_cast<const T *>(a.q) + (int64_t)b * a.q_st[0] + (int64_t)kh * a.group * a.q_st[2];
   const T *gb = static_cast<const T *>(a.dout) + (int64_t)b * a.g_st[0] + (int64_t)kh * a.group * a.g_st[2];
   const uint32_t magic = (1u << 20) / (uint32_t)a.group + 1;  // n / group of n < group + 64 <= 576 as n * magic >> 20
-  // byte offsets of this lane's slots from the first token of the row tile
-  auto issue = [&](int rt, int buf) {
-    const int r0 = rt * BM, i0 = __builtin_amdgcn_readfirstlane(r0 / a.group), g0 = r0 - i0 * a.group;
-    const u32x4_t qs = make_srd(qb + (int64_t)i0 * a.q_st[1]), gs = make_srd(gb + (int64_t)i0 * a.g_st[1]);
-    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + wave * LOADS * 1024);
+  // Byte offsets of this lane's slots from the row tile's first token, whose head is g0 of
+  // the group: the same for every tile where the group's heads divide a tile.
+  const uint32_t qt_ld = (uint32_t)a.q_st[1] * sizeof(T), qh_ld = (uint32_t)a.q_st[2] * sizeof(T);
+  const uint32_t gt_ld = (uint32_t)a.g_st[1] * sizeof(T), gh_ld = (uint32_t)a.g_st[2] * sizeof(T);
+  const bool fixed = BM % a.group == 0;
+  uint32_t q_off[LOADS], g_off[LOADS];
+  auto offsets = [&](int g0) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int slot = (wave * LOADS + i) * 64 + lane, lr = slot / Tile::CPR;
-      const int d = ((slot % Tile::CPR) ^ Tile::swz(lr)) * Tile::V;
-      const uint32_t n = (uint32_t)(g0 + lr), di = (n * magic) >> 20, dg = n - di * a.group;
-      const bool in = r0 + lr < valid && d < a.dim;
-      const uint32_t qo = (uint32_t)((di * a.q_st[1] + dg * a.q_st[2] + d) * (int64_t)sizeof(T));
-      const uint32_t go = (uint32_t)((di * a.g_st[1] + dg * a.g_st[2] + d) * (int64_t)sizeof(T));
-      lds_dma16(qs, lds + i * 1024, in ? qo : kOob, 0);
-      lds_dma16(gs, lds + Tile::BYTES + i * 1024, in ? go : kOob, 0);
+      const uint32_t d = ((slot % Tile::CPR) ^ Tile::swz(lr)) * Tile::V;
+      const uint32_t n = (uint32_t)(g0 + lr), di = (n * magic) >> 20, dg = n - di * (uint32_t)a.group;
+      q_off[i] = d < (uint32_t)a.dim ? di * qt_ld + dg * qh_ld + d * (uint32_t)sizeof(T) : kOob;
+      g_off[i] = d < (uint32_t)a.dim ? di * gt_ld + dg * gh_ld + d * (uint32_t)sizeof(T) : kOob;
+    }
+  };
+  offsets(0);
+  auto issue = [&](int rt, int buf) {
+    const int r0 = rt * BM, i0 = __builtin_amdgcn_readfirstlane(r0 / a.group);
+    if (!fixed) offsets(r0 - i0 * a.group);
+    const u32x4_t qs = make_srd(qb + (int64_t)i0 * a.q_st[1]), gs = make_srd(gb + (int64_t)i0 * a.g_st[1]);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + wave * LOADS * 1024);
+    const int left = valid - r0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const bool in = ((wave * LOADS + i) * 64 + lane) / Tile::CPR < left;
+      lds_dma16(qs, lds + i * 1024, in ? q_off[i] : kOob, 0);
+      lds_dma16(gs, lds + Tile::BYTES + i * 1024, in ? g_off[i] : kOob, 0);
     }
   };
   // rows that do not count, and those without a key (m = l = -inf), have p = 0
@@ -253,20 +290,24 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         s = mma(Tile::by_row(qt, 32 * n, ks, lane), kf[ks], s);
-        dp = mma(Tile::by_row(gt, 32 * n, ks, lane), vf[ks], dp);
+        if (DK) dp = mma(Tile::by_row(gt, 32 * n, ks, lane), vf[ks], dp);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, l2[i]));
-        dp[i] *= s[i];
+        if (DK) dp[i] *= s[i];
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const Frag p = operand<T>(s, j), ds = operand<T>(dp, j);
+        if constexpr (DV) {
+          const Frag p = operand<T>(s, j);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          dv[d] = mma(Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane), p, dv[d]);
-          dk[d] = mma(Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane), ds, dk[d]);
+          for (int d = 0; d < DB; ++d) dv[d] = mma(Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane), p, dv[d]);
+        }
+        if constexpr (DK) {
+          const Frag ds = operand<T>(dp, j);
+#pragma unroll
+          for (int d = 0; d < DB; ++d) dk[d] = mma(Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane), ds, dk[d]);
         }
       }
     }
@@ -277,7 +318,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
   }
-  if (a.parts > 1) {
+  if (a.splits > 1) {
     const int64_t all = (int64_t)a.pairs * a.kv_len;
     float *p = a.part + (((int64_t)split * 2) * all + (int64_t)pair * a.kv_len + key) * a.dim4;
 #pragma unroll
@@ -286,8 +327,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
       for (int q = 0; q < 4; ++q) {
         const int e = 32 * d + 8 * q + 4 * lh;
         if (e >= a.dim4) continue;
-        *reinterpret_cast<float4 *>(p + e) = make_float4(dk[d][4 * q], dk[d][4 * q + 1], dk[d][4 * q + 2], dk[d][4 * q + 3]);
-        *reinterpret_cast<float4 *>(p + all * a.dim4 + e) = make_float4(dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
+        if (DK) *reinterpret_cast<float4 *>(p + e) = make_float4(dk[d][4 * q], dk[d][4 * q + 1], dk[d][4 * q + 2], dk[d][4 * q + 3]);
+        if (DV) *reinterpret_cast<float4 *>(p + all * a.dim4 + e) = make_float4(dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
       }
     return;
   }
@@ -298,8 +339,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void atten
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int e = 32 * d + 8 * q + 4 * lh;
-      store4<T>(yk, e, a.dim, a.dk_vec, dk[d][4 * q] * a.scale, dk[d][4 * q + 1] * a.scale, dk[d][4 * q + 2] * a.scale, dk[d][4 * q + 3] * a.scale);
-      store4<T>(yv, e, a.dim, a.dv_vec, dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
+      if (DK) store4<T>(yk, e, a.dim, a.dk_vec, dk[d][4 * q] * a.scale, dk[d][4 * q + 1] * a.scale, dk[d][4 * q + 2] * a.scale, dk[d][4 * q + 3] * a.scale);
+      if (DV) store4<T>(yv, e, a.dim, a.dv_vec, dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
     }
 }
 
@@ -315,7 +356,7 @@ __global__ __launch_bounds__(256) void attend_sum_kernel(AttendArgs a) {
   const int d = (int)(i - row * per) * 4;
   const int which = blockIdx.y, each = DQ ? 1 : 2;
   float o[4] = {};
-  for (int p = 0; p < a.parts; ++p) {
+  for (int p = 0; p < a.splits; ++p) {
     const float4 v = *reinterpret_cast<const float4 *>(a.part + ((p * each + which) * all + row) * a.dim4 + d);
     o[0] += v.x;
     o[1] += v.y;
@@ -338,22 +379,20 @@ __global__ __launch_bounds__(256) void attend_sum_kernel(AttendArgs a) {
   store4<T>(y, d, a.dim, vec, o[0] * scale, o[1] * scale, o[2] * scale, o[3] * scale);
 }
 
-template <typename T, int DP, int RW, int KW>
+template <typename T, int DP, int RW>
 hipError_t dq(const AttendArgs &a, hipStream_t s) {
-  constexpr int BN = sizeof(T) == 2 && KW * 4 * 64 * DP * 2 <= 128 * 1024 ? 64 : 32;
+  constexpr int KW = attend_key_waves(sizeof(T), DP, RW), BN = attend_tile_keys(sizeof(T), DP, KW);
   const int64_t rows = (int64_t)a.q_len * a.group, tiles = ceil_div(rows, 32 * RW);
   hapi_launch(attend_dq_kernel<T, DP, RW, KW, BN>, dim3((uint32_t)(tiles * a.splits * a.pairs)), dim3(64 * RW * KW), 0, s, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.parts == 1) return e;
+  if (e != hipSuccess || a.splits == 1) return e;
   hapi_launch(attend_sum_kernel<T, true>, dim3((uint32_t)ceil_div(rows * a.pairs * (a.dim4 / 4), 256)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T, int DP>
 hipError_t dq_rows(const AttendArgs &a, hipStream_t s) {
   const int rw = attend_row_waves((int64_t)a.q_len * a.group);
-  if (rw == 4) return dq<T, DP, 4, 1>(a, s);
-  if (rw == 2) return dq<T, DP, 2, 2>(a, s);
-  return dq<T, DP, 1, (sizeof(T) == 4 && DP > 64) ? 2 : 4>(a, s);
+  return rw == 4 ? dq<T, DP, 4>(a, s) : rw == 2 ? dq<T, DP, 2>(a, s) : dq<T, DP, 1>(a, s);
 }
 template <typename T>
 hipError_t dq_dim(const AttendArgs &a, hipStream_t s) {
@@ -366,9 +405,15 @@ hipError_t dq_dim(const AttendArgs &a, hipStream_t s) {
 template <typename T, int DP>
 hipError_t dkv(const AttendArgs &a, hipStream_t s) {
   constexpr int BM = sizeof(T) == 2 ? 64 : 32;
-  hapi_launch(attend_dkv_kernel<T, DP, BM>, dim3((uint32_t)(ceil_div(a.kv_len, 128) * a.splits * a.pairs)), dim3(256), 0, s, a);
+  const dim3 grid((uint32_t)(ceil_div(a.kv_len, 128) * a.splits * a.pairs)), block(256);
+  if constexpr (sizeof(T) == 2 && DP == 128) {
+    hapi_launch(attend_dkv_kernel<T, DP, BM, true, false>, grid, block, 0, s, a);
+    hapi_launch(attend_dkv_kernel<T, DP, BM, false, true>, grid, block, 0, s, a);
+  } else {
+    hapi_launch(attend_dkv_kernel<T, DP, BM, true, true>, grid, block, 0, s, a);
+  }
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.parts == 1) return e;
+  if (e != hipSuccess || a.splits == 1) return e;
   hapi_launch(attend_sum_kernel<T, false>, dim3((uint32_t)ceil_div((int64_t)a.kv_len * a.pairs * (a.dim4 / 4), 256), 2), dim3(256), 0, s, a);
   return hipGetLastError();
 }
