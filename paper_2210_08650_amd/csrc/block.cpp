@@ -234,16 +234,18 @@ int read_rotary(const hapi_rotary_desc *d, Rotary &r) {
   TRY(read_strides(d->k_stride, d->length, d->kv_heads, d->head_dim, "k", a.x_st[1]));
   TRY(read_strides(d->q_out_stride, d->length, d->heads, d->head_dim, "q_out", a.y_st[0]));
   TRY(read_strides(d->k_out_stride, d->length, d->kv_heads, d->head_dim, "k_out", a.y_st[1]));
-  // as many values at once as the pairs and what is not rotated divide into
+  // As many values at once as the pairs' two sides and what is not rotated divide into;
+  // neighbours lie together with what is not rotated.
+  const int64_t side = d->neighbours ? 0 : pairs, rest = d->head_dim - 2 * side;
   r.v = r.bf16 ? 8 : 4;
-  while (r.v > 1 && (pairs % r.v != 0 || (d->head_dim - 2 * pairs) % (2 * r.v) != 0)) r.v /= 2;
+  while (r.v > 1 && (side % r.v != 0 || rest % (2 * r.v) != 0)) r.v /= 2;
   // Up to 8 heads a lane, so that it forms sines and cosines once for them, as long as
   // the CUs' 2048 lanes each are filled.
   int lanes = 4;
   while (lanes < 64 && lanes * 2 * r.v < d->head_dim) lanes *= 2;
   const int64_t heads = (int64_t)d->heads + d->kv_heads;
   const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, a.tokens * heads * lanes / (kCus * 2048)));
-  a.head_groups = (int32_t)ceil_div(heads, each);
+  for (int w = 0; w < 2; ++w) a.head_groups[w] = (int32_t)ceil_div(a.heads[w], each);
   return HAPI_OK;
 }
 

@@ -36,7 +36,7 @@ hipError_t launch_grad_norm(const double *part, int64_t parts, float *norm, hipS
 
 constexpr int kRotaryMaxDim = 256;
 constexpr int kRotaryAxes = 4;
-constexpr int kRotaryParts = 1024;  // partial sums of the gammas' gradients, at most
+constexpr int kRotaryParts = 512;  // partial sums of either gamma's gradient, at most
 
 struct RotaryArgs {
   const void *x[2], *dy[2];       // of q and of k
@@ -47,12 +47,12 @@ struct RotaryArgs {
   const int64_t *positions;       // [axes][tokens]
   const double *freq;             // [pairs]
   const int64_t *lens;            // [batch] or null
-  float *part;                    // [blocks][2][dim]
+  float *part;                    // [2][blocks][dim]
   float *dgamma[2];
   int64_t tokens;
   int32_t len, dim, pairs, axes;
   int32_t first[kRotaryAxes];     // an axis' first pair
-  int32_t head_groups;            // groups of lanes that share a token's heads
+  int32_t head_groups[2];         // groups of lanes that share a token's heads
   float eps, inv_dim;
   bool norm, neighbours;
 };

@@ -5,7 +5,7 @@
 // it: V values of either side of the pairs, 16 bytes each where widths, strides and
 // addresses allow it; what is not rotated goes as pairs that turn by nothing.  A lane
 // keeps its pairs over the heads of a token, so that angles, sines and cosines are
-// formed once for all of them.  The angle is position times frequency in float64,
+// formed once for all of them; q and k go to blocks of their own, each with one gamma.  The angle is position times frequency in float64,
 // reduced to a part of a turn there: in float32 its rounding at position 1e6 would be
 // 0.03 radians.  Norm, rotation and sums are float32, outputs are rounded once.
 //
@@ -22,102 +22,116 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T>
-__device__ __forceinline__ float widen(T v) {
-  if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)v << 16);
-  else return v;
-}
-
-// V values from p on; n: how many there are (V = 1: it may be none).
+// V values of a row as they lie in memory; zeros where there are none.
 template <typename T, int V>
-__device__ __forceinline__ void load(const T *p, bool there, float (&f)[V]) {
-  if constexpr (V == 1) {
-    f[0] = there ? widen(*p) : 0.0f;
-  } else {
-    T v[V];
-    __builtin_memcpy(v, p, V * sizeof(T));
+struct Raw {
+  T v[V];
+  __device__ __forceinline__ void load(const T *p, bool there) {
+    // one load of all of them, the element's alignment is enough for it on this hardware
 #pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = widen(v[j]);
+    for (int j = 0; j < V; ++j) v[j] = T{};
+    if (there) __builtin_memcpy(v, p, V * sizeof(T));
   }
-}
-template <typename T, int V>
-__device__ __forceinline__ void store(T *p, bool there, const float (&f)[V]) {
-  if constexpr (V == 1) {
-    if (there) {
-      if constexpr (sizeof(T) == 2) *p = f2bf(f[0]);
-      else *p = f[0];
+  __device__ __forceinline__ void widen(float *f) const {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if constexpr (sizeof(T) == 2) f[j] = __uint_as_float((uint32_t)v[j] << 16);
+      else f[j] = v[j];
     }
-  } else {
-    T v[V];
-    if constexpr (sizeof(T) == 2) {
+  }
+};
+template <typename T, int V>
+__device__ __forceinline__ void store(T *p, bool there, const float *f) {
+  if (!there) return;
+  T v[V];
+  if constexpr (sizeof(T) == 2) {
+    if constexpr (V == 1) {
+      v[0] = f2bf(f[0]);
+    } else {
 #pragma unroll
       for (int j = 0; j < V; j += 2) {
         const uint32_t w = f2bf2(f[j], f[j + 1]);
         __builtin_memcpy(v + j, &w, 4);
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = f[j];
     }
-    __builtin_memcpy(p, v, V * sizeof(T));
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = f[j];
   }
+  __builtin_memcpy(p, v, V * sizeof(T));
 }
 
-// LV lanes of a vector, NU units (V pairs each) of a lane.
+// LV lanes of a vector, NU units (V pairs each) of a lane.  blockIdx.y: q or k, where both
+// are there.
 template <typename T, int V, int LV, int NU, bool NEIGHBOURS, bool BACK>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
   constexpr int GPB = kThreads / LV;
   __shared__ float acc_s[BACK ? kThreads * 2 * V * NU : 1];
+  const int w = a.heads[0] > 0 ? blockIdx.y : 1;
   const int lane = threadIdx.x % LV;
-  const int D = a.dim, P = a.pairs;
+  const int D = a.dim, P = a.pairs, heads = a.heads[w], groups = a.head_groups[w];
   // where this lane's units lie
   int ea[NU], eb[NU];
-  bool there[NU], second[NU];
-  double freq[NU][V];
-  int axis[NU][V];  // kRotaryAxes: not rotated
-  float gamma[2][NU][2 * V];
+  uint32_t axis[NU];  // four bits for each pair; kRotaryAxes: not rotated
+  float gamma[NU][2 * V];
 #pragma unroll
   for (int n = 0; n < NU; ++n) {
     const int u = lane + n * LV;
-    const bool turns = u * V < P;
-    ea[n] = turns && !NEIGHBOURS ? u * V : 2 * u * V;
-    eb[n] = turns && !NEIGHBOURS ? P + u * V : 2 * u * V + V;
-    there[n] = ea[n] < D;
-    second[n] = eb[n] < D;
+    const bool halves = u * V < P && !NEIGHBOURS;
+    ea[n] = halves ? u * V : 2 * u * V;
+    eb[n] = halves ? P + u * V : 2 * u * V + V;
+    axis[n] = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      freq[n][j] = turns ? a.freq[u * V + j] : 0.0;
-      axis[n][j] = kRotaryAxes;
-      if (turns) {
+      const int i = u * V + j;
+      uint32_t x = i < P ? 0 : kRotaryAxes;
 #pragma unroll
-        for (int x = 0; x < kRotaryAxes; ++x)
-          if (x < a.axes && u * V + j >= a.first[x]) axis[n][j] = x;
-      }
+      for (int k = 1; k < kRotaryAxes; ++k)
+        if (i < P && k < a.axes && i >= a.first[k]) x = k;
+      axis[n] |= x << (4 * j);
     }
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-      for (int j = 0; j < 2 * V; ++j) {
-        const int e = j < V ? ea[n] + j : eb[n] + j - V;
-        gamma[w][n][j] = a.norm && a.heads[w] > 0 && there[n] && e < D ? a.gamma[w][e] : 1.0f;
-      }
+    for (int j = 0; j < 2 * V; ++j) {
+      const int e = j < V ? ea[n] + j : eb[n] + j - V;
+      gamma[n][j] = a.norm && e < D ? a.gamma[w][e] : 1.0f;
+    }
   }
-  float dg[2][NU][2 * V];
+  float dg[NU][2 * V];
 #pragma unroll
-  for (int w = 0; w < 2; ++w)
+  for (int n = 0; n < NU; ++n)
 #pragma unroll
-    for (int n = 0; n < NU; ++n)
-#pragma unroll
-      for (int j = 0; j < 2 * V; ++j) dg[w][n][j] = 0.0f;
+    for (int j = 0; j < 2 * V; ++j) dg[n][j] = 0.0f;
 
-  const int groups = a.head_groups, heads = a.heads[0] + a.heads[1];
   const uint32_t total = (uint32_t)(a.tokens * groups);  // < 2^31
   for (uint32_t g = blockIdx.x * GPB + threadIdx.x / LV; g < total; g += gridDim.x * GPB) {
     const uint32_t token = g / (uint32_t)groups;
     const int first_head = (int)(g - token * groups);
     const uint32_t b = token / (uint32_t)a.len, l = token - b * a.len;
     const bool counts = !a.lens || (int64_t)l < a.lens[b];
-    double pos[kRotaryAxes + 1];
+    const int64_t x0 = (int64_t)b * a.x_st[w][0] + (int64_t)l * a.x_st[w][1];
+    const int64_t y0 = (int64_t)b * a.y_st[w][0] + (int64_t)l * a.y_st[w][1];
+    const T *xp = static_cast<const T *>(a.x[w]) + x0, *dyp = static_cast<const T *>(a.dy[w]) + y0;
+    T *out = static_cast<T *>(a.y[w]) + (BACK ? x0 : y0);
+    const int64_t x_step = a.x_st[w][2], y_step = a.y_st[w][2], out_step = BACK ? x_step : y_step;
+    // a head's values as they lie in memory, the next one's on their way during this one's
+    // arithmetic; backward: dy and x
+    Raw<T, V> src[NU][2], xs[BACK ? NU : 1][2];
+    auto fetch = [&](int h) {
+#pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        const bool there = counts && h < heads && ea[n] < D, second = there && eb[n] < D;
+        const T *p = BACK ? dyp + h * y_step : xp + h * x_step;
+        src[n][0].load(p + ea[n], there);
+        src[n][1].load(p + eb[n], second);
+        if constexpr (BACK) {
+          const T *q = xp + h * x_step;
+          xs[n][0].load(q + ea[n], there && a.norm);
+          xs[n][1].load(q + eb[n], second && a.norm);
+        }
+      }
+    };
+    fetch(first_head);
+    double pos[kRotaryAxes];
 #pragma unroll
     for (int x = 0; x < kRotaryAxes; ++x) pos[x] = x < a.axes && counts ? (double)a.positions[x * a.tokens + token] : 0.0;
     float cs[NU][V], sn[NU][V];
@@ -127,44 +141,27 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
       for (int j = 0; j < V; ++j) {
         double p = 0.0;
 #pragma unroll
-        for (int x = 0; x < kRotaryAxes; ++x) p = axis[n][j] == x ? pos[x] : p;
+        for (int x = 0; x < kRotaryAxes; ++x) p = ((axis[n] >> (4 * j)) & 15) == x ? pos[x] : p;
+        const int i = (lane + n * LV) * V + j;
+        const double freq = i < P ? a.freq[i] : 0.0;  // read again for each token: 16 registers fewer for the heads' values
         // part of a turn, in [-1/2, 1/2]
-        double turn = p * freq[n][j] * 0.15915494309189535;
+        double turn = p * freq * 0.15915494309189535;
         turn -= rint(turn);
         sincospif(2.0f * (float)turn, &sn[n][j], &cs[n][j]);
         if (BACK) sn[n][j] = -sn[n][j];
       }
     for (int h = first_head; h < heads; h += groups) {
-      const int w = h >= a.heads[0];
-      const int64_t hh = w ? h - a.heads[0] : h;
-      const int64_t xo = (int64_t)b * a.x_st[w][0] + (int64_t)l * a.x_st[w][1] + hh * a.x_st[w][2];
-      const int64_t yo = (int64_t)b * a.y_st[w][0] + (int64_t)l * a.y_st[w][1] + hh * a.y_st[w][2];
-      // forward: v = x; backward: v = dy, x = x
-      float v[NU][2 * V], x[NU][2 * V];
-      const T *src = static_cast<const T *>(BACK ? a.dy[w] : a.x[w]) + (BACK ? yo : xo);
-      const T *xs = static_cast<const T *>(a.x[w]) + xo;
+      float v[NU][2 * V], x[BACK ? NU : 1][2 * V];
 #pragma unroll
       for (int n = 0; n < NU; ++n) {
-        float lo[V], hi[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) lo[j] = hi[j] = 0.0f;
-        if (counts && there[n]) {
-          load<T, V>(src + ea[n], true, lo);
-          load<T, V>(src + eb[n], second[n], hi);
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[n][j] = lo[j], v[n][V + j] = hi[j];
-        if (BACK) {
-#pragma unroll
-          for (int j = 0; j < V; ++j) lo[j] = hi[j] = 0.0f;
-          if (counts && there[n] && a.norm) {
-            load<T, V>(xs + ea[n], true, lo);
-            load<T, V>(xs + eb[n], second[n], hi);
-          }
-#pragma unroll
-          for (int j = 0; j < V; ++j) x[n][j] = lo[j], x[n][V + j] = hi[j];
+        src[n][0].widen(v[n]);
+        src[n][1].widen(v[n] + V);
+        if constexpr (BACK) {
+          xs[n][0].widen(x[n]);
+          xs[n][1].widen(x[n] + V);
         }
       }
+      fetch(h + groups);
       auto rotate = [&](int n) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -175,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
           q = q0 * cs[n][j] + p0 * sn[n][j];
         }
       };
-      if (!BACK) {
+      if constexpr (!BACK) {
         if (a.norm) {
           float ss = 0.0f;
 #pragma unroll
@@ -188,7 +185,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
 #pragma unroll
           for (int n = 0; n < NU; ++n)
 #pragma unroll
-            for (int j = 0; j < 2 * V; ++j) v[n][j] = counts ? v[n][j] * r * (w ? gamma[1][n][j] : gamma[0][n][j]) : 0.0f;
+            for (int j = 0; j < 2 * V; ++j) v[n][j] = counts ? v[n][j] * r * gamma[n][j] : 0.0f;
         }
 #pragma unroll
         for (int n = 0; n < NU; ++n) rotate(n);
@@ -202,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
 #pragma unroll
             for (int j = 0; j < 2 * V; ++j) {
               ss = fmaf(x[n][j], x[n][j], ss);
-              ex = fmaf(v[n][j] * (w ? gamma[1][n][j] : gamma[0][n][j]), x[n][j], ex);
+              ex = fmaf(v[n][j] * gamma[n][j], x[n][j], ex);
             }
 #pragma unroll
           for (int o = LV / 2; o >= 1; o >>= 1) {
@@ -216,63 +213,57 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
 #pragma unroll
             for (int j = 0; j < 2 * V; ++j) {
               const float hx = x[n][j] * r, u = v[n][j];
-              if (w) dg[1][n][j] = fmaf(u, hx, dg[1][n][j]);
-              else dg[0][n][j] = fmaf(u, hx, dg[0][n][j]);
-              v[n][j] = counts ? r * (u * (w ? gamma[1][n][j] : gamma[0][n][j]) - hx * c) : 0.0f;
+              if (counts) dg[n][j] = fmaf(u, hx, dg[n][j]);
+              v[n][j] = counts ? r * (u * gamma[n][j] - hx * c) : 0.0f;
             }
         }
       }
-      T *dst = static_cast<T *>(a.y[w]) + (BACK ? xo : yo);
+      T *dst = out + h * out_step;
 #pragma unroll
-      for (int n = 0; n < NU; ++n)
-        if (there[n]) {
-          float lo[V], hi[V];
-#pragma unroll
-          for (int j = 0; j < V; ++j) lo[j] = v[n][j], hi[j] = v[n][V + j];
-          store<T, V>(dst + ea[n], true, lo);
-          store<T, V>(dst + eb[n], second[n], hi);
-        }
+      for (int n = 0; n < NU; ++n) {
+        store<T, V>(dst + ea[n], ea[n] < D, v[n]);
+        store<T, V>(dst + eb[n], eb[n] < D, v[n] + V);
+      }
     }
   }
   if constexpr (BACK) {
     if (!a.norm) return;
     // a column's sum over the block's groups of lanes
-    for (int w = 0; w < 2; ++w) {
-      if (a.heads[w] == 0) continue;
-      __syncthreads();
 #pragma unroll
-      for (int n = 0; n < NU; ++n)
+    for (int n = 0; n < NU; ++n)
 #pragma unroll
-        for (int j = 0; j < 2 * V; ++j) acc_s[(n * 2 * V + j) * kThreads + threadIdx.x] = w ? dg[1][n][j] : dg[0][n][j];
-      __syncthreads();
-      for (int i = threadIdx.x; i < LV * NU * 2 * V; i += kThreads) {
-        const int ln = i % LV, k = i / LV, n = k / (2 * V), j = k % (2 * V);
-        const int u = ln + n * LV;
-        const bool turns = u * V < P;
-        const int e = j < V ? (turns && !NEIGHBOURS ? u * V : 2 * u * V) + j : (turns && !NEIGHBOURS ? P + u * V : 2 * u * V + V) + j - V;
-        if ((turns && !NEIGHBOURS ? u * V : 2 * u * V) >= D || e >= D) continue;
-        float s = 0.0f;
-        for (int q = 0; q < GPB; ++q) s += acc_s[k * kThreads + q * LV + ln];
-        a.part[((int64_t)blockIdx.x * 2 + w) * D + e] = s;
-      }
+      for (int j = 0; j < 2 * V; ++j) acc_s[(n * 2 * V + j) * kThreads + threadIdx.x] = dg[n][j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < LV * NU * 2 * V; i += kThreads) {
+      const int ln = i % LV, k = i / LV, n = k / (2 * V), j = k % (2 * V);
+      const int u = ln + n * LV;
+      const bool halves = u * V < P && !NEIGHBOURS;
+      const int e = j < V ? (halves ? u * V : 2 * u * V) + j : (halves ? P + u * V : 2 * u * V + V) + j - V;
+      if (e >= D) continue;
+      float s = 0.0f;
+      for (int q = 0; q < GPB; ++q) s += acc_s[k * kThreads + q * LV + ln];
+      a.part[((int64_t)w * gridDim.x + blockIdx.x) * D + e] = s;
     }
   }
 }
 
-// dgamma of q and k: 16 columns a block, 16 slices of the parts.
-__global__ __launch_bounds__(256) void rotary_reduce_kernel(RotaryArgs a, int parts) {
-  __shared__ double s[16][17];
+// dgamma of q and of k: 16 columns a block, the parts over 64 threads each.
+__global__ __launch_bounds__(1024) void rotary_reduce_kernel(RotaryArgs a, int parts) {
+  __shared__ double s[64][17];
   const int c = threadIdx.x & 15, slice = threadIdx.x >> 4;
   const int e = blockIdx.x * 16 + c, w = blockIdx.y;
   if (a.heads[w] == 0) return;
   double t = 0.0;
-  if (e < a.dim)
-    for (int p = slice; p < parts; p += 16) t += (double)a.part[((int64_t)p * 2 + w) * a.dim + e];
+  if (e < a.dim) {
+#pragma unroll 8
+    for (int p = slice; p < parts; p += 64) t += (double)a.part[((int64_t)w * parts + p) * a.dim + e];
+  }
   s[slice][c] = t;
   __syncthreads();
   if (slice == 0 && e < a.dim) {
+    t = 0.0;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) t += s[i][c];
+    for (int i = 0; i < 64; ++i) t += s[i][c];
     a.dgamma[w][e] = (float)t;
   }
 }
@@ -280,11 +271,13 @@ __global__ __launch_bounds__(256) void rotary_reduce_kernel(RotaryArgs a, int pa
 template <typename T, int V, int LV, int NU>
 hipError_t run(const RotaryArgs &a, bool back, hipStream_t s) {
   constexpr int gpb = kThreads / LV;
-  const int64_t want = ceil_div(a.tokens * a.head_groups, gpb);
-  const int64_t most = back && a.norm ? kRotaryParts : kMaxLaunchThreads / kThreads;
-  const dim3 grid((uint32_t)(want < most ? want : most)), block(kThreads);
+  const int64_t groups = a.head_groups[0] > a.head_groups[1] ? a.head_groups[0] : a.head_groups[1];
+  const int64_t want = ceil_div(a.tokens * groups, gpb);
+  const int64_t most = back && a.norm ? kRotaryParts : kMaxLaunchThreads / kThreads / 2;
+  const dim3 grid((uint32_t)(want < most ? want : most), a.heads[0] > 0 && a.heads[1] > 0 ? 2 : 1), block(kThreads);
+  const dim3 columns((a.dim + 15) / 16, 2);
   if (want == 0) {  // no tokens: the gammas' gradients are sums of nothing
-    hapi_launch(rotary_reduce_kernel, dim3((a.dim + 15) / 16, 2), dim3(256), 0, s, a, 0);
+    hapi_launch(rotary_reduce_kernel, columns, dim3(1024), 0, s, a, 0);
     return hipGetLastError();
   }
   if (a.neighbours) {
@@ -296,7 +289,7 @@ hipError_t run(const RotaryArgs &a, bool back, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !back || !a.norm) return e;
-  hapi_launch(rotary_reduce_kernel, dim3((a.dim + 15) / 16, 2), dim3(256), 0, s, a, (int)grid.x);
+  hapi_launch(rotary_reduce_kernel, columns, dim3(1024), 0, s, a, (int)grid.x);
   return hipGetLastError();
 }
 

@@ -94,7 +94,7 @@ def rotary_backward(dy, x, gamma, positions, freq, sections, neighbours=False, e
         return [(g, u * g.abs() * (1 + 2 ** -7) + 2 * eg + TINY)]
     x = torch.where(counts, x.double(), 0.0)
     gamma = gamma.double()
-    r = 1.0 / torch.sqrt((x * x).mean(-1, keepdim=True) + eps)
+    r = torch.where(counts, 1.0 / torch.sqrt((x * x).mean(-1, keepdim=True) + eps), 0.0)  # padding is in no sum
     h = x * r
     k = (2 * math.sqrt(d) + 8) * F
     eh = k * h.abs()
