@@ -53,43 +53,64 @@ struct Vec<float> {
 template <typename T, typename F>
 __device__ __forceinline__ void walk(const T *in, int64_t from, int64_t to, F &&f) {
   constexpr int N = Vec<T>::N, U = 4;
-  for (int64_t at = from + threadIdx.x * N; at < to; at += (int64_t)U * kThreads * N) {
+  constexpr int STEP = kThreads * N;
+  int64_t at = from + threadIdx.x * N;
+  // whole steps of the block without a question
+  for (const int64_t whole = to - U * STEP; at - threadIdx.x * N <= whole; at += U * STEP) {
     T v[U][N];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t i = at + (int64_t)u * kThreads * N;
-      if (i + N <= to) {
-        __builtin_memcpy(v[u], in + i, 16);
-      } else {
+    for (int u = 0; u < U; ++u) __builtin_memcpy(v[u], in + at + u * STEP, 16);
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[u][j] = i + j < to ? in[i + j] : T{};
-      }
+    for (int u = 0; u < U; ++u) f(at + u * STEP, v[u]);
+  }
+  for (; at < to; at += STEP) {
+    T v[N];
+    if (at + N <= to) {
+      __builtin_memcpy(v, in + at, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = at + j < to ? in[at + j] : T{};
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) f(at + (int64_t)u * kThreads * N, v[u]);
+    f(at, v);
   }
 }
 
-// Calls f(tensor, first value, end) for each of this block's segments.
-template <typename F>
+// Calls f(in, out, is float32, first value, end) for each of this block's segments.  The
+// tensors' entries stay in the lanes of each wave (two to a lane), so that finding a
+// segment's tensor is a comparison and a count, with no chain of loads.
+template <bool OUT, typename F>
 __device__ __forceinline__ void segments(const GradArgs &a, F &&f) {
-  const int total = a.seg[a.count];
+  static_assert(kGradTensors <= 128, "two entries to a lane");
+  const int lane = threadIdx.x & 63, total = a.seg[a.count];
+  int first[2];
+  uint64_t in[2], out[2], size[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int t = lane + 64 * i;
+    const bool there = t < a.count;
+    first[i] = there ? a.seg[t] : INT32_MAX;
+    in[i] = there ? (uint64_t)(uintptr_t)a.in[t] : 0;
+    out[i] = there && OUT ? (uint64_t)(uintptr_t)a.out[t] : 0;
+    size[i] = there ? (uint64_t)a.size[t] : 0;
+  }
+  auto of = [](const uint64_t (&v)[2], int t) {
+    const uint64_t x = t < 64 ? v[0] : v[1];
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, t & 63), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), t & 63);
+    return (uint64_t)hi << 32 | lo;
+  };
   for (int s = blockIdx.x; s < total; s += gridDim.x) {
-    int lo = 0, hi = a.count - 1;  // the last tensor whose first segment is <= s
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.seg[mid] <= s) lo = mid;
-      else hi = mid - 1;
-    }
-    const int64_t from = (int64_t)(s - a.seg[lo]) * a.seg_size;
-    const int64_t to = from + a.seg_size < a.size[lo] ? from + a.seg_size : a.size[lo];
-    f(lo, from, to);
+    // the last tensor whose first segment is <= s
+    const int t = __popcll(__ballot(first[0] <= s)) + __popcll(__ballot(first[1] <= s)) - 1;
+    const int start = t < 64 ? __builtin_amdgcn_readlane(first[0], t & 63) : __builtin_amdgcn_readlane(first[1], t & 63);
+    const int64_t n = (int64_t)of(size, t), from = (int64_t)(s - start) * a.seg_size;
+    const int64_t to = from + a.seg_size < n ? from + a.seg_size : n;
+    f((const void *)(uintptr_t)of(in, t), (void *)(uintptr_t)of(out, t), (bool)(a.f32[t >> 5] >> (t & 31) & 1), from, to);
   }
 }
 
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(GradArgs a) {
   double sum = 0.0;
-  segments(a, [&](int t, int64_t from, int64_t to) {
+  segments<false>(a, [&](const void *in, void *, bool f32, int64_t from, int64_t to) {
     auto add = [&](auto *p) {
       typedef std::remove_const_t<std::remove_pointer_t<decltype(p)>> T;
       walk(p, from, to, [&](int64_t, const T *v) {
@@ -100,8 +121,8 @@ __global__ __launch_bounds__(kThreads) void grad_squares_kernel(GradArgs a) {
         }
       });
     };
-    if (a.f32[t >> 5] >> (t & 31) & 1) add(static_cast<const float *>(a.in[t]));
-    else add(static_cast<const uint16_t *>(a.in[t]));
+    if (f32) add(static_cast<const float *>(in));
+    else add(static_cast<const uint16_t *>(in));
   });
   sum = block_sum(sum);
   if (threadIdx.x == 0) a.part[blockIdx.x] = sum;
@@ -112,8 +133,8 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
   if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
   // a norm that is not finite is the caller's to see: it changes no gradient
   const double factor = norm > a.max_norm && norm < INFINITY ? a.max_norm / norm : 1.0;
-  segments(a, [&](int t, int64_t from, int64_t to) {
-    if (factor == 1.0 && a.in[t] == a.out[t]) return;
+  segments<true>(a, [&](const void *in, void *out, bool f32, int64_t from, int64_t to) {
+    if (factor == 1.0 && in == out) return;
     auto scale = [&](auto *p, auto *o) {
       typedef std::remove_pointer_t<decltype(o)> T;
       constexpr int N = Vec<T>::N;
@@ -130,8 +151,8 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
         }
       });
     };
-    if (a.f32[t >> 5] >> (t & 31) & 1) scale(static_cast<const float *>(a.in[t]), static_cast<float *>(a.out[t]));
-    else scale(static_cast<const uint16_t *>(a.in[t]), static_cast<uint16_t *>(a.out[t]));
+    if (f32) scale(static_cast<const float *>(in), static_cast<float *>(out));
+    else scale(static_cast<const uint16_t *>(in), static_cast<uint16_t *>(out));
   });
 }
 
