@@ -390,9 +390,10 @@ int check_attend_inputs(const Attend &t, const void *q, const void *k, const voi
   return HAPI_OK;
 }
 
-// Whether four values of every row can be stored at once.
-bool vec4(const Attend &t, const void *p, const int64_t *st) {
-  return t.a.dim % 4 == 0 && st[0] % 4 == 0 && st[1] % 4 == 0 && st[2] % 4 == 0 && (uintptr_t)p % (4 * t.esz) == 0;
+// What of every row can be stored at once: bit 0, four values; bit 1, 16 bytes.
+int at_once(const Attend &t, const void *p, const int64_t *st) {
+  const auto fits = [&](int n) { return t.a.dim % n == 0 && st[0] % n == 0 && st[1] % n == 0 && st[2] % n == 0 && (uintptr_t)p % (n * t.esz) == 0; };
+  return (fits(4) ? 1 : 0) | (fits(t.v) ? 2 : 0);
 }
 
 // A copy of in, [batch][tokens][heads], with aligned rows, and its strides.
@@ -541,7 +542,7 @@ int hapi_cross_attention_forward(const hapi_attention_desc *desc, const void *q,
   a.mask = mask;
   a.y = o;
   for (int i = 0; i < 3; ++i) a.y_st[i] = a.o_st[i];
-  a.y_vec = vec4(t, o, a.o_st);
+  a.y_vec = at_once(t, o, a.o_st);
   a.stats = reinterpret_cast<float2 *>(stats);
   a.splits = t.fwd_splits;
   a.part_ml = reinterpret_cast<float4 *>(base + t.o_ml);
@@ -584,9 +585,9 @@ int hapi_cross_attention_backward(const hapi_attention_desc *desc, const void *q
     a.dv_st[i] = a.v_st[i];
     a.g_st[i] = a.o_st[i];
   }
-  a.dq_vec = vec4(t, dq, a.dq_st);
-  a.dk_vec = vec4(t, dk, a.dk_st);
-  a.dv_vec = vec4(t, dv, a.dv_st);
+  a.dq_vec = at_once(t, dq, a.dq_st);
+  a.dk_vec = at_once(t, dk, a.dk_st);
+  a.dv_vec = at_once(t, dv, a.dv_st);
   TRY(stage_inputs(t, q, k, v, base, s));
   a.o = o;
   a.dout = dout;

@@ -159,13 +159,13 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
       }
   }
   sum += __shfl_xor(sum, 32, 64);
+  __syncthreads();  // the tiles' place is used again
   if constexpr (KW > 1) {
     // the waves that share rows: the others' sums to the first one's, a register of all
     // lanes after another, in the tiles' place
     constexpr int REGS = 3 + 16 * DB;
     static_assert((KW - 1) * RW * REGS * 256 <= KW * 2 * STAGE, "the tiles' place");
     float *box = reinterpret_cast<float *>(smem);
-    __syncthreads();
     if (wk > 0) {
       float *to = box + ((wk - 1) * RW + wr) * REGS * 64 + lane;
       to[0] = ref, to[64] = sum, to[128] = m;
@@ -175,9 +175,9 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
         for (int i = 0; i < 16; ++i) to[(3 + 16 * d + i) * 64] = o[d][i];
     }
     __syncthreads();
-    if (wk > 0) return;
 #pragma unroll
     for (int w = 0; w < KW - 1; ++w) {
+      if (wk > 0) break;
       const float *from = box + (w * RW + wr) * REGS * 64 + lane;
       const float ref2 = from[0], sum2 = from[64], m2 = from[128];
       // a part without a key has no weight, and its ref no say
@@ -192,14 +192,16 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * w1 + from[(3 + 16 * d + i) * 64] * w2;
     }
+    __syncthreads();  // one wave of rows may be ahead of another
   }
-  if (r >= rows) return;
   if (!counts) {  // padding between rows that count: as a row without keys
     m = -INFINITY, ref = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = zeros();
   }
+  if (KW > 1 && wk > 0) return;
   if (a.splits > 1) {
+    if (r >= rows) return;
     const int64_t at = ((int64_t)split * a.pairs + pair) * rows + r;
     float *p = a.part + at * a.dim4;
 #pragma unroll
@@ -215,12 +217,10 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
   const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
   const int64_t h = kh * a.group + qg;
   T *y = static_cast<T *>(a.y) + (int64_t)b * a.y_st[0] + (int64_t)qi * a.y_st[1] + h * a.y_st[2];
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      store4<T>(y, 32 * d + 8 * q + 4 * lh, a.dim, a.y_vec, o[d][4 * q] * inv, o[d][4 * q + 1] * inv, o[d][4 * q + 2] * inv,
-                o[d][4 * q + 3] * inv);
+  typedef RowsOut<T, DB> Out;
+  static_assert(RW * Out::BYTES <= KW * 2 * STAGE, "the tiles' place");
+  Out::store(o, inv, r < rows ? y : nullptr, a.dim, a.y_vec & 1, a.y_vec & 2, smem + wr * Out::BYTES, lane);
+  if (r >= rows) return;
   if (lh == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = row_stats(m, ref, sum, a.scale);
 }
 
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const int b = pair / a.kv_heads;
   const int64_t h = (int64_t)(pair - b * a.kv_heads) * a.group + (r - qi * a.group);
   T *y = static_cast<T *>(a.y) + (int64_t)b * a.y_st[0] + (int64_t)qi * a.y_st[1] + h * a.y_st[2];
-  store4<T>(y, d, a.dim, a.y_vec, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  store4<T>(y, d, a.dim, a.y_vec & 1, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
   if (d == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = row_stats(m, ref, sum, a.scale);
 }
 

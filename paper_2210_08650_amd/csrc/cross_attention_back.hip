@@ -126,12 +126,12 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 64 ? 2 : 1) v
       }
     }
   }
+  __syncthreads();  // the tiles' place is used again
   if constexpr (KW > 1) {
     // the waves that share rows: the others' sums to the first one, a register of all
     // lanes after another, in the tiles' place
     static_assert((KW - 1) * RW * DB * 16 * 256 <= KW * 2 * STAGE, "the tiles' place");
     float *box = reinterpret_cast<float *>(smem);
-    __syncthreads();
     if (wk > 0) {
       float *to = box + ((wk - 1) * RW + wr) * DB * 1024 + lane;
 #pragma unroll
@@ -140,18 +140,20 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 64 ? 2 : 1) v
         for (int i = 0; i < 16; ++i) to[(16 * d + i) * 64] = dq[d][i];
     }
     __syncthreads();
-    if (wk > 0) return;
 #pragma unroll
     for (int w = 0; w < KW - 1; ++w) {
+      if (wk > 0) break;
       const float *from = box + (w * RW + wr) * DB * 1024 + lane;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) dq[d][i] += from[(16 * d + i) * 64];
     }
+    __syncthreads();  // one wave of rows may be ahead of another
   }
-  if (r >= rows) return;
+  if (KW > 1 && wk > 0) return;
   if (a.splits > 1) {
+    if (r >= rows) return;
     float *p = a.part + (((int64_t)split * a.pairs + pair) * rows + r) * a.dim4;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -163,12 +165,9 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 64 ? 2 : 1) v
     return;
   }
   T *y = static_cast<T *>(a.dq) + (int64_t)b * a.dq_st[0] + (int64_t)qi * a.dq_st[1] + h * a.dq_st[2];
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      store4<T>(y, 32 * d + 8 * q + 4 * lh, a.dim, a.dq_vec, dq[d][4 * q] * a.scale, dq[d][4 * q + 1] * a.scale,
-                dq[d][4 * q + 2] * a.scale, dq[d][4 * q + 3] * a.scale);
+  typedef RowsOut<T, DB> Out;
+  static_assert(RW * Out::BYTES <= KW * 2 * STAGE, "the tiles' place");
+  Out::store(dq, a.scale, r < rows ? y : nullptr, a.dim, a.dq_vec & 1, a.dq_vec & 2, smem + wr * Out::BYTES, lane);
 }
 
 // BM rows at a time past 4 x 32 keys.
@@ -194,13 +193,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dkv_kernel
   if (a.mask && counts) counts = a.mask[(int64_t)b * a.kv_len + key] != 0;
   const T *kp = static_cast<const T *>(a.k) + (int64_t)b * a.k_st[0] + (int64_t)key * a.k_st[1] + (int64_t)kh * a.k_st[2];
   const T *vp = static_cast<const T *>(a.v) + (int64_t)b * a.v_st[0] + (int64_t)key * a.v_st[1] + (int64_t)kh * a.v_st[2];
-  Frag kf[KS], vf[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    kf[ks] = row_frag<T>(kp, ks, lh, a.dim, counts);
-    if (DK) vf[ks] = row_frag<T>(vp, ks, lh, a.dim, counts);
-  }
-
   const int valid = tile * 128 < kv_valid ? q_valid * a.group : 0, row_tiles = (valid + BM - 1) / BM;
   const int t0 = (int)((int64_t)row_tiles * split / a.splits), t1 = (int)((int64_t)row_tiles * (split + 1) / a.splits);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
@@ -256,9 +248,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dkv_kernel
   f32x16_t dk[DB], dv[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
+  Frag kf[KS], vf[KS];
+  if (t0 < t1) issue(t0, 0);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    kf[ks] = row_frag<T>(kp, ks, lh, a.dim, counts);
+    if (DK) vf[ks] = row_frag<T>(vp, ks, lh, a.dim, counts);
+  }
   if (t0 < t1) {
     load_side(t0);
-    issue(t0, 0);
     store_side(0);
   }
   for (int rt = t0; rt < t1; ++rt) {
@@ -313,12 +311,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dkv_kernel
     }
     if (rt + 1 < t1) store_side(buf ^ 1);
   }
-  if (key >= a.kv_len) return;
   if (!counts) {  // whatever the rows hold (0 times NaN)
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
   }
   if (a.splits > 1) {
+    if (key >= a.kv_len) return;
     const int64_t all = (int64_t)a.pairs * a.kv_len;
     float *p = a.part + (((int64_t)split * 2) * all + (int64_t)pair * a.kv_len + key) * a.dim4;
 #pragma unroll
@@ -334,14 +332,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dkv_kernel
   }
   T *yk = static_cast<T *>(a.dk) + (int64_t)b * a.dk_st[0] + (int64_t)key * a.dk_st[1] + (int64_t)kh * a.dk_st[2];
   T *yv = static_cast<T *>(a.dv) + (int64_t)b * a.dv_st[0] + (int64_t)key * a.dv_st[1] + (int64_t)kh * a.dv_st[2];
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int e = 32 * d + 8 * q + 4 * lh;
-      if (DK) store4<T>(yk, e, a.dim, a.dk_vec, dk[d][4 * q] * a.scale, dk[d][4 * q + 1] * a.scale, dk[d][4 * q + 2] * a.scale, dk[d][4 * q + 3] * a.scale);
-      if (DV) store4<T>(yv, e, a.dim, a.dv_vec, dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
-    }
+  typedef RowsOut<T, DB> Out;
+  constexpr int HALF = 2 * STAGE >= 8 * Out::BYTES ? 4 * Out::BYTES : 0;  // places of their own, or one after the other
+  static_assert(4 * Out::BYTES <= 2 * STAGE, "the tiles' place");
+  __syncthreads();
+  if (DK) Out::store(dk, a.scale, key < a.kv_len ? yk : nullptr, a.dim, a.dk_vec & 1, a.dk_vec & 2, smem + wave * Out::BYTES, lane);
+  if (DV) Out::store(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim, a.dv_vec & 1, a.dv_vec & 2, smem + HALF + wave * Out::BYTES, lane);
 }
 
 // Adds the parts: a thread has four values of a row of dq, or of a key's dk (blockIdx.y
@@ -370,11 +366,11 @@ __global__ __launch_bounds__(256) void attend_sum_kernel(AttendArgs a) {
   if (DQ) {
     const int qi = r / a.group;
     y = static_cast<T *>(a.dq) + (int64_t)b * a.dq_st[0] + (int64_t)qi * a.dq_st[1] + (int64_t)(kh * a.group + r - qi * a.group) * a.dq_st[2];
-    vec = a.dq_vec;
+    vec = a.dq_vec & 1;
   } else {
     const int64_t *st = which ? a.dv_st : a.dk_st;
     y = static_cast<T *>(which ? a.dv : a.dk) + (int64_t)b * st[0] + (int64_t)r * st[1] + (int64_t)kh * st[2];
-    vec = which ? a.dv_vec : a.dk_vec;
+    vec = (which ? a.dv_vec : a.dk_vec) & 1;
   }
   store4<T>(y, d, a.dim, vec, o[0] * scale, o[1] * scale, o[2] * scale, o[3] * scale);
 }
