@@ -96,7 +96,7 @@ constexpr int attend_key_waves(int esz, int padded_dim, int row_waves) {
   return fit < 1 ? 1 : fit < most ? (fit == 3 ? 2 : fit) : most;
 }
 constexpr int attend_tile_keys(int esz, int padded_dim, int key_waves) {
-  return esz == 2 && key_waves * 4 * 64 * padded_dim * esz <= 65536 ? 64 : 32;
+  return esz == 2 && key_waves * 4 * 64 * padded_dim * esz <= (key_waves > 1 ? 32768 : 65536) ? 64 : 32;
 }
 // Rows from any layout to [batch][tokens][heads][ld], zeros from dim on.
 struct StageArgs {

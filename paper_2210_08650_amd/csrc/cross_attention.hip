@@ -233,23 +233,38 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const int64_t row = i / per;
   if (row >= all) return;
   const int d = (int)(i - row * per) * 4;
-  float m = -INFINITY, ref = -INFINITY;
-  for (int p = 0; p < a.splits; ++p) {
-    const float4 ml = a.part_ml[p * all + row];
-    m = fmaxf(m, ml.z);
-    if (ml.z > -INFINITY) ref = fmaxf(ref, ml.x);
-  }
-  if (ref == -INFINITY) ref = 0.0f;  // no key: sums of 0
-  float sum = 0.0f, o[4] = {};
-  for (int p = 0; p < a.splits; ++p) {
-    const float4 ml = a.part_ml[p * all + row];
-    const float4 v = *reinterpret_cast<const float4 *>(a.part + (p * all + row) * a.dim4 + d);
-    const float w = ml.z > -INFINITY ? __builtin_amdgcn_exp2f((ml.x - ref) * a.c) : 0.0f;
-    sum = fmaf(ml.y, w, sum);
-    o[0] = fmaf(v.x, w, o[0]);
-    o[1] = fmaf(v.y, w, o[1]);
-    o[2] = fmaf(v.z, w, o[2]);
-    o[3] = fmaf(v.w, w, o[3]);
+  float m = -INFINITY, ref = 0.0f, sum = 0.0f, o[4] = {};
+  for (int p0 = 0; p0 < a.splits; p0 += 8) {  // the loads of 8 parts in flight
+    float4 ml[8], v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = p0 + i < a.splits ? p0 + i : a.splits - 1;
+      ml[i] = a.part_ml[p * all + row];
+      v[i] = *reinterpret_cast<const float4 *>(a.part + (p * all + row) * a.dim4 + d);
+    }
+    // parts without a key have no weight, and their ref no say
+    float both = m > -INFINITY ? ref : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (p0 + i >= a.splits) ml[i].z = -INFINITY;
+      if (ml[i].z > -INFINITY) both = fmaxf(both, ml[i].x);
+    }
+    if (both == -INFINITY) both = 0.0f;
+    const float w0 = m > -INFINITY ? __builtin_amdgcn_exp2f((ref - both) * a.c) : 0.0f;
+    sum *= w0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= w0;
+    ref = both;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = ml[i].z > -INFINITY ? __builtin_amdgcn_exp2f((ml[i].x - ref) * a.c) : 0.0f;
+      m = fmaxf(m, ml[i].z);
+      sum = fmaf(ml[i].y, w, sum);
+      o[0] = fmaf(v[i].x, w, o[0]);
+      o[1] = fmaf(v[i].y, w, o[1]);
+      o[2] = fmaf(v[i].z, w, o[2]);
+      o[3] = fmaf(v[i].w, w, o[3]);
+    }
   }
   const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
   const int pair = (int)(row / rows), r = (int)(row - pair * rows), qi = r / a.group;

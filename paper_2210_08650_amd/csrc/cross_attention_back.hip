@@ -21,7 +21,7 @@ namespace hapi {
 namespace {
 
 template <typename T, int DP, int RW, int KW, int BN>
-__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void attend_dq_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? (DP <= 64 && RW > 1 ? 3 : 2) : DP <= 64 ? 2 : 1) void attend_dq_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BN> Tile;
   typedef Loader<T, DP, BN, RW> Load;
   typedef typename Elem<T>::Frag Frag;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 64 ? 2 : 1) v
     __builtin_amdgcn_sched_barrier(0);
     if (now == 0) continue;
     const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE, *vt = kt + Tile::BYTES;
-#pragma unroll
+#pragma unroll 1
     for (int n = 0; n < NT; ++n) {
       f32x16_t s = less_m, dp = less_delta;  // scores less m, dp less delta
 #pragma unroll
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 64 ? 2 : 1) v
 
 // BM rows at a time past 4 x 32 keys.
 template <typename T, int DP, int BM, bool DK, bool DV>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dkv_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void attend_dkv_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BM> Tile;
   typedef typename Elem<T>::Frag Frag;
   constexpr int KS = DP / 16, DB = DP / 32, STAGE = 2 * Tile::BYTES, LOADS = Tile::DMAS / 4;
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dkv_kernel
     }
     __builtin_amdgcn_sched_barrier(0);
     const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES;
-#pragma unroll
+#pragma unroll 1
     for (int n = 0; n < BM / 32; ++n) {
       typedef float f32x4_t __attribute__((ext_vector_type(4)));
       f32x16_t s, dp, l2;  // scores less m, dp less delta
@@ -352,12 +352,21 @@ __global__ __launch_bounds__(256) void attend_sum_kernel(AttendArgs a) {
   const int d = (int)(i - row * per) * 4;
   const int which = blockIdx.y, each = DQ ? 1 : 2;
   float o[4] = {};
-  for (int p = 0; p < a.splits; ++p) {
-    const float4 v = *reinterpret_cast<const float4 *>(a.part + ((p * each + which) * all + row) * a.dim4 + d);
-    o[0] += v.x;
-    o[1] += v.y;
-    o[2] += v.z;
-    o[3] += v.w;
+  for (int p0 = 0; p0 < a.splits; p0 += 8) {  // 8 loads in flight
+    float4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = p0 + i < a.splits ? p0 + i : a.splits - 1;
+      v[i] = *reinterpret_cast<const float4 *>(a.part + ((p * each + which) * all + row) * a.dim4 + d);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = p0 + i < a.splits ? 1.0f : 0.0f;
+      o[0] = fmaf(v[i].x, w, o[0]);
+      o[1] = fmaf(v[i].y, w, o[1]);
+      o[2] = fmaf(v[i].z, w, o[2]);
+      o[3] = fmaf(v[i].w, w, o[3]);
+    }
   }
   const float scale = DQ || which == 0 ? a.scale : 1.0f;
   const int pair = (int)(row / rows), r = (int)(row - pair * rows), b = pair / a.kv_heads, kh = pair - b * a.kv_heads;
