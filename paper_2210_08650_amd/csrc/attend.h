@@ -147,6 +147,18 @@ struct Loader {
   }
 };
 
+// Until at most N of this wave's loads and DMAs are in flight and its LDS reads are done.
+// The builtin, not asm: the compiler then knows that what was loaded before a loop has
+// arrived; it would else wait for it at its first use in every turn, and so for the DMAs
+// that the turn has just started.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // The keys of a tile that take part: a bit for each of up to 64.
 __device__ __forceinline__ uint64_t key_bits(int64_t left) {
   return left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0;

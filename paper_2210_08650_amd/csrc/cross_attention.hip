@@ -93,8 +93,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
   for (int step = 0; step < steps; ++step) {
     // this wave's DMAs have landed and its reads of the last tile are done; after the
     // barrier, everyone's
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+    wait_loads<0>();
     if constexpr (RW > 1) __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);

@@ -92,8 +92,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? (DP <= 64 && RW > 1 
   for (int d = 0; d < DB; ++d) dq[d] = zeros();
   if (steps > 0) issue(0);
   for (int step = 0; step < steps; ++step) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+    wait_loads<0>();
     if constexpr (RW > 1) __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
@@ -229,20 +228,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
       lds_dma16(gs, lds + Tile::BYTES + i * 1024, in ? g_off[i] : kOob, 0);
     }
   };
-  // rows that do not count, and those without a key (m = l = -inf), have p = 0
-  float sm, sl, sd;
+  // The rows' statistics: looked at only when they are stored, so that they are on their
+  // way during a tile's products.
+  float2 st;
+  float sd;
   auto load_side = [&](int rt) {
-    sm = INFINITY, sl = 0.0f, sd = 0.0f;
     const int r = rt * BM + t;
+    st = make_float2(-INFINITY, 0.0f), sd = 0.0f;
     if (t < BM && r < valid) {
       const int qi = r / a.group;
-      const float2 st = a.stats[((int64_t)b * a.q_len + qi) * a.heads + kh * a.group + (r - qi * a.group)];
-      if (st.x != -INFINITY) sm = st.x, sl = st.y * kLog2e;
+      st = a.stats[((int64_t)b * a.q_len + qi) * a.heads + kh * a.group + (r - qi * a.group)];
       sd = a.delta[(int64_t)pair * rows + r];
     }
   };
+  // rows that do not count, and those without a key (m = l = -inf), have p = 0
   auto store_side = [&](int buf) {
-    if (t < BM) side[buf][0][t] = -sm, side[buf][1][t] = -sl, side[buf][2][t] = -sd;
+    const bool some = st.x != -INFINITY;
+    if (t < BM) side[buf][0][t] = some ? -st.x : -INFINITY, side[buf][1][t] = some ? -st.y * kLog2e : 0.0f, side[buf][2][t] = -sd;
   };
 
   f32x16_t dk[DB], dv[DB];
@@ -261,8 +263,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
   }
   for (int rt = t0; rt < t1; ++rt) {
     const int buf = (rt - t0) & 1;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+    wait_loads<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
