@@ -619,13 +619,13 @@ int hapi_rotary_backward(const hapi_rotary_desc *desc, const void *dq_out, const
 typedef struct {
   int32_t dtype;              /* hapi_dtype of q, k, v, o and their gradients */
   int32_t head_dim;           /* 1 .. 128 */
-  int32_t heads, kv_heads;    /* heads a multiple of kv_heads, at most 512 times */
+  int32_t heads, kv_heads;    /* heads, at most 2^20, a multiple of kv_heads, at most 512 times */
   int64_t batch, q_len, kv_len;  /* >= 0; at most 2^24 tiles of 32 to 128 queries or keys */
   /* Elements between batch entries, tokens and heads, as in hapi_rotary_desc; three
    * zeros: contiguous [batch, tokens, heads, head_dim].  q: q and dq; k: k and dk; v: v and
    * dv; o: o and dout. */
   int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
-  float scale;                /* > 0; 0 = 1 / sqrt(head_dim) */
+  float scale;                /* > 0, at most 2^126; 0 = 1 / sqrt(head_dim) */
   int32_t reserved;           /* must be 0 */
   void *stream;               /* hipStream_t; NULL = the null stream */
   void *workspace;            /* device scratch, 256-byte aligned */

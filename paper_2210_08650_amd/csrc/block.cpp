@@ -303,10 +303,11 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
   if (d->head_dim > kAttendMaxDim) return fail(HAPI_E_UNSUPPORTED, "head_dim %d (at most %d)", d->head_dim, kAttendMaxDim);
   if (d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads)
     return fail(HAPI_E_INVAL, "heads must be a multiple of kv_heads, both >= 1");
+  if (d->heads > 1 << 20) return fail(HAPI_E_UNSUPPORTED, "%d heads (at most 2^20)", d->heads);
   if (d->heads / d->kv_heads > kAttendMaxGroup)
     return fail(HAPI_E_UNSUPPORTED, "%d heads share a key head (at most %d)", d->heads / d->kv_heads, kAttendMaxGroup);
   if (d->batch < 0 || d->q_len < 0 || d->kv_len < 0) return fail(HAPI_E_INVAL, "batch, q_len and kv_len must be >= 0");
-  if (!(d->scale >= 0.0f) || !std::isfinite(d->scale)) return fail(HAPI_E_INVAL, "scale must be finite and > 0, or 0");
+  if (!(d->scale >= 0.0f && d->scale <= 0x1p126f)) return fail(HAPI_E_INVAL, "scale must be in (0, 2^126], or 0");  // times log2(e) it is finite
   t = Attend{};
   AttendArgs &a = t.a;
   constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxTiles = (int64_t)1 << 24;  // 2^32 threads are too many for a launch

@@ -232,7 +232,8 @@ def test_attention_struct_matches_the_header():
     (dict(dtype=2), H.HAPI_E_INVAL), (dict(dim=0), H.HAPI_E_INVAL), (dict(dim=129), H.HAPI_E_UNSUPPORTED), (dict(heads=0), H.HAPI_E_INVAL),
     (dict(kv_heads=0), H.HAPI_E_INVAL), (dict(heads=5), H.HAPI_E_INVAL), (dict(heads=513, kv_heads=1), H.HAPI_E_UNSUPPORTED),
     (dict(batch=-1), H.HAPI_E_INVAL), (dict(q_len=-1), H.HAPI_E_INVAL), (dict(kv_len=-1), H.HAPI_E_INVAL), (dict(scale=-1.0), H.HAPI_E_INVAL),
-    (dict(scale=float("nan")), H.HAPI_E_INVAL), (dict(scale=float("inf")), H.HAPI_E_INVAL), (dict(q_len=1 << 31), H.HAPI_E_UNSUPPORTED),
+    (dict(scale=float("nan")), H.HAPI_E_INVAL), (dict(scale=float("inf")), H.HAPI_E_INVAL), (dict(scale=3e38), H.HAPI_E_INVAL),
+    (dict(batch=0, heads=1 << 30, kv_heads=1 << 30), H.HAPI_E_UNSUPPORTED), (dict(q_len=1 << 31), H.HAPI_E_UNSUPPORTED),
     (dict(kv_len=1 << 31), H.HAPI_E_UNSUPPORTED), (dict(batch=1 << 23), H.HAPI_E_UNSUPPORTED), (dict(batch=1 << 14, kv_len=1 << 20), H.HAPI_E_UNSUPPORTED),
     (dict(q_stride=(1, 2, -3)), H.HAPI_E_INVAL), (dict(v_stride=(1 << 41, 1, 1)), H.HAPI_E_UNSUPPORTED)])
 def test_attention_descriptor_refusals(kw, code):
