@@ -668,22 +668,23 @@ def _strides(field, given):
         field[:] = [int(x) for x in given]
 
 
-def _contiguous(length, heads, dim):
-    return (length * heads * dim, heads * dim, dim)
+def _layout(dtype, batch, length, heads, dim, strides):
+    """What a [batch, tokens, heads, head_dim] argument has to be: type, sizes, strides."""
+    want = tuple(int(x) for x in strides) if any(strides) else (length * heads * dim, heads * dim, dim)
+    return _TORCH_TYPES.get(dtype), (batch, length, heads, dim), want + (1,)
 
 
-def _heads(dev, p, name, dtype, shape, field):
-    """The address of a [batch, tokens, heads, head_dim] argument; of a tensor the
-    type, sizes, strides and device have to be the descriptor's and the current ones."""
+def _heads(dev, p, name, layout):
+    """The address of an argument of that layout; a tensor has to be on the current device."""
     if p is None or type(p) is int:
         return p
     if not hasattr(p, "data_ptr"):
         return _ptr(p)
+    dtype, shape, want = layout
     if p.dtype is not dtype or p.shape != shape:
         raise HapiError(HAPI_E_INVAL, f"{name} must be {dtype} of shape {shape}, got {p.dtype} {tuple(p.shape)}")
-    want = tuple(field) if any(field) else _contiguous(*shape[1:])
-    if p.numel() and any(n > 1 and a != b for n, a, b in zip(shape, p.stride(), want + (1,))):
-        raise HapiError(HAPI_E_INVAL, f"{name} must have strides {want + (1,)}, got {tuple(p.stride())}")
+    if p.stride() != want and p.numel() and any(n > 1 and a != b for n, a, b in zip(shape, p.stride(), want)):
+        raise HapiError(HAPI_E_INVAL, f"{name} must have strides {want}, got {tuple(p.stride())}")
     if p.get_device() != dev:
         raise HapiError(HAPI_E_INVAL, f"{name} is on {p.device}, not on the current GPU")
     return p.data_ptr()
@@ -691,6 +692,8 @@ def _heads(dev, p, name, dtype, shape, field):
 
 def _flat(dev, p, name, dtype, shape):
     """The address of an argument that must be contiguous."""
+    if p is None or type(p) is int:
+        return p
     if hasattr(p, "is_contiguous") and not p.is_contiguous():
         raise HapiError(HAPI_E_INVAL, f"{name} must be contiguous, got strides {tuple(p.stride())}")
     return _tensor(dev, p, name, dtype, shape)
@@ -698,7 +701,8 @@ def _flat(dev, p, name, dtype, shape):
 
 class Rotary(_TailDesc):
     """Owns a ``hapi_rotary_desc``.  ``sections``: the pairs of each axis.  Strides are
-    (batch, token, head), in elements; empty: contiguous."""
+    (batch, token, head), in elements; empty: contiguous.  Tensors are checked against
+    the sizes given here."""
     _struct = hapi_rotary_desc
 
     def __init__(self, dtype, batch, length, heads, kv_heads, head_dim, sections=(), neighbours=False, norm=True, eps=1e-6,
@@ -715,42 +719,47 @@ class Rotary(_TailDesc):
         _strides(c.k_stride, k_stride)
         _strides(c.q_out_stride, q_out_stride)
         _strides(c.k_out_stride, k_out_stride)
+        of = lambda n, st: _layout(c.dtype, c.batch, c.length, n, c.head_dim, st)
+        self.q, self.k = of(c.heads, c.q_stride), of(c.kv_heads, c.k_stride)
+        self.q_out, self.k_out = of(c.heads, c.q_out_stride), of(c.kv_heads, c.k_out_stride)
+        self.flat = (c.head_dim,), (c.axes, c.batch, c.length), (sum(c.sections),), (c.batch,)
 
 
 def hapi_rotary_workspace_bytes(desc: Rotary) -> int:
     return _check(_lib.hapi_rotary_workspace_bytes(desc.ref))
 
 
-def _rotary_common(c, dev, q_gamma, k_gamma, positions, freq, lens):
-    return (_tensor(dev, q_gamma, "q_gamma", _F32, (c.head_dim,)), _tensor(dev, k_gamma, "k_gamma", _F32, (c.head_dim,)),
-            _flat(dev, positions, "positions", torch.int64, (c.axes, c.batch, c.length)),
-            _flat(dev, freq, "freq", torch.float64, (sum(c.sections),)), _flat(dev, lens, "lens", torch.int64, (c.batch,)))
+def _rotary_common(desc, dev, q_gamma, k_gamma, positions, freq, lens):
+    dim, places, pairs, batch = desc.flat
+    return (_tensor(dev, q_gamma, "q_gamma", _F32, dim), _tensor(dev, k_gamma, "k_gamma", _F32, dim),
+            _flat(dev, positions, "positions", torch.int64, places), _flat(dev, freq, "freq", torch.float64, pairs),
+            _flat(dev, lens, "lens", torch.int64, batch))
 
 
 def hapi_rotary_forward(desc: Rotary, q, k, q_gamma, k_gamma, positions, freq, lens, q_out, k_out) -> None:
-    c, dev = desc.c, _device()
-    t, qs, ks = _TORCH_TYPES.get(c.dtype), (c.batch, c.length, c.heads, c.head_dim), (c.batch, c.length, c.kv_heads, c.head_dim)
+    dev = _device()
     _check(_lib.hapi_rotary_forward(
-        desc.ref, _heads(dev, q, "q", t, qs, c.q_stride), _heads(dev, k, "k", t, ks, c.k_stride),
-        *_rotary_common(c, dev, q_gamma, k_gamma, positions, freq, lens),
-        _heads(dev, q_out, "q_out", t, qs, c.q_out_stride), _heads(dev, k_out, "k_out", t, ks, c.k_out_stride)))
+        desc.ref, _heads(dev, q, "q", desc.q), _heads(dev, k, "k", desc.k),
+        *_rotary_common(desc, dev, q_gamma, k_gamma, positions, freq, lens),
+        _heads(dev, q_out, "q_out", desc.q_out), _heads(dev, k_out, "k_out", desc.k_out)))
 
 
 def hapi_rotary_backward(desc: Rotary, dq_out, dk_out, q, k, q_gamma, k_gamma, positions, freq, lens, dq, dk, dq_gamma,
                          dk_gamma) -> None:
-    c, dev = desc.c, _device()
-    t, qs, ks = _TORCH_TYPES.get(c.dtype), (c.batch, c.length, c.heads, c.head_dim), (c.batch, c.length, c.kv_heads, c.head_dim)
+    dev = _device()
+    dim = desc.flat[0]
     _check(_lib.hapi_rotary_backward(
-        desc.ref, _heads(dev, dq_out, "dq_out", t, qs, c.q_out_stride), _heads(dev, dk_out, "dk_out", t, ks, c.k_out_stride),
-        _heads(dev, q, "q", t, qs, c.q_stride), _heads(dev, k, "k", t, ks, c.k_stride),
-        *_rotary_common(c, dev, q_gamma, k_gamma, positions, freq, lens),
-        _heads(dev, dq, "dq", t, qs, c.q_stride), _heads(dev, dk, "dk", t, ks, c.k_stride),
-        _tensor(dev, dq_gamma, "dq_gamma", _F32, (c.head_dim,)), _tensor(dev, dk_gamma, "dk_gamma", _F32, (c.head_dim,))))
+        desc.ref, _heads(dev, dq_out, "dq_out", desc.q_out), _heads(dev, dk_out, "dk_out", desc.k_out),
+        _heads(dev, q, "q", desc.q), _heads(dev, k, "k", desc.k),
+        *_rotary_common(desc, dev, q_gamma, k_gamma, positions, freq, lens),
+        _heads(dev, dq, "dq", desc.q), _heads(dev, dk, "dk", desc.k),
+        _tensor(dev, dq_gamma, "dq_gamma", _F32, dim), _tensor(dev, dk_gamma, "dk_gamma", _F32, dim)))
 
 
 class Attention(_TailDesc):
     """Owns a ``hapi_attention_desc``.  Strides are (batch, token, head), in elements;
-    empty: contiguous.  ``scale = 0`` is 1 / sqrt(head_dim)."""
+    empty: contiguous.  ``scale = 0`` is 1 / sqrt(head_dim).  Tensors are checked against
+    the sizes given here."""
     _struct = hapi_attention_desc
 
     def __init__(self, dtype, batch, q_len, kv_len, heads, kv_heads, head_dim, scale=0.0, q_stride=(), k_stride=(),
@@ -763,33 +772,34 @@ class Attention(_TailDesc):
         _strides(c.k_stride, k_stride)
         _strides(c.v_stride, v_stride)
         _strides(c.o_stride, o_stride)
+        of = lambda l, n, st: _layout(c.dtype, c.batch, l, n, c.head_dim, st)
+        self.q, self.o = of(c.q_len, c.heads, c.q_stride), of(c.q_len, c.heads, c.o_stride)
+        self.k, self.v = of(c.kv_len, c.kv_heads, c.k_stride), of(c.kv_len, c.kv_heads, c.v_stride)
+        self.flat = (c.batch,), (c.batch, c.kv_len), (c.batch, c.q_len, c.heads, 2)
 
 
 def hapi_cross_attention_workspace_bytes(desc: Attention, backward: bool = False) -> int:
     return _check(_lib.hapi_cross_attention_workspace_bytes(desc.ref, int(bool(backward))))
 
 
-def _attention_inputs(c, dev, q, k, v, q_lens, kv_lens, mask):
-    t, ks = _TORCH_TYPES.get(c.dtype), (c.batch, c.kv_len, c.kv_heads, c.head_dim)
-    byte = mask.dtype if getattr(mask, "dtype", None) in (torch.bool, torch.uint8) else torch.bool
-    return (_heads(dev, q, "q", t, (c.batch, c.q_len, c.heads, c.head_dim), c.q_stride),
-            _heads(dev, k, "k", t, ks, c.k_stride), _heads(dev, v, "v", t, ks, c.v_stride),
-            _flat(dev, q_lens, "q_lens", torch.int64, (c.batch,)), _flat(dev, kv_lens, "kv_lens", torch.int64, (c.batch,)),
-            _flat(dev, mask, "mask", byte, (c.batch, c.kv_len)))
+def _attention_inputs(desc, dev, q, k, v, q_lens, kv_lens, mask):
+    batch, keys, _ = desc.flat
+    byte = torch.uint8 if getattr(mask, "dtype", None) is torch.uint8 else torch.bool
+    return (_heads(dev, q, "q", desc.q), _heads(dev, k, "k", desc.k), _heads(dev, v, "v", desc.v),
+            _flat(dev, q_lens, "q_lens", torch.int64, batch), _flat(dev, kv_lens, "kv_lens", torch.int64, batch),
+            _flat(dev, mask, "mask", byte, keys))
 
 
 def hapi_cross_attention_forward(desc: Attention, q, k, v, q_lens, kv_lens, mask, o, stats) -> None:
-    c, dev = desc.c, _device()
-    t, qs = _TORCH_TYPES.get(c.dtype), (c.batch, c.q_len, c.heads, c.head_dim)
+    dev = _device()
     _check(_lib.hapi_cross_attention_forward(
-        desc.ref, *_attention_inputs(c, dev, q, k, v, q_lens, kv_lens, mask), _heads(dev, o, "o", t, qs, c.o_stride),
-        _flat(dev, stats, "stats", _F32, qs[:3] + (2,))))
+        desc.ref, *_attention_inputs(desc, dev, q, k, v, q_lens, kv_lens, mask), _heads(dev, o, "o", desc.o),
+        _flat(dev, stats, "stats", _F32, desc.flat[2])))
 
 
 def hapi_cross_attention_backward(desc: Attention, q, k, v, q_lens, kv_lens, mask, o, stats, dout, dq, dk, dv) -> None:
-    c, dev = desc.c, _device()
-    t, qs, ks = _TORCH_TYPES.get(c.dtype), (c.batch, c.q_len, c.heads, c.head_dim), (c.batch, c.kv_len, c.kv_heads, c.head_dim)
+    dev = _device()
     _check(_lib.hapi_cross_attention_backward(
-        desc.ref, *_attention_inputs(c, dev, q, k, v, q_lens, kv_lens, mask), _heads(dev, o, "o", t, qs, c.o_stride),
-        _flat(dev, stats, "stats", _F32, qs[:3] + (2,)), _heads(dev, dout, "dout", t, qs, c.o_stride),
-        _heads(dev, dq, "dq", t, qs, c.q_stride), _heads(dev, dk, "dk", t, ks, c.k_stride), _heads(dev, dv, "dv", t, ks, c.v_stride)))
+        desc.ref, *_attention_inputs(desc, dev, q, k, v, q_lens, kv_lens, mask), _heads(dev, o, "o", desc.o),
+        _flat(dev, stats, "stats", _F32, desc.flat[2]), _heads(dev, dout, "dout", desc.o),
+        _heads(dev, dq, "dq", desc.q), _heads(dev, dk, "dk", desc.k), _heads(dev, dv, "dv", desc.v)))
