@@ -350,10 +350,12 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
   // Few rows: the keys over as many workgroups as fill the CUs, some tiles to each wave.
   const int padded = (int)up(d->head_dim, 32), kw = attend_key_waves(t.esz, padded, rw), bn = attend_tile_keys(t.esz, padded, kw);
   const int64_t wgs = ceil_div(rows, 32 * rw) * pairs, want = (!t.bf16 && padded > 64 ? 1 : 2) * kCus;  // as many as run at once
-  const int64_t key_tiles = ceil_div(d->kv_len, bn);
-  t.fwd_splits = wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, key_tiles / (4 * kw), 64}));
+  // A float32 tile's products take eight times as long as a bf16 one's, so one of them is
+  // worth a part of its own; of the others four.
+  const int64_t key_tiles = ceil_div(d->kv_len, bn), least = t.bf16 ? 4 : 1;
+  t.fwd_splits = wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, key_tiles / (least * kw), 64}));
   const int64_t kwgs = ceil_div(d->kv_len, 128) * pairs, row_tiles = ceil_div(rows, t.bf16 ? 64 : 32);
-  t.dkv_splits = kwgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / kwgs, row_tiles / 4, 64}));
+  t.dkv_splits = kwgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / kwgs, row_tiles / least, 64}));
 
   const int64_t all = pairs * rows, keys = pairs * d->kv_len;
   int64_t o = 0;

@@ -104,9 +104,11 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
     const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE, *vt = kt + Tile::BYTES;
     f32x16_t s[NT];  // scores less ref
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int ks = 0; ks < KS; ++ks) {
+      if (DP == 96 && ks == KS - 1 && 16 * ks >= a.dim) break;  // heads of 80: five sixths of 96
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], ks == 0 ? start : s[n]);
+    }
     if (now != ALL) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {

@@ -106,6 +106,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? (DP <= 64 && RW > 1 
       f32x16_t s = less_m, dp = less_delta;  // scores less m, dp less delta
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
+        if (DP == 96 && ks == KS - 1 && 16 * ks >= a.dim) break;  // heads of 80: five sixths of 96
         s = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], s);
         dp = mma(Tile::by_row(vt, 32 * n, ks, lane), gf[ks], dp);
       }
@@ -288,6 +289,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
       }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
+        if (DP == 96 && ks == KS - 1 && 16 * ks >= a.dim) break;
         s = mma(Tile::by_row(qt, 32 * n, ks, lane), kf[ks], s);
         if (DK) dp = mma(Tile::by_row(gt, 32 * n, ks, lane), vf[ks], dp);
       }
