@@ -354,8 +354,9 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
   // worth a part of its own; of the others four.
   const int64_t key_tiles = ceil_div(d->kv_len, bn), least = t.bf16 ? 4 : 1;
   t.fwd_splits = wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, key_tiles / (least * kw), 64}));
+  const int64_t dkv_want = padded > 96 ? kCus : want;  // one workgroup a CU
   const int64_t kwgs = ceil_div(d->kv_len, 128) * pairs, row_tiles = ceil_div(rows, t.bf16 ? 64 : 32);
-  t.dkv_splits = kwgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / kwgs, row_tiles / least, 64}));
+  t.dkv_splits = kwgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({dkv_want / kwgs, row_tiles / least, 64}));
 
   const int64_t all = pairs * rows, keys = pairs * d->kv_len;
   int64_t o = 0;

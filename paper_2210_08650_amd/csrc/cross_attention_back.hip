@@ -170,6 +170,44 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? (DP <= 64 && RW > 1 
   Out::store(dq, a.scale, r < rows ? y : nullptr, a.dim, a.dq_vec & 1, a.dq_vec & 2, smem + wr * Out::BYTES, lane);
 }
 
+// How WAVES waves bring tiles of rows, q and dout, to LDS.  The rows are the tokens of a
+// group's heads, so a lane's offsets from the tile's first token depend on that row's head
+// in the group: the same for every tile where the group's heads divide a tile.
+template <typename T, int DP, int BM, int WAVES>
+struct RowLoader {
+  typedef hapi::Tile<T, DP, BM> Tile;
+  static constexpr int LOADS = Tile::DMAS / WAVES;
+  uint32_t q_off[LOADS], g_off[LOADS];
+  __device__ __forceinline__ void offsets(const AttendArgs &a, int g0, int wave, int lane) {
+    const uint32_t qt_ld = (uint32_t)a.q_st[1] * sizeof(T), qh_ld = (uint32_t)a.q_st[2] * sizeof(T);
+    const uint32_t gt_ld = (uint32_t)a.g_st[1] * sizeof(T), gh_ld = (uint32_t)a.g_st[2] * sizeof(T);
+    const uint32_t magic = (1u << 20) / (uint32_t)a.group + 1;  // n / group of n < group + 64 <= 576 as n * magic >> 20
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int slot = (wave * LOADS + i) * 64 + lane, lr = slot / Tile::CPR;
+      const uint32_t d = ((slot % Tile::CPR) ^ Tile::swz(lr)) * Tile::V;
+      const uint32_t n = (uint32_t)(g0 + lr), di = (n * magic) >> 20, dg = n - di * (uint32_t)a.group;
+      q_off[i] = d < (uint32_t)a.dim ? di * qt_ld + dg * qh_ld + d * (uint32_t)sizeof(T) : kOob;
+      g_off[i] = d < (uint32_t)a.dim ? di * gt_ld + dg * gh_ld + d * (uint32_t)sizeof(T) : kOob;
+    }
+  }
+  __device__ __forceinline__ void init(const AttendArgs &a, int wave, int lane) { offsets(a, 0, wave, lane); }
+  // Row tile rt of `valid` rows to lds; q's rows, then dout's.  qb, gb: the group's first head.
+  __device__ __forceinline__ void issue(const AttendArgs &a, const T *qb, const T *gb, int rt, int valid, uint32_t lds, int wave, int lane) {
+    const int r0 = rt * BM, i0 = __builtin_amdgcn_readfirstlane(r0 / a.group);
+    if (BM % a.group != 0) offsets(a, r0 - i0 * a.group, wave, lane);
+    const u32x4_t qs = make_srd(qb + (int64_t)i0 * a.q_st[1]), gs = make_srd(gb + (int64_t)i0 * a.g_st[1]);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * LOADS * 1024);
+    const int left = valid - r0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const bool in = ((wave * LOADS + i) * 64 + lane) / Tile::CPR < left;
+      lds_dma16(qs, to + i * 1024, in ? q_off[i] : kOob, 0);
+      lds_dma16(gs, to + Tile::BYTES + i * 1024, in ? g_off[i] : kOob, 0);
+    }
+  }
+};
+
 // BM rows at a time past 4 x 32 keys.
 template <typename T, int DP, int BM, bool DK, bool DV>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void attend_dkv_kernel(AttendArgs a) {
@@ -198,37 +236,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
   const T *qb = static_cast<const T *>(a.q) + (int64_t)b * a.q_st[0] + (int64_t)kh * a.group * a.q_st[2];
   const T *gb = static_cast<const T *>(a.dout) + (int64_t)b * a.g_st[0] + (int64_t)kh * a.group * a.g_st[2];
-  const uint32_t magic = (1u << 20) / (uint32_t)a.group + 1;  // n / group of n < group + 64 <= 576 as n * magic >> 20
-  // Byte offsets of this lane's slots from the row tile's first token, whose head is g0 of
-  // the group: the same for every tile where the group's heads divide a tile.
-  const uint32_t qt_ld = (uint32_t)a.q_st[1] * sizeof(T), qh_ld = (uint32_t)a.q_st[2] * sizeof(T);
-  const uint32_t gt_ld = (uint32_t)a.g_st[1] * sizeof(T), gh_ld = (uint32_t)a.g_st[2] * sizeof(T);
-  const bool fixed = BM % a.group == 0;
-  uint32_t q_off[LOADS], g_off[LOADS];
-  auto offsets = [&](int g0) {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int slot = (wave * LOADS + i) * 64 + lane, lr = slot / Tile::CPR;
-      const uint32_t d = ((slot % Tile::CPR) ^ Tile::swz(lr)) * Tile::V;
-      const uint32_t n = (uint32_t)(g0 + lr), di = (n * magic) >> 20, dg = n - di * (uint32_t)a.group;
-      q_off[i] = d < (uint32_t)a.dim ? di * qt_ld + dg * qh_ld + d * (uint32_t)sizeof(T) : kOob;
-      g_off[i] = d < (uint32_t)a.dim ? di * gt_ld + dg * gh_ld + d * (uint32_t)sizeof(T) : kOob;
-    }
-  };
-  offsets(0);
-  auto issue = [&](int rt, int buf) {
-    const int r0 = rt * BM, i0 = __builtin_amdgcn_readfirstlane(r0 / a.group);
-    if (!fixed) offsets(r0 - i0 * a.group);
-    const u32x4_t qs = make_srd(qb + (int64_t)i0 * a.q_st[1]), gs = make_srd(gb + (int64_t)i0 * a.g_st[1]);
-    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + wave * LOADS * 1024);
-    const int left = valid - r0;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const bool in = ((wave * LOADS + i) * 64 + lane) / Tile::CPR < left;
-      lds_dma16(qs, lds + i * 1024, in ? q_off[i] : kOob, 0);
-      lds_dma16(gs, lds + Tile::BYTES + i * 1024, in ? g_off[i] : kOob, 0);
-    }
-  };
+  RowLoader<T, DP, BM, 4> load;
+  load.init(a, wave, lane);
+  auto issue = [&](int rt, int buf) { load.issue(a, qb, gb, rt, valid, lds0 + buf * STAGE, wave, lane); };
   // The rows' statistics: looked at only when they are stored, so that they are on their
   // way during a tile's products.
   float2 st;
@@ -343,6 +353,186 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
   if (DV) Out::store(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim, a.dv_vec & 1, a.dv_vec & 2, smem + HALF + wave * Out::BYTES, lane);
 }
 
+// dk and dv of 128-value heads in 16 bits.  A wave that kept 32 keys' k, v, dk and dv would
+// take 366 registers, one wave to a SIMD, and dk and dv in kernels of their own form the
+// scores and their exponentials twice (2 x 4096 x 4096, 16 + 4 heads: 890 us, 415 + 300
+// us).  Here two waves share 32 keys: each forms P and dS of one half of a tile's 64 rows,
+// passes them on in LDS as operands, and sums half the values of dk and dv over all 64.
+// A tile's products with P and dS are those of the step after the one that forms them, so
+// that they stand beside the next exponentials, which need nothing of them.
+__global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
+  typedef uint16_t T;
+  constexpr int DP = 128, BM = 64, KS = DP / 16, DB = 2, WAVES = 8;
+  typedef hapi::Tile<T, DP, BM> Tile;
+  typedef typename Elem<T>::Frag Frag;
+  constexpr int STAGE = 2 * Tile::BYTES, LOADS = Tile::DMAS / WAVES;
+  static_assert(LOADS * WAVES == Tile::DMAS, "as many DMAs to every wave");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[3 * STAGE];
+  // P and dS: [key group][half of the rows][16 rows][P, dS][lane]
+  __shared__ __attribute__((aligned(1024))) uint8_t passed[4 * 2 * 2 * 2 * 1024];
+  __shared__ __attribute__((aligned(16))) float side[2][3][BM];  // less m, l log2(e), delta
+
+  const int t = threadIdx.x, lane = t & 63, col = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6), kg = wave & 3, half = wave >> 2;
+  const int rows = a.q_len * a.group, tiles = (a.kv_len + 127) / 128;
+  const Place at = place(a, tiles);
+  const int tile = at.tile, split = at.split, pair = at.pair, b = at.b, kh = at.kh;
+  const int q_valid = clamped(a.q_lens, b, a.q_len), kv_valid = clamped(a.kv_lens, b, a.kv_len);
+
+  // this lane's key
+  const int key = tile * 128 + kg * 32 + col;
+  bool counts = key < kv_valid;
+  if (a.mask && counts) counts = a.mask[(int64_t)b * a.kv_len + key] != 0;
+  const T *kp = static_cast<const T *>(a.k) + (int64_t)b * a.k_st[0] + (int64_t)key * a.k_st[1] + (int64_t)kh * a.k_st[2];
+  const T *vp = static_cast<const T *>(a.v) + (int64_t)b * a.v_st[0] + (int64_t)key * a.v_st[1] + (int64_t)kh * a.v_st[2];
+
+  const int valid = tile * 128 < kv_valid ? q_valid * a.group : 0, row_tiles = (valid + BM - 1) / BM;
+  const int t0 = (int)((int64_t)row_tiles * split / a.splits), t1 = (int)((int64_t)row_tiles * (split + 1) / a.splits);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+  const T *qb = static_cast<const T *>(a.q) + (int64_t)b * a.q_st[0] + (int64_t)kh * a.group * a.q_st[2];
+  const T *gb = static_cast<const T *>(a.dout) + (int64_t)b * a.g_st[0] + (int64_t)kh * a.group * a.g_st[2];
+  RowLoader<T, DP, BM, WAVES> load;
+  load.init(a, wave, lane);
+  auto issue = [&](int rt, int buf) { load.issue(a, qb, gb, rt, valid, lds0 + buf * STAGE, wave, lane); };
+  float2 st;
+  float sd;
+  auto load_side = [&](int rt) {
+    const int r = rt * BM + t;
+    st = make_float2(-INFINITY, 0.0f), sd = 0.0f;
+    if (t < BM && r < valid) {
+      const int qi = r / a.group;
+      st = a.stats[((int64_t)b * a.q_len + qi) * a.heads + kh * a.group + (r - qi * a.group)];
+      sd = a.delta[(int64_t)pair * rows + r];
+    }
+  };
+  auto store_side = [&](int buf) {
+    const bool some = st.x != -INFINITY;
+    if (t < BM) side[buf][0][t] = some ? -st.x : -INFINITY, side[buf][1][t] = some ? -st.y * kLog2e : 0.0f, side[buf][2][t] = -sd;
+  };
+
+  f32x16_t dk[DB], dv[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
+  Frag kf[KS], vf[KS];
+  if (t0 < t1) issue(t0, 0);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    kf[ks] = row_frag<T>(kp, ks, lh, a.dim, counts);
+    vf[ks] = row_frag<T>(vp, ks, lh, a.dim, counts);
+  }
+  if (t0 < t1) {
+    load_side(t0);
+    store_side(0);
+  }
+  f32x16_t s, dp, l2;  // scores less m, dp less delta of this wave's half
+  auto scores = [&](int buf, int sb) {
+    typedef float f32x4_t __attribute__((ext_vector_type(4)));
+    const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int i = 32 * half + 8 * q + 4 * lh;
+      const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[sb][0][i]);
+      const f32x4_t y = *reinterpret_cast<const f32x4_t *>(&side[sb][1][i]);
+      const f32x4_t z = *reinterpret_cast<const f32x4_t *>(&side[sb][2][i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e], l2[4 * q + e] = y[e], dp[4 * q + e] = z[e];
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      s = mma(Tile::by_row(qt, 32 * half, ks, lane), kf[ks], s);
+      dp = mma(Tile::by_row(gt, 32 * half, ks, lane), vf[ks], dp);
+    }
+  };
+  auto probabilities = [&]() {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, l2[i]));
+      dp[i] *= s[i];
+    }
+  };
+  uint8_t *const mine = passed + ((kg * 2 + half) * 4) * 1024 + lane * 16;
+  auto pass = [&]() {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      *reinterpret_cast<Frag *>(mine + (2 * j) * 1024) = operand<T>(s, j);
+      *reinterpret_cast<Frag *>(mine + (2 * j + 1) * 1024) = operand<T>(dp, j);
+    }
+  };
+  auto sums = [&](int buf) {
+    const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // 16 rows each
+      const uint8_t *from = passed + ((kg * 2 + (i >> 1)) * 4 + 2 * (i & 1)) * 1024 + lane * 16;
+      const Frag p = *reinterpret_cast<const Frag *>(from), ds = *reinterpret_cast<const Frag *>(from + 1024);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        dv[d] = mma(Tile::by_column(gt, 16 * i, 64 * half + 32 * d, lane), p, dv[d]);
+        dk[d] = mma(Tile::by_column(qt, 16 * i, 64 * half + 32 * d, lane), ds, dk[d]);
+      }
+    }
+  };
+  auto meet = [&]() {
+    wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto meet_lds = [&]() {  // DMAs and loads stay in flight
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((63 & 15) | ((63 >> 4) << 14) | (7 << 4));
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int buf = 0;  // of tile rt
+  for (int rt = t0; rt < t1; ++rt) {
+    const int next = buf == 2 ? 0 : buf + 1, last = buf == 0 ? 2 : buf - 1;
+    meet();  // tile rt is there; so are the last tile's P and dS
+    if (rt + 1 < t1) {
+      load_side(rt + 1);
+      issue(rt + 1, next);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    scores(buf, (rt - t0) & 1);
+    if (rt > t0) sums(last);
+    probabilities();
+    meet_lds();  // all have read the last tile's P and dS
+    pass();
+    if (rt + 1 < t1) store_side((rt + 1 - t0) & 1);
+    buf = next;
+  }
+  meet();
+  if (t0 < t1) sums(buf == 0 ? 2 : buf - 1);
+  if (!counts) {  // whatever the rows hold (0 times NaN)
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
+  }
+  const int d0 = 64 * half;
+  if (a.splits > 1) {
+    if (key >= a.kv_len) return;
+    const int64_t all = (int64_t)a.pairs * a.kv_len;
+    float *p = a.part + (((int64_t)split * 2) * all + (int64_t)pair * a.kv_len + key) * a.dim4;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int e = d0 + 32 * d + 8 * q + 4 * lh;
+        if (e >= a.dim4) continue;
+        *reinterpret_cast<float4 *>(p + e) = make_float4(dk[d][4 * q], dk[d][4 * q + 1], dk[d][4 * q + 2], dk[d][4 * q + 3]);
+        *reinterpret_cast<float4 *>(p + all * a.dim4 + e) = make_float4(dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
+      }
+    return;
+  }
+  T *yk = static_cast<T *>(a.dk) + (int64_t)b * a.dk_st[0] + (int64_t)key * a.dk_st[1] + (int64_t)kh * a.dk_st[2] + d0;
+  T *yv = static_cast<T *>(a.dv) + (int64_t)b * a.dv_st[0] + (int64_t)key * a.dv_st[1] + (int64_t)kh * a.dv_st[2] + d0;
+  typedef RowsOut<T, DB> Out;
+  static_assert(2 * WAVES * Out::BYTES <= 3 * STAGE, "the tiles' place");
+  __syncthreads();
+  Out::store(dk, a.scale, key < a.kv_len ? yk : nullptr, a.dim - d0, a.dk_vec & 1, a.dk_vec & 2, smem + wave * Out::BYTES, lane);
+  Out::store(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim - d0, a.dv_vec & 1, a.dv_vec & 2, smem + (WAVES + wave) * Out::BYTES, lane);
+}
+
 // Adds the parts: a thread has four values of a row of dq, or of a key's dk (blockIdx.y
 // = 0) or dv.
 template <typename T, bool DQ>
@@ -415,8 +605,7 @@ hipError_t dkv(const AttendArgs &a, hipStream_t s) {
   constexpr int BM = sizeof(T) == 2 ? 64 : 32;
   const dim3 grid((uint32_t)(ceil_div(a.kv_len, 128) * a.splits * a.pairs)), block(256);
   if constexpr (sizeof(T) == 2 && DP == 128) {
-    hapi_launch(attend_dkv_kernel<T, DP, BM, true, false>, grid, block, 0, s, a);
-    hapi_launch(attend_dkv_kernel<T, DP, BM, false, true>, grid, block, 0, s, a);
+    hapi_launch(attend_dkv_pair_kernel, grid, dim3(512), 0, s, a);
   } else {
     hapi_launch(attend_dkv_kernel<T, DP, BM, true, true>, grid, block, 0, s, a);
   }
