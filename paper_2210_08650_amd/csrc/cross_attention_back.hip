@@ -15,6 +15,8 @@
 // parts of dq could be added by atomics or went through memory (4 bytes of each value
 // for every 128 keys).  P and dS are rounded to the operands' type for the matrix
 // cores; all sums are float32.
+#include <type_traits>
+
 #include "attend.h"
 
 namespace hapi {
@@ -424,32 +426,8 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
     load_side(t0);
     store_side(0);
   }
-  f32x16_t s, dp, l2;  // scores less m, dp less delta of this wave's half
-  auto scores = [&](int buf, int sb) {
-    typedef float f32x4_t __attribute__((ext_vector_type(4)));
-    const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int i = 32 * half + 8 * q + 4 * lh;
-      const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[sb][0][i]);
-      const f32x4_t y = *reinterpret_cast<const f32x4_t *>(&side[sb][1][i]);
-      const f32x4_t z = *reinterpret_cast<const f32x4_t *>(&side[sb][2][i]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e], l2[4 * q + e] = y[e], dp[4 * q + e] = z[e];
-    }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      s = mma(Tile::by_row(qt, 32 * half, ks, lane), kf[ks], s);
-      dp = mma(Tile::by_row(gt, 32 * half, ks, lane), vf[ks], dp);
-    }
-  };
-  auto probabilities = [&]() {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, l2[i]));
-      dp[i] *= s[i];
-    }
-  };
+  typedef float f32x4_t __attribute__((ext_vector_type(4)));
+  f32x16_t s, dp;  // scores less m, dp less delta of this wave's half; then P and dS
   uint8_t *const mine = passed + ((kg * 2 + half) * 4) * 1024 + lane * 16;
   auto pass = [&]() {
 #pragma unroll
@@ -458,17 +436,68 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
       *reinterpret_cast<Frag *>(mine + (2 * j + 1) * 1024) = operand<T>(dp, j);
     }
   };
-  auto sums = [&](int buf) {
-    const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {  // 16 rows each
-      const uint8_t *from = passed + ((kg * 2 + (i >> 1)) * 4 + 2 * (i & 1)) * 1024 + lane * 16;
-      const Frag p = *reinterpret_cast<const Frag *>(from), ds = *reinterpret_cast<const Frag *>(from + 1024);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        dv[d] = mma(Tile::by_column(gt, 16 * i, 64 * half + 32 * d, lane), p, dv[d]);
-        dk[d] = mma(Tile::by_column(qt, 16 * i, 64 * half + 32 * d, lane), ds, dk[d]);
+  // A step: FORMS the scores of tile `buf` and the probabilities, SUMS the last tile's
+  // products.  What a product reads is read two products ahead, and two exponentials'
+  // arithmetic stands behind each pair of the sums' products: left to itself the compiler
+  // reads right before each product, and puts all exponentials behind the last one.
+  auto step = [&](auto forms, auto sums, int buf, int sb, int last) {
+    constexpr bool FORMS = decltype(forms)::value, SUMS = decltype(sums)::value;
+    constexpr int F = FORMS ? KS : 0, N = F + (SUMS ? 8 : 0), AHEAD = 1;
+    const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES, *q_last = smem + last * STAGE, *g_last = q_last + Tile::BYTES;
+    Frag row_q[KS], row_g[KS], col_q[8], col_g[8], p[4], ds[4];
+    f32x4_t l2[4];
+    auto read = [&](int i) {
+      if (i < F) {
+        row_q[i] = Tile::by_row(qt, 32 * half, i, lane);
+        row_g[i] = Tile::by_row(gt, 32 * half, i, lane);
+        return;
       }
+      const int c = i - F, r = c >> 1, d = 64 * half + 32 * (c & 1);  // 16 rows from 16 r on, 32 values
+      if ((c & 1) == 0) {
+        const uint8_t *from = passed + ((kg * 2 + (r >> 1)) * 4 + 2 * (r & 1)) * 1024 + lane * 16;
+        p[r] = *reinterpret_cast<const Frag *>(from);
+        ds[r] = *reinterpret_cast<const Frag *>(from + 1024);
+        if (FORMS) l2[r] = *reinterpret_cast<const f32x4_t *>(&side[sb][1][32 * half + 8 * r + 4 * lh]);
+      }
+      col_g[c] = Tile::by_column(g_last, 16 * r, d, lane);
+      col_q[c] = Tile::by_column(q_last, 16 * r, d, lane);
+    };
+    auto probability = [&](int i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, l2[i >> 2][i & 3]));
+      dp[i] *= s[i];
+    };
+    if (FORMS) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int i = 32 * half + 8 * q + 4 * lh;
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[sb][0][i]);
+        const f32x4_t z = *reinterpret_cast<const f32x4_t *>(&side[sb][2][i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e], dp[4 * q + e] = z[e];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read(i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (i + AHEAD < N) read(i + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < F) {
+        s = mma(row_q[i], kf[i], s);
+        dp = mma(row_g[i], vf[i], dp);
+      } else {
+        const int c = i - F;
+        dv[c & 1] = mma(col_g[c], p[c >> 1], dv[c & 1]);
+        dk[c & 1] = mma(col_q[c], ds[c >> 1], dk[c & 1]);
+        if (FORMS) probability(2 * c), probability(2 * c + 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (FORMS && !SUMS) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) l2[q] = *reinterpret_cast<const f32x4_t *>(&side[sb][1][32 * half + 8 * q + 4 * lh]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) probability(i);
     }
   };
   auto meet = [&]() {
@@ -485,6 +514,8 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
+  const std::true_type yes;
+  const std::false_type no;
   int buf = 0;  // of tile rt
   for (int rt = t0; rt < t1; ++rt) {
     const int next = buf == 2 ? 0 : buf + 1, last = buf == 0 ? 2 : buf - 1;
@@ -494,16 +525,15 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
       issue(rt + 1, next);
     }
     __builtin_amdgcn_sched_barrier(0);
-    scores(buf, (rt - t0) & 1);
-    if (rt > t0) sums(last);
-    probabilities();
+    if (rt > t0) step(yes, yes, buf, (rt - t0) & 1, last);
+    else step(yes, no, buf, 0, last);
     meet_lds();  // all have read the last tile's P and dS
     pass();
     if (rt + 1 < t1) store_side((rt + 1 - t0) & 1);
     buf = next;
   }
   meet();
-  if (t0 < t1) sums(buf == 0 ? 2 : buf - 1);
+  if (t0 < t1) step(no, yes, 0, 0, buf == 0 ? 2 : buf - 1);
   if (!counts) {  // whatever the rows hold (0 times NaN)
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
