@@ -37,8 +37,8 @@ __device__ __forceinline__ f32x16_t mma(f32x8_t a, f32x8_t b, f32x16_t c) {
   for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
   return c;
 }
-// A block of one value: a product's accumulator may start from it, which subtracts a
-// row's number without an instruction of its own.
+// A block of one value: the forward pass' scores start from it in bf16, which subtracts a
+// row's reference without an instruction of its own.
 __device__ __forceinline__ f32x16_t block_of(float v) {
   f32x16_t z;
 #pragma unroll
@@ -56,6 +56,30 @@ __device__ __forceinline__ typename Elem<T>::Frag operand(const f32x16_t &s, int
     else f[e] = s[8 * j + e];
   }
   return f;
+}
+
+// The waves to a SIMD that a kernel's registers are to leave room for: `want`, or as many as
+// fit with the workgroup's LDS of a CU's 160 KB, if fewer.
+constexpr int least_waves(int want, int waves, int lds) {
+  const int fit = (160 * 1024 / lds * waves + 3) / 4;
+  return fit < 1 ? 1 : fit < want ? fit : want;
+}
+
+// acc += A(0) f[0] + A(1) f[1], 32 values of k.  In float32 the products are summed by
+// themselves first: a row's sum over thousands of keys is then one of block sums, with a
+// rounding for each 32 keys and not for each two (1 x 200 x 16384, heads of 128: dv off by
+// 1.1e-6 of its length, so 4e-7).
+template <typename T, typename A>
+__device__ __forceinline__ void add_products(f32x16_t &acc, A &&a, const typename Elem<T>::Frag (&f)[2]) {
+  if constexpr (sizeof(T) == 2) {
+    acc = mma(a(0), f[0], acc);
+    acc = mma(a(1), f[1], acc);
+  } else {
+    f32x16_t t = mma(a(0), f[0], zeros());
+    t = mma(a(1), f[1], t);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] += t[i];
+  }
 }
 
 // ROWS rows of DP values in LDS, 16-byte slots permuted within a row so that both

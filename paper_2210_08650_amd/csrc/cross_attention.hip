@@ -9,12 +9,13 @@
 // registers and one exchange with the other half-wave, and the probabilities are the
 // next product's operand as they are, o^T = V^T P^T, with V^T read transposed from LDS.
 //
-// One pass with a running sum about a reference score, which the products' accumulators
-// start from: the difference costs no instruction, and it is formed before the scale,
-// so that no rounding of ref c is in it.  The reference moves, and what is summed is
-// rescaled, only when a tile's largest score goes past it by more than a factor of 2^8.  Scores, statistics and sums are float32; probabilities are
-// rounded to the operands' type for the matrix cores (2^-8 of each in bf16, the sum is
-// of the unrounded ones), the output once.
+// One pass with a running sum about a reference score, which bf16 products'
+// accumulators start from: the difference costs no instruction, and it is formed before
+// the scale, so that no rounding of ref c is in it.  The reference moves, and what is
+// summed is rescaled, only when a tile's largest score goes past it by more than a factor
+// of 2^8.  Scores, statistics and sums are float32; probabilities are rounded to the
+// operands' type for the matrix cores (2^-8 of each in bf16, the sum is of the unrounded
+// ones), the output once.
 //
 // Keys that take no part are zeros in LDS, whatever memory holds, and their scores are
 // -inf, so NaN in padding reaches nothing.  Where rows are few, the keys are split over
@@ -30,7 +31,7 @@ __device__ __forceinline__ float2 row_stats(float m, float ref, float sum, float
 }
 
 template <typename T, int DP, int RW, int KW, int BN>
-__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) void attend_forward_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 96 ? 2 : 1, RW * KW, KW * 4 * hapi::Tile<T, DP, BN>::BYTES)) void attend_forward_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BN> Tile;
   typedef Loader<T, DP, BN, RW> Load;
   typedef typename Elem<T>::Frag Frag;
@@ -84,6 +85,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
   // m: the largest score so far; ref: what is subtracted from the scores, the same until
   // a tile goes past it by more than 2^8 in the probabilities; sum: of this half-wave's keys
   float m = -INFINITY, ref = 0.0f, sum = 0.0f;
+  // float32 scores are formed by themselves: sums that start at -ref would round by its size
+  constexpr bool FROM_REF = sizeof(T) == 2;
   f32x16_t start = zeros();
   bool first = true;
   const float slack = 8.0f / a.c;
@@ -107,7 +110,13 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
     for (int ks = 0; ks < KS; ++ks) {
       if (DP == 96 && ks == KS - 1 && 16 * ks >= a.dim) break;  // heads of 80: five sixths of 96
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], ks == 0 ? start : s[n]);
+      for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], ks > 0 ? s[n] : FROM_REF ? start : zeros());
+    }
+    if constexpr (!FROM_REF) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] -= ref;
     }
     if (now != ALL) {
 #pragma unroll
@@ -151,13 +160,12 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 || DP <= 96 ? 2 : 1) v
         sum += s[n][i];
       }
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
+      const Frag p[2] = {operand<T>(s[n], 0), operand<T>(s[n], 1)};
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const Frag p = operand<T>(s[n], j);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = mma(Tile::by_column(vt, 32 * n + 16 * j, 32 * d, lane), p, o[d]);
-      }
+      for (int d = 0; d < DB; ++d)
+        add_products<T>(o[d], [&](int j) { return Tile::by_column(vt, 32 * n + 16 * j, 32 * d, lane); }, p);
+    }
   }
   sum += __shfl_xor(sum, 32, 64);
   __syncthreads();  // the tiles' place is used again

@@ -22,8 +22,23 @@
 namespace hapi {
 namespace {
 
+constexpr int kFewKeys = 128;
+
+// Whether a mask leaves at most kFewKeys of n keys.
+__device__ __forceinline__ bool few_kept(const uint8_t *mask, int n, int lane) {
+  int kept = 0;
+  for (int k = 0; k < n && kept <= kFewKeys; k += 256) {
+    bool on[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) on[i] = k + 64 * i + lane < n && mask[k + 64 * i + lane] != 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) kept += __popcll(__ballot(on[i]));
+  }
+  return kept <= kFewKeys;
+}
+
 template <typename T, int DP, int RW, int KW, int BN>
-__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? (DP <= 64 && RW > 1 ? 3 : 2) : DP <= 64 ? 2 : 1) void attend_dq_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 64 && RW > 1 ? 3 : 2) : DP <= 64 ? 2 : 1, RW * KW, KW * 4 * hapi::Tile<T, DP, BN>::BYTES)) void attend_dq_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BN> Tile;
   typedef Loader<T, DP, BN, RW> Load;
   typedef typename Elem<T>::Frag Frag;
@@ -55,7 +70,6 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? (DP <= 64 && RW > 1 
     for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[e], delta);
   }
   delta += __shfl_xor(delta, 32, 64);
-  if (split == 0 && wk == 0 && r < rows && lh == 0) a.delta[(int64_t)pair * rows + r] = delta;
   // a row without a key has m = l = -inf: its p are to be 0
   float m = INFINITY, l2 = 0.0f;
   if (counts) {
@@ -64,68 +78,109 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? (DP <= 64 && RW > 1 
   }
 
   const int key_tiles = tile * RW * 32 < q_valid * a.group ? (kv_valid + BN - 1) / BN : 0;
-  const int t0 = (int)((int64_t)key_tiles * split / a.splits), t1 = (int)((int64_t)key_tiles * (split + 1) / a.splits);
-  const int steps = (t1 - t0 + KW - 1) / KW;
   Load lk, lv;
   lk.init(a.k_st[1], a.dim, wr, lane);
   lv.init(a.v_st[1], a.dim, wr, lane);
   const T *kp = static_cast<const T *>(a.k) + (int64_t)b * a.k_st[0] + (int64_t)kh * a.k_st[2];
   const T *vp = static_cast<const T *>(a.v) + (int64_t)b * a.v_st[0] + (int64_t)kh * a.v_st[2];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem + wk * 2 * STAGE;
+  constexpr uint64_t ALL = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
 
-  uint64_t keep = 0;
-  auto issue = [&](int step) {
-    const int kt = t0 + step * KW + wk;
-    keep = kt < t1 ? key_bits(kv_valid - (int64_t)kt * BN) : 0;
-    if (keep && a.mask) {
+  // the keys of tile kt that take part
+  auto bits_of = [&](int kt) {
+    uint64_t keep = key_bits(kv_valid - (int64_t)kt * BN);
+    if (a.mask) {
       const bool in = (keep >> lane) & 1;
       keep &= __ballot(in && a.mask[(int64_t)b * a.kv_len + (int64_t)kt * BN + (in ? lane : 0)] != 0);
     }
-    if (kt >= t1) return;
-    const uint32_t at = lds0 + (step & 1) * STAGE;
+    return keep;
+  };
+  auto bring = [&](int kt, uint64_t keep, int buf) {
+    const uint32_t at = lds0 + buf * STAGE;
     lk.issue(kp + (int64_t)kt * BN * a.k_st[1], at, keep, wr);
     lv.issue(vp + (int64_t)kt * BN * a.v_st[1], at + Tile::BYTES, keep, wr);
   };
-  constexpr uint64_t ALL = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
+  auto meet = [&]() {
+    wait_loads<0>();
+    if constexpr (RW > 1) __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // p (dp - less) of 32 keys, 0 for those that take no part
+  auto scores = [&](const uint8_t *kt, int n, uint64_t keep, float less) {
+    const uint8_t *vt = kt + Tile::BYTES;
+    f32x16_t s = zeros(), dp = zeros();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (DP == 96 && ks == KS - 1 && 16 * ks >= a.dim) break;  // heads of 80: five sixths of 96
+      s = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], s);
+      dp = mma(Tile::by_row(vt, 32 * n, ks, lane), gf[ks], dp);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i] - m, a.c, -l2)) * (dp[i] - less);
+    if (keep != ALL) {
+      const uint32_t bits = (uint32_t)(keep >> (32 * n)) >> (4 * lh);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1)) s[i] = 0.0f;
+    }
+    return s;
+  };
 
-  const f32x16_t less_m = block_of(-m), less_delta = block_of(-delta);
+  // Of few keys delta is formed again, as the sum of p dp, from all of them: o as it was
+  // rounded is off by up to 2^-8, which dp - delta shows the more, the fewer keys there are
+  // to average it (bf16, 4 keys: dq off by 0.0030 of its length, so 0.0024; past 128 keys
+  // it adds less than a tenth of what rounding dS does), and of one key dS is 0, as
+  // its score is formed here as the forward pass formed m.
+  bool few = kv_valid <= kFewKeys;
+  if (!few && a.mask) few = few_kept(a.mask + (int64_t)b * a.kv_len, kv_valid, lane);
+  if (few) {
+    float sum = 0.0f;
+    for (int kt = 0; kt < key_tiles; ++kt) {
+      const uint64_t keep = bits_of(kt);
+      if (keep == 0) continue;
+      meet();  // the tile before has been read
+      bring(kt, keep, 0);
+      meet();
+#pragma unroll 1
+      for (int n = 0; n < NT; ++n) {
+        const f32x16_t s = scores(smem + wk * 2 * STAGE, n, keep, 0.0f);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += s[i];
+      }
+    }
+    delta = sum + __shfl_xor(sum, 32, 64);
+    meet();
+  }
+  if (split == 0 && wk == 0 && r < rows && lh == 0) a.delta[(int64_t)pair * rows + r] = delta;
+
+  // the split's tiles of keys; wave wk takes every KW-th
+  const int t0 = (int)((int64_t)key_tiles * split / a.splits), t1 = (int)((int64_t)key_tiles * (split + 1) / a.splits);
+  const int steps = (t1 - t0 + KW - 1) / KW;
+  uint64_t keep = 0;
+  auto issue = [&](int step) {
+    const int kt = t0 + step * KW + wk;
+    keep = kt < t1 ? bits_of(kt) : 0;
+    if (kt < t1) bring(kt, keep, step & 1);
+  };
   f32x16_t dq[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) dq[d] = zeros();
   if (steps > 0) issue(0);
   for (int step = 0; step < steps; ++step) {
-    wait_loads<0>();
-    if constexpr (RW > 1) __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+    meet();
     const uint64_t now = keep;
     if (step + 1 < steps) issue(step + 1);
     __builtin_amdgcn_sched_barrier(0);
     if (now == 0) continue;
-    const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE, *vt = kt + Tile::BYTES;
+    const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE;
 #pragma unroll 1
     for (int n = 0; n < NT; ++n) {
-      f32x16_t s = less_m, dp = less_delta;  // scores less m, dp less delta
+      const f32x16_t s = scores(kt, n, now, delta);
+      const Frag ds[2] = {operand<T>(s, 0), operand<T>(s, 1)};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        if (DP == 96 && ks == KS - 1 && 16 * ks >= a.dim) break;  // heads of 80: five sixths of 96
-        s = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], s);
-        dp = mma(Tile::by_row(vt, 32 * n, ks, lane), gf[ks], dp);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -l2)) * dp[i];
-      if (now != ALL) {
-        const uint32_t bits = (uint32_t)(now >> (32 * n)) >> (4 * lh);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1)) s[i] = 0.0f;
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const Frag ds = operand<T>(s, j);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) dq[d] = mma(Tile::by_column(kt, 32 * n + 16 * j, 32 * d, lane), ds, dq[d]);
-      }
+      for (int d = 0; d < DB; ++d)
+        add_products<T>(dq[d], [&](int j) { return Tile::by_column(kt, 32 * n + 16 * j, 32 * d, lane); }, ds);
     }
   }
   __syncthreads();  // the tiles' place is used again
@@ -211,7 +266,7 @@ struct RowLoader {
 };
 
 // BM rows at a time past 4 x 32 keys.
-template <typename T, int DP, int BM, bool DK, bool DV>
+template <typename T, int DP, int BM>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void attend_dkv_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BM> Tile;
   typedef typename Elem<T>::Frag Frag;
@@ -268,7 +323,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     kf[ks] = row_frag<T>(kp, ks, lh, a.dim, counts);
-    if (DK) vf[ks] = row_frag<T>(vp, ks, lh, a.dim, counts);
+    vf[ks] = row_frag<T>(vp, ks, lh, a.dim, counts);
   }
   if (t0 < t1) {
     load_side(t0);
@@ -289,40 +344,42 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
 #pragma unroll 1
     for (int n = 0; n < BM / 32; ++n) {
       typedef float f32x4_t __attribute__((ext_vector_type(4)));
-      f32x16_t s, dp, l2;  // scores less m, dp less delta
+      // bf16 scores start from less m, which subtracts it without an instruction
+      constexpr bool FROM_M = sizeof(T) == 2;
+      f32x16_t s = zeros(), dp = zeros();
+      if constexpr (FROM_M) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int at = 32 * n + 8 * q + 4 * lh;
-        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[buf][0][at]);
-        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(&side[buf][1][at]);
-        const f32x4_t z = *reinterpret_cast<const f32x4_t *>(&side[buf][2][at]);
+        for (int q = 0; q < 4; ++q) {
+          const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[buf][0][32 * n + 8 * q + 4 * lh]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e], l2[4 * q + e] = y[e], dp[4 * q + e] = z[e];
+          for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e];
+        }
       }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         if (DP == 96 && ks == KS - 1 && 16 * ks >= a.dim) break;
         s = mma(Tile::by_row(qt, 32 * n, ks, lane), kf[ks], s);
-        if (DK) dp = mma(Tile::by_row(gt, 32 * n, ks, lane), vf[ks], dp);
+        dp = mma(Tile::by_row(gt, 32 * n, ks, lane), vf[ks], dp);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, l2[i]));
-        if (DK) dp[i] *= s[i];
-      }
+      for (int q = 0; q < 4; ++q) {
+        const int at = 32 * n + 8 * q + 4 * lh;
+        f32x4_t less_m = {};
+        if constexpr (!FROM_M) less_m = *reinterpret_cast<const f32x4_t *>(&side[buf][0][at]);
+        const f32x4_t less_l = *reinterpret_cast<const f32x4_t *>(&side[buf][1][at]);
+        const f32x4_t less_delta = *reinterpret_cast<const f32x4_t *>(&side[buf][2][at]);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if constexpr (DV) {
-          const Frag p = operand<T>(s, j);
-#pragma unroll
-          for (int d = 0; d < DB; ++d) dv[d] = mma(Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane), p, dv[d]);
-        }
-        if constexpr (DK) {
-          const Frag ds = operand<T>(dp, j);
-#pragma unroll
-          for (int d = 0; d < DB; ++d) dk[d] = mma(Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane), ds, dk[d]);
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * q + e;
+          s[i] = __builtin_amdgcn_exp2f(fmaf(FROM_M ? s[i] : s[i] + less_m[e], a.c, less_l[e]));
+          dp[i] = s[i] * (dp[i] + less_delta[e]);
         }
       }
+      const Frag p[2] = {operand<T>(s, 0), operand<T>(s, 1)}, ds[2] = {operand<T>(dp, 0), operand<T>(dp, 1)};
+#pragma unroll
+      for (int d = 0; d < DB; ++d) add_products<T>(dv[d], [&](int j) { return Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane); }, p);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) add_products<T>(dk[d], [&](int j) { return Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane); }, ds);
     }
     if (rt + 1 < t1) store_side(buf ^ 1);
   }
@@ -340,8 +397,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
       for (int q = 0; q < 4; ++q) {
         const int e = 32 * d + 8 * q + 4 * lh;
         if (e >= a.dim4) continue;
-        if (DK) *reinterpret_cast<float4 *>(p + e) = make_float4(dk[d][4 * q], dk[d][4 * q + 1], dk[d][4 * q + 2], dk[d][4 * q + 3]);
-        if (DV) *reinterpret_cast<float4 *>(p + all * a.dim4 + e) = make_float4(dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
+        *reinterpret_cast<float4 *>(p + e) = make_float4(dk[d][4 * q], dk[d][4 * q + 1], dk[d][4 * q + 2], dk[d][4 * q + 3]);
+        *reinterpret_cast<float4 *>(p + all * a.dim4 + e) = make_float4(dv[d][4 * q], dv[d][4 * q + 1], dv[d][4 * q + 2], dv[d][4 * q + 3]);
       }
     return;
   }
@@ -351,8 +408,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
   constexpr int HALF = 2 * STAGE >= 8 * Out::BYTES ? 4 * Out::BYTES : 0;  // places of their own, or one after the other
   static_assert(4 * Out::BYTES <= 2 * STAGE, "the tiles' place");
   __syncthreads();
-  if (DK) Out::store(dk, a.scale, key < a.kv_len ? yk : nullptr, a.dim, a.dk_vec & 1, a.dk_vec & 2, smem + wave * Out::BYTES, lane);
-  if (DV) Out::store(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim, a.dv_vec & 1, a.dv_vec & 2, smem + HALF + wave * Out::BYTES, lane);
+  Out::store(dk, a.scale, key < a.kv_len ? yk : nullptr, a.dim, a.dk_vec & 1, a.dk_vec & 2, smem + wave * Out::BYTES, lane);
+  Out::store(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim, a.dv_vec & 1, a.dv_vec & 2, smem + HALF + wave * Out::BYTES, lane);
 }
 
 // dk and dv of 128-value heads in 16 bits.  A wave that kept 32 keys' k, v, dk and dv would
@@ -427,7 +484,7 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
     store_side(0);
   }
   typedef float f32x4_t __attribute__((ext_vector_type(4)));
-  f32x16_t s, dp;  // scores less m, dp less delta of this wave's half; then P and dS
+  f32x16_t s, dp;  // scores and dP of this wave's half, then P and dS
   uint8_t *const mine = passed + ((kg * 2 + half) * 4) * 1024 + lane * 16;
   auto pass = [&]() {
 #pragma unroll
@@ -445,7 +502,12 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
     constexpr int F = FORMS ? KS : 0, N = F + (SUMS ? 8 : 0), AHEAD = 1;
     const uint8_t *qt = smem + buf * STAGE, *gt = qt + Tile::BYTES, *q_last = smem + last * STAGE, *g_last = q_last + Tile::BYTES;
     Frag row_q[KS], row_g[KS], col_q[8], col_g[8], p[4], ds[4];
-    f32x4_t l2[4];
+    f32x4_t less_l[4], less_delta[4];
+    auto rows_of = [&](int q) {
+      const int at = 32 * half + 8 * q + 4 * lh;
+      less_l[q] = *reinterpret_cast<const f32x4_t *>(&side[sb][1][at]);
+      less_delta[q] = *reinterpret_cast<const f32x4_t *>(&side[sb][2][at]);
+    };
     auto read = [&](int i) {
       if (i < F) {
         row_q[i] = Tile::by_row(qt, 32 * half, i, lane);
@@ -457,23 +519,21 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
         const uint8_t *from = passed + ((kg * 2 + (r >> 1)) * 4 + 2 * (r & 1)) * 1024 + lane * 16;
         p[r] = *reinterpret_cast<const Frag *>(from);
         ds[r] = *reinterpret_cast<const Frag *>(from + 1024);
-        if (FORMS) l2[r] = *reinterpret_cast<const f32x4_t *>(&side[sb][1][32 * half + 8 * r + 4 * lh]);
       }
       col_g[c] = Tile::by_column(g_last, 16 * r, d, lane);
       col_q[c] = Tile::by_column(q_last, 16 * r, d, lane);
     };
     auto probability = [&](int i) {
-      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, l2[i >> 2][i & 3]));
-      dp[i] *= s[i];
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, less_l[i >> 2][i & 3]));
+      dp[i] = s[i] * (dp[i] + less_delta[i >> 2][i & 3]);
     };
-    if (FORMS) {
+    if (FORMS) {  // scores start from less m
+      dp = zeros();
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int i = 32 * half + 8 * q + 4 * lh;
-        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[sb][0][i]);
-        const f32x4_t z = *reinterpret_cast<const f32x4_t *>(&side[sb][2][i]);
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[sb][0][32 * half + 8 * q + 4 * lh]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e], dp[4 * q + e] = z[e];
+        for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e];
       }
     }
 #pragma unroll
@@ -487,6 +547,7 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
         dp = mma(row_g[i], vf[i], dp);
       } else {
         const int c = i - F;
+        if (FORMS && (c & 1) == 0) rows_of(c >> 1);
         dv[c & 1] = mma(col_g[c], p[c >> 1], dv[c & 1]);
         dk[c & 1] = mma(col_q[c], ds[c >> 1], dk[c & 1]);
         if (FORMS) probability(2 * c), probability(2 * c + 1);
@@ -495,7 +556,7 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
     }
     if (FORMS && !SUMS) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) l2[q] = *reinterpret_cast<const f32x4_t *>(&side[sb][1][32 * half + 8 * q + 4 * lh]);
+      for (int q = 0; q < 4; ++q) rows_of(q);
 #pragma unroll
       for (int i = 0; i < 16; ++i) probability(i);
     }
@@ -637,7 +698,7 @@ hipError_t dkv(const AttendArgs &a, hipStream_t s) {
   if constexpr (sizeof(T) == 2 && DP == 128) {
     hapi_launch(attend_dkv_pair_kernel, grid, dim3(512), 0, s, a);
   } else {
-    hapi_launch(attend_dkv_kernel<T, DP, BM, true, true>, grid, block, 0, s, a);
+    hapi_launch(attend_dkv_kernel<T, DP, BM>, grid, block, 0, s, a);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;

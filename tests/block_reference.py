@@ -196,8 +196,13 @@ class Attention:
         vt = self.v.transpose(-1, -2).contiguous()
         dp = g @ vt
         edp = 4 * math.sqrt(self.d) * F * (g.abs() @ vt.abs())
-        delta = (g * od).sum(-1, keepdim=True)
-        ede = 4 * math.sqrt(self.d) * F * (g * od).abs().sum(-1, keepdim=True)
+        # delta is the sum of p dp; of more than 128 keys it may be that of dout and o as o
+        # was rounded, which is off by a known difference
+        delta = (p * dp).sum(-1, keepdim=True)
+        many = (self.on.sum(-1, keepdim=True) > 128).double()
+        sums = (p * dp.abs()).sum(-1, keepdim=True) + (g * od).abs().sum(-1, keepdim=True)
+        ede = 4 * math.sqrt(max(self.d, self.lk)) * F * sums + (p * edp + ep * dp.abs()).sum(-1, keepdim=True)
+        ede = ede + many * ((g * od).sum(-1, keepdim=True) - delta).abs()
         ds = p * (dp - delta)
         eds = ep * (dp - delta).abs() + p * (edp + ede + 2 * F * (dp.abs() + delta.abs())) + FLUSH * on
         kq, kk = 4 * math.sqrt(max(self.lk, 1)) * F, 4 * math.sqrt(max(self.lq * self.n, 1)) * F

@@ -171,6 +171,19 @@ def test_rising_and_falling_scores():
             c.check()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_one_key_has_no_gradient_of_scores(dtype):
+    """Of one key p is 1 whatever its score: dq and dk are 0, not roundings."""
+    for c in (Case(23, dtype, 3, 40, 1, 4, 2, 64), Case(24, dtype, 2, 5, 900, 4, 1, 128, kv_lens=[1, 1]),
+              Case(25, dtype, 1, 70, 700, 2, 2, 80, mask=0.0)):
+        if c.mask is not None:
+            c.mask[:, 600] = True
+        o, st = c.forward()
+        dq, dk, _ = c.backward(o, st)
+        assert not bool(dq.any()) and not bool(dk.any())
+        c.check()
+
+
 def test_every_length_around_a_tile():
     for lk in list(range(1, 70, 3)) + [95, 96, 97, 127, 128, 129, 191, 192, 193, 255, 256, 257]:
         Case(lk, BF, 2, 5, lk, 2, 1, 64).check()
