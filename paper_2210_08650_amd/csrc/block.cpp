@@ -607,6 +607,11 @@ int hapi_cross_attention_backward(const hapi_attention_desc *desc, const void *q
   a.stats = reinterpret_cast<float2 *>(const_cast<float *>(stats));
   a.delta = reinterpret_cast<float *>(base + t.o_delta);
   a.part = reinterpret_cast<float *>(base + t.o_part);
+  if (attend_few_rows(t.bf16, a) && ((t.fwd_splits == 1 && t.dkv_splits == 1) || 4 * a.pairs >= 3 * kCus)) {
+    a.splits = 1;
+    HIP_TRY(launch_attend_few_rows(a, s));
+    return HAPI_OK;
+  }
   if (a.q_len > 0) {
     a.splits = t.fwd_splits;
     HIP_TRY(launch_attend_dq(t.bf16, a, s));

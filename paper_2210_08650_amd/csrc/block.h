@@ -110,5 +110,17 @@ hipError_t launch_attend_stage(bool bf16, const StageArgs &a, hipStream_t s);
 hipError_t launch_attend_forward(bool bf16, const AttendArgs &a, hipStream_t s);
 hipError_t launch_attend_dq(bool bf16, const AttendArgs &a, hipStream_t s);   // delta, too
 hipError_t launch_attend_dkv(bool bf16, const AttendArgs &a, hipStream_t s);
+// All three in one kernel: bf16 heads of up to 64 values whose rows a workgroup's waves have
+// between them, a workgroup for each group of heads.  dq's kernel and dk's and dv's form
+// the scores twice, but split a group's keys over workgroups where groups are few.  Measured,
+// their time against this one's: 1536 groups x 64 rows x 197 keys 79 against 57 us, 4 groups
+// 17 against 13 us, 192 groups x 2048 keys 79 against 69 us, 128 groups x 4096 keys 98
+// against 125 us, 64 groups x 2048 keys 41 against 64 us.  So it is taken where neither
+// kernel would split, and from 192 groups on.
+inline bool attend_few_rows(bool bf16, const AttendArgs &a) {
+  const int64_t rows = (int64_t)a.q_len * a.group;
+  return bf16 && a.dim <= 64 && rows > 0 && rows <= 64 && a.kv_len > 0;
+}
+hipError_t launch_attend_few_rows(const AttendArgs &a, hipStream_t s);
 
 }  // namespace hapi

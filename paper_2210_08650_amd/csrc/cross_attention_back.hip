@@ -1,5 +1,5 @@
-// Cross attention, backward, in two kernels without atomics, so that results do not
-// vary.  With p = exp(scale (s - m) - l) from the forward pass's statistics:
+// Cross attention, backward, without atomics, so that results do not vary.  With
+// p = exp(scale (s - m) - l) from the forward pass's statistics:
 //   dv = p^T dout, dp = dout v^T, ds = p (dp - delta), delta = sum of dout o,
 //   dq = scale ds k, dk = scale ds^T q.
 //
@@ -10,9 +10,10 @@
 // heads that share them (their sum is that of its registers): S = Q K^T and dP = dout
 // V^T own a key in a lane, so P and dS are the operands of dv^T = dout^T P and
 // dk^T = Q^T dS as they are.
+// Few rows: all three in one kernel, below.
 //
-// Scores and dP are formed in both kernels, seven products where five would do if the
-// parts of dq could be added by atomics or went through memory (4 bytes of each value
+// Scores and dP are formed in both of the first two, seven products where five would do if
+// the parts of dq could be added by atomics or went through memory (4 bytes of each value
 // for every 128 keys).  P and dS are rounded to the operands' type for the matrix
 // cores; all sums are float32.
 #include <type_traits>
@@ -234,6 +235,7 @@ template <typename T, int DP, int BM, int WAVES>
 struct RowLoader {
   typedef hapi::Tile<T, DP, BM> Tile;
   static constexpr int LOADS = Tile::DMAS / WAVES;
+  static_assert(LOADS * WAVES == Tile::DMAS, "as many DMAs to every wave");
   uint32_t q_off[LOADS], g_off[LOADS];
   __device__ __forceinline__ void offsets(const AttendArgs &a, int g0, int wave, int lane) {
     const uint32_t qt_ld = (uint32_t)a.q_st[1] * sizeof(T), qh_ld = (uint32_t)a.q_st[2] * sizeof(T);
@@ -624,6 +626,265 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
   Out::store(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim - d0, a.dv_vec & 1, a.dv_vec & 2, smem + (WAVES + wave) * Out::BYTES, lane);
 }
 
+// dq, dk and dv of few rows, 16-bit heads of up to 64 values: a workgroup has all of the
+// rows of a group's heads, q and dout in LDS, so that a key's scores are formed once and
+// k and v are read once, five products and not seven.  A wave takes blocks of 32 keys, k
+// in LDS and v in registers, forms P and dS as dk's and dv's kernel does, and has a
+// block's dk and dv when it has been through the rows.  dS goes through LDS to be the
+// operand of dq^T = K^T dS^T, which a wave sums over its keys and the workgroup over its
+// waves.  A wave's tiles are its own: none waits for another before the last sum.
+// 128 x 64 x 197, 12 heads of 64: 57 us, 3.6 TB/s of what it has to move (dq's kernel and
+// dk's and dv's: 31 + 48 us); registers leave two workgroups a CU, whose loads and stores
+// do not cover each other's products wholly.
+template <int DP, int RB>
+__global__ __launch_bounds__(256, 2) void attend_few_rows_kernel(AttendArgs a) {
+  typedef uint16_t T;
+  typedef typename Elem<T>::Frag Frag;
+  typedef float f32x4_t __attribute__((ext_vector_type(4)));
+  constexpr int ROWS = 32 * RB, KS = DP / 16, DB = DP / 32, WAVES = 4;
+  typedef hapi::Tile<T, DP, ROWS> Rows;
+  typedef hapi::Tile<T, DP, 32> Keys;
+  typedef hapi::Tile<T, ROWS, 32> Turned;  // dS, a key's rows side by side
+  constexpr int OWN = 2 * Keys::BYTES + Turned::BYTES;  // a wave's: keys, dS, keys
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * Rows::BYTES + WAVES * OWN];
+  __shared__ __attribute__((aligned(16))) float side[3][ROWS];  // less m, less l log2(e), less delta
+  __shared__ float sums[WAVES][ROWS];
+
+  const int t = threadIdx.x, lane = t & 63, col = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int rows = a.q_len * a.group;
+  const Place at = place(a, 1);
+  const int b = at.b, kh = at.kh;
+  const int q_valid = clamped(a.q_lens, b, a.q_len), kv_valid = clamped(a.kv_lens, b, a.kv_len);
+  const int valid = q_valid * a.group, key_blocks = (a.kv_len + 31) / 32, some_blocks = valid > 0 ? (kv_valid + 31) / 32 : 0;
+  const T *kb = static_cast<const T *>(a.k) + (int64_t)b * a.k_st[0] + (int64_t)kh * a.k_st[2];
+  const T *vb = static_cast<const T *>(a.v) + (int64_t)b * a.v_st[0] + (int64_t)kh * a.v_st[2];
+  const T *qb = static_cast<const T *>(a.q) + (int64_t)b * a.q_st[0] + (int64_t)kh * a.group * a.q_st[2];
+  const T *gb = static_cast<const T *>(a.dout) + (int64_t)b * a.g_st[0] + (int64_t)kh * a.group * a.g_st[2];
+  const T *ob = static_cast<const T *>(a.o) + (int64_t)b * a.o_st[0] + (int64_t)kh * a.group * a.o_st[2];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+  uint8_t *const own = smem + 2 * Rows::BYTES + wave * OWN;
+  const uint32_t own0 = lds0 + 2 * Rows::BYTES + wave * OWN;
+  constexpr int TURN = Keys::BYTES, SECOND = Keys::BYTES + Turned::BYTES;
+
+  Loader<T, DP, 32, 1> load;
+  load.init(a.k_st[1], a.dim, 0, lane);
+  Frag vf[KS], vn[KS];  // v of the block, and of the next
+  bool counts = false, counts_next = false;  // this lane's key of the block, and of the next
+  auto bring = [&](int n, int buf) {
+    const int key = n * 32 + col;
+    counts_next = key < kv_valid;
+    if (a.mask && counts_next) counts_next = a.mask[(int64_t)b * a.kv_len + key] != 0;
+    load.issue(kb + (int64_t)n * 32 * a.k_st[1], own0 + (buf ? SECOND : 0), __ballot(counts_next), 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) vn[ks] = row_frag<T>(vb + (int64_t)key * a.v_st[1], ks, lh, a.dim, counts_next);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (some_blocks > 0) {
+    constexpr int LOADERS = Rows::DMAS < WAVES ? Rows::DMAS : WAVES;
+    if (wave < LOADERS) {
+      RowLoader<T, DP, ROWS, LOADERS> rl;
+      rl.init(a, wave, lane);
+      rl.issue(a, qb, gb, 0, valid, lds0, wave, lane);
+    }
+  }
+  if (wave < some_blocks) bring(wave, 0);
+  // the rows' statistics and delta; rows that do not count, and those without a key (m = l =
+  // -inf), have p = 0
+  constexpr int PER = 256 / ROWS < DP / 8 ? 256 / ROWS : DP / 8;  // threads of a row
+  if (t < ROWS * PER) {
+    const int r = t / PER, qi = r / a.group, qg = r - qi * a.group;
+    const bool there = r < valid;
+    const T *gp = gb + (int64_t)qi * a.g_st[1] + (int64_t)qg * a.g_st[2], *op = ob + (int64_t)qi * a.o_st[1] + (int64_t)qg * a.o_st[2];
+    float2 st = make_float2(-INFINITY, 0.0f);
+    if (there) st = a.stats[((int64_t)b * a.q_len + qi) * a.heads + kh * a.group + qg];
+    float delta = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DP / 8 / PER; ++i) {
+      const int d = t % PER + i * PER;  // 8 values
+      const Frag g = row_frag<T>(gp, d >> 1, d & 1, a.dim, there), o = row_frag<T>(op, d >> 1, d & 1, a.dim, there);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)g[e], (float)o[e], delta);
+    }
+#pragma unroll
+    for (int x = 1; x < PER; x *= 2) delta += __shfl_xor(delta, x, 64);
+    if (t % PER == 0) {
+      const bool some = st.x != -INFINITY;
+      side[0][r] = some ? -st.x : -INFINITY;
+      side[1][r] = some ? -st.y * kLog2e : 0.0f;
+      side[2][r] = -delta;
+    }
+  }
+  wait_loads<0>();
+  __syncthreads();
+
+  const uint8_t *qt = smem, *gt = smem + Rows::BYTES;
+  f32x16_t s, dp;
+  // P and dP of rows 32 n on; scores start from less m, or from 0 as in the forward pass
+  auto scores = [&](auto from_m, int n, const uint8_t *kt) {
+    dp = zeros();
+    s = zeros();
+    if constexpr (decltype(from_m)::value) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(&side[0][32 * n + 8 * q + 4 * lh]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * q + e] = x[e];
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      s = mma(Rows::by_row(qt, 32 * n, ks, lane), Keys::by_row(kt, 0, ks, lane), s);
+      dp = mma(Rows::by_row(gt, 32 * n, ks, lane), vf[ks], dp);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4_t less_l = *reinterpret_cast<const f32x4_t *>(&side[1][32 * n + 8 * q + 4 * lh]);
+      f32x4_t less_m = {};
+      if constexpr (!decltype(from_m)::value) less_m = *reinterpret_cast<const f32x4_t *>(&side[0][32 * n + 8 * q + 4 * lh]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[4 * q + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * q + e] + less_m[e], a.c, less_l[e]));
+    }
+  };
+
+  auto take = [&]() {
+    counts = counts_next;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) vf[ks] = vn[ks];
+  };
+
+  // of few keys delta is the sum of p dp, as in dq's kernel
+  bool few = kv_valid <= kFewKeys;
+  if (!few && a.mask) few = few_kept(a.mask + (int64_t)b * a.kv_len, kv_valid, lane);
+  if (few && some_blocks > 0) {
+    f32x16_t sum[RB];
+#pragma unroll
+    for (int n = 0; n < RB; ++n) sum[n] = zeros();
+    for (int kn = wave; kn < some_blocks; kn += WAVES) {
+      if (kn > wave) bring(kn, 0);
+      wait_loads<0>();
+      take();
+#pragma unroll
+      for (int n = 0; n < RB; ++n) {
+        scores(std::false_type(), n, own);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[n][i] += counts ? s[i] * dp[i] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < RB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int x = 1; x < 32; x *= 2) sum[n][i] += __shfl_xor(sum[n][i], x, 64);
+        if (col == 0) sums[wave][32 * n + 8 * (i >> 2) + 4 * lh + (i & 3)] = sum[n][i];
+      }
+    if (some_blocks > WAVES && wave < some_blocks) bring(wave, 0);
+    __syncthreads();
+    if (t < ROWS) side[2][t] = -(((sums[0][t] + sums[1][t]) + sums[2][t]) + sums[3][t]);
+    wait_loads<0>();
+    __syncthreads();
+  }
+
+  f32x16_t dq[RB][DB];
+#pragma unroll
+  for (int n = 0; n < RB; ++n)
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dq[n][d] = zeros();
+  T *const yk = static_cast<T *>(a.dk) + (int64_t)b * a.dk_st[0] + (int64_t)kh * a.dk_st[2];
+  T *const yv = static_cast<T *>(a.dv) + (int64_t)b * a.dv_st[0] + (int64_t)kh * a.dv_st[2];
+  int buf = 0;
+  for (int kn = wave; kn < key_blocks; kn += WAVES, buf ^= 1) {
+    f32x16_t dk[DB], dv[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
+    if (kn < some_blocks) {
+      take();
+      if (kn + WAVES < some_blocks) bring(kn + WAVES, buf ^ 1);
+      const uint8_t *kt = own + (buf ? SECOND : 0);
+#pragma unroll
+      for (int n = 0; n < RB; ++n) {
+        scores(std::true_type(), n, kt);
+        const Frag p[2] = {operand<T>(s, 0), operand<T>(s, 1)};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4_t less_delta = *reinterpret_cast<const f32x4_t *>(&side[2][32 * n + 8 * q + 4 * lh]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dp[4 * q + e] = s[4 * q + e] * (dp[4 * q + e] + less_delta[e]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const Frag ds = operand<T>(dp, j);
+          // rows 32 n + 16 j + 4 lh + 0 .. 3 and 8 more; a key that takes no part has none
+          union {
+            Frag f;
+            uint2 h[2];
+          } u = {ds};
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            *reinterpret_cast<uint2 *>(own + TURN + col * Turned::PITCH + (((4 * n + 2 * j + h) ^ Turned::swz(col)) * 16) + 8 * lh) =
+                counts ? u.h[h] : make_uint2(0, 0);
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            dv[d] = mma(Rows::by_column(gt, 32 * n + 16 * j, 32 * d, lane), p[j], dv[d]);
+            dk[d] = mma(Rows::by_column(qt, 32 * n + 16 * j, 32 * d, lane), ds, dk[d]);
+          }
+        }
+      }
+      asm volatile("" ::: "memory");  // a wave's LDS accesses are in order
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const Frag kc = Keys::by_column(kt, 16 * j, 32 * d, lane);
+#pragma unroll
+          for (int n = 0; n < RB; ++n) dq[n][d] = mma(kc, Turned::by_column(own + TURN, 16 * j, 32 * n, lane), dq[n][d]);
+        }
+      wait_loads<0>();  // the next block's: not for the stores that follow
+      if (!counts) {  // whatever the rows hold (0 times NaN)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) dk[d] = zeros(), dv[d] = zeros();
+      }
+    }
+    // turned where this block's keys and dS were
+    const int key = kn * 32 + col;
+    uint8_t *turn = own + (buf ? TURN : 0);
+    typedef RowsOut<T, DB> Out;
+    static_assert(Out::BYTES <= Keys::BYTES + Turned::BYTES, "the tiles' place");
+    Out::store(dk, a.scale, key < a.kv_len ? yk + (int64_t)key * a.dk_st[1] : nullptr, a.dim, a.dk_vec & 1, a.dk_vec & 2, turn, lane);
+    asm volatile("" ::: "memory");
+    Out::store(dv, 1.0f, key < a.kv_len ? yv + (int64_t)key * a.dv_st[1] : nullptr, a.dim, a.dv_vec & 1, a.dv_vec & 2, turn, lane);
+    asm volatile("" ::: "memory");
+  }
+
+  // dq: the waves' sums, a register of all lanes after another, in the tiles' place
+  static_assert(WAVES * RB * DB * 4096 <= sizeof(smem) && RB * DB <= WAVES, "the tiles' place");
+  float *const box = reinterpret_cast<float *>(smem);
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < RB; ++n)
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) box[((wave * RB + n) * DB + d) * 1024 + i * 64 + lane] = dq[n][d][i];
+  __syncthreads();
+  if (wave >= RB * DB) return;
+  const int n = wave / DB, d = wave % DB, r = 32 * n + col;  // this wave's block
+  f32x16_t all[1];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float *from = box + wave * 1024 + i * 64 + lane;
+    all[0][i] = ((from[0] + from[RB * DB * 1024]) + from[2 * RB * DB * 1024]) + from[3 * RB * DB * 1024];
+  }
+  const int qi = r / a.group, qg = r - qi * a.group;
+  T *y = static_cast<T *>(a.dq) + (int64_t)b * a.dq_st[0] + (int64_t)qi * a.dq_st[1] + (int64_t)(kh * a.group + qg) * a.dq_st[2] + 32 * d;
+  asm volatile("" ::: "memory");
+  // turned in the place of the first wave's part, which this wave alone has read
+  typedef RowsOut<T, 1> Out;
+  static_assert(Out::BYTES <= 4096, "a block's place");
+  Out::store(all, a.scale, r < rows ? y : nullptr, a.dim - 32 * d, a.dq_vec & 1, a.dq_vec & 2, smem + wave * 4096, lane);
+}
+
 // Adds the parts: a thread has four values of a row of dq, or of a key's dk (blockIdx.y
 // = 0) or dv.
 template <typename T, bool DQ>
@@ -713,10 +974,21 @@ hipError_t dkv_dim(const AttendArgs &a, hipStream_t s) {
   return dkv<T, 128>(a, s);
 }
 
+template <int DP>
+hipError_t few_rows(const AttendArgs &a, hipStream_t s) {
+  const dim3 grid((uint32_t)a.pairs), block(256);
+  if (a.q_len * a.group <= 32) hapi_launch(attend_few_rows_kernel<DP, 1>, grid, block, 0, s, a);
+  else hapi_launch(attend_few_rows_kernel<DP, 2>, grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_attend_dq(bool bf16, const AttendArgs &a, hipStream_t s) {
   return bf16 ? dq_dim<uint16_t>(a, s) : dq_dim<float>(a, s);
+}
+hipError_t launch_attend_few_rows(const AttendArgs &a, hipStream_t s) {
+  return a.dim <= 32 ? few_rows<32>(a, s) : few_rows<64>(a, s);
 }
 hipError_t launch_attend_dkv(bool bf16, const AttendArgs &a, hipStream_t s) {
   return bf16 ? dkv_dim<uint16_t>(a, s) : dkv_dim<float>(a, s);

@@ -184,6 +184,21 @@ def test_one_key_has_no_gradient_of_scores(dtype):
         c.check()
 
 
+@pytest.mark.parametrize("b,lq,lk,h,kv,d", [
+    (1, 5, 1200, 2, 2, 64), (1, 50, 1200, 2, 1, 32), (200, 3, 600, 1, 1, 40), (100, 20, 700, 6, 2, 64), (2, 64, 130, 4, 4, 64),
+    (3, 13, 260, 10, 2, 24), (2, 1, 33, 64, 1, 64), (2, 31, 1, 2, 1, 64), (2, 65, 300, 2, 2, 64)])
+def test_few_rows(b, lq, lk, h, kv, d):
+    """Heads of up to 64 rows, one group's or many's: keys split over workgroups or not."""
+    c = Case(31, BF, b, lq, lk, h, kv, d)
+    c.check()
+    lens = torch.arange(b, device="cuda") * 97
+    Case(32, BF, b, lq, lk, h, kv, d, q_lens=(lens % (lq + 1)).tolist(), kv_lens=(lens % (lk + 1)).tolist()).check()
+    Case(33, BF, b, lq, lk, h, kv, d, mask=0.7).check()
+    c = Case(34, BF, b, lq, lk, h, kv, d, mask=0.0)  # few kept keys, in some blocks only
+    c.mask[:, lk // 3::97] = True
+    c.check()
+
+
 def test_every_length_around_a_tile():
     for lk in list(range(1, 70, 3)) + [95, 96, 97, 127, 128, 129, 191, 192, 193, 255, 256, 257]:
         Case(lk, BF, 2, 5, lk, 2, 1, 64).check()
