@@ -25,6 +25,14 @@ namespace {
 
 constexpr int kFewKeys = 128;
 
+// Where a call has few rows, the roundings of its P and dS to bf16 do not average (a row
+// of one token against two keys: dq off by 0.0028 of its length, so 0.0017).  FINE kernels
+// multiply by what the rounding left, too: this, as operands.
+__device__ __forceinline__ void keep_rest(f32x16_t &s) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] -= (float)(__bf16)s[i];
+}
+
 // Whether a mask leaves at most kFewKeys of n keys.
 __device__ __forceinline__ bool few_kept(const uint8_t *mask, int n, int lane) {
   int kept = 0;
@@ -38,7 +46,7 @@ __device__ __forceinline__ bool few_kept(const uint8_t *mask, int n, int lane) {
   return kept <= kFewKeys;
 }
 
-template <typename T, int DP, int RW, int KW, int BN>
+template <typename T, int DP, int RW, int KW, int BN, bool FINE>
 __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 64 && RW > 1 ? 3 : 2) : DP <= 64 ? 2 : 1, RW * KW, KW * 4 * hapi::Tile<T, DP, BN>::BYTES)) void attend_dq_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BN> Tile;
   typedef Loader<T, DP, BN, RW> Load;
@@ -177,11 +185,15 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
     const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE;
 #pragma unroll 1
     for (int n = 0; n < NT; ++n) {
-      const f32x16_t s = scores(kt, n, now, delta);
-      const Frag ds[2] = {operand<T>(s, 0), operand<T>(s, 1)};
+      f32x16_t s = scores(kt, n, now, delta);
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
-        add_products<T>(dq[d], [&](int j) { return Tile::by_column(kt, 32 * n + 16 * j, 32 * d, lane); }, ds);
+      for (int turn = 0; turn < (FINE ? 2 : 1); ++turn) {
+        const Frag ds[2] = {operand<T>(s, 0), operand<T>(s, 1)};
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+          add_products<T>(dq[d], [&](int j) { return Tile::by_column(kt, 32 * n + 16 * j, 32 * d, lane); }, ds);
+        if (FINE) keep_rest(s);
+      }
     }
   }
   __syncthreads();  // the tiles' place is used again
@@ -268,8 +280,8 @@ struct RowLoader {
 };
 
 // BM rows at a time past 4 x 32 keys.
-template <typename T, int DP, int BM>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void attend_dkv_kernel(AttendArgs a) {
+template <typename T, int DP, int BM, bool FINE>
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : (DP <= 64 ? 3 : 2) - (FINE && DP > 32)) void attend_dkv_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BM> Tile;
   typedef typename Elem<T>::Frag Frag;
   constexpr int KS = DP / 16, DB = DP / 32, STAGE = 2 * Tile::BYTES, LOADS = Tile::DMAS / 4;
@@ -377,11 +389,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
           dp[i] = s[i] * (dp[i] + less_delta[e]);
         }
       }
-      const Frag p[2] = {operand<T>(s, 0), operand<T>(s, 1)}, ds[2] = {operand<T>(dp, 0), operand<T>(dp, 1)};
 #pragma unroll
-      for (int d = 0; d < DB; ++d) add_products<T>(dv[d], [&](int j) { return Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane); }, p);
+      for (int turn = 0; turn < (FINE ? 2 : 1); ++turn) {
+        const Frag p[2] = {operand<T>(s, 0), operand<T>(s, 1)}, ds[2] = {operand<T>(dp, 0), operand<T>(dp, 1)};
 #pragma unroll
-      for (int d = 0; d < DB; ++d) add_products<T>(dk[d], [&](int j) { return Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane); }, ds);
+        for (int d = 0; d < DB; ++d) add_products<T>(dv[d], [&](int j) { return Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane); }, p);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) add_products<T>(dk[d], [&](int j) { return Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane); }, ds);
+        if (FINE) keep_rest(s), keep_rest(dp);
+      }
     }
     if (rt + 1 < t1) store_side(buf ^ 1);
   }
@@ -421,6 +437,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (DP <= 64 ? 3 : 2) : 1) void 
 // passes them on in LDS as operands, and sums half the values of dk and dv over all 64.
 // A tile's products with P and dS are those of the step after the one that forms them, so
 // that they stand beside the next exponentials, which need nothing of them.
+// FINE: a tile has two turns, the second one's P and dS are what rounding the first one's
+// left; LDS has no place for both at once.
+template <bool FINE>
 __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
   typedef uint16_t T;
   constexpr int DP = 128, BM = 64, KS = DP / 16, DB = 2, WAVES = 8;
@@ -579,20 +598,23 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
   };
   const std::true_type yes;
   const std::false_type no;
-  int buf = 0;  // of tile rt
-  for (int rt = t0; rt < t1; ++rt) {
+  constexpr int MORE = FINE;
+  const int u0 = t0 << MORE, u1 = t1 << MORE;  // turns
+  int buf = 0;  // of the turn's tile
+  for (int u = u0; u < u1; ++u) {
     const int next = buf == 2 ? 0 : buf + 1, last = buf == 0 ? 2 : buf - 1;
-    meet();  // tile rt is there; so are the last tile's P and dS
-    if (rt + 1 < t1) {
-      load_side(rt + 1);
-      issue(rt + 1, next);
+    meet();  // the tile is there; so are the last turn's P and dS
+    if (u + 1 < u1) {
+      load_side((u + 1) >> MORE);
+      issue((u + 1) >> MORE, next);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (rt > t0) step(yes, yes, buf, (rt - t0) & 1, last);
+    if (u > u0) step(yes, yes, buf, (u - u0) & 1, last);
     else step(yes, no, buf, 0, last);
-    meet_lds();  // all have read the last tile's P and dS
+    if (u & MORE) keep_rest(s), keep_rest(dp);
+    meet_lds();  // all have read the last turn's P and dS
     pass();
-    if (rt + 1 < t1) store_side((rt + 1 - t0) & 1);
+    if (u + 1 < u1) store_side((u + 1 - u0) & 1);
     buf = next;
   }
   meet();
@@ -636,8 +658,8 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
 // 128 x 64 x 197, 12 heads of 64: 57 us, 3.6 TB/s of what it has to move (dq's kernel and
 // dk's and dv's: 31 + 48 us); registers leave two workgroups a CU, whose loads and stores
 // do not cover each other's products wholly.
-template <int DP, int RB>
-__global__ __launch_bounds__(256, 2) void attend_few_rows_kernel(AttendArgs a) {
+template <int DP, int RB, bool FINE>
+__global__ __launch_bounds__(256, FINE && DP * RB > 64 ? 1 : 2) void attend_few_rows_kernel(AttendArgs a) {
   typedef uint16_t T;
   typedef typename Elem<T>::Frag Frag;
   typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -645,7 +667,8 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, ROWS> Rows;
   typedef hapi::Tile<T, DP, 32> Keys;
   typedef hapi::Tile<T, ROWS, 32> Turned;  // dS, a key's rows side by side
-  constexpr int OWN = 2 * Keys::BYTES + Turned::BYTES;  // a wave's: keys, dS, keys
+  constexpr int TURNS = FINE ? 2 : 1;  // dS, and what its rounding left
+  constexpr int OWN = 2 * Keys::BYTES + TURNS * Turned::BYTES;  // a wave's: keys, dS, keys
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * Rows::BYTES + WAVES * OWN];
   __shared__ __attribute__((aligned(16))) float side[3][ROWS];  // less m, less l log2(e), less delta
   __shared__ float sums[WAVES][ROWS];
@@ -665,7 +688,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows_kernel(AttendArgs a) {
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
   uint8_t *const own = smem + 2 * Rows::BYTES + wave * OWN;
   const uint32_t own0 = lds0 + 2 * Rows::BYTES + wave * OWN;
-  constexpr int TURN = Keys::BYTES, SECOND = Keys::BYTES + Turned::BYTES;
+  constexpr int TURN = Keys::BYTES, SECOND = Keys::BYTES + TURNS * Turned::BYTES;
 
   Loader<T, DP, 32, 1> load;
   load.init(a.k_st[1], a.dim, 0, lane);
@@ -805,7 +828,6 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows_kernel(AttendArgs a) {
 #pragma unroll
       for (int n = 0; n < RB; ++n) {
         scores(std::true_type(), n, kt);
-        const Frag p[2] = {operand<T>(s, 0), operand<T>(s, 1)};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const f32x4_t less_delta = *reinterpret_cast<const f32x4_t *>(&side[2][32 * n + 8 * q + 4 * lh]);
@@ -813,22 +835,26 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows_kernel(AttendArgs a) {
           for (int e = 0; e < 4; ++e) dp[4 * q + e] = s[4 * q + e] * (dp[4 * q + e] + less_delta[e]);
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const Frag ds = operand<T>(dp, j);
-          // rows 32 n + 16 j + 4 lh + 0 .. 3 and 8 more; a key that takes no part has none
-          union {
-            Frag f;
-            uint2 h[2];
-          } u = {ds};
+        for (int turn = 0; turn < TURNS; ++turn) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            *reinterpret_cast<uint2 *>(own + TURN + col * Turned::PITCH + (((4 * n + 2 * j + h) ^ Turned::swz(col)) * 16) + 8 * lh) =
-                counts ? u.h[h] : make_uint2(0, 0);
+          for (int j = 0; j < 2; ++j) {
+            const Frag p = operand<T>(s, j), ds = operand<T>(dp, j);
+            // rows 32 n + 16 j + 4 lh + 0 .. 3 and 8 more; a key that takes no part has none
+            union {
+              Frag f;
+              uint2 h[2];
+            } u = {ds};
+            uint8_t *to = own + TURN + turn * Turned::BYTES + col * Turned::PITCH + 8 * lh;
 #pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            dv[d] = mma(Rows::by_column(gt, 32 * n + 16 * j, 32 * d, lane), p[j], dv[d]);
-            dk[d] = mma(Rows::by_column(qt, 32 * n + 16 * j, 32 * d, lane), ds, dk[d]);
+            for (int h = 0; h < 2; ++h)
+              *reinterpret_cast<uint2 *>(to + ((4 * n + 2 * j + h) ^ Turned::swz(col)) * 16) = counts ? u.h[h] : make_uint2(0, 0);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+              dv[d] = mma(Rows::by_column(gt, 32 * n + 16 * j, 32 * d, lane), p, dv[d]);
+              dk[d] = mma(Rows::by_column(qt, 32 * n + 16 * j, 32 * d, lane), ds, dk[d]);
+            }
           }
+          if (FINE) keep_rest(s), keep_rest(dp);
         }
       }
       asm volatile("" ::: "memory");  // a wave's LDS accesses are in order
@@ -838,7 +864,10 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows_kernel(AttendArgs a) {
         for (int d = 0; d < DB; ++d) {
           const Frag kc = Keys::by_column(kt, 16 * j, 32 * d, lane);
 #pragma unroll
-          for (int n = 0; n < RB; ++n) dq[n][d] = mma(kc, Turned::by_column(own + TURN, 16 * j, 32 * n, lane), dq[n][d]);
+          for (int turn = 0; turn < TURNS; ++turn)
+#pragma unroll
+            for (int n = 0; n < RB; ++n)
+              dq[n][d] = mma(kc, Turned::by_column(own + TURN + turn * Turned::BYTES, 16 * j, 32 * n, lane), dq[n][d]);
         }
       wait_loads<0>();  // the next block's: not for the stores that follow
       if (!counts) {  // whatever the rows hold (0 times NaN)
@@ -933,7 +962,13 @@ template <typename T, int DP, int RW>
 hipError_t dq(const AttendArgs &a, hipStream_t s) {
   constexpr int KW = attend_key_waves(sizeof(T), DP, RW), BN = attend_tile_keys(sizeof(T), DP, KW);
   const int64_t rows = (int64_t)a.q_len * a.group, tiles = ceil_div(rows, 32 * RW);
-  hapi_launch(attend_dq_kernel<T, DP, RW, KW, BN>, dim3((uint32_t)(tiles * a.splits * a.pairs)), dim3(64 * RW * KW), 0, s, a);
+  const dim3 grid((uint32_t)(tiles * a.splits * a.pairs)), block(64 * RW * KW);
+  if constexpr (sizeof(T) == 2) {
+    if (attend_fine(a)) hapi_launch(attend_dq_kernel<T, DP, RW, KW, BN, true>, grid, block, 0, s, a);
+    else hapi_launch(attend_dq_kernel<T, DP, RW, KW, BN, false>, grid, block, 0, s, a);
+  } else {
+    hapi_launch(attend_dq_kernel<T, DP, RW, KW, BN, false>, grid, block, 0, s, a);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   hapi_launch(attend_sum_kernel<T, true>, dim3((uint32_t)ceil_div(rows * a.pairs * (a.dim4 / 4), 256)), dim3(256), 0, s, a);
@@ -957,9 +992,13 @@ hipError_t dkv(const AttendArgs &a, hipStream_t s) {
   constexpr int BM = sizeof(T) == 2 ? 64 : 32;
   const dim3 grid((uint32_t)(ceil_div(a.kv_len, 128) * a.splits * a.pairs)), block(256);
   if constexpr (sizeof(T) == 2 && DP == 128) {
-    hapi_launch(attend_dkv_pair_kernel, grid, dim3(512), 0, s, a);
+    if (attend_fine(a)) hapi_launch(attend_dkv_pair_kernel<true>, grid, dim3(512), 0, s, a);
+    else hapi_launch(attend_dkv_pair_kernel<false>, grid, dim3(512), 0, s, a);
+  } else if constexpr (sizeof(T) == 2) {
+    if (attend_fine(a)) hapi_launch(attend_dkv_kernel<T, DP, BM, true>, grid, block, 0, s, a);
+    else hapi_launch(attend_dkv_kernel<T, DP, BM, false>, grid, block, 0, s, a);
   } else {
-    hapi_launch(attend_dkv_kernel<T, DP, BM>, grid, block, 0, s, a);
+    hapi_launch(attend_dkv_kernel<T, DP, BM, false>, grid, block, 0, s, a);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
@@ -977,8 +1016,11 @@ hipError_t dkv_dim(const AttendArgs &a, hipStream_t s) {
 template <int DP>
 hipError_t few_rows(const AttendArgs &a, hipStream_t s) {
   const dim3 grid((uint32_t)a.pairs), block(256);
-  if (a.q_len * a.group <= 32) hapi_launch(attend_few_rows_kernel<DP, 1>, grid, block, 0, s, a);
-  else hapi_launch(attend_few_rows_kernel<DP, 2>, grid, block, 0, s, a);
+  const bool one = a.q_len * a.group <= 32, fine = attend_fine(a);
+  if (one && fine) hapi_launch(attend_few_rows_kernel<DP, 1, true>, grid, block, 0, s, a);
+  else if (one) hapi_launch(attend_few_rows_kernel<DP, 1, false>, grid, block, 0, s, a);
+  else if (fine) hapi_launch(attend_few_rows_kernel<DP, 2, true>, grid, block, 0, s, a);
+  else hapi_launch(attend_few_rows_kernel<DP, 2, false>, grid, block, 0, s, a);
   return hipGetLastError();
 }
 
