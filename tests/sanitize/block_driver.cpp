@@ -180,6 +180,14 @@ hipError_t launch_attend_dkv(bool bf16, const AttendArgs &a, hipStream_t) {
   ++g_dkv;
   return hipSuccess;
 }
+hipError_t launch_attend_few_rows(const AttendArgs &a, hipStream_t) {
+  check_attend(true, a, true);
+  const int64_t rows = (int64_t)a.q_len * a.group;
+  EXPECT(rows >= 1 && rows <= 64 && a.dim <= 64 && a.kv_len >= 1 && a.splits == 1 && a.pairs <= kBlocks);
+  ++g_dq;
+  ++g_dkv;
+  return hipSuccess;
+}
 }  // namespace hapi
 
 static void attention(int dtype, int64_t b, int64_t q, int64_t k, int heads, int kv, int dim, int layout) {
