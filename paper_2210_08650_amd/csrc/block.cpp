@@ -234,16 +234,27 @@ int read_rotary(const hapi_rotary_desc *d, Rotary &r) {
   TRY(read_strides(d->k_stride, d->length, d->kv_heads, d->head_dim, "k", a.x_st[1]));
   TRY(read_strides(d->q_out_stride, d->length, d->heads, d->head_dim, "q_out", a.y_st[0]));
   TRY(read_strides(d->k_out_stride, d->length, d->kv_heads, d->head_dim, "k_out", a.y_st[1]));
-  // As many values at once as the pairs' two sides and what is not rotated divide into;
-  // neighbours lie together with what is not rotated.
+  // As many values at once as the pairs' two sides and what is not rotated divide into
+  // (128 x 197 tokens of 24 heads of 64 in bf16: 32 us, one value at a time 61); neighbours
+  // lie together with what is not rotated.
   const int64_t side = d->neighbours ? 0 : pairs, rest = d->head_dim - 2 * side;
   r.v = r.bf16 ? 8 : 4;
   while (r.v > 1 && (side % r.v != 0 || rest % (2 * r.v) != 0)) r.v /= 2;
-  // Up to 8 heads a lane, so that it forms sines and cosines once for them, as long as
-  // the CUs' 2048 lanes each are filled.
-  int lanes = 4;
-  while (lanes < 64 && lanes * 2 * r.v < d->head_dim) lanes *= 2;
+  // A lane forms the sines of its pairs one after another, so few vectors are shared by
+  // more lanes, down to two pairs each (1 x 197 tokens: 3.9 us, with 8 pairs 5.7; backward
+  // 5.5 and 8.5), until the CUs have 1024 lanes each (12 x 197: 11.5 us with 4 pairs, 12.9
+  // with 2).
   const int64_t heads = (int64_t)d->heads + d->kv_heads;
+  const auto lanes_of = [&](int v) {
+    int n = 4;
+    while (n < 64 && n * 2 * v < d->head_dim) n *= 2;
+    return n;
+  };
+  while (r.v > 2 && a.tokens * heads * lanes_of(r.v) < kCus * 1024) r.v /= 2;
+  // Up to 8 heads a lane, so that it forms sines and cosines once for them, as long as
+  // the CUs' 2048 lanes each are filled (1 x 197 tokens with all 12 heads a lane: 13.6 us
+  // where one takes 5.7; 3 x 4099 tokens in float32: 46.1 and, with 8, 45.2).
+  const int lanes = lanes_of(r.v);
   const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, a.tokens * heads * lanes / (kCus * 2048)));
   for (int w = 0; w < 2; ++w) a.head_groups[w] = (int32_t)ceil_div(a.heads[w], each);
   return HAPI_OK;

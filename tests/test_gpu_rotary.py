@@ -127,6 +127,16 @@ def test_rotary(shape, dtype, neighbours):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("batch,length,heads,kv_heads,dim,sections,neighbours,pad", [
+    (8, 3001, 4, 2, 64, (16, 16), False, 0), (3, 5003, 3, 1, 128, (24, 16, 24), True, 8), (2, 4099, 15, 5, 80, (40,), False, 0),
+    (7, 1009, 12, 4, 72, (8, 8), False, 0), (2, 3001, 8, 8, 96, (12, 12), True, 16)])
+def test_many_tokens(batch, length, heads, kv_heads, dim, sections, neighbours, pad, dtype):
+    """Enough vectors for 16 bytes a lane; some sequences shorter."""
+    lens = [(length * (i + 1)) // batch - 3 * i for i in range(batch)]
+    Case(41, dtype, batch, length, heads, kv_heads, dim, sections, neighbours=neighbours, pad=pad, lens=lens).check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("shape", SHAPES[3:12])
 def test_without_norm(shape, dtype):
     Case(1, dtype, *shape, norm=False).check()
