@@ -620,7 +620,8 @@ typedef struct {
   int32_t dtype;              /* hapi_dtype of q, k, v, o and their gradients */
   int32_t head_dim;           /* 1 .. 128 */
   int32_t heads, kv_heads;    /* heads, at most 2^20, a multiple of kv_heads, at most 512 times */
-  int64_t batch, q_len, kv_len;  /* >= 0; at most 2^24 tiles of 32 to 128 queries or keys */
+  int64_t batch, q_len, kv_len;  /* >= 0; fewer than 2^24 tiles of 32 to 128 queries or of
+                                    128 keys (bf16 heads past 96 values: 2^23 of keys) */
   /* Elements between batch entries, tokens and heads, as in hapi_rotary_desc; three
    * zeros: contiguous [batch, tokens, heads, head_dim].  q: q and dq; k: k and dk; v: v and
    * dv; o: o and dout. */

@@ -88,7 +88,8 @@ int next_gradients(const hapi_gradient_desc *d, int &i, GradArgs &a) {
     ++a.count;
   }
   // Segments that fill the blocks, of 2048 to 32,768 values: a block's first loads
-  // wait for its search of the tensor.
+  // wait for its search of the tensor (32,768 always: 2 million values in two float32
+  // tensors 5.5 + 10.7 us, so 4.0 + 6.8).
   a.seg_size = 32768;
   while (a.seg_size > 2048 && total / a.seg_size < 2 * kGradBlocks) a.seg_size /= 2;
   int64_t seg = 0;
@@ -327,8 +328,10 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
     return fail(HAPI_E_UNSUPPORTED, "batch, kv_len and q_len times heads / kv_heads must be at most 2^30");
   const int64_t pairs = d->batch * d->kv_heads, rows = d->q_len * group;
   const int rw = attend_row_waves(rows);
-  if (pairs >= kMaxTiles || ceil_div(rows, 32 * rw) * pairs >= kMaxTiles || ceil_div(d->kv_len, 128) * pairs >= kMaxTiles)
-    return fail(HAPI_E_UNSUPPORTED, "more than 2^24 tiles of queries or keys");
+  // tiles of keys of bf16 heads past 96 values have 512 threads, others 256
+  const int64_t key_tiles_most = d->dtype == HAPI_BF16 && d->head_dim > 96 ? kMaxTiles / 2 : kMaxTiles;
+  if (pairs >= kMaxTiles || ceil_div(rows, 32 * rw) * pairs >= kMaxTiles || ceil_div(d->kv_len, 128) * pairs >= key_tiles_most)
+    return fail(HAPI_E_UNSUPPORTED, "too many tiles of queries or keys (2^24, or 2^23 of keys of bf16 heads past 96 values)");
   t.bf16 = d->dtype == HAPI_BF16;
   t.esz = t.bf16 ? 2 : 4;
   t.v = 16 / t.esz;
@@ -362,7 +365,11 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
   const int padded = (int)up(d->head_dim, 32), kw = attend_key_waves(t.esz, padded, rw), bn = attend_tile_keys(t.esz, padded, kw);
   const int64_t wgs = ceil_div(rows, 32 * rw) * pairs, want = (!t.bf16 && padded > 64 ? 1 : 2) * kCus;  // as many as run at once
   // A float32 tile's products take eight times as long as a bf16 one's, so one of them is
-  // worth a part of its own; of the others four.
+  // worth a part of its own; of the others four.  Forward and join with 1, 2, 4 and 16 of
+  // them: 1 x 1 x 8192, 16 + 4 heads of 128, 21, 21, 18 and 32 us; 4 x 8 x 2000, 8 + 2 heads
+  // of 96, 15, 13, 14 and 37; 1 x 300 x 600, 4 heads of 128, 14, 14, 17 and 19.  float32, 3 x
+  // 77 x 1021, 12 + 4 heads of 80: the same with 1 and 4; 2 x 100 x 500, 8 heads of 128, 16 and
+  // 28.
   const int64_t key_tiles = ceil_div(d->kv_len, bn), least = t.bf16 ? 4 : 1;
   t.fwd_splits = wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, key_tiles / (least * kw), 64}));
   const int64_t dkv_want = padded > 96 ? kCus : want;  // one workgroup a CU

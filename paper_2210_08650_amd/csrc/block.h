@@ -9,7 +9,7 @@ namespace hapi {
 // ----------------------------------------------------------------- gradients
 
 constexpr int kGradTensors = 120;   // of a launch: their addresses are its arguments (4 KB at most)
-constexpr int kGradBlocks = 1024;   // of a launch, and its partial sums, at most
+constexpr int kGradBlocks = 1024;   // of a launch, and its partial sums, at most; 2048 were slower
 constexpr int kGradSumLaunches = 4; // partial sums of as many launches are joined by the blocks that need them
 
 struct GradArgs {
@@ -87,14 +87,18 @@ struct AttendArgs {
   float *delta;                      // [pairs][rows] sum of dout o
 };
 
-// A workgroup's waves have 4 x 32, 2 x 32 or 32 rows between them.
+// A workgroup's waves have 4 x 32, 2 x 32 or 32 rows between them: no more than there are
+// (4 x 32 always: forward 128 x 64 x 197, 12 heads of 64, 26.7 for 24.9 us, 16 x 1 x 8192, 16 +
+// 4 heads of 128, 40.1 for 38.8; 4 x 8 x 2000, 8 + 2 heads of 96, 9.3 for 10).
 inline int attend_row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 // Up to four waves in all: those that share rows take other keys, in tiles of their own,
-// two of them in flight; 64 KB of the LDS, so that a CU runs two workgroups.
+// two of them in flight; 64 KB of the LDS, so that a CU runs two workgroups (one wave alone:
+// the forward cases above 26.4 and 41.1 us, dq of 1 x 1 x 8192 16.8 for 13.5).
 constexpr int attend_key_waves(int esz, int padded_dim, int row_waves) {
   const int fit = 65536 / (4 * 32 * padded_dim * esz), most = 4 / row_waves;
   return fit < 1 ? 1 : fit < most ? (fit == 3 ? 2 : fit) : most;
 }
+// 64 keys of 16 bits to a tile where the LDS then holds them twice, 32 of 32 bits.
 constexpr int attend_tile_keys(int esz, int padded_dim, int key_waves) {
   return esz == 2 && key_waves * 4 * 64 * padded_dim * esz <= (key_waves > 1 ? 32768 : 65536) ? 64 : 32;
 }

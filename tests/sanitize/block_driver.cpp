@@ -174,7 +174,8 @@ hipError_t launch_attend_dq(bool bf16, const AttendArgs &a, hipStream_t) {
 hipError_t launch_attend_dkv(bool bf16, const AttendArgs &a, hipStream_t) {
   check_attend(bf16, a, true);
   const int64_t rows = (int64_t)a.q_len * a.group;
-  EXPECT(ceil_div(a.kv_len, 128) * a.splits * a.pairs <= kBlocks);
+  // 512 threads for 128 keys of bf16 heads past 96 values, else 256; all of a launch: 32 bits
+  EXPECT(ceil_div(a.kv_len, 128) * a.splits * a.pairs * (bf16 && a.dim > 96 ? 512 : 256) <= kMaxLaunchThreads);
   if (rows > 0) region("delta", a.delta, a.pairs * rows * 4);
   if (a.splits > 1) region("dkv", a.part, a.splits * 2 * a.pairs * (int64_t)a.kv_len * a.dim4 * 4);
   ++g_dkv;

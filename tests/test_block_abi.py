@@ -243,6 +243,14 @@ def test_attention_descriptor_refusals(kw, code):
     _raises(code, H.hapi_cross_attention_backward, d, *AB)
 
 
+def test_attention_launches_of_32_bit_thread_counts():
+    """128 keys of bf16 heads past 96 values are 512 threads of the backward pass."""
+    for dtype, dim, most in ((BF, 97, 23), (BF, 96, 24), (F32, 128, 24)):
+        kw = dict(dtype=dtype, dim=dim, q_len=1, heads=1, kv_heads=1, kv_len=1)
+        _raises(H.HAPI_E_UNSUPPORTED, H.hapi_cross_attention_workspace_bytes, _attend(batch=1 << most, **kw), True)
+        assert H.hapi_cross_attention_workspace_bytes(_attend(batch=(1 << most) - 1, **kw), True) >= 0
+
+
 def test_attention_pointer_refusals():
     d = _attend()
     d.c.reserved = 1
