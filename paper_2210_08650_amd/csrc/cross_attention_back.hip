@@ -283,7 +283,10 @@ struct RowLoader {
   }
 };
 
-// BM rows at a time past 4 x 32 keys.
+// BM rows at a time past 4 x 32 keys.  float32 products add to dk and dv directly: sums by
+// themselves as in dq and o take registers that 128-value heads do not have (2 x 1000 x 1000,
+// 8 heads: 210 us, so 166) and gain little on what the products' own roundings leave (2 x
+// 4096 rows to a key: dk off by 6.6e-7 of its length, so 8.2e-7).
 template <typename T, int DP, int BM, bool FINE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : (DP <= 64 ? 3 : 2) - (FINE && DP > 32)) void attend_dkv_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BM> Tile;
@@ -397,9 +400,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : (DP <= 64 ? 3 : 2) - (FIN
       for (int turn = 0; turn < (FINE ? 2 : 1); ++turn) {
         const Frag p[2] = {operand<T>(s, 0), operand<T>(s, 1)}, ds[2] = {operand<T>(dp, 0), operand<T>(dp, 1)};
 #pragma unroll
-        for (int d = 0; d < DB; ++d) add_products<T>(dv[d], [&](int j) { return Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane); }, p);
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int d = 0; d < DB; ++d) add_products<T>(dk[d], [&](int j) { return Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane); }, ds);
+          for (int j = 0; j < 2; ++j) dv[d] = mma(Tile::by_column(gt, 32 * n + 16 * j, 32 * d, lane), p[j], dv[d]);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) dk[d] = mma(Tile::by_column(qt, 32 * n + 16 * j, 32 * d, lane), ds[j], dk[d]);
         if (FINE) keep_rest(s), keep_rest(dp);
       }
     }
