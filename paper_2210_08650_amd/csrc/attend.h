@@ -67,8 +67,8 @@ constexpr int least_waves(int want, int waves, int lds) {
 
 // acc += A(0) f[0] + A(1) f[1], 32 values of k.  In float32 the products are summed by
 // themselves first: a row's sum over thousands of keys is then one of block sums, with a
-// rounding for each 32 keys and not for each two (1 x 200 x 16384, heads of 128: dv off by
-// 1.1e-6 of its length, so 4e-7).
+// rounding for each 32 keys and not for each two (1 x 200 x 16384, heads of 128: o off by
+// 6.2e-7 of its length, so 4.6e-7, dq by 1.2e-6 and 7.5e-7).
 template <typename T, typename A>
 __device__ __forceinline__ void add_products(f32x16_t &acc, A &&a, const typename Elem<T>::Frag (&f)[2]) {
   if constexpr (sizeof(T) == 2) {
