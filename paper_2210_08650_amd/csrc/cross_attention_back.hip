@@ -795,7 +795,10 @@ __global__ __launch_bounds__(256, FINE && DP * RB > 64 ? 1 : 2) void attend_few_
 #pragma unroll
     for (int n = 0; n < RB; ++n) sum[n] = zeros();
     for (int kn = wave; kn < some_blocks; kn += WAVES) {
-      if (kn > wave) bring(kn, 0);
+      if (kn > wave) {
+        wait_loads<0>();  // the block before has been read
+        bring(kn, 0);
+      }
       wait_loads<0>();
       take();
 #pragma unroll
@@ -813,7 +816,10 @@ __global__ __launch_bounds__(256, FINE && DP * RB > 64 ? 1 : 2) void attend_few_
         for (int x = 1; x < 32; x *= 2) sum[n][i] += __shfl_xor(sum[n][i], x, 64);
         if (col == 0) sums[wave][32 * n + 8 * (i >> 2) + 4 * lh + (i & 3)] = sum[n][i];
       }
-    if (some_blocks > WAVES && wave < some_blocks) bring(wave, 0);
+    if (some_blocks > WAVES && wave < some_blocks) {
+      wait_loads<0>();
+      bring(wave, 0);
+    }
     __syncthreads();
     if (t < ROWS) side[2][t] = -(((sums[0][t] + sums[1][t]) + sums[2][t]) + sums[3][t]);
     wait_loads<0>();

@@ -186,7 +186,8 @@ def test_one_key_has_no_gradient_of_scores(dtype):
 
 @pytest.mark.parametrize("b,lq,lk,h,kv,d", [
     (1, 5, 1200, 2, 2, 64), (1, 50, 1200, 2, 1, 32), (200, 3, 600, 1, 1, 40), (100, 20, 700, 6, 2, 64), (2, 64, 130, 4, 4, 64),
-    (3, 13, 260, 10, 2, 24), (2, 1, 33, 64, 1, 64), (2, 31, 1, 2, 1, 64), (2, 65, 300, 2, 2, 64)])
+    (3, 13, 260, 10, 2, 24), (2, 1, 33, 64, 1, 64), (2, 31, 1, 2, 1, 64), (2, 65, 300, 2, 2, 64), (40, 10, 300, 2, 1, 32),
+    (40, 30, 300, 2, 1, 32), (200, 40, 70, 1, 1, 17)])
 def test_few_rows(b, lq, lk, h, kv, d):
     """Heads of up to 64 rows, one group's or many's: keys split over workgroups or not."""
     c = Case(31, BF, b, lq, lk, h, kv, d)
@@ -197,6 +198,18 @@ def test_few_rows(b, lq, lk, h, kv, d):
     c = Case(34, BF, b, lq, lk, h, kv, d, mask=0.0)  # few kept keys, in some blocks only
     c.mask[:, lk // 3::97] = True
     c.check()
+
+
+@pytest.mark.parametrize("b,lq,lk,h,kv,d", [
+    (2, 150, 300, 4, 2, 128), (3, 100, 190, 4, 4, 96), (2, 300, 77, 2, 1, 64), (4, 90, 130, 2, 2, 32), (1, 40, 700, 16, 4, 120),
+    (9, 7, 90, 10, 2, 72), (3, 20, 1000, 12, 12, 128), (20, 33, 100, 1, 1, 128), (2, 257, 31, 3, 1, 96)])
+def test_more_than_512_rows(b, lq, lk, h, kv, d):
+    """Calls whose gradients take P and dS as they are rounded."""
+    assert b * lq * h > 512
+    Case(35, BF, b, lq, lk, h, kv, d).check()
+    lens = torch.arange(1, b + 1, device="cuda") * 61
+    Case(36, BF, b, lq, lk, h, kv, d, q_lens=(lens % (lq + 1)).tolist(), kv_lens=(lens % (lk + 1)).tolist(), pad=8).check()
+    Case(37, BF, b, lq, lk, h, kv, d, mask=0.5).check()
 
 
 def test_every_length_around_a_tile():
