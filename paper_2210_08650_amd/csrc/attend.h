@@ -8,6 +8,8 @@
 // operand is read from LDS in that order (by_column).
 #pragma once
 
+#include <type_traits>
+
 #include "block.h"
 #include "gemm_util.h"
 
@@ -229,46 +231,59 @@ __device__ __forceinline__ void store4(T *row, int d, int dim, bool vec, float v
 }
 
 // A wave's 32 rows of out^T, acc[d] the values 32 d + 8 q + 4 lh + e of row lane % 32, times
-// `by`, to memory: to is this lane's row (null: none).  Where rows allow it (vec16) they
-// are turned in `turn`, the wave's part of the LDS, and stored 16 bytes a lane, whole rows
-// to consecutive lanes; stores of the lanes' own values would be 16 bytes of each of 32
-// rows, and the L2 takes a request for every such piece.
+// `by`, to memory: to is this lane's row (null: none), vec what of a row can be stored at
+// once.  16-bit rows that allow 16 bytes at once are turned in `turn`, the wave's part of
+// the LDS, and stored whole to consecutive lanes; stores of the lanes' own values would be
+// up to 16 bytes of each of 32 rows, and the L2 takes a request for every such piece.
+// PAIRS: so are rows that allow two values but not four.  Forward and dq, which store more
+// than they read where rows are many: 16 x 3182 x 97, 16 + 8 heads of 86, 253 us, so 146, and
+// 429, so 310; dk and dv gained nothing, and 8 bytes a lane (64 x 64 x 197, heads of 60) are
+// faster as they are, forward 14.3 us for 15.6.
 template <typename T, int DB>
 struct RowsOut {
   static constexpr bool TURNS = sizeof(T) == 2;  // 32-bit values make 32 bytes of a row as they are
   static constexpr int PITCH = 32 * DB * (int)sizeof(T) + 16, BYTES = TURNS ? 32 * PITCH : 0;
-  static __device__ __forceinline__ void store(const f32x16_t (&acc)[DB], float by, T *to, int dim, bool vec4, bool vec16,
-                                               uint8_t *turn, int lane) {
-    const int lh = lane >> 5;
-    if (!TURNS || !vec16) {
-      if (to) {
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            store4<T>(to, 32 * d + 8 * q + 4 * lh, dim, vec4, acc[d][4 * q] * by, acc[d][4 * q + 1] * by, acc[d][4 * q + 2] * by,
-                      acc[d][4 * q + 3] * by);
-      }
-      return;
-    }
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint8_t *at = turn + (lane & 31) * PITCH + (32 * d + 8 * q + 4 * lh) * (int)sizeof(T);
-        const float v0 = acc[d][4 * q] * by, v1 = acc[d][4 * q + 1] * by, v2 = acc[d][4 * q + 2] * by, v3 = acc[d][4 * q + 3] * by;
-        *reinterpret_cast<uint2 *>(at) = make_uint2(f2bf2(v0, v1), f2bf2(v2, v3));
-      }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    constexpr int PER = 32 * DB * (int)sizeof(T) / 16, V = 16 / (int)sizeof(T);  // 16-byte slots of a row
+  // Rows from LDS, N values a lane.
+  template <int N>
+  static __device__ __forceinline__ void rows(T *to, int dim, const uint8_t *turn, int lane) {
+    typedef std::conditional_t<N == 8, uint4, uint32_t> Slot;
+    constexpr int PER = 32 * DB / N;  // slots of a row
     const uint64_t mine = (uint64_t)(uintptr_t)to;
 #pragma unroll
     for (int i = 0; i < 32 * PER / 64; ++i) {
       const int slot = i * 64 + lane, row = slot / PER, c = slot % PER;
       const uint32_t lo = __shfl((uint32_t)mine, row, 64), hi = __shfl((uint32_t)(mine >> 32), row, 64);
       T *p = reinterpret_cast<T *>((uintptr_t)((uint64_t)hi << 32 | lo));
-      const uint4 v = *reinterpret_cast<const uint4 *>(turn + row * PITCH + c * 16);
-      if (p && c * V < dim) *reinterpret_cast<uint4 *>(p + c * V) = v;
+      const Slot v = *reinterpret_cast<const Slot *>(turn + row * PITCH + c * sizeof(Slot));
+      if (p && c * N < dim) *reinterpret_cast<Slot *>(p + c * N) = v;
+    }
+  }
+  template <bool PAIRS>
+  static __device__ __forceinline__ void store(const f32x16_t (&acc)[DB], float by, T *to, int dim, int vec, uint8_t *turn, int lane) {
+    const int lh = lane >> 5;
+    if (!TURNS || !(vec & 2 || (PAIRS && vec == 4))) {
+      if (to) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            store4<T>(to, 32 * d + 8 * q + 4 * lh, dim, vec & 1, acc[d][4 * q] * by, acc[d][4 * q + 1] * by, acc[d][4 * q + 2] * by,
+                      acc[d][4 * q + 3] * by);
+      }
+      return;
+    }
+    if constexpr (TURNS) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint8_t *at = turn + (lane & 31) * PITCH + (32 * d + 8 * q + 4 * lh) * (int)sizeof(T);
+          const float v0 = acc[d][4 * q] * by, v1 = acc[d][4 * q + 1] * by, v2 = acc[d][4 * q + 2] * by, v3 = acc[d][4 * q + 3] * by;
+          *reinterpret_cast<uint2 *>(at) = make_uint2(f2bf2(v0, v1), f2bf2(v2, v3));
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (!PAIRS || vec & 2) rows<8>(to, dim, turn, lane);
+      else rows<2>(to, dim, turn, lane);
     }
   }
 };

@@ -412,10 +412,11 @@ int check_attend_inputs(const Attend &t, const void *q, const void *k, const voi
   return HAPI_OK;
 }
 
-// What of every row can be stored at once: bit 0, four values; bit 1, 16 bytes.
+// What of every row can be stored at once: bit 0, four values; bit 1, 16 bytes; bit 2, two
+// values.
 int at_once(const Attend &t, const void *p, const int64_t *st) {
   const auto fits = [&](int n) { return t.a.dim % n == 0 && st[0] % n == 0 && st[1] % n == 0 && st[2] % n == 0 && (uintptr_t)p % (n * t.esz) == 0; };
-  return (fits(4) ? 1 : 0) | (fits(t.v) ? 2 : 0);
+  return (fits(4) ? 1 : 0) | (fits(t.v) ? 2 : 0) | (fits(2) ? 4 : 0);
 }
 
 // A copy of in, [batch][tokens][heads], with aligned rows, and its strides.

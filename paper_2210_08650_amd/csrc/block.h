@@ -73,7 +73,7 @@ struct AttendArgs {
   int64_t q_st[3], k_st[3], v_st[3], o_st[3], g_st[3];  // elements; g: of dout
   void *y, *dq, *dk, *dv;            // y: o as it is written
   int64_t y_st[3], dq_st[3], dk_st[3], dv_st[3];
-  int32_t y_vec, dq_vec, dk_vec, dv_vec;  // 1: four values can be stored at once; 2: 16 bytes
+  int32_t y_vec, dq_vec, dk_vec, dv_vec;  // 1: four values can be stored at once; 2: 16 bytes; 4: two values
   float2 *stats;                     // [batch][q_len][heads] (largest score, log of the sum)
   const int64_t *q_lens, *kv_lens;
   const uint8_t *mask;               // [batch][kv_len] or null

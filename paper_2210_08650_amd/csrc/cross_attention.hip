@@ -235,7 +235,7 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 9
   T *y = static_cast<T *>(a.y) + (int64_t)b * a.y_st[0] + (int64_t)qi * a.y_st[1] + h * a.y_st[2];
   typedef RowsOut<T, DB> Out;
   static_assert(RW * Out::BYTES <= KW * 2 * STAGE, "the tiles' place");
-  Out::store(o, inv, r < rows ? y : nullptr, a.dim, a.y_vec & 1, a.y_vec & 2, smem + wr * Out::BYTES, lane);
+  Out::template store<true>(o, inv, r < rows ? y : nullptr, a.dim, a.y_vec, smem + wr * Out::BYTES, lane);
   if (r >= rows) return;
   if (lh == 0) a.stats[((int64_t)b * a.q_len + qi) * a.heads + h] = row_stats(m, ref, sum, a.scale);
 }

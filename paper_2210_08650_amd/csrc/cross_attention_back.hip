@@ -241,7 +241,7 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
   T *y = static_cast<T *>(a.dq) + (int64_t)b * a.dq_st[0] + (int64_t)qi * a.dq_st[1] + h * a.dq_st[2];
   typedef RowsOut<T, DB> Out;
   static_assert(RW * Out::BYTES <= KW * 2 * STAGE, "the tiles' place");
-  Out::store(dq, a.scale, r < rows ? y : nullptr, a.dim, a.dq_vec & 1, a.dq_vec & 2, smem + wr * Out::BYTES, lane);
+  Out::template store<true>(dq, a.scale, r < rows ? y : nullptr, a.dim, a.dq_vec, smem + wr * Out::BYTES, lane);
 }
 
 // How WAVES waves bring tiles of rows, q and dout, to LDS.  The rows are the tokens of a
@@ -437,8 +437,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : (DP <= 64 ? 3 : 2) - (FIN
   constexpr int HALF = 2 * STAGE >= 8 * Out::BYTES ? 4 * Out::BYTES : 0;  // places of their own, or one after the other
   static_assert(4 * Out::BYTES <= 2 * STAGE, "the tiles' place");
   __syncthreads();
-  Out::store(dk, a.scale, key < a.kv_len ? yk : nullptr, a.dim, a.dk_vec & 1, a.dk_vec & 2, smem + wave * Out::BYTES, lane);
-  Out::store(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim, a.dv_vec & 1, a.dv_vec & 2, smem + HALF + wave * Out::BYTES, lane);
+  Out::template store<false>(dk, a.scale, key < a.kv_len ? yk : nullptr, a.dim, a.dk_vec, smem + wave * Out::BYTES, lane);
+  Out::template store<false>(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim, a.dv_vec, smem + HALF + wave * Out::BYTES, lane);
 }
 
 // dk and dv of 128-value heads in 16 bits.  A wave that kept 32 keys' k, v, dk and dv would
@@ -655,8 +655,8 @@ __global__ __launch_bounds__(512, 2) void attend_dkv_pair_kernel(AttendArgs a) {
   typedef RowsOut<T, DB> Out;
   static_assert(2 * WAVES * Out::BYTES <= 3 * STAGE, "the tiles' place");
   __syncthreads();
-  Out::store(dk, a.scale, key < a.kv_len ? yk : nullptr, a.dim - d0, a.dk_vec & 1, a.dk_vec & 2, smem + wave * Out::BYTES, lane);
-  Out::store(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim - d0, a.dv_vec & 1, a.dv_vec & 2, smem + (WAVES + wave) * Out::BYTES, lane);
+  Out::template store<false>(dk, a.scale, key < a.kv_len ? yk : nullptr, a.dim - d0, a.dk_vec, smem + wave * Out::BYTES, lane);
+  Out::template store<false>(dv, 1.0f, key < a.kv_len ? yv : nullptr, a.dim - d0, a.dv_vec, smem + (WAVES + wave) * Out::BYTES, lane);
 }
 
 // dq, dk and dv of few rows, 16-bit heads of up to 64 values: a workgroup has all of the
@@ -897,9 +897,9 @@ __global__ __launch_bounds__(256, FINE && DP * RB > 64 ? 1 : 2) void attend_few_
     uint8_t *turn = own + (buf ? TURN : 0);
     typedef RowsOut<T, DB> Out;
     static_assert(Out::BYTES <= Keys::BYTES + Turned::BYTES, "the tiles' place");
-    Out::store(dk, a.scale, key < a.kv_len ? yk + (int64_t)key * a.dk_st[1] : nullptr, a.dim, a.dk_vec & 1, a.dk_vec & 2, turn, lane);
+    Out::template store<false>(dk, a.scale, key < a.kv_len ? yk + (int64_t)key * a.dk_st[1] : nullptr, a.dim, a.dk_vec, turn, lane);
     asm volatile("" ::: "memory");
-    Out::store(dv, 1.0f, key < a.kv_len ? yv + (int64_t)key * a.dv_st[1] : nullptr, a.dim, a.dv_vec & 1, a.dv_vec & 2, turn, lane);
+    Out::template store<false>(dv, 1.0f, key < a.kv_len ? yv + (int64_t)key * a.dv_st[1] : nullptr, a.dim, a.dv_vec, turn, lane);
     asm volatile("" ::: "memory");
   }
 
@@ -928,7 +928,7 @@ __global__ __launch_bounds__(256, FINE && DP * RB > 64 ? 1 : 2) void attend_few_
   // turned in the place of the first wave's part, which this wave alone has read
   typedef RowsOut<T, 1> Out;
   static_assert(Out::BYTES <= 4096, "a block's place");
-  Out::store(all, a.scale, r < rows ? y : nullptr, a.dim - 32 * d, a.dq_vec & 1, a.dq_vec & 2, smem + wave * 4096, lane);
+  Out::template store<false>(all, a.scale, r < rows ? y : nullptr, a.dim - 32 * d, a.dq_vec, smem + wave * 4096, lane);
 }
 
 // Adds the parts: a thread has four values of a row of dq, or of a key's dk (blockIdx.y
