@@ -112,53 +112,71 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 9
     __builtin_amdgcn_sched_barrier(0);
     if (now == 0) continue;  // the same for all waves of wk
     const uint8_t *kt = smem + wk * 2 * STAGE + (step & 1) * STAGE, *vt = kt + Tile::BYTES;
-    f32x16_t s[NT];  // scores less ref
+    f32x16_t s[NT];  // scores, FROM_REF: less ref
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       if (DP == 96 && ks == KS - 1 && 16 * ks >= a.dim) break;  // heads of 80: five sixths of 96
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), qf[ks], ks > 0 ? s[n] : FROM_REF ? start : zeros());
     }
-    if constexpr (!FROM_REF) {
+    // -inf for keys that take no part; the row's largest
+    auto masked = [&]() {
+      if (now != ALL) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint32_t bits = (uint32_t)(now >> (32 * n)) >> (4 * lh);
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1)) s[n][i] = -INFINITY;
+        }
+      }
+      float mx = -INFINITY;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] -= ref;
-    }
-    if (now != ALL) {
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
+      return fmaxf(mx, __shfl_xor(mx, 32, 64));
+    };
+    auto subtract = [&](float by) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint32_t bits = (uint32_t)(now >> (32 * n)) >> (4 * lh);
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1)) s[n][i] = -INFINITY;
-      }
-    }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    m = fmaxf(m, ref + mx);
+        for (int i = 0; i < 16; ++i) s[n][i] -= by;
+    };
+    float mx = masked();
     // the first key of a row sets its ref, whatever its size
-    const bool moves = mx > slack || (first && mx > -INFINITY);
+    const bool moves = (FROM_REF ? mx : mx - ref) > slack || (first && mx > -INFINITY);
+    bool less_ref = FROM_REF;  // what s and mx are
+    if (FROM_REF && __any(moves && !first)) {
+      // Scores less a ref far below them have lost their low bits to its size: they are
+      // formed again by themselves, with q from memory (a loop about both, with q in its
+      // registers: 2 x 4096 x 4096 348 us for 308).
+      less_ref = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n] = zeros();
+#pragma unroll 1
+      for (int ks = 0; ks < KS; ++ks) {
+        const Frag f = row_frag<T>(qp, ks, lh, a.dim, counts);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), f, s[n]);
+      }
+      mx = masked();
+    }
+    m = fmaxf(m, less_ref ? ref + mx : mx);
     if (__any(moves)) {
-      const float by = moves ? mx : 0.0f;
-      const float alpha = first ? 1.0f : __builtin_amdgcn_exp2f(-by * a.c);
+      const float to = moves ? mx : ref;  // a first ref is 0, so mx is the score itself
+      const float alpha = first ? 1.0f : __builtin_amdgcn_exp2f((ref - to) * a.c);
+      if (FROM_REF) subtract(less_ref ? to - ref : to);
       first = first && !moves;
-      ref += by;
+      ref = to;
       start = block_of(-ref);
       sum *= alpha;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] -= by;
     }
+    if (!FROM_REF) subtract(ref);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
