@@ -185,9 +185,12 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// The keys of a tile that take part: a bit for each of up to 64.
-__device__ __forceinline__ uint64_t key_bits(int64_t left) {
-  return left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0;
+// The keys of a tile of BN: a bit for each, of all of them and of the first `left`.
+template <int BN>
+constexpr uint64_t kAllKeys = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
+template <int BN>
+constexpr uint64_t key_bits(int64_t left) {
+  return left >= BN ? kAllKeys<BN> : left > 0 ? (1ull << left) - 1 : 0;
 }
 
 // A wave's 8 values of k of a row in memory: values 16 ks + 8 lh .. + 7, zeros past dim

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 9
   uint64_t keep = 0;  // of the tile in flight
   auto issue = [&](int step) {
     const int kt = t0 + step * KW + wk;
-    keep = kt < t1 ? key_bits(kv_valid - (int64_t)kt * BN) : 0;
+    keep = kt < t1 ? key_bits<BN>(kv_valid - (int64_t)kt * BN) : 0;
     if (keep && a.mask) {
       const bool in = (keep >> lane) & 1;
       keep &= __ballot(in && a.mask[(int64_t)b * a.kv_len + (int64_t)kt * BN + (in ? lane : 0)] != 0);
@@ -97,7 +97,6 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 9
   f32x16_t start = zeros();
   bool first = true;
   const float slack = 8.0f / a.c;
-  constexpr uint64_t ALL = BN == 64 ? ~0ull : (1ull << BN) - 1;
 
   if (steps > 0) issue(0);
   for (int step = 0; step < steps; ++step) {
@@ -121,7 +120,7 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 9
     }
     // -inf for keys that take no part; the row's largest
     auto masked = [&]() {
-      if (now != ALL) {
+      if (now != kAllKeys<BN>) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const uint32_t bits = (uint32_t)(now >> (32 * n)) >> (4 * lh);

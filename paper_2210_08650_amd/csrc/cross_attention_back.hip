@@ -97,11 +97,10 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
   const T *kp = static_cast<const T *>(a.k) + (int64_t)b * a.k_st[0] + (int64_t)kh * a.k_st[2];
   const T *vp = static_cast<const T *>(a.v) + (int64_t)b * a.v_st[0] + (int64_t)kh * a.v_st[2];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem + wk * 2 * STAGE;
-  constexpr uint64_t ALL = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
 
   // the keys of tile kt that take part
   auto bits_of = [&](int kt) {
-    uint64_t keep = key_bits(kv_valid - (int64_t)kt * BN);
+    uint64_t keep = key_bits<BN>(kv_valid - (int64_t)kt * BN);
     if (a.mask) {
       const bool in = (keep >> lane) & 1;
       keep &= __ballot(in && a.mask[(int64_t)b * a.kv_len + (int64_t)kt * BN + (in ? lane : 0)] != 0);
@@ -131,7 +130,7 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i] - m, a.c, -l2)) * (dp[i] - less);
-    if (keep != ALL) {
+    if (keep != kAllKeys<BN>) {
       const uint32_t bits = (uint32_t)(keep >> (32 * n)) >> (4 * lh);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
