@@ -656,8 +656,9 @@ int64_t hapi_cross_attention_workspace_bytes(const hapi_attention_desc *desc, in
 int hapi_cross_attention_forward(const hapi_attention_desc *desc, const void *q, const void *k, const void *v,
                                  const int64_t *q_lens, const int64_t *kv_lens, const uint8_t *mask, void *o, float *stats);
 
-/* Gradients of sum(dout o); o and stats are the forward pass's.  dq of padding and of rows
- * without a key, and dk and dv of keys that take no part, are 0; dk and dv of a key head
+/* Gradients of sum(dout o); o and stats are the forward pass's, o and the gradients
+ * element-aligned, dout 16-byte aligned when head_dim and o_stride are whole 16-byte
+ * multiples, else element-aligned.  dq of padding and of rows without a key, and dk and dv of keys that take no part, are 0; dk and dv of a key head
  * are sums over its query heads.  Tensors that share memory between batch entries or heads
  * (a stride of 0) have no gradient here (HAPI_E_INVAL).  Errors as forward. */
 int hapi_cross_attention_backward(const hapi_attention_desc *desc, const void *q, const void *k, const void *v,

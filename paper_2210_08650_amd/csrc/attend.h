@@ -194,7 +194,8 @@ constexpr uint64_t key_bits(int64_t left) {
 }
 
 // A wave's 8 values of k of a row in memory: values 16 ks + 8 lh .. + 7, zeros past dim
-// (whole 16-byte slots are inside or outside).
+// (whole 16-byte slots are inside or outside).  The row needs its elements' alignment only:
+// o lies where the forward pass was told to write it (loads of 16 bytes need no more here).
 template <typename T>
 __device__ __forceinline__ typename Elem<T>::Frag row_frag(const T *row, int ks, int lh, int dim, bool there) {
   typedef typename Elem<T>::Frag Frag;
@@ -203,13 +204,13 @@ __device__ __forceinline__ typename Elem<T>::Frag row_frag(const T *row, int ks,
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = 0;
   if constexpr (sizeof(T) == 2) {
-    if (there && d < dim) f = *reinterpret_cast<const Frag *>(row + d);
+    if (there && d < dim) __builtin_memcpy(&f, row + d, 16);
   } else {
     typedef float f32x4_t __attribute__((ext_vector_type(4)));
     f32x4_t h[2] = {};
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (there && d + 4 * i < dim) h[i] = *reinterpret_cast<const f32x4_t *>(row + d + 4 * i);
+      if (there && d + 4 * i < dim) __builtin_memcpy(&h[i], row + d + 4 * i, 16);
     f = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
   }
   return f;

@@ -583,7 +583,7 @@ int hapi_cross_attention_backward(const hapi_attention_desc *desc, const void *q
   if (t.batch == 0 || (a.q_len == 0 && a.kv_len == 0)) return HAPI_OK;
   TRY(check_attend_inputs(t, q, k, v, q_lens, kv_lens, mask));
   if (a.q_len > 0) {
-    TRY(check_ptr(o, t.stage_o ? t.esz : 16, "o"));
+    TRY(check_ptr(o, t.esz, "o"));
     TRY(check_ptr(stats, 8, "stats"));
     TRY(check_ptr(dout, t.stage_o ? t.esz : 16, "dout"));
     TRY(check_ptr(dq, t.esz, "dq"));

@@ -69,7 +69,7 @@ constexpr int kAttendMaxGroup = 512;  // query heads of a key head
 // The rows of one key head's problem are its query heads' tokens: row r is token
 // r / group, head r % group of the group.
 struct AttendArgs {
-  const void *q, *k, *v, *o, *dout;  // as the kernels read them: 16-byte aligned rows
+  const void *q, *k, *v, *o, *dout;  // as the kernels read them: 16-byte aligned rows (o: whole 16-byte slots)
   int64_t q_st[3], k_st[3], v_st[3], o_st[3], g_st[3];  // elements; g: of dout
   void *y, *dq, *dk, *dv;            // y: o as it is written
   int64_t y_st[3], dq_st[3], dk_st[3], dv_st[3];
