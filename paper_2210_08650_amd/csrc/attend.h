@@ -171,6 +171,18 @@ struct Loader {
     for (int i = 0; i < LOADS; ++i)
       lds_dma16(srd, lds + (wave * LOADS + i) * 1024, (keep >> row[i]) & 1 ? off[i] : kOob, 0);
   }
+  // The tile's rows are the rows list[0 .. ROWS) of base, within 2^31 bytes of it.
+  static __device__ __forceinline__ void gather(const void *base, int64_t stride, int dim, const int *list, uint32_t lds, uint64_t keep, int wave,
+                                                int lane) {
+    const u32x4_t srd = make_srd(base);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * LOADS * 1024), ld = (uint32_t)stride * (uint32_t)sizeof(T);
+#pragma unroll 1  // rare, and its offsets would take registers from the kernel's loop
+    for (int i = 0; i < LOADS; ++i) {
+      const int slot = (wave * LOADS + i) * 64 + lane, r = slot / Tile::CPR, c = (slot % Tile::CPR) ^ Tile::swz(r);
+      const bool there = ((keep >> r) & 1) && c * Tile::V < dim;
+      lds_dma16(srd, to + i * 1024, there ? (uint32_t)list[r] * ld + (uint32_t)(c * 16) : kOob, 0);
+    }
+  }
 };
 
 // Until at most N of this wave's loads and DMAs are in flight and its LDS reads are done.

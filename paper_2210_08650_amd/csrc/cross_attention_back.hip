@@ -37,17 +37,28 @@ __device__ __forceinline__ void keep_rest(f32x16_t &s) {
   for (int i = 0; i < 16; ++i) s[i] -= (float)(__bf16)s[i];
 }
 
-// Whether a mask leaves at most kFewKeys of n keys.
-__device__ __forceinline__ bool few_kept(const uint8_t *mask, int n, int lane) {
+// How many of n keys a mask leaves, or more than kFewKeys as soon as it is that many.  The
+// first kFewKeys of them to list (or null), in order.
+__device__ __forceinline__ int kept_keys(const uint8_t *mask, int n, int lane, int *list) {
   int kept = 0;
-  for (int k = 0; k < n && kept <= kFewKeys; k += 256) {
-    bool on[4];
+  auto count = [&](auto loads, int k) {  // loads in flight, of 64 keys each
+    constexpr int N = decltype(loads)::value;
+    bool on[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) on[i] = k + 64 * i + lane < n && mask[k + 64 * i + lane] != 0;
+    for (int i = 0; i < N; ++i) on[i] = k + 64 * i + lane < n && mask[k + 64 * i + lane] != 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) kept += __popcll(__ballot(on[i]));
-  }
-  return kept <= kFewKeys;
+    for (int i = 0; i < N; ++i) {
+      const uint64_t bits = __ballot(on[i]);
+      if (list && bits != 0 && kept < kFewKeys) {
+        const int at = kept + __popcll(bits & ((1ull << lane) - 1));
+        if (on[i] && at < kFewKeys) list[at] = k + 64 * i + lane;
+      }
+      kept += __popcll(bits);
+    }
+  };
+  count(std::integral_constant<int, 4>(), 0);  // most masks are told by these
+  for (int k = 256; k < n && kept <= kFewKeys; k += 1024) count(std::integral_constant<int, 16>(), k);
+  return __builtin_amdgcn_readfirstlane(kept);
 }
 
 template <typename T, int DP, int RW, int KW, int BN, bool FINE>
@@ -56,7 +67,9 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
   typedef Loader<T, DP, BN, RW> Load;
   typedef typename Elem<T>::Frag Frag;
   constexpr int KS = DP / 16, DB = DP / 32, NT = BN / 32, STAGE = 2 * Tile::BYTES;
+  static_assert(kFewKeys % BN == 0, "whole tiles of listed keys");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[KW * 2 * STAGE];
+  __shared__ int list[kFewKeys];  // keys that a mask leaves
 
   const int t = threadIdx.x, lane = t & 63, col = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wr = wave % RW, wk = wave / RW;
@@ -90,7 +103,23 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
     if (st.x != -INFINITY) m = st.x, l2 = st.y * kLog2e;
   }
 
-  const int key_tiles = tile * RW * 32 < q_valid * a.group ? (kv_valid + BN - 1) / BN : 0;
+  // Of few keys that a mask leaves of many, only they are brought, one after another in the
+  // tiles, as long as 32-bit offsets reach them all: a walk over every tile, which each
+  // workgroup made twice, took longer than all keys do (a step with 100 keys left: float32 1 x
+  // 20 x 16384, 8 heads of 64, 655 us, now 143, and 118 with all of them; 2 x 300 x 16384, 8 +
+  // 2 heads of 128 in bf16, 434, now 215, and 250).
+  bool few = kv_valid <= kFewKeys, listed = false;
+  int keys = kv_valid;
+  if (!few && a.mask) {
+    const int kept = kept_keys(a.mask + (int64_t)b * a.kv_len, kv_valid, lane, wave == 0 ? list : nullptr);
+    few = kept <= kFewKeys;
+    const int64_t ld = a.k_st[1] > a.v_st[1] ? a.k_st[1] : a.v_st[1];
+    listed = few && (kv_valid * ld + a.dim) * (int64_t)sizeof(T) < (int64_t)kOob - 16;
+    if (listed) keys = kept;
+    __syncthreads();
+  }
+  keys = __builtin_amdgcn_readfirstlane(keys);
+  const int key_tiles = tile * RW * 32 < q_valid * a.group ? (keys + BN - 1) / BN : 0;
   Load lk, lv;
   lk.init(a.k_st[1], a.dim, wr, lane);
   lv.init(a.v_st[1], a.dim, wr, lane);
@@ -100,8 +129,8 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
 
   // the keys of tile kt that take part
   auto bits_of = [&](int kt) {
-    uint64_t keep = key_bits<BN>(kv_valid - (int64_t)kt * BN);
-    if (a.mask) {
+    uint64_t keep = key_bits<BN>(keys - (int64_t)kt * BN);
+    if (a.mask && !listed) {
       const bool in = (keep >> lane) & 1;
       keep &= __ballot(in && a.mask[(int64_t)b * a.kv_len + (int64_t)kt * BN + (in ? lane : 0)] != 0);
     }
@@ -109,6 +138,11 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
   };
   auto bring = [&](int kt, uint64_t keep, int buf) {
     const uint32_t at = lds0 + buf * STAGE;
+    if (listed) {
+      Load::gather(kp, a.k_st[1], a.dim, list + kt * BN, at, keep, wr, lane);
+      Load::gather(vp, a.v_st[1], a.dim, list + kt * BN, at + Tile::BYTES, keep, wr, lane);
+      return;
+    }
     lk.issue(kp + (int64_t)kt * BN * a.k_st[1], at, keep, wr);
     lv.issue(vp + (int64_t)kt * BN * a.v_st[1], at + Tile::BYTES, keep, wr);
   };
@@ -144,8 +178,6 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 ? (DP <= 6
   // to average it (bf16, 4 keys: dq off by 0.0030 of its length, so 0.0024; past 128 keys
   // it adds less than a tenth of what rounding dS does), and of one key dS is 0, as
   // its score is formed here as the forward pass formed m.
-  bool few = kv_valid <= kFewKeys;
-  if (!few && a.mask) few = few_kept(a.mask + (int64_t)b * a.kv_len, kv_valid, lane);
   if (few) {
     float sum = 0.0f;
     for (int kt = 0; kt < key_tiles; ++kt) {
@@ -788,7 +820,7 @@ __global__ __launch_bounds__(256, FINE && DP * RB > 64 ? 1 : 2) void attend_few_
 
   // of few keys delta is the sum of p dp, as in dq's kernel
   bool few = kv_valid <= kFewKeys;
-  if (!few && a.mask) few = few_kept(a.mask + (int64_t)b * a.kv_len, kv_valid, lane);
+  if (!few && a.mask) few = kept_keys(a.mask + (int64_t)b * a.kv_len, kv_valid, lane, nullptr) <= kFewKeys;
   if (few && some_blocks > 0) {
     f32x16_t sum[RB];
 #pragma unroll
@@ -800,6 +832,7 @@ __global__ __launch_bounds__(256, FINE && DP * RB > 64 ? 1 : 2) void attend_few_
       }
       wait_loads<0>();
       take();
+      if (!__any(counts)) continue;  // a mask leaves none of the block
 #pragma unroll
       for (int n = 0; n < RB; ++n) {
         scores(std::false_type(), n, own);
