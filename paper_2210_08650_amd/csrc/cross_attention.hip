@@ -176,13 +176,18 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 9
         for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
     }
     if (!FROM_REF) subtract(ref);
+    // Probabilities of 32 keys are summed by themselves: the roundings of thousands of equal
+    // ones to a running sum would all go one way (16384 keys: off by 1.1e-4 of it, so 4e-6).
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
+      float own = 0.0f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         s[n][i] = __builtin_amdgcn_exp2f(s[n][i] * a.c);
-        sum += s[n][i];
+        own += s[n][i];
       }
+      sum += own;
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const Frag p[2] = {operand<T>(s[n], 0), operand<T>(s[n], 1)};

@@ -4,8 +4,9 @@ import math
 import pytest
 import torch
 
+import paper_2210_08650_amd as H
 from tests import block_reference as R
-from tests.test_gpu_cross_attention import BF, F32, Case
+from tests.test_gpu_cross_attention import BF, CODE, F32, Case
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +30,29 @@ def test_keys_far_below_the_rest_come_first(b, lq, lk, h, kv, d, first, far, dty
     z, ez = ref.z[..., first:], ref.ez[..., first:]
     off = (m - z.amax(-1)).abs()
     assert bool((off <= ez.amax(-1) + 4 * R.F * (z.abs().amax(-1) + 1)).all()), float(off.max())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("less", [0.375, 0.75, 1.5, 2.5])
+def test_sums_of_many_equal_probabilities(less, dtype):
+    """One key and 16383 whose scores are `less` below it, in calls whose keys are not split:
+    the sum is 1 + 16383 exp(-less).  Equal terms round the same way each time, so a sum of n of
+    them is off by up to n / 2 units F of itself: a lane's 16 of 32 keys 8, 512 times 32 keys
+    256; exp2, its argument and the joins take less than 16 more.  o is a mean of ones: its own sums
+    (16 products of a block, 512 blocks) are as far off, the quotient twice that."""
+    b, lk, heads, d = 1, 16384, 300, 128
+    q = torch.zeros(b, 1, heads, d, dtype=dtype, device="cuda")
+    q[..., 0] = 1.0
+    k = torch.zeros(b, lk, 1, d, dtype=dtype, device="cuda")
+    k[:, 1:, :, 0] = -less
+    v = torch.ones_like(k)
+    k, v = (x.expand(b, lk, heads, d) for x in (k, v))
+    desc = H.Attention(CODE[dtype], b, 1, lk, heads, heads, d, scale=1.0, k_stride=k.stride()[:3], v_stride=v.stride()[:3],
+                       stream=torch.cuda.current_stream())
+    assert H.hapi_cross_attention_workspace_bytes(desc) == 0  # no parts
+    o, st = torch.empty_like(q), torch.empty(b, 1, heads, 2, device="cuda")
+    H.hapi_cross_attention_forward(desc, q, k, v, None, None, None, o, st)
+    want = math.log1p((lk - 1) * math.exp(-less))
+    assert not bool(st[..., 0].any())
+    assert float((st[..., 1].double() - want).abs().max()) <= 280 * R.F + 2 * R.F * want
+    assert float((o.double() - 1.0).abs().max()) <= (2 * 280 * R.F if dtype == F32 else R.U[BF])
