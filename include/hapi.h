@@ -652,6 +652,8 @@ int64_t hapi_cross_attention_workspace_bytes(const hapi_attention_desc *desc, in
  *             backward pass reads (apart, so that a row of large scores keeps its l)
  * Keys that take no part and padding are not read as numbers: they may be NaN.  A row
  * without a key (or whose every score is -inf), and padding, has o = 0 and m = l = -inf.
+ * A row with a score that is NaN has o and l NaN, and m the largest of the others (NaN where
+ * there is none).
  * Errors: HAPI_E_INVAL, HAPI_E_UNSUPPORTED, HAPI_E_NOMEM, HAPI_E_DEVICE. */
 int hapi_cross_attention_forward(const hapi_attention_desc *desc, const void *q, const void *k, const void *v,
                                  const int64_t *q_lens, const int64_t *kv_lens, const uint8_t *mask, void *o, float *stats);

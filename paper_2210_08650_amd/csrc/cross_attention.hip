@@ -32,8 +32,10 @@
 namespace hapi {
 namespace {
 
-// (largest score, log of the sum about it) from the sum about ref.
+// (largest score, log of the sum about it) from the sum about ref.  A row of NaN alone has
+// no largest score, and is no row without a key.
 __device__ __forceinline__ float2 row_stats(float m, float ref, float sum, float scale) {
+  if (m == -INFINITY && sum != sum) m = sum;
   return make_float2(m, m == -INFINITY ? -INFINITY : logf(sum) - (m - ref) * scale);
 }
 

@@ -56,3 +56,28 @@ def test_sums_of_many_equal_probabilities(less, dtype):
     assert not bool(st[..., 0].any())
     assert float((st[..., 1].double() - want).abs().max()) <= 280 * R.F + 2 * R.F * want
     assert float((o.double() - 1.0).abs().max()) <= (2 * 280 * R.F if dtype == F32 else R.U[BF])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lq,lk,d", [(40, 80, 64), (3, 3000, 128), (200, 50, 32)])
+def test_statistics_of_nan(lq, lk, d, dtype):
+    """A query of NaN is no query without a key: its statistics are NaN, as its output, and so
+    are all gradients that it reaches.  A key of NaN leaves a row the others' maximum."""
+    c = Case(52, dtype, 2, lq, lk, 4, 2, d)
+    c.q[1, 2, 3, 1] = math.nan
+    o, st = c.forward()
+    bad = torch.zeros(2, lq, 4, dtype=torch.bool, device="cuda")
+    bad[1, 2, 3] = True
+    assert torch.equal(torch.isnan(o).all(-1), bad) and torch.equal(torch.isnan(st).all(-1), bad) and torch.equal(torch.isnan(st).any(-1), bad)
+    dq, dk, dv = c.backward(o, st)
+    assert torch.equal(torch.isnan(dq).all(-1), bad) and torch.equal(torch.isnan(dq).any(-1), bad)
+    for g in (dk, dv):
+        nan = torch.isnan(g)
+        assert bool(nan[1, :, 1].all()) and int(nan.sum()) == lk * d
+    c = Case(53, dtype, 1, lq, lk, 2, 2, d)
+    ref = c.reference()
+    c.k[0, 0, 1] = math.nan
+    o, st = c.forward()
+    assert bool(torch.isnan(o[:, :, 1]).all()) and bool(torch.isnan(st[:, :, 1, 1]).all()) and not bool(torch.isnan(o[:, :, 0]).any())
+    z, ez = ref.z[0, 1, :, 1:], ref.ez[0, 1, :, 1:]
+    assert bool(((st[0, :, 1, 0] - z.amax(-1)).abs() <= ez.amax(-1) + 4 * R.F * (z.abs().amax(-1) + 1)).all())
