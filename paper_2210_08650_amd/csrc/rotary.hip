@@ -172,8 +172,10 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
           float &p = NEIGHBOURS ? v[n][2 * j] : v[n][j];
           float &q = NEIGHBOURS ? v[n][2 * j + 1] : v[n][V + j];
           const float p0 = p, q0 = q;
-          p = p0 * cs[n][j] - q0 * sn[n][j];
-          q = q0 * cs[n][j] + p0 * sn[n][j];
+          // what is not rotated stays as it is: 0 times its neighbour may be 0 times infinity
+          const bool turns = (lane + n * LV) * V + j < P;
+          p = turns ? p0 * cs[n][j] - q0 * sn[n][j] : p0;
+          q = turns ? q0 * cs[n][j] + p0 * sn[n][j] : q0;
         }
       };
       if constexpr (!BACK) {
