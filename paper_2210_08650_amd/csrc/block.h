@@ -56,8 +56,8 @@ struct RotaryArgs {
   float eps, inv_dim;
   bool norm, neighbours;
 };
-// Values of a pair's side that one lane handles: 16 bytes of them where all widths,
-// strides and addresses allow it.
+// v: values of a pair's side that one lane handles, 16 bytes of them where the widths divide
+// into them and the call is large enough, at their elements' alignment.
 hipError_t launch_rotary_forward(bool bf16, int v, const RotaryArgs &a, hipStream_t s);
 hipError_t launch_rotary_backward(bool bf16, int v, const RotaryArgs &a, hipStream_t s);
 

@@ -2,10 +2,11 @@
 // forward and backward.
 //
 // A vector (one head of one token) belongs to LV lanes of a wave, a lane to V pairs of
-// it: V values of either side of the pairs, 16 bytes each where widths, strides and
-// addresses allow it; what is not rotated goes as pairs that turn by nothing.  A lane
-// keeps its pairs over the heads of a token, so that angles, sines and cosines are
-// formed once for all of them; q and k go to blocks of their own, each with one gamma.
+// it: V values of either side of the pairs, 16 bytes each where the widths divide into them
+// and the call is large enough (strides and addresses need their elements' alignment only);
+// what is not rotated goes as pairs that do not turn.  A lane keeps its pairs over the heads
+// of a token, so that angles, sines and cosines are formed once for all of them; q and k go
+// to blocks of their own, each with one gamma.
 // The angle is position times frequency in float64, reduced to a part of a turn there:
 // in float32 its rounding at position 1e6 would be 0.03 radians.  Norm, rotation and sums
 // are float32, outputs are rounded once.

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from tests import block_reference as R
+import paper_2210_08650_amd as H
 from tests.test_gpu_rotary import BF, F32, Case
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +33,37 @@ def test_values_that_are_not_rotated_keep_their_bits(batch, length, heads, kv_he
             for got, src in ((y[i], c.x[i]), (dx[i], c.dy[i])):
                 assert torch.equal(got[..., p:].contiguous().view(bits), src[..., p:].contiguous().view(bits))
                 assert bool(torch.isfinite(got[..., :p]).all())
+
+
+def _moved(x):
+    """The same values from one element past an aligned address."""
+    y = torch.empty(x.numel() + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape)
+    y.copy_(x)
+    return y
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("batch,length,heads,kv_heads,dim,sections,neighbours", [
+    (8, 3001, 4, 2, 64, (16, 16), False), (3, 5003, 6, 2, 128, (24, 16, 24), True), (5, 2003, 15, 5, 80, (40,), False)])
+def test_many_tokens_at_any_element(batch, length, heads, kv_heads, dim, sections, neighbours, dtype):
+    """Calls of enough vectors for 16 bytes a lane, which are then loaded and stored at their
+    elements' alignment: odd strides, and the same bits one element past an aligned address."""
+    widest = 8 if dtype == BF else 4
+    lanes = 4
+    while lanes * 2 * widest < dim:
+        lanes *= 2
+    assert batch * length * (heads + kv_heads) * lanes >= 256 * 1024
+    lens = [(length * (i + 1)) // batch - 3 * i for i in range(batch)]
+    Case(92, dtype, batch, length, heads, kv_heads, dim, sections, neighbours=neighbours, pad=1, lens=lens).check()
+    c = Case(93, dtype, batch, length, heads, kv_heads, dim, sections, neighbours=neighbours, lens=lens)
+    y = c.forward()
+    dx, dg = c.backward()
+    x, dy, out = [_moved(v) for v in c.x], [_moved(v) for v in c.dy], [_moved(torch.zeros_like(v)) for v in c.x]
+    d = c.desc()
+    H.hapi_rotary_forward(d, *x, *c.gamma, c.positions, c.freq, c.lens, *out)
+    assert all(torch.equal(a, b) for a, b in zip(out, y))
+    g = [torch.empty_like(v) for v in dg]
+    H.hapi_rotary_backward(d, *dy, *x, *c.gamma, c.positions, c.freq, c.lens, *out, *g)
+    torch.cuda.synchronize()
+    c.ws.check()
+    assert all(torch.equal(a, b) for a, b in zip(out + g, dx + dg))
