@@ -600,7 +600,8 @@ int64_t hapi_rotary_workspace_bytes(const hapi_rotary_desc *desc);
  *   freq       [P] float64: radians a step
  *   lens       [batch] int64 or NULL: tokens from lens[b] on are padding: they are not
  *              read (they may be NaN), and their outputs are 0
- *   q_out, k_out  outputs; each may be q or k itself where their strides are the same
+ *   q_out, k_out  outputs; q_out may be q itself, and k_out k, where their strides are the
+ *              same (q_out must not be k, nor k_out q: both are worked on at once)
  * Errors: HAPI_E_INVAL, HAPI_E_UNSUPPORTED, HAPI_E_DEVICE. */
 int hapi_rotary_forward(const hapi_rotary_desc *desc, const void *q, const void *k, const float *q_gamma, const float *k_gamma,
                         const int64_t *positions, const double *freq, const int64_t *lens, void *q_out, void *k_out);
@@ -608,7 +609,7 @@ int hapi_rotary_forward(const hapi_rotary_desc *desc, const void *q, const void 
 /* dq, dk (of the strides of q and k; 0 for padding), and float32 [head_dim] dq_gamma and
  * dk_gamma, sums over batch, tokens and heads (NULL without a norm; zeros of no tokens).
  * q and k are the forward pass's inputs (not read without a norm).  dq may be dq_out
- * itself where their strides are the same.  Errors as forward; HAPI_E_NOMEM. */
+ * itself, and dk dk_out, where their strides are the same.  Errors as forward; HAPI_E_NOMEM. */
 int hapi_rotary_backward(const hapi_rotary_desc *desc, const void *dq_out, const void *dk_out, const void *q, const void *k,
                          const float *q_gamma, const float *k_gamma, const int64_t *positions, const double *freq,
                          const int64_t *lens, void *dq, void *dk, float *dq_gamma, float *dk_gamma);

@@ -293,6 +293,24 @@ int check_both(const Rotary &r, const void *q, const void *k, const char *q_name
   return HAPI_OK;
 }
 
+// Outputs in place of inputs: each in its own input's, with the same strides; q and k are
+// worked on at once, so neither is written where the other is read or written.
+int check_places(const Rotary &r, const void *const (&in)[2], const int64_t (&in_st)[2][3], const void *const (&out)[2],
+                 const int64_t (&out_st)[2][3], const char *const (&in_name)[2], const char *const (&out_name)[2]) {
+  for (int w = 0; w < 2; ++w) {
+    if (r.a.heads[w] == 0) continue;
+    const int64_t extent[3] = {r.batch, r.a.len, r.a.heads[w]};
+    for (int i = 0; in[w] == out[w] && i < 3; ++i)
+      if (extent[i] > 1 && in_st[w][i] != out_st[w][i])
+        return fail(HAPI_E_INVAL, "%s may be %s only where their strides are the same", out_name[w], in_name[w]);
+    if (r.a.heads[1 - w] > 0 && in[0] != in[1] && out[w] == in[1 - w])
+      return fail(HAPI_E_INVAL, "%s must not be %s", out_name[w], in_name[1 - w]);
+  }
+  if (r.a.heads[0] > 0 && r.a.heads[1] > 0 && in[0] != in[1] && out[0] == out[1])
+    return fail(HAPI_E_INVAL, "%s and %s are the same", out_name[0], out_name[1]);
+  return HAPI_OK;
+}
+
 // ----------------------------------------------------------- cross attention
 
 struct Attend {
@@ -496,6 +514,7 @@ int hapi_rotary_forward(const hapi_rotary_desc *desc, const void *q, const void 
   TRY(check_both(r, q_out, k_out, "q_out", "k_out"));
   TRY(check_apart(r.a.y_st[0], r.batch, r.a.len, r.a.heads[0], r.a.dim, "q_out"));
   TRY(check_apart(r.a.y_st[1], r.batch, r.a.len, r.a.heads[1], r.a.dim, "k_out"));
+  TRY(check_places(r, {q, k}, r.a.x_st, {q_out, k_out}, r.a.y_st, {"q", "k"}, {"q_out", "k_out"}));
   TRY(check_stream(desc->stream));
   r.a.x[0] = q;
   r.a.x[1] = k;
@@ -526,6 +545,10 @@ int hapi_rotary_backward(const hapi_rotary_desc *desc, const void *dq_out, const
     r.a.dgamma[w] = dgamma[w];
   }
   TRY(check_workspace(desc->workspace, desc->workspace_bytes, rotary_workspace(r)));
+  if (r.a.tokens > 0) {
+    TRY(check_places(r, {dq_out, dk_out}, r.a.y_st, {dq, dk}, r.a.x_st, {"dq_out", "dk_out"}, {"dq", "dk"}));
+    if (r.a.norm) TRY(check_places(r, {q, k}, r.a.x_st, {dq, dk}, r.a.x_st, {"q", "k"}, {"dq", "dk"}));
+  }
   TRY(check_stream(desc->stream));
   r.a.x[0] = q;
   r.a.x[1] = k;
