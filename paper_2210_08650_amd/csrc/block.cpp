@@ -368,6 +368,12 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
   TRY(read_strides(d->k_stride, d->kv_len, d->kv_heads, d->head_dim, "k", a.k_st));
   TRY(read_strides(d->v_stride, d->kv_len, d->kv_heads, d->head_dim, "v", a.v_st));
   TRY(read_strides(d->o_stride, d->q_len, d->heads, d->head_dim, "o", a.o_st));
+  // An extent of one has no stride: whatever is given, it costs no copy and no narrow store.
+  const int64_t extents[2][3] = {{d->batch, d->q_len, d->heads}, {d->batch, d->kv_len, d->kv_heads}};
+  for (int i = 0; i < 3; ++i) {
+    if (extents[0][i] == 1) a.q_st[i] = a.o_st[i] = 0;
+    if (extents[1][i] == 1) a.k_st[i] = a.v_st[i] = 0;
+  }
   // The kernels read whole 16-byte slots, at 32-bit offsets from a tile's first token.
   const auto staged = [&](const int64_t *st, int64_t heads) {
     return d->head_dim % t.v != 0 || st[0] % t.v != 0 || st[1] % t.v != 0 || st[2] % t.v != 0 || st[1] > 1 << 20 ||

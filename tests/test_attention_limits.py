@@ -17,3 +17,16 @@ def test_backward_takes_the_address_that_the_forward_pass_wrote_to(dtype, size):
     assert "dout must be 16-byte" in _raises(H.HAPI_E_INVAL, H.hapi_cross_attention_backward, d, *at(8, P + size))
     odd = _attend(dtype=dtype, dim=63).set(workspace_bytes=0)
     _raises(H.HAPI_E_NOMEM, H.hapi_cross_attention_backward, odd, *at(8, P + size))
+
+
+@pytest.mark.parametrize("kw,strides", [
+    (dict(batch=1), (7, None, None)), (dict(batch=1, q_len=1, kv_len=1), (3, 5, None)), (dict(heads=1, kv_heads=1), (None, None, 33)),
+    (dict(batch=1, q_len=1, kv_len=1), (1, (1 << 21) + 1, None)), (dict(batch=1, heads=1, kv_heads=1, q_len=300, kv_len=300), (9, None, 1 << 35))])
+def test_strides_of_one_entry_cost_nothing(kw, strides):
+    """The stride of an extent of one says nothing about where values lie."""
+    sizes = dict(dict(batch=2, q_len=3, kv_len=5, heads=4, kv_heads=2, dim=64), **kw)
+    of = lambda length, heads: tuple(s if s is not None else w for s, w in zip(strides, (length * heads * 64, heads * 64, 64)))
+    q, k = of(sizes["q_len"], sizes["heads"]), of(sizes["kv_len"], sizes["kv_heads"])
+    for back in (False, True):
+        plain = H.hapi_cross_attention_workspace_bytes(_attend(**sizes), back)
+        assert H.hapi_cross_attention_workspace_bytes(_attend(q_stride=q, k_stride=k, v_stride=k, o_stride=q, **sizes), back) == plain

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2210_08650_amd as H
-from tests.test_gpu_cross_attention import BF, F32, Case
+from tests.test_gpu_cross_attention import BF, CODE, F32, Case
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,27 @@ def test_outputs_and_o_at_any_element(b, lq, lk, h, kv, d, dtype):
     torch.cuda.synchronize()
     c.ws.check()
     assert all(torch.equal(a, w) for a, w in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_strides_of_one_entry(dtype):
+    """Odd and huge strides where there is one entry, one token or one head: read and written
+    as without them, by the same kernels."""
+    for b, lq, lk, h, kv in ((1, 40, 300, 4, 2), (3, 1, 1, 2, 1), (2, 70, 90, 1, 1), (1, 1, 700, 1, 1)):
+        c = Case(62, dtype, b, lq, lk, h, kv, 64)
+        o, st = c.forward()
+        want = [o, st] + c.backward(o, st)
+
+        def odd(x):
+            s = [77 + (1 << 22) * i if n == 1 else w for i, (n, w) in enumerate(zip(x.shape[:3], x.stride()))]
+            return x.as_strided(x.shape, (*s, 1))
+        c.q, c.k, c.v, c.dout = (odd(x) for x in (c.q, c.k, c.v, c.dout))
+        st_of = lambda x: x.stride()[:3]
+        d = H.Attention(CODE[dtype], b, lq, lk, h, kv, 64, 0.0, st_of(c.q), st_of(c.k), st_of(c.v), st_of(c.dout), stream=torch.cuda.current_stream())
+        ws = torch.empty(max(1, H.hapi_cross_attention_workspace_bytes(d, True)), dtype=torch.uint8, device="cuda")
+        d.set(workspace=ws, workspace_bytes=ws.numel())
+        got = [odd(torch.empty(x.shape, dtype=dtype, device="cuda")) for x in (c.q, c.q, c.k, c.v)]
+        st = torch.empty_like(want[1])
+        H.hapi_cross_attention_forward(d, c.q, c.k, c.v, None, None, None, got[0], st)
+        H.hapi_cross_attention_backward(d, c.q, c.k, c.v, None, None, None, got[0], st, c.dout, *got[1:])
+        assert all(torch.equal(a, w) for a, w in zip([got[0], st] + got[1:], want))
