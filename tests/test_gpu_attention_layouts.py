@@ -58,3 +58,14 @@ def test_strides_of_one_entry(dtype):
         H.hapi_cross_attention_forward(d, c.q, c.k, c.v, None, None, None, got[0], st)
         H.hapi_cross_attention_backward(d, c.q, c.k, c.v, None, None, None, got[0], st, c.dout, *got[1:])
         assert all(torch.equal(a, w) for a, w in zip([got[0], st] + got[1:], want))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("dim", [2, 6, 30, 34, 50, 62, 86, 98, 126])
+def test_even_widths(dim, dtype):
+    """Widths of 2 modulo 4, whose rows allow two values at once, dense and with such strides;
+    and whole widths with strides of 2 modulo 4."""
+    Case(63, dtype, 2, 45, 77, 4, 2, dim).check()
+    Case(64, dtype, 2, 150, 70, 2, 2, dim, pad=4, mask=0.7).check()
+    Case(65, dtype, 3, 1, 600, 4, 1, dim, pad=2).check()
+    Case(66, dtype, 1, 200, 130, 2, 1, dim + 2, pad=2, transposed=True, q_lens=[150], kv_lens=[111]).check()
