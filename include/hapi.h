@@ -568,7 +568,9 @@ int hapi_distill_backward(const hapi_head_desc *desc, const void *x, const void 
  * The first sections[0] pairs turn by the position on axis 0, the next sections[1] by
  * that on axis 1, ...; P pairs in all.  Pair i is the values (i, P + i), or with
  * neighbours = 1 (2 i, 2 i + 1); values from 2 P on are not rotated.  axes = 0 is the norm
- * alone.  Angles are formed in float64 (off by |t| 2^-52 or so), the rest is float32. */
+ * alone.  Angles are formed in float64 (off by |t| 2^-52 or so), the rest is float32, and so
+ * mean(x^2) has to lie in its range.  Values that are not rotated keep their bits without a
+ * norm. */
 typedef struct {
   int32_t dtype;              /* hapi_dtype of q, k, their outputs and gradients */
   int32_t head_dim;           /* 1 .. 256 */
@@ -616,7 +618,13 @@ int hapi_rotary_backward(const hapi_rotary_desc *desc, const void *dq_out, const
 
 /* Cross attention: queries attend to an encoder's states of another length.  Per query
  * head h, with the key head h / (heads / kv_heads), over the keys that take part:
- *   o = softmax(scale q k^T) v */
+ *   o = softmax(scale q k^T) v
+ * Scores, statistics, sums and the outputs before their rounding are float32.  In bf16 the
+ * probabilities p, and in the backward pass p and their gradients ds, are rounded to bf16 for
+ * the second product (2^-8 of each; outputs are off by 1.4 times what rounding them alone
+ * leaves); the backward pass of calls of up to 512 rows (batch * q_len * heads) also
+ * multiplies by what that rounding left.  So the last bits of a row's results may depend on
+ * the call's other sizes. */
 typedef struct {
   int32_t dtype;              /* hapi_dtype of q, k, v, o and their gradients */
   int32_t head_dim;           /* 1 .. 128 */
@@ -679,7 +687,7 @@ typedef struct {
                                  grads[i] itself; NULL: every one grads[i] itself */
   const int64_t *sizes;       /* host [count]: values, 0 .. 2^38 */
   const int32_t *dtypes;      /* host [count]: hapi_dtype */
-  float max_norm;             /* finite, > 0; hapi_gradient_norm does not use it */
+  float max_norm;             /* finite, > 0, in either call; hapi_gradient_clip uses it */
   void *stream;               /* hipStream_t; NULL = the null stream */
   void *workspace;            /* device scratch, 256-byte aligned */
   size_t workspace_bytes;

@@ -387,7 +387,9 @@ int read_attend(const hapi_attention_desc *d, Attend &t) {
 
   // Few rows: the keys over as many workgroups as fill the CUs, some tiles to each wave.
   const int padded = (int)up(d->head_dim, 32), kw = attend_key_waves(t.esz, padded, rw), bn = attend_tile_keys(t.esz, padded, kw);
-  const int64_t wgs = ceil_div(rows, 32 * rw) * pairs, want = (!t.bf16 && padded > 64 ? 1 : 2) * kCus;  // as many as run at once
+  // Two workgroups a CU, and one of float32 heads past 64 values, whose registers leave no more
+  // (but for the forward pass of 65 to 96 values, which would run two).
+  const int64_t wgs = ceil_div(rows, 32 * rw) * pairs, want = (!t.bf16 && padded > 64 ? 1 : 2) * kCus;
   // A float32 tile's products take eight times as long as a bf16 one's, so one of them is
   // worth a part of its own; of the others four.  Forward and join with 1, 2, 4 and 16 of
   // them: 1 x 1 x 8192, 16 + 4 heads of 128, 21, 21, 18 and 32 us; 4 x 8 x 2000, 8 + 2 heads

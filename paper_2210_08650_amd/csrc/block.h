@@ -115,10 +115,12 @@ hipError_t launch_attend_forward(bool bf16, const AttendArgs &a, hipStream_t s);
 hipError_t launch_attend_dq(bool bf16, const AttendArgs &a, hipStream_t s);   // delta, too
 hipError_t launch_attend_dkv(bool bf16, const AttendArgs &a, hipStream_t s);
 // Whether P and dS of bf16 heads are multiplied with both halves, them as they are rounded
-// and what the rounding left.  In calls of up to 512 rows their roundings do not average to
-// the 1.4 times of the output's own rounding that larger calls have (213 rows x 2 heads x 9
-// keys: dq off by 1.5 times as much as by its rounding alone, now 1.0 times), and there are
-// few products: 8 heads x 50 x 600 of 64 values 18 us with either, 16 x 1 x 4096, 16 heads
+// and what the rounding left.  Over a large call the two roundings leave 1.4 times what the
+// output's own does; a single row of few keys may be off by more, and a small call is all
+// such rows (213 rows x 2 heads x 9 keys: dq off by 1.5 times as much as by its rounding
+// alone, now 1.0 times).  So it is the call's rows that count, not the row's own sizes, and a
+// row's last bits differ between a call of 512 rows and one of more.  Few rows are few
+// products: 8 heads x 50 x 600 of 64 values 18 us with either, 16 x 1 x 4096, 16 heads
 // of 64, 105 against 111 us, of 128, 460 against 536 us.
 inline bool attend_fine(const AttendArgs &a) { return (int64_t)a.pairs * a.group * a.q_len <= 512; }
 // All three in one kernel: bf16 heads of up to 64 values whose rows a workgroup's waves have

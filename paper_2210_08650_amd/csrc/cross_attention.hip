@@ -18,11 +18,11 @@
 // ones), the output once.
 //
 // Bound by the matrix pipes and what stands between their products: 2 x 4096 x 4096, 16 + 4
-// heads of 128 in bf16, 310 us, 0.89 PF/s, pipes busy 46%, exponentials and rounding take
-// the issue slots of most others.  By memory where rows are few: 16 x 1 x 8192, lengths from
-// 1 to 8192, 39 us, 4.5 TB/s of the keys that take part; 128 x 64 x 197, 12 heads of 64, 24.9
-// us, 4.1 TB/s.  float32 of 3 x 77 x 1021, heads of 80, 23 us: pipes busy 38%, three or four
-// tiles to a wave.
+// heads of 128 in bf16, 305 to 317 us, 0.87 to 0.90 PF/s, pipes busy 47%, exponentials and
+// rounding take the issue slots of most others.  By memory where rows are few: 16 x 1 x 8192,
+// lengths from three tenths of 8192 to all, 38.5 us, 4.5 TB/s of the keys that take part; 128 x
+// 64 x 197, 12 heads of 64, 24.7 us, 4.2 TB/s.  float32 of 3 x 77 x 1021, heads of 80, 23 us:
+// pipes busy 38%, three or four tiles to a wave.
 //
 // Keys that take no part are zeros in LDS, whatever memory holds, and their scores are
 // -inf, so NaN in padding reaches nothing.  Where rows are few, the keys are split over

@@ -17,8 +17,9 @@
 // for every 128 keys).  P and dS are rounded to the operands' type for the matrix
 // cores; all sums are float32.
 //
-// Bound by the matrix pipes: 2 x 4096 x 4096, 16 + 4 heads of 128 in bf16, dq 415 us, 0.99
-// PF/s of its three products, pipes busy 54%; dk and dv 585 us, 0.94 PF/s of four, 50%.
+// Bound by the matrix pipes: 2 x 4096 x 4096, 16 + 4 heads of 128 in bf16, dq 418 to 429
+// us, 0.96 to 0.99 PF/s of its three products, pipes busy 54%; dk and dv 581 to 597 us, 0.92 to
+// 0.95 PF/s of four, 50%.
 // float32 of 3 x 77 x 1021, 12 + 4 heads of 80: 31 and 38 us, 43% and 50%.
 #include <type_traits>
 
