@@ -144,28 +144,30 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 9
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[n][i] -= by;
     };
-    float mx = masked();
+    const float mx = masked();
     // the first key of a row sets its ref, whatever its size
     const bool moves = (FROM_REF ? mx : mx - ref) > slack || (first && mx > -INFINITY);
-    bool less_ref = FROM_REF;  // what s and mx are
-    if (FROM_REF && __any(moves && !first)) {
-      // Scores less a ref far below them have lost their low bits to its size: they are
-      // formed again by themselves, with q from memory (a loop about both, with q in its
-      // registers: 2 x 4096 x 4096 348 us for 308).
-      less_ref = false;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) s[n] = zeros();
-#pragma unroll 1
-      for (int ks = 0; ks < KS; ++ks) {
-        const Frag f = row_frag<T>(qp, ks, lh, a.dim, counts);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), f, s[n]);
-      }
-      mx = masked();
-    }
-    m = fmaxf(m, less_ref ? ref + mx : mx);
+    float top = FROM_REF ? ref + mx : mx;
     if (__any(moves)) {
-      const float to = moves ? mx : ref;  // a first ref is 0, so mx is the score itself
+      bool less_ref = FROM_REF;  // what s is
+      // Scores less a ref far below 0 that are themselves nearer to it have lost their low
+      // bits to its size (2^-24 of it; down to 2^-32 in the probabilities that is less than
+      // 2^-16 of them): they are formed again by themselves, with q from memory (a loop about
+      // both, with q in its registers: 2 x 4096 x 4096 348 us for 308; whenever ref moves: 435
+      // us for scores that spread over 10 units, 311 so).
+      if (FROM_REF && __any(moves && !first && ref * a.c < -32.0f && -ref > 2.0f * fabsf(top))) {
+        less_ref = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n] = zeros();
+#pragma unroll 1
+        for (int ks = 0; ks < KS; ++ks) {
+          const Frag f = row_frag<T>(qp, ks, lh, a.dim, counts);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) s[n] = mma(Tile::by_row(kt, 32 * n, ks, lane), f, s[n]);
+        }
+        top = masked();
+      }
+      const float to = moves ? top : ref;
       const float alpha = first ? 1.0f : __builtin_amdgcn_exp2f((ref - to) * a.c);
       if (FROM_REF) subtract(less_ref ? to - ref : to);
       first = first && !moves;
@@ -177,6 +179,7 @@ __global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 9
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
     }
+    m = fmaxf(m, top);
     if (!FROM_REF) subtract(ref);
     // Probabilities of 32 keys are summed by themselves: the roundings of thousands of equal
     // ones to a running sum would all go one way (16384 keys: off by 1.1e-4 of it, so 4e-6).

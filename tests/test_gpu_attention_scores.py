@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("far", [1e6, 1e30])
+@pytest.mark.parametrize("far", [30.0, 100.0, 250.0, 1000.0, 1e6, 1e30])
 @pytest.mark.parametrize("b,lq,lk,h,kv,d,first", [
     (1, 3, 200, 2, 2, 64, 64), (1, 5, 700, 4, 1, 64, 512), (2, 40, 400, 2, 2, 32, 256), (1, 150, 300, 2, 1, 128, 128),
     (1, 70, 300, 3, 3, 96, 64), (300, 1, 160, 2, 1, 128, 96)])
