@@ -13,15 +13,16 @@
 // accumulators start from: the difference costs no instruction, and it is formed before
 // the scale, so that no rounding of ref c is in it.  The reference moves, and what is
 // summed is rescaled, only when a tile's largest score goes past it by more than a factor
-// of 2^8.  Scores, statistics and sums are float32; probabilities are rounded to the
-// operands' type for the matrix cores (2^-8 of each in bf16, the sum is of the unrounded
-// ones), the output once.
+// of 2^8; a tile whose scores it would have blurred by its size is formed again without it.
+// Scores, statistics and sums are float32; probabilities are rounded to the operands' type
+// for the matrix cores (2^-8 of each in bf16, the sum is of the unrounded ones), the output
+// once.
 //
 // Bound by the matrix pipes and what stands between their products: 2 x 4096 x 4096, 16 + 4
-// heads of 128 in bf16, 305 to 317 us, 0.87 to 0.90 PF/s, pipes busy 47%, exponentials and
+// heads of 128 in bf16, 304 to 317 us, 0.87 to 0.90 PF/s, pipes busy 47%, exponentials and
 // rounding take the issue slots of most others.  By memory where rows are few: 16 x 1 x 8192,
-// lengths from three tenths of 8192 to all, 38.5 us, 4.5 TB/s of the keys that take part; 128 x
-// 64 x 197, 12 heads of 64, 24.7 us, 4.2 TB/s.  float32 of 3 x 77 x 1021, heads of 80, 23 us:
+// lengths from three tenths of 8192 to all, 38 us, 4.6 TB/s of the keys that take part; 128 x
+// 64 x 197, 12 heads of 64, 24.4 us, 4.2 TB/s.  float32 of 3 x 77 x 1021, heads of 80, 23 us:
 // pipes busy 38%, three or four tiles to a wave.
 //
 // Keys that take no part are zeros in LDS, whatever memory holds, and their scores are
@@ -40,7 +41,7 @@ __device__ __forceinline__ float2 row_stats(float m, float ref, float sum, float
 }
 
 template <typename T, int DP, int RW, int KW, int BN>
-__global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 || DP <= 96 ? 2 : 1, RW * KW, KW * 4 * hapi::Tile<T, DP, BN>::BYTES)) void attend_forward_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * RW * KW, least_waves(sizeof(T) == 2 && DP <= 32 ? 4 : sizeof(T) == 2 || DP <= 96 ? 2 : 1, RW * KW, KW * 4 * hapi::Tile<T, DP, BN>::BYTES)) void attend_forward_kernel(AttendArgs a) {
   typedef hapi::Tile<T, DP, BN> Tile;
   typedef Loader<T, DP, BN, RW> Load;
   typedef typename Elem<T>::Frag Frag;
